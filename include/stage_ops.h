@@ -137,6 +137,54 @@ int stage_op_attention_bwd_noalloc(void* stream, int32_t dtype, int32_t mb, int3
                                    const void* k, const void* v, int64_t ld, const void* o, const void* dout, int64_t ldo,
                                    const float* lse, void* dq, void* dk, void* dv, int64_t ldd, int32_t impl);
 
+/* Packed sequences: a microbatch of T tokens that holds ndocs documents one behind the other, document n owning the tokens
+ * offsets[n] .. offsets[n+1]-1; tokens before offsets[0] and from offsets[ndocs] on belong to no document (padding).  A token
+ * sees the tokens of its own document up to itself and the first prefix[n] tokens of it, also those behind itself.
+ * stage_op_doc_ranges writes the table that stage_op_attention_docs_* read: ranges[t] = int32 (first and end of the keys that token t
+ * sees, first and end of the rows that see token t), zeros for tokens of no document.  It depends on the documents only: one call
+ * per microbatch serves all layers, forward and backward.
+ * offsets: device int32[ndocs+1], non-decreasing (a document may be empty) and in [0, T]; prefix: device int32[ndocs], cut to the
+ * document's length, or NULL for none; ranges: device int32[T, 4], 16-byte aligned.  The offsets live on the device and are not
+ * checked: other values make documents of unspecified tokens, but never ranges outside [0, T]. */
+int stage_op_doc_ranges(void* stream, int32_t T, int32_t ndocs, const int32_t* offsets, const int32_t* prefix, int32_t* ranges);
+
+/* Softmax attention inside packed documents.  With i over the T tokens and j over the keys that i sees (ranges):
+ *   u_ij = scale q_i.k_j;  s_ij = softcap tanh(u_ij / softcap) (softcap = 0: u_ij) - slopes[h] |i - j| (slopes NULL: nothing)
+ *   o_i = sum_j softmax_j(s_ij) v_j;  lse_i = log sum_j exp(s_ij).
+ * A token of no document gets o = 0 and lse = -inf; its q, k and v may hold anything.
+ * Shared key heads: nh query heads, nkv key heads, nh a multiple of nkv; query head h reads key head h / (nh / nkv).  q and o: rows of nh
+ * heads, d wide, strides ldq and ldo; k and v: rows of nkv heads, stride ldkv; lse: float[nh, T]; slopes: device float[nh].
+ * d: a multiple of 8 up to 128.  Rows start at multiples of 16 bytes and strides are at most 2^22 elements; T * nh < 2^31.
+ * scale > 0 and softcap >= 0 are finite.  No output overlaps an input or another output.  T = 0 does nothing.
+ * inf or NaN in a token's q, k, v or dout reaches only the rows that see the token, here and in the gradients below. */
+int stage_op_attention_docs_fwd(void* stream, int32_t dtype, int32_t T, int32_t nh, int32_t nkv, int32_t d, const void* q, int64_t ldq,
+                                const void* k, const void* v, int64_t ldkv, const int32_t* ranges, float scale, float softcap,
+                                const float* slopes, void* o, int64_t ldo, float* lse);
+/* Gradients dq (stride lddq), dk and dv (stride lddkv, summed over the query heads that share a key head) from dout (stride ldo), with o
+ * and lse as the forward left them.  Tokens of no document get zeros.  slopes are constants.  No atomics: a repeat gives the same bits.
+ * scratch: device, 256-byte aligned, at least stage_op_attention_docs_bwd_scratch_bytes (host only; negative STAGE_ERR_ARG for
+ * invalid sizes), the caller's, free again when the call's work on the stream has finished; calls that may overlap need scratch
+ * of their own.  STAGE_ERR_WORKSPACE when it is missing, misaligned or too small. */
+int64_t stage_op_attention_docs_bwd_scratch_bytes(int32_t dtype, int32_t T, int32_t nh, int32_t nkv, int32_t d);
+int stage_op_attention_docs_bwd(void* stream, int32_t dtype, int32_t T, int32_t nh, int32_t nkv, int32_t d, const void* q, int64_t ldq,
+                                const void* k, const void* v, int64_t ldkv, const int32_t* ranges, float scale, float softcap,
+                                const float* slopes, const void* o, const void* dout, int64_t ldo, const float* lse, void* dq,
+                                int64_t lddq, void* dk, void* dv, int64_t lddkv, void* scratch, int64_t scratch_bytes);
+
+/* Rotary positions with several axes (time, height and width of video, height and width of images; one axis: text with positions of
+ * its own, as packed documents have), of nq query heads and nk key heads (0: k is not read) in one pass.  Axis a turns sections[a] of the
+ * d/2 adjacent pairs (2i, 2i+1) of every head, the first sections[0] of them with axis 0 and so on; sections: HOST int32[naxes], not
+ * negative, their sum d/2; naxes <= STAGE_OP_ROPE_MAX_AXES.  positions: device int32[naxes, T], any values.
+ * Pair i of token t turns by the angle sign * positions[a, t] * f_i, (u, w) -> (u cos - w sin, u sin + w cos), with f_i = base^(-2i/d), or
+ * (own_spectrum != 0) f_i = base^(-j/sections[a]) for the j-th pair of its axis.  Angles are formed in double precision.
+ * sign = 1, or -1: the inverse rotation, which is also the gradient.  The results may take the place of the inputs (the same pointer and
+ * stride); no other overlap.  d: a multiple of 8 up to 256.  Rows start at multiples of 16 bytes, strides are at most 2^22
+ * elements. */
+#define STAGE_OP_ROPE_MAX_AXES 4
+int stage_op_rope_axes(void* stream, int32_t dtype, int32_t T, int32_t nq, int32_t nk, int32_t d, const void* q, int64_t ldq,
+                       const void* k, int64_t ldk, const int32_t* positions, int32_t naxes, const int32_t* sections,
+                       int32_t own_spectrum, float base, int32_t sign, void* q_out, int64_t ldq_out, void* k_out, int64_t ldk_out);
+
 /* x[t,:] = E[ids[t],:] ; dE[id,:] += sum of dx rows of the tokens carrying id (token order). */
 int stage_op_embed(void* stream, int32_t dtype, int32_t T, int32_t H, int32_t V, const int32_t* ids, const void* E,
                    void* x, const void* dx, float* dE, int32_t backward);

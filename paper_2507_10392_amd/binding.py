@@ -129,6 +129,13 @@ def lib():
         L.stage_op_attention_bwd_rope.argtypes = L.stage_op_attention_bwd.argtypes + [vp]
         L.stage_op_attention_bwd_noalloc.argtypes = [vp, i32, i32, i32, i32, i32, vp, vp, vp, i64, vp, vp, i64, vp, vp, vp, vp,
                                                      i64, i32]
+        L.stage_op_rope_axes.argtypes = [vp, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, i32, C.POINTER(i32), i32, f32, i32, vp, i64, vp, i64]
+        L.stage_op_doc_ranges.argtypes = [vp, i32, i32, vp, vp, vp]
+        L.stage_op_attention_docs_fwd.argtypes = [vp, i32, i32, i32, i32, i32, vp, i64, vp, vp, i64, vp, f32, f32, vp, vp, i64, vp]
+        L.stage_op_attention_docs_bwd_scratch_bytes.argtypes = [i32, i32, i32, i32, i32]
+        L.stage_op_attention_docs_bwd_scratch_bytes.restype = i64
+        L.stage_op_attention_docs_bwd.argtypes = [vp, i32, i32, i32, i32, i32, vp, i64, vp, vp, i64, vp, f32, f32, vp, vp, vp, i64, vp, vp, i64,
+                                                  vp, vp, i64, vp, i64]
         L.stage_op_embed.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, i32]
         L.stage_op_cross_entropy.argtypes = [vp, i32, i32, i32, vp, i64, vp, vp, vp, vp, f32, i32]
         L.stage_op_adamw.argtypes = [vp, i32, i64, i64, vp, vp, vp, vp, vp, f32, f32, f32, f32, f32, i64, f32]
@@ -365,3 +372,20 @@ def wgrad_parts(stream, dtype, M, N, K_each, K_last, A_parts, lda, B_parts, ldb,
     code = lib().stage_op_wgrad_parts(stream, dtype, M, N, K_each, K_last, n, pa, lda, pb, ldb, _ptr(Cbuf), ldc, batch, sA, sB, sC, impl)
     if code != STAGE_OK:
         raise StageError(code, "stage_op_wgrad_parts")
+
+
+def rope_axes(stream, dtype, T, nq, nk, d, q, ldq, k, ldk, positions, sections, own_spectrum, base, sign, q_out, ldq_out, k_out, ldk_out):
+    """stage_op_rope_axes with a list of the sections' pairs."""
+    n = len(sections)
+    code = lib().stage_op_rope_axes(stream, dtype, T, nq, nk, d, _ptr(q), ldq, _ptr(k), ldk, _ptr(positions), n, (C.c_int32 * n)(*sections),
+                                    int(own_spectrum), base, sign, _ptr(q_out), ldq_out, _ptr(k_out), ldk_out)
+    if code != STAGE_OK:
+        raise StageError(code, "stage_op_rope_axes")
+
+
+def attention_docs_bwd_scratch_bytes(dtype, T, nh, nkv, d):
+    """stage_op_attention_docs_bwd_scratch_bytes (host only)."""
+    n = lib().stage_op_attention_docs_bwd_scratch_bytes(dtype, T, nh, nkv, d)
+    if n < 0:
+        raise StageError(-n, "stage_op_attention_docs_bwd_scratch_bytes")
+    return n

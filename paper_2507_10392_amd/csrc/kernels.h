@@ -216,6 +216,32 @@ hipError_t attn_bwd(hipStream_t st, DType dt, int mb, int S, int nh, int d, cons
                     const void* v, int64_t ld, const void* o, const void* dout, int64_t ldo, const float* lse,
                     float* delta, void* dq, void* dk, void* dv, int64_t ldd, const float2* rope, int force);
 
+// Packed documents: tokens 0 .. T-1 of a microbatch, document n owning offsets[n] .. offsets[n+1]-1.  ranges[t] = (first and end of the keys
+// that token t sees, first and end of the rows that see it); zeros for tokens of no document.
+hipError_t doc_ranges(hipStream_t st, int T, int ndocs, const int32_t* offsets, const int32_t* prefix, int32_t* ranges);
+// Attention over these ranges: s_ij = cap(scale q_i.k_j) - slopes[h] |i - j|, cap(u) = softcap tanh(u / softcap) or, softcap = 0, u.  Heads are
+// d <= 128 wide columns of the rows; query head h reads key head h / (nh / nkv).  lse: float[nh, T].
+struct DocAttn {
+  int T, nh, nkv, d;
+  const void *q, *k, *v; int64_t ldq, ldkv;
+  const int32_t* ranges;
+  float scale, softcap; const float* slopes;
+  const void* dout; void* o; int64_t ldo; float* lse;      // o, lse: results of the forward, inputs of the backward
+  void* dq; int64_t lddq; void *dk, *dv; int64_t lddkv;
+  float* delta;                                            // backward: [nh, T], dO_i . O_i
+};
+hipError_t attn_docs_fwd(hipStream_t st, DType dt, const DocAttn& a);
+int64_t attn_docs_bwd_scratch(DType dt, int T, int nh, int nkv, int d);   // bytes
+hipError_t attn_docs_bwd(hipStream_t st, DType dt, const DocAttn& a, void* scratch);
+
+// Rotary positions with several axes: n heads, d wide, of rows in and out (which may be the same).  Pair i of a head turns with the position
+// positions[a, t] of the axis a in whose section of pairs it lies, by base^(-2i/d) per position, or (own_spectrum) by base^(-j/n) as
+// pair j of the n pairs of its section.
+constexpr int ROPE_AXES_MAX_D = 256;
+struct RopeHeads { const void* in; void* out; int64_t ld_in, ld_out; int n; };
+hipError_t rope_axes(hipStream_t st, DType dt, int T, int d, const RopeHeads& q, const RopeHeads& k, const int32_t* positions, int naxes,
+                     const int32_t* sections, int own_spectrum, double base, int sign);
+
 // x[t,:] = E[ids[t],:] (rows of ids outside [0,V) give zeros).  keep (or NULL) receives the ids.
 hipError_t embed_fwd(hipStream_t st, DType dt, int T, int H, int V, const int32_t* ids, const void* E, void* x, int32_t* keep = nullptr);
 // dE[id,:] += sum over the tokens with that id, added in increasing token order.

@@ -12,6 +12,15 @@ namespace {
 int rc(hipError_t e) { return e == hipSuccess ? STAGE_OK : STAGE_ERR_DEVICE; }
 bool dt_ok(int d) { return d == 0 || d == 1 || d == 2; }
 int vec_of(int d) { return d == 0 ? 4 : 8; }
+// n heads, d wide, side by side in rows of stride ld that 16-byte accesses can walk.  Strides are bounded so that 64 rows stay within the 32-bit
+// offsets of a buffer descriptor.
+bool rows_ok(int dtype, const void* p, int64_t ld, int n, int d) {
+  return p && !((uintptr_t)p & 15) && ld >= (int64_t)n * d && ld % vec_of(dtype) == 0 && ld <= (1 << 22);
+}
+bool words_ok(const void* p) { return !((uintptr_t)p & 3); }   // floats or whole numbers, or nothing
+bool docs_shape_ok(int dtype, int T, int nh, int nkv, int d) {
+  return dt_ok(dtype) && T >= 0 && nh >= 1 && nkv >= 1 && nh % nkv == 0 && d >= 8 && d % 8 == 0 && d <= 128 && (int64_t)T * nh <= INT32_MAX;
+}
 
 // Scratch of stage_op_attention_bwd_noalloc: the row sums delta[mb, nh, S] that the dQ kernel leaves for the dK/dV
 // kernel.  A file-scope device array, so every GPU the library runs on holds one copy of it (4 MiB) from the moment
@@ -246,6 +255,74 @@ int stage_op_attention_bwd_noalloc(void* stream, int32_t dtype, int32_t mb, int3
   // order, so nothing of an earlier call's content needs clearing.
   return stage_op_attention_bwd_rope(stream, dtype, mb, S, nh, d, q, k, v, ld, o, dout, ldo, lse, delta, dq, dk, dv, ldd,
                                      impl, nullptr);
+}
+
+int stage_op_rope_axes(void* stream, int32_t dtype, int32_t T, int32_t nq, int32_t nk, int32_t d, const void* q, int64_t ldq, const void* k,
+                       int64_t ldk, const int32_t* positions, int32_t naxes, const int32_t* sections, int32_t own_spectrum, float base,
+                       int32_t sign, void* q_out, int64_t ldq_out, void* k_out, int64_t ldk_out) {
+  if (!dt_ok(dtype) || T < 0 || nq < 1 || nk < 0 || d < 8 || d % 8 || d > ROPE_AXES_MAX_D || naxes < 1 || naxes > STAGE_OP_ROPE_MAX_AXES ||
+      !sections || (sign != 1 && sign != -1) || !(base > 0.f) || std::isinf(base))
+    return STAGE_ERR_ARG;
+  int64_t pairs = 0;
+  for (int a = 0; a < naxes; ++a) {
+    if (sections[a] < 0) return STAGE_ERR_ARG;
+    pairs += sections[a];
+  }
+  if (pairs != d / 2) return STAGE_ERR_ARG;
+  if (!rows_ok(dtype, q, ldq, nq, d) || !rows_ok(dtype, q_out, ldq_out, nq, d) || !positions || !words_ok(positions)) return STAGE_ERR_ARG;
+  if (nk > 0 && (!rows_ok(dtype, k, ldk, nk, d) || !rows_ok(dtype, k_out, ldk_out, nk, d))) return STAGE_ERR_ARG;
+  if (((int64_t)nq + nk) * d > (1 << 24)) return STAGE_ERR_ARG;   // the kernel's index inside a block of tokens
+  if (T == 0) return STAGE_OK;
+  return rc(rope_axes((hipStream_t)stream, (DType)dtype, T, d, RopeHeads{q, q_out, ldq, ldq_out, nq}, RopeHeads{k, k_out, ldk, ldk_out, nk}, positions,
+                      naxes, sections, own_spectrum != 0, base, sign));
+}
+
+int stage_op_doc_ranges(void* stream, int32_t T, int32_t ndocs, const int32_t* offsets, const int32_t* prefix, int32_t* ranges) {
+  if (T < 0 || ndocs < 0 || ndocs == INT32_MAX || !offsets || !ranges || ((uintptr_t)ranges & 15) || !words_ok(offsets) || !words_ok(prefix)) return STAGE_ERR_ARG;
+  if (T == 0) return STAGE_OK;
+  return rc(doc_ranges((hipStream_t)stream, T, ndocs, offsets, prefix, ranges));
+}
+
+namespace {
+// The arguments that both directions of attention_docs share.
+bool docs_ok(int32_t dtype, int32_t T, int32_t nh, int32_t nkv, int32_t d, const void* q, int64_t ldq, const void* k, const void* v, int64_t ldkv,
+             const int32_t* ranges, float scale, float softcap, const float* slopes, const void* o, int64_t ldo, const float* lse) {
+  return docs_shape_ok(dtype, T, nh, nkv, d) && rows_ok(dtype, q, ldq, nh, d) && rows_ok(dtype, k, ldkv, nkv, d) && rows_ok(dtype, v, ldkv, nkv, d) &&
+         rows_ok(dtype, o, ldo, nh, d) && ranges && !((uintptr_t)ranges & 15) && scale > 0.f && !std::isinf(scale) && softcap >= 0.f &&
+         !std::isinf(softcap) && words_ok(slopes) && lse && words_ok(lse);
+}
+}  // namespace
+
+int stage_op_attention_docs_fwd(void* stream, int32_t dtype, int32_t T, int32_t nh, int32_t nkv, int32_t d, const void* q, int64_t ldq, const void* k,
+                                const void* v, int64_t ldkv, const int32_t* ranges, float scale, float softcap, const float* slopes, void* o,
+                                int64_t ldo, float* lse) {
+  if (!docs_ok(dtype, T, nh, nkv, d, q, ldq, k, v, ldkv, ranges, scale, softcap, slopes, o, ldo, lse)) return STAGE_ERR_ARG;
+  if (T == 0) return STAGE_OK;
+  DocAttn a = {};
+  a.T = T; a.nh = nh; a.nkv = nkv; a.d = d; a.q = q; a.ldq = ldq; a.k = k; a.v = v; a.ldkv = ldkv; a.ranges = ranges; a.scale = scale;
+  a.softcap = softcap; a.slopes = slopes; a.o = o; a.ldo = ldo; a.lse = lse;
+  return rc(attn_docs_fwd((hipStream_t)stream, (DType)dtype, a));
+}
+
+int64_t stage_op_attention_docs_bwd_scratch_bytes(int32_t dtype, int32_t T, int32_t nh, int32_t nkv, int32_t d) {
+  if (!docs_shape_ok(dtype, T, nh, nkv, d)) return -STAGE_ERR_ARG;
+  return attn_docs_bwd_scratch((DType)dtype, T, nh, nkv, d);
+}
+
+int stage_op_attention_docs_bwd(void* stream, int32_t dtype, int32_t T, int32_t nh, int32_t nkv, int32_t d, const void* q, int64_t ldq, const void* k,
+                                const void* v, int64_t ldkv, const int32_t* ranges, float scale, float softcap, const float* slopes, const void* o,
+                                const void* dout, int64_t ldo, const float* lse, void* dq, int64_t lddq, void* dk, void* dv, int64_t lddkv,
+                                void* scratch, int64_t scratch_bytes) {
+  if (!docs_ok(dtype, T, nh, nkv, d, q, ldq, k, v, ldkv, ranges, scale, softcap, slopes, o, ldo, lse) || !rows_ok(dtype, dout, ldo, nh, d) ||
+      !rows_ok(dtype, dq, lddq, nh, d) || !rows_ok(dtype, dk, lddkv, nkv, d) || !rows_ok(dtype, dv, lddkv, nkv, d))
+    return STAGE_ERR_ARG;
+  if (T == 0) return STAGE_OK;
+  if (!scratch || ((uintptr_t)scratch & 255) || scratch_bytes < attn_docs_bwd_scratch((DType)dtype, T, nh, nkv, d)) return STAGE_ERR_WORKSPACE;
+  DocAttn a = {};
+  a.T = T; a.nh = nh; a.nkv = nkv; a.d = d; a.q = q; a.ldq = ldq; a.k = k; a.v = v; a.ldkv = ldkv; a.ranges = ranges; a.scale = scale;
+  a.softcap = softcap; a.slopes = slopes; a.o = const_cast<void*>(o); a.dout = dout; a.ldo = ldo; a.lse = const_cast<float*>(lse);
+  a.dq = dq; a.lddq = lddq; a.dk = dk; a.dv = dv; a.lddkv = lddkv;
+  return rc(attn_docs_bwd((hipStream_t)stream, (DType)dtype, a, scratch));
 }
 
 int stage_op_embed(void* stream, int32_t dtype, int32_t T, int32_t H, int32_t V, const int32_t* ids, const void* E,
