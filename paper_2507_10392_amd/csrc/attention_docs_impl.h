@@ -1,0 +1,596 @@
+// Flash-style attention inside packed documents on the matrix cores, forward and backward, of one element type (bf16, half and float each
+// build it: attention_docs_*.hip).
+//
+// The T x T scores are never stored.  A block of rows reads only the keys that its documents' ranges span, from the first of them on:
+// tiles begin at that key, whatever its number, and rows past the span's end read as zeros.  A wave skips tiles that none of its rows
+// sees, and compares row by row only where not all of its rows see the whole tile.  Query heads that share a key head share a workgroup,
+// which then holds 32 rows of four heads instead of 128 rows of one and walks fewer keys that some of its rows do not see.
+//
+// The backward is two kernels without atomics: dQ by blocks of rows, dK and dV by blocks of keys over all the query heads of a key head;
+// both form the weights again from the saved log-sum-exp.
+//
+// 16-bit types round the weights P and the score gradients dS to their type for the second product: half a step of each term, about what the
+// result's own rounding costs.  Half's range is helped by powers of two, taken out at the end: P goes in times 2^7 or 2^14, dS relative to the
+// largest dO of its row (dQ) or of the rows so far (dK).
+#pragma once
+#include "attention_docs_tiles.h"
+
+namespace zs {
+namespace {
+
+template <typename E> constexpr bool HALF = __is_same(E, f16);
+template <typename E> constexpr float P_LAG = HALF<E> ? 7.f : 0.f;     // forward: weights are at most 2^(8 + lag)
+template <typename E> constexpr float P_SHIFT = HALF<E> ? 14.f : 0.f;  // backward: weights times 2^shift
+template <typename E> constexpr int ROWS_LONG = sizeof(E) == 4 ? 32 : 64;   // rows of a tile where a wave takes all of them
+// 2^-e for the exponent e of x > 0, within what halves times it can use; 1 for 0, inf and NaN
+__device__ __forceinline__ float unit_of(float x) {
+  const int e = (int)((__float_as_uint(x) >> 23) & 255) - 127;
+  return e > 60 || e < -60 ? 1.f : __uint_as_float((unsigned)(127 - e) << 23);
+}
+
+// Blocks of rows behind one another, the last (under a causal mask the longest) first, all heads of a block before the next one; key heads in
+// the fastest place, so that the blocks of a key head stay on an XCD where there are 8 of them and find its keys in its L2.
+struct DocBlock { int block, kv, h; };
+__device__ __forceinline__ DocBlock row_block(const DocAttn& a, int heads, int rows) {   // heads of a key head in a workgroup, rows of a block
+  const int group = a.nh / a.nkv, sets = a.nkv * (group / heads), blocks = (a.T + rows - 1) / rows;
+  const int set = (int)blockIdx.x % sets, kv = set % a.nkv;
+  return DocBlock{blocks - 1 - (int)blockIdx.x / sets, kv, kv * group + set / a.nkv * heads};
+}
+
+// Calls of their own, not inlined, so that the registers of the kernels' loops are not planned around them.
+template <typename E, int NW>
+__device__ __attribute__((noinline)) void redo_fwd(DocRedo<NW>* redo, int groups, int row_groups, int t0, const int32_t* ranges, int T, int d, const E* q,
+                                                   int64_t ldq, const E* k, const E* v, int64_t ldkv, float scale, float softcap, const float* slopes,
+                                                   E* o, int64_t ldo) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for_dealt_rows(redo->masks, groups, NW, wave, [&](int g, int r) {
+    const int h = g / row_groups, i = t0 + 32 * (g % row_groups) + r;
+    const int4 range = doc_range((const int4*)ranges, i, T);
+    doc_fwd_row<E>(redo->rows[wave], i, range.x, range.y, d, DocRows<E>{q + h * d, ldq}, DocRows<E>{k, ldkv}, DocRows<E>{v, ldkv}, scale,
+                   DocScore{softcap, slopes ? slopes[h] : 0.f}, lane, [&](int c, float x) { o[i * ldo + h * d + c] = from_f<E>(x); });
+  });
+}
+
+// ------------------------------------------------------------------------------------------ forward
+// Four waves.  KS = 1: each has 32 rows of its own and walks all keys of a tile, two workgroups to a CU.  KS = 4: the four share 32 rows, each takes
+// 32 keys of a tile, and their sums meet at the end: for few rows.
+template <typename E, int D, int KS, int ROWS, int NBUF>
+__global__ __launch_bounds__(256, KS == 1 ? 2 : 1) void doc_fwd_kernel(DocAttn a, int heads) {
+  typedef Tile<E, D> TL;
+  typedef Mat<E> M;
+  constexpr int NW = 4, GROUPS = NW / KS, SUB = ROWS / 32 / KS, TILE = ROWS * TL::LD;
+  constexpr float LAG = P_LAG<E>;
+  constexpr size_t LOOP = NBUF * 2 * TILE * sizeof(E), END = sizeof(DocRedo<NW>) + 16 + GROUPS * 32 * TL::LD * sizeof(E);
+  __shared__ __align__(16) char smem_raw[LOOP > END ? LOOP : END];
+  static_assert(LOOP >= (size_t)(KS - 1) * GROUPS * TL::BLOCKS * 4 * 64 * 16, "");
+  E* smem = reinterpret_cast<E*>(smem_raw);                                                       // [NBUF][keys | values]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int ks = wave / GROUPS, grp = wave % GROUPS, row_groups = GROUPS / heads, h_in = grp / row_groups, dd = a.d;
+  const DocBlock blk = row_block(a, heads, 32 * row_groups);
+  const int t0 = blk.block * 32 * row_groups, w0 = t0 + 32 * (grp % row_groups), my_q = w0 + (lane & 31), h = blk.h + h_in;
+  const E* qh = (const E*)a.q + h * dd;
+  const E *kh = (const E*)a.k + blk.kv * dd, *vh = (const E*)a.v + blk.kv * dd;
+  const Span all = block_span<false>(a.ranges, t0, 32 * row_groups, a.T, lane);
+  const int4 range = my_q < a.T ? doc_range((const int4*)a.ranges, my_q, a.T) : make_int4(0, 0, 0, 0);
+  typename M::vec qf[TL::FRAGS];
+  TL::load_frags(qf, qh, a.ldq, my_q, a.T, lane, dd);
+  const DocScale sc = doc_scale<E>(a, h);
+  const int lo = range.x, seen = max(range.y - range.x, 0);   // keys
+  const Span mine = span_of(range.x, range.y);
+  const int tiles = (all.hi - all.lo + ROWS - 1) / ROWS;
+
+  TileLoad<E, D, ROWS, 256> kr, vr;
+  f32x16 oacc[TL::BLOCKS];
+#pragma unroll
+  for (int i = 0; i < TL::BLOCKS; ++i) oacc[i] = f32x16{};
+  float m = -INFINITY, l = 0.f;   // the reference of the weights, and their sum
+  if (tiles > 0) {
+    kr.fetch(kh, a.ldkv, all.lo, all.hi, tid, dd);
+    vr.fetch(vh, a.ldkv, all.lo, all.hi, tid, dd);
+    if (NBUF == 2) {
+      kr.put(smem, tid);
+      vr.put(smem + TILE, tid);
+      __syncthreads();
+    }
+  }
+  const float f = sc.factor();
+  for (int t = 0; t < tiles; ++t) {
+    const int key0 = all.lo + t * ROWS, at = NBUF == 2 ? (t & 1) * 2 * TILE : 0;
+    if (NBUF == 1) {
+      kr.put(smem, tid);
+      vr.put(smem + TILE, tid);
+      __syncthreads();
+    }
+    if (t + 1 < tiles) {
+      kr.fetch(kh, a.ldkv, key0 + ROWS, all.hi, tid, dd);
+      vr.fetch(vh, a.ldkv, key0 + ROWS, all.hi, tid, dd);
+    }
+    const E *Kt = smem + at + ks * 32 * SUB * TL::LD, *Vt = Kt + TILE;
+    const int kb = key0 + ks * 32 * SUB;
+    if (kb < mine.hi && kb + 32 * SUB > mine.lo) {
+      f32x16 s[SUB];
+#pragma unroll
+      for (int j = 0; j < SUB; ++j) {
+        s[j] = f32x16{};
+#pragma unroll
+        for (int c = 0; c < TL::FRAGS; ++c) s[j] = M::rows(TL::frag(Kt, 32 * j, c, lane), qf[c], s[j]);
+      }
+#pragma unroll
+      for (int j = 0; j < SUB; ++j) doc_scores<E>(s[j], sc, (float)(kb + 32 * j + 4 * (lane >> 5) - my_q));
+      if (kb < mine.all_lo || kb + 32 * SUB > mine.all_hi) {   // not every row sees every key
+#pragma unroll
+        for (int j = 0; j < SUB; ++j) {
+          const int from = kb + 32 * j + 4 * (lane >> 5) - lo;
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if ((unsigned)(from + 8 * (r >> 2) + (r & 3)) >= (unsigned)seen) s[j][r] = -INFINITY;
+        }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < SUB; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[j][r]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * f;   // f > 0
+      // The reference moves only when some row's maximum has outgrown it by 2^8: weights are at most 2^(8 + LAG), the sums and the result refer to the
+      // same reference whenever it moves.
+      if (__any(mx > m + (8.f + LAG))) {
+        const float mn = fmaxf(m, mx - LAG), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+        l *= alpha;
+        m = mn;
+#pragma unroll
+        for (int i = 0; i < TL::BLOCKS; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) oacc[i][r] *= alpha;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;   // no key seen so far: every weight is exp2(-inf)
+      float part[2] = {0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < SUB; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(s[j][r], f, -ref));
+          s[j][r] = p;
+          part[r & 1] += p;
+        }
+      const float sum = part[0] + part[1];
+      l += sum + __shfl_xor(sum, 32, 64);
+#pragma unroll
+      for (int j = 0; j < SUB; ++j)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const typename M::col8 pf = M::pack(s[j], u);
+#pragma unroll
+          for (int b = 0; b < TL::BLOCKS; ++b) oacc[b] = M::cols(M::template col<TL::LD>(Vt, 32 * j + 16 * u, 32 * b, lane), pf, oacc[b]);
+        }
+    }
+    if (NBUF == 2 && t + 1 < tiles) {   // the other buffer was last read before the barrier that ended the iteration before
+      kr.put(smem + ((t + 1) & 1) * 2 * TILE, tid);
+      vr.put(smem + ((t + 1) & 1) * 2 * TILE + TILE, tid);
+    }
+    __syncthreads();
+  }
+  if constexpr (KS > 1) {
+    float* stat = reinterpret_cast<float*>(smem_raw);   // [KS][m | l][32]
+    if (lane < 32) {
+      stat[ks * 64 + lane] = m;
+      stat[ks * 64 + 32 + lane] = l;
+    }
+    __syncthreads();
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < KS; ++w) top = fmaxf(top, stat[w * 64 + (lane & 31)]);
+    const float ref = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f(m - ref);
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < KS; ++w) l += stat[w * 64 + 32 + (lane & 31)] * __builtin_amdgcn_exp2f(stat[w * 64 + (lane & 31)] - ref);
+    m = top;
+#pragma unroll
+    for (int i = 0; i < TL::BLOCKS; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) oacc[i][r] *= alpha;
+    __syncthreads();
+    merge_waves<TL::BLOCKS>(oacc, reinterpret_cast<f32x4*>(smem_raw), ks, KS, lane);
+  }
+  const bool live = seen > 0 && my_q < a.T;
+  DocRedo<NW>& redo = *reinterpret_cast<DocRedo<NW>*>(smem_raw);
+  const unsigned again = redo_rows<NW>(redo, grp, ks == 0, ks == 0 && live && !(mark_of(oacc) + l * 0.f == 0.f));
+  if (ks == 0) {
+    if (!live) {
+#pragma unroll
+      for (int i = 0; i < TL::BLOCKS; ++i) oacc[i] = f32x16{};
+    }
+    TL::store(oacc, live ? 1.f / l : 0.f, reinterpret_cast<E*>(smem_raw + (sizeof(redo) + 15) / 16 * 16) + grp * 32 * TL::LD, (E*)a.o + h * dd, a.ldo, w0, a.T,
+              lane, dd, again);
+    if (lane < 32 && my_q < a.T)
+      a.lse[(int64_t)h * a.T + my_q] = live ? (float)((double)m * 0.6931471805599453 + (double)logf(l)) : -INFINITY;
+  }
+  if (__builtin_expect(any_row(redo.masks, GROUPS, lane), 0))
+    redo_fwd<E, NW>(&redo, GROUPS, row_groups, t0, a.ranges, a.T, dd, (const E*)a.q + blk.h * dd, a.ldq, kh, vh, a.ldkv, a.scale, a.softcap,
+                    a.slopes ? a.slopes + blk.h : nullptr, (E*)a.o + blk.h * dd, a.ldo);
+}
+
+// ------------------------------------------------------------------------------------------ dQ
+// dQ^T += K^T dS^T, dS^T = P^T (dP^T - delta), dP^T = V dO^T.  Waves as in the forward; the one that has a row's dO forms its delta = dO.o and leaves
+// it, and in half the row's largest |dO|, for the other kernel.
+template <typename E, int NW>
+__device__ __attribute__((noinline)) void redo_dq(DocRedo<NW>* redo, int groups, int row_groups, int t0, const int32_t* ranges, int T, int d, const E* q,
+                                                  int64_t ldq, const E* k, const E* v, int64_t ldkv, const E* dout, int64_t ldo, const float* lse,
+                                                  const float* delta, float scale, float softcap, const float* slopes, E* dq, int64_t lddq) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for_dealt_rows(redo->masks, groups, NW, wave, [&](int g, int r) {
+    const int h = g / row_groups, i = t0 + 32 * (g % row_groups) + r;
+    const int4 range = doc_range((const int4*)ranges, i, T);
+    doc_dq_row<E>(redo->rows[wave], i, range.x, range.y, d, DocRows<E>{q + h * d, ldq}, DocRows<E>{k, ldkv}, DocRows<E>{v, ldkv},
+                  DocRows<E>{dout + h * d, ldo}, lse[(int64_t)h * T + i], delta[(int64_t)h * T + i], scale, DocScore{softcap, slopes ? slopes[h] : 0.f}, lane,
+                  [&](int c, float x) { dq[i * lddq + h * d + c] = from_f<E>(x); });
+  });
+}
+
+template <typename E, int D, int KS, int ROWS, int NBUF>
+__global__ __launch_bounds__(256, KS == 1 && sizeof(E) == 2 ? 2 : 1) void doc_dq_kernel(DocAttn a, int heads) {
+  typedef Tile<E, D> TL;
+  typedef Mat<E> M;
+  constexpr int NW = 4, GROUPS = NW / KS, SUB = ROWS / 32 / KS, TILE = ROWS * TL::LD;
+  constexpr size_t LOOP = NBUF * 2 * TILE * sizeof(E), END = sizeof(DocRedo<NW>) + 16 + GROUPS * 32 * TL::LD * sizeof(E);
+  __shared__ __align__(16) char smem_raw[LOOP > END ? LOOP : END];
+  static_assert(LOOP >= (size_t)(KS - 1) * GROUPS * TL::BLOCKS * 4 * 64 * 16, "");
+  E* smem = reinterpret_cast<E*>(smem_raw);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int ks = wave / GROUPS, grp = wave % GROUPS, row_groups = GROUPS / heads, h_in = grp / row_groups, dd = a.d;
+  const DocBlock blk = row_block(a, heads, 32 * row_groups);
+  const int t0 = blk.block * 32 * row_groups, w0 = t0 + 32 * (grp % row_groups), my_q = w0 + (lane & 31), h = blk.h + h_in;
+  const E *kh = (const E*)a.k + blk.kv * dd, *vh = (const E*)a.v + blk.kv * dd;
+  const Span all = block_span<false>(a.ranges, t0, 32 * row_groups, a.T, lane);
+  const int4 range = my_q < a.T ? doc_range((const int4*)a.ranges, my_q, a.T) : make_int4(0, 0, 0, 0);
+  const int lo = range.x, seen = max(range.y - range.x, 0);
+  const bool live = seen > 0 && my_q < a.T;
+  typename M::vec qf[TL::FRAGS], dof[TL::FRAGS];
+  TL::load_frags(qf, (const E*)a.q + h * dd, a.ldq, my_q, a.T, lane, dd);
+  TL::load_frags(dof, (const E*)a.dout + h * dd, a.ldo, my_q, a.T, lane, dd);
+  const int64_t stat = (int64_t)h * a.T + min(my_q, a.T - 1);
+  const float lse2 = live ? a.lse[stat] * DOC_LOG2E : 0.f;
+  const DocScale sc = doc_scale<E>(a, h);
+  const Span mine = span_of(range.x, range.y);
+  const int tiles = (all.hi - all.lo + ROWS - 1) / ROWS;
+  TileLoad<E, D, ROWS, 256> kr, vr;
+  if (tiles > 0) {   // in flight while delta is formed
+    kr.fetch(kh, a.ldkv, all.lo, all.hi, tid, dd);
+    vr.fetch(vh, a.ldkv, all.lo, all.hi, tid, dd);
+  }
+  float delta = 0.f, largest = 0.f;
+  {
+    typename M::vec of[TL::FRAGS];
+    TL::load_frags(of, (const E*)a.o + h * dd, a.ldo, my_q, a.T, lane, dd);
+#pragma unroll
+    for (int c = 0; c < TL::FRAGS; ++c)
+#pragma unroll
+      for (int e = 0; e < TL::VN; ++e) {
+        delta = fmaf((float)dof[c][e], (float)of[c][e], delta);
+        if constexpr (HALF<E>) largest = fmaxf(largest, fabsf((float)dof[c][e]));
+      }
+    delta += __shfl_xor(delta, 32, 64);
+    if constexpr (HALF<E>) largest = fmaxf(largest, __shfl_xor(largest, 32, 64));
+    if (ks == 0 && lane < 32 && my_q < a.T) {
+      a.delta[stat] = delta;
+      if constexpr (HALF<E>) a.delta[(int64_t)a.nh * a.T + stat] = largest;
+    }
+  }
+  const float unit = HALF<E> ? unit_of(largest) : 1.f;
+  f32x16 acc[TL::BLOCKS];
+#pragma unroll
+  for (int i = 0; i < TL::BLOCKS; ++i) acc[i] = f32x16{};
+  if (NBUF == 2 && tiles > 0) {
+    kr.put(smem, tid);
+    vr.put(smem + TILE, tid);
+    __syncthreads();
+  }
+  for (int t = 0; t < tiles; ++t) {
+    const int key0 = all.lo + t * ROWS, at = NBUF == 2 ? (t & 1) * 2 * TILE : 0;
+    if (NBUF == 1) {
+      kr.put(smem, tid);
+      vr.put(smem + TILE, tid);
+      __syncthreads();
+    }
+    if (t + 1 < tiles) {
+      kr.fetch(kh, a.ldkv, key0 + ROWS, all.hi, tid, dd);
+      vr.fetch(vh, a.ldkv, key0 + ROWS, all.hi, tid, dd);
+    }
+    const E *Kt = smem + at + ks * 32 * SUB * TL::LD, *Vt = Kt + TILE;
+    const int kb0 = key0 + ks * 32 * SUB;
+    if (kb0 < mine.hi && kb0 + 32 * SUB > mine.lo) {
+      const bool part = kb0 < mine.all_lo || kb0 + 32 * SUB > mine.all_hi;
+#pragma unroll
+      for (int j = 0; j < SUB; ++j) {
+        const int kb = kb0 + 32 * j;
+        f32x16 s = f32x16{}, dp = f32x16{};
+#pragma unroll
+        for (int c = 0; c < TL::FRAGS; ++c) {
+          s = M::rows(TL::frag(Kt, 32 * j, c, lane), qf[c], s);
+          dp = M::rows(TL::frag(Vt, 32 * j, c, lane), dof[c], dp);
+        }
+        doc_weights<E>(s, dp, sc, (float)(kb + 4 * (lane >> 5) - my_q), 0.f, unit, [&](int) { return lse2; }, [&](int) { return delta; });
+        if (part) {
+          const int from = kb + 4 * (lane >> 5) - lo;
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if ((unsigned)(from + 8 * (r >> 2) + (r & 3)) >= (unsigned)seen) dp[r] = 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const typename M::col8 df = M::pack(dp, u);
+#pragma unroll
+          for (int b = 0; b < TL::BLOCKS; ++b) acc[b] = M::cols(M::template col<TL::LD>(Kt, 32 * j + 16 * u, 32 * b, lane), df, acc[b]);
+        }
+      }
+    }
+    if (NBUF == 2 && t + 1 < tiles) {
+      kr.put(smem + ((t + 1) & 1) * 2 * TILE, tid);
+      vr.put(smem + ((t + 1) & 1) * 2 * TILE + TILE, tid);
+    }
+    __syncthreads();
+  }
+  if constexpr (KS > 1) merge_waves<TL::BLOCKS>(acc, reinterpret_cast<f32x4*>(smem_raw), ks, KS, lane);
+  DocRedo<NW>& redo = *reinterpret_cast<DocRedo<NW>*>(smem_raw);
+  const unsigned again = redo_rows<NW>(redo, grp, ks == 0, ks == 0 && live && !(mark_of(acc) == 0.f));
+  if (ks == 0) {
+    if (!live) {
+#pragma unroll
+      for (int i = 0; i < TL::BLOCKS; ++i) acc[i] = f32x16{};
+    }
+    TL::store(acc, a.scale / unit, reinterpret_cast<E*>(smem_raw + (sizeof(redo) + 15) / 16 * 16) + grp * 32 * TL::LD, (E*)a.dq + h * dd, a.lddq, w0, a.T,
+              lane, dd, again);
+  }
+  if (__builtin_expect(any_row(redo.masks, GROUPS, lane), 0))   // the rows' delta: written by this workgroup, before its barrier
+    redo_dq<E, NW>(&redo, GROUPS, row_groups, t0, a.ranges, a.T, dd, (const E*)a.q + blk.h * dd, a.ldq, kh, vh, a.ldkv, (const E*)a.dout + blk.h * dd, a.ldo,
+                   a.lse + (int64_t)blk.h * a.T, a.delta + (int64_t)blk.h * a.T, a.scale, a.softcap, a.slopes ? a.slopes + blk.h : nullptr,
+                   (E*)a.dq + blk.h * dd, a.lddq);
+}
+
+// ------------------------------------------------------------------------------------------ dK, dV
+// dV^T += dO^T P, dK^T += Q^T dS with S = Q K^T: lanes are keys, registers rows.  KG groups of 32 keys, each with QS waves, which share out the rows of a
+// tile; a wave's V rows sit in LDS, which leaves registers for two waves per SIMD.
+template <typename E, int NW>
+__device__ __attribute__((noinline)) void redo_dkv(DocRedo<NW>* redo, int groups, int t0, const int32_t* ranges, int T, int d, int group, const E* q,
+                                                   int64_t ldq, const E* k, const E* v, int64_t ldkv, const E* dout, int64_t ldo, const float* lse,
+                                                   const float* delta, float scale, float softcap, const float* slopes, E* dk, E* dv, int64_t lddkv) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for_dealt_rows(redo->masks, groups, NW, wave, [&](int g, int r) {
+    const int j = t0 + 32 * g + r;
+    const int4 range = doc_range((const int4*)ranges, j, T);
+    wave_lds_order();
+    row_to_lds(redo->rows[wave], k + j * ldkv, d, lane);
+    row_to_lds(redo->rows[wave] + 128, v + j * ldkv, d, lane);
+    wave_lds_order();
+    float xk[2] = {0.f, 0.f}, xv[2] = {0.f, 0.f};
+    for (int h = 0; h < group; ++h)
+      doc_dkv_head<E>(redo->rows[wave], j, range.z, range.w, d, DocRows<E>{q + h * d, ldq}, DocRows<E>{dout + h * d, ldo}, lse + (int64_t)h * T,
+                      delta + (int64_t)h * T, scale, DocScore{softcap, slopes ? slopes[h] : 0.f}, lane, xk, xv);
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+      if (64 * c + lane < d) {
+        dk[j * lddkv + 64 * c + lane] = from_f<E>(xk[c] * scale);
+        dv[j * lddkv + 64 * c + lane] = from_f<E>(xv[c]);
+      }
+  });
+}
+
+template <typename E, int D, int KG, int QS, int ROWS, int NBUF>
+__global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __launch_bounds__(64 * KG * QS) void doc_dkv_kernel(DocAttn a) {
+  typedef Tile<E, D> TL;
+  typedef Mat<E> M;
+  constexpr int NW = KG * QS, NT = 64 * NW, SUB = ROWS / 32 / QS, TILE = ROWS * TL::LD, STATS = HALF<E> ? 3 : 2;
+  struct Lds {
+    E tile[NBUF][2][TILE];          // Q, dO
+    float stat[NBUF][STATS][ROWS];  // log-sum-exp in powers of two, delta, (half) largest |dO|
+    E v[KG * 32 * TL::LD];
+  };
+  static_assert(ROWS <= NT, "");
+  __shared__ __align__(16) char smem_raw[sizeof(Lds)];
+  static_assert(sizeof(smem_raw) >= sizeof(DocRedo<NW>) + 16 + KG * 32 * TL::LD * sizeof(E), "");
+  static_assert(sizeof(smem_raw) >= (size_t)(QS - 1) * KG * TL::BLOCKS * 4 * 64 * 16, "");
+  Lds& lds = *reinterpret_cast<Lds*>(smem_raw);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int qs = wave / KG, kg = wave % KG, dd = a.d, group = a.nh / a.nkv;
+  const int kv = (int)blockIdx.x % a.nkv, t0 = (int)blockIdx.x / a.nkv * 32 * KG;   // early keys, under a causal mask seen by the most rows, first
+  const int w0 = t0 + 32 * kg, my_k = w0 + (lane & 31);
+  const E *kh = (const E*)a.k + kv * dd, *vh = (const E*)a.v + kv * dd;
+  const Span all = block_span<true>(a.ranges, t0, 32 * KG, a.T, lane);
+  const int4 range = my_k < a.T ? doc_range((const int4*)a.ranges, my_k, a.T) : make_int4(0, 0, 0, 0);
+  const int lo = range.z, seen = max(range.w - range.z, 0);
+  typename M::vec kf[TL::FRAGS];
+  TL::load_frags(kf, kh, a.ldkv, my_k, a.T, lane, dd);
+  const Span mine = span_of(range.z, range.w);
+  const int tiles = (all.hi - all.lo + ROWS - 1) / ROWS, total = tiles * group;
+  E* Vw = lds.v + kg * 32 * TL::LD;
+  if (qs == 0) {
+    typename M::vec vf[TL::FRAGS];
+    constexpr int P = D / TL::VN;
+#pragma unroll
+    for (int i = 0; i < TL::FRAGS; ++i) {
+      const int p = lane + 64 * i, r = p / P, c = p % P * TL::VN;
+      vf[i] = typename M::vec{};
+      if (w0 + r < a.T && c < dd) vf[i] = *reinterpret_cast<const typename M::vec*>(vh + (w0 + r) * a.ldkv + c);
+    }
+#pragma unroll
+    for (int i = 0; i < TL::FRAGS; ++i) {
+      const int p = lane + 64 * i;
+      *reinterpret_cast<typename M::vec*>(Vw + p / P * TL::LD + p % P * TL::VN) = vf[i];
+    }
+  }
+  TileLoad<E, D, ROWS, NT> qr, dr;
+  float sr[STATS];
+  auto fetch = [&](int h, int row0) {
+    qr.fetch((const E*)a.q + h * dd, a.ldq, row0, all.hi, tid, dd);
+    dr.fetch((const E*)a.dout + h * dd, a.ldo, row0, all.hi, tid, dd);
+    if (tid < ROWS) {
+      const int64_t at = (int64_t)h * a.T + min(row0 + tid, a.T - 1);
+      sr[0] = a.lse[at];
+      sr[1] = a.delta[at];
+      if constexpr (HALF<E>) sr[2] = a.delta[(int64_t)a.nh * a.T + at];
+    }
+  };
+  auto put = [&](int buf, int row0) {
+    qr.put(lds.tile[buf][0], tid);
+    dr.put(lds.tile[buf][1], tid);
+    if (tid < ROWS) {   // rows past the end: zeros, whose weights 1 meet rows of zeros
+      const bool in = row0 + tid < all.hi;
+      lds.stat[buf][0][tid] = in ? sr[0] * DOC_LOG2E : 0.f;
+      lds.stat[buf][1][tid] = in ? sr[1] : 0.f;
+      if constexpr (HALF<E>) lds.stat[buf][2][tid] = in ? sr[2] : 0.f;
+    }
+  };
+  f32x16 dk[TL::BLOCKS], dv[TL::BLOCKS];
+#pragma unroll
+  for (int i = 0; i < TL::BLOCKS; ++i) dk[i] = dv[i] = f32x16{};
+  float unit = 0.f;   // half: of the score gradients, none yet
+  int h = kv * group, t = 0;
+  if (total > 0) {
+    fetch(h, all.lo);
+    if (NBUF == 2) put(0, all.lo);
+  }
+  __syncthreads();
+  DocScale sc = doc_scale<E>(a, h);
+  for (int it = 0; it < total; ++it) {
+    const int row0 = all.lo + t * ROWS, buf = NBUF == 2 ? it & 1 : 0;
+    const int tn = t + 1 < tiles ? t + 1 : 0, hn = tn ? h : h + 1, rown = all.lo + tn * ROWS;
+    if (NBUF == 1) {
+      put(0, row0);
+      __syncthreads();
+    }
+    if (it + 1 < total) fetch(hn, rown);
+    const E *Qt = lds.tile[buf][0] + qs * 32 * SUB * TL::LD, *Dt = lds.tile[buf][1] + qs * 32 * SUB * TL::LD;
+    const int rb0 = row0 + qs * 32 * SUB;
+    if (rb0 < mine.hi && rb0 + 32 * SUB > mine.lo) {
+      const bool part = rb0 < mine.all_lo || rb0 + 32 * SUB > mine.all_hi;
+#pragma unroll
+      for (int j = 0; j < SUB; ++j) {
+        const int rb = rb0 + 32 * j;
+        const float* st = lds.stat[buf][0] + qs * 32 * SUB + 32 * j;
+        f32x16 s = f32x16{}, dp = f32x16{};
+#pragma unroll
+        for (int c = 0; c < TL::FRAGS; ++c) {
+          s = M::rows(TL::frag(Qt, 32 * j, c, lane), kf[c], s);
+          dp = M::rows(TL::frag(Dt, 32 * j, c, lane), TL::frag(Vw, 0, c, lane), dp);
+        }
+        if constexpr (HALF<E>) {   // the unit follows the largest |dO| so far
+          const float top = wave_max(st[2 * ROWS + (lane & 31)]), now = unit_of(top);
+          if (top > 0.f && (unit == 0.f || now < unit)) {
+            const float f = unit == 0.f ? 1.f : now / unit;
+            unit = now;
+#pragma unroll
+            for (int b = 0; b < TL::BLOCKS; ++b)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) dk[b][r] *= f;
+          }
+        }
+        f32x4 lse2[4], delta[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          lse2[c] = *reinterpret_cast<const f32x4*>(st + 8 * c + 4 * (lane >> 5));
+          delta[c] = *reinterpret_cast<const f32x4*>(st + ROWS + 8 * c + 4 * (lane >> 5));
+        }
+        doc_weights<E>(s, dp, sc, (float)(rb + 4 * (lane >> 5) - my_k), P_SHIFT<E>, HALF<E> ? unit / 16384.f : 1.f,
+                       [&](int r) { return lse2[r >> 2][r & 3]; }, [&](int r) { return delta[r >> 2][r & 3]; });
+        if (part) {
+          const int from = rb + 4 * (lane >> 5) - lo;
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if ((unsigned)(from + 8 * (r >> 2) + (r & 3)) >= (unsigned)seen) s[r] = dp[r] = 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const typename M::col8 pf = M::pack(s, u), df = M::pack(dp, u);
+#pragma unroll
+          for (int b = 0; b < TL::BLOCKS; ++b) {
+            dv[b] = M::cols(M::template col<TL::LD>(Dt, 32 * j + 16 * u, 32 * b, lane), pf, dv[b]);
+            dk[b] = M::cols(M::template col<TL::LD>(Qt, 32 * j + 16 * u, 32 * b, lane), df, dk[b]);
+          }
+        }
+      }
+    }
+    if (NBUF == 2 && it + 1 < total) put(buf ^ 1, rown);
+    __syncthreads();
+    if (hn != h && it + 1 < total) sc = doc_scale<E>(a, hn);
+    t = tn;
+    h = hn;
+  }
+  if constexpr (HALF<E>) {
+    if constexpr (QS > 1) {   // the waves that share keys bring theirs to the unit of 1 before they add
+      const float f = unit == 0.f ? 1.f : 1.f / unit;
+#pragma unroll
+      for (int b = 0; b < TL::BLOCKS; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dk[b][r] *= f;
+      unit = 1.f;
+    }
+  }
+  if constexpr (QS > 1) {
+    f32x4* red = reinterpret_cast<f32x4*>(smem_raw) + kg * (QS - 1) * TL::BLOCKS * 4 * 64;
+    merge_waves<TL::BLOCKS>(dv, red, qs, QS, lane);
+    merge_waves<TL::BLOCKS>(dk, red, qs, QS, lane);
+  }
+  const bool live = seen > 0 && my_k < a.T;
+  DocRedo<NW>& redo = *reinterpret_cast<DocRedo<NW>*>(smem_raw);
+  const unsigned again = redo_rows<NW>(redo, kg, qs == 0, qs == 0 && live && !(mark_of(dk) + mark_of(dv) == 0.f));
+  if (qs == 0) {
+    if (!live) {
+#pragma unroll
+      for (int i = 0; i < TL::BLOCKS; ++i) dk[i] = dv[i] = f32x16{};
+    }
+    E* to = reinterpret_cast<E*>(smem_raw + (sizeof(redo) + 15) / 16 * 16) + kg * 32 * TL::LD;
+    TL::store(dv, HALF<E> ? 1.f / 16384.f : 1.f, to, (E*)a.dv + kv * dd, a.lddkv, w0, a.T, lane, dd, again);
+    TL::store(dk, HALF<E> && unit != 0.f ? a.scale / unit : a.scale, to, (E*)a.dk + kv * dd, a.lddkv, w0, a.T, lane, dd, again);
+  }
+  if (__builtin_expect(any_row(redo.masks, KG, lane), 0))
+    redo_dkv<E, NW>(&redo, KG, t0, a.ranges, a.T, dd, group, (const E*)a.q + kv * group * dd, a.ldq, kh, vh, a.ldkv, (const E*)a.dout + kv * group * dd,
+                    a.ldo, a.lse + (int64_t)kv * group * a.T, a.delta + (int64_t)kv * group * a.T, a.scale, a.softcap,
+                    a.slopes ? a.slopes + kv * group : nullptr, (E*)a.dk + kv * dd, (E*)a.dv + kv * dd, a.lddkv);
+}
+
+// Heads of a key head that share a workgroup of `groups` waves.
+inline int doc_heads(const DocAttn& a, int groups) {
+  const int group = a.nh / a.nkv;
+  return groups % 4 == 0 && group % 4 == 0 ? 4 : groups % 2 == 0 && group % 2 == 0 ? 2 : 1;
+}
+// Few blocks of 128 rows: waves share 32 rows, so that there are four times as many workgroups.
+inline bool doc_few(int64_t rows_times_heads) { return cdiv(rows_times_heads, 128) < 256; }
+
+template <typename E, int D> hipError_t doc_fwd(hipStream_t st, const DocAttn& a) {
+  if (doc_few((int64_t)a.T * a.nh)) {
+    hipLaunchKernelGGL((doc_fwd_kernel<E, D, 4, 128, sizeof(E) == 4 ? 1 : 2>), dim3((unsigned)(cdiv(a.T, 32) * a.nh)), dim3(256), 0, st, a, 1);
+  } else {
+    const int heads = doc_heads(a, 4);
+    hipLaunchKernelGGL((doc_fwd_kernel<E, D, 1, ROWS_LONG<E>, 2>), dim3((unsigned)(cdiv(a.T, 128 / heads) * (a.nh / heads))), dim3(256), 0, st, a, heads);
+  }
+  return hipGetLastError();
+}
+template <typename E, int D> hipError_t doc_bwd(hipStream_t st, const DocAttn& a) {
+  if (doc_few((int64_t)a.T * a.nh)) {
+    hipLaunchKernelGGL((doc_dq_kernel<E, D, 4, 128, sizeof(E) == 4 ? 1 : 2>), dim3((unsigned)(cdiv(a.T, 32) * a.nh)), dim3(256), 0, st, a, 1);
+  } else {
+    const int heads = doc_heads(a, 4);
+    hipLaunchKernelGGL((doc_dq_kernel<E, D, 1, ROWS_LONG<E>, 2>), dim3((unsigned)(cdiv(a.T, 128 / heads) * (a.nh / heads))), dim3(256), 0, st, a, heads);
+  }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (doc_few((int64_t)a.T * a.nkv)) {
+    hipLaunchKernelGGL((doc_dkv_kernel<E, D, 1, 4, 128, 1>), dim3((unsigned)(cdiv(a.T, 32) * a.nkv)), dim3(256), 0, st, a);
+  } else if constexpr (sizeof(E) == 4) {
+    hipLaunchKernelGGL((doc_dkv_kernel<E, D, 4, 1, 32, 2>), dim3((unsigned)(cdiv(a.T, 128) * a.nkv)), dim3(256), 0, st, a);
+  } else {
+    hipLaunchKernelGGL((doc_dkv_kernel<E, D, 4, 2, 64, 2>), dim3((unsigned)(cdiv(a.T, 128) * a.nkv)), dim3(512), 0, st, a);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Heads are padded with zeros to D = 64, 96 or 128.
+template <typename E> hipError_t doc_attention(hipStream_t st, const DocAttn& a, bool backward) {
+  if (a.d <= 64) return backward ? doc_bwd<E, 64>(st, a) : doc_fwd<E, 64>(st, a);
+  if (a.d <= 96) return backward ? doc_bwd<E, 96>(st, a) : doc_fwd<E, 96>(st, a);
+  return backward ? doc_bwd<E, 128>(st, a) : doc_fwd<E, 128>(st, a);
+}
+
+}  // namespace zs

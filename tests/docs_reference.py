@@ -4,7 +4,8 @@ The bounds are worst cases of the roundings that the kernels make, element by el
 - scores: sums of d exact products in fp32, (d + 8) 2^-24 of the sum of absolute values; the cap, the bias and the change to powers of two,
   a few 2^-24 of their magnitudes.  An absolute error e of a score is a relative one of its weight.
 - weights and their derivatives go into the second product in the tensors' type: half a step, u = finfo.eps / 2, of each, and in half
-  never less than half the smallest subnormal step, 2^-25.
+  never less than half the smallest subnormal step, 2^-25.  In fp32 and bf16 a weight below the smallest normal number, 2^-126, may become zero
+  (exp(-87.4) = 2^-126.1 does on the hardware): off by up to 2^-126, times what the weight is multiplied by.
 - that product's sums of n terms in fp32: (n + 8) 2^-24 of the sum of absolute values.
 - the result: u of itself."""
 import math
@@ -113,7 +114,7 @@ def forward_bounds(c, dtype, q, k, v):
     pv, n = p @ V.abs(), m.sum(1).double()
     e = (err * m).amax(-1) + (n + 8) * E24       # of a weight, relative; the row sum's too
     up = 0.0 if dtype == 0 else u
-    ob = (2 * e[..., None] + up + (n[:, None] + 8) * E24) * pv + (0.0 if dtype == 0 else tiny) * (m.double() @ V.abs())
+    ob = (2 * e[..., None] + up + (n[:, None] + 8) * E24) * pv + tiny * (m.double() @ V.abs())
     ob = ob + u * ((p @ V).abs() + ob) + tiny
     lse = torch.logsumexp(s.masked_fill(~m, -1e300), -1)
     return rows(ob), e + 4 * lse.abs() * E24 * (n > 0)
@@ -140,11 +141,11 @@ def _backward(c, dtype, q, k, v, o, lse, dout):
     if dtype is None:
         return rows(ds @ K) * c.scale, shared(ds.transpose(1, 2) @ Q) * c.scale, shared(p.transpose(1, 2) @ D)
     u, tiny = round_step(dtype)
-    up, t = (0.0, 0.0) if dtype == 0 else (u, tiny)
+    up, t = 0.0 if dtype == 0 else u, tiny
     e = err + 8 * E24
     # of ds: the weight's error, that of dp - delta (sums of d products), that of the slope
     size = D.abs() @ V.abs().transpose(1, 2) + (D.abs() * O.abs()).sum(-1, keepdim=True)
-    dds = ds.abs() * (e + 8 * E24) + p * slope * size * (c.d + 8) * E24 + p * (dp - delta).abs() * 8 * E24 * (c.softcap > 0)
+    dds = ds.abs() * (e + 8 * E24) + p * slope * size * (c.d + 8) * E24 + p * (dp - delta).abs() * 8 * E24 * (c.softcap > 0) + 2.0 ** -126 * size
     n = float(max(c.lengths, default=0))
     sums = lambda terms, errs: errs + terms * (up + (n + 8) * E24)
     # in half, ds is rounded in steps that may be as coarse as 2^-25 of the largest magnitude that its rows' gradient has

@@ -180,18 +180,20 @@ def test_non_finite_values_stay_in_their_document(gpu_device, dtype, value, name
     rows = (hidden < 60) | (hidden >= 140)                # rows that do not see token 60
     if name in ("q", "dout"):
         rows = hidden != 60                               # only its own row takes part in the forward
+    want, wl = ref.forward(c, r.q, r.k, r.v)
     bo, bl = ref.forward_bounds(c, dtype, r.q, r.k, r.v)
-    saved = clean[:2]
-    bounds = ref.backward_bounds(c, dtype, r.q, r.k, r.v, *saved, r.dout)
-    ref.within(o[rows], clean[0][rows], 2 * bo[rows], "o")
-    ref.within(lse[:, rows], clean[1][:, rows], 2 * bl[:, rows], "lse")
-    ref.within(dq[rows], clean[2][rows], 2 * bounds[0][rows], "dq")
+    ref.within(o[rows], want[rows], bo[rows], "o")
+    ref.within(lse[:, rows], wl[:, rows], bl[:, rows], "lse")
+    # the gradients' formulas with what this run saved: a row that was computed again may have an o that rounds otherwise
+    saved = (torch.where(rows[:, None], o, clean[0]), torch.where(rows, lse, clean[1]))
+    want, bounds = (f(*x, r.q, r.k, r.v, *saved, r.dout) for f, x in ((ref.backward, (c,)), (ref.backward_bounds, (c, dtype))))
+    ref.within(dq[rows], want[0][rows], bounds[0][rows], "dq")
     # keys whose rows are all fine: after a bad key or value, those of the rows that see it are not
     keys = (hidden < 40) | (hidden >= 140)
     if name in ("q", "dout"):
         keys = (hidden < 40) | (hidden > 60)
-    ref.within(dk[keys], clean[3][keys], 2 * bounds[1][keys], "dk")
-    ref.within(dv[keys], clean[4][keys], 2 * bounds[2][keys], "dv")
+    ref.within(dk[keys], want[1][keys], bounds[1][keys], "dk")
+    ref.within(dv[keys], want[2][keys], bounds[2][keys], "dv")
     if math.isnan(value):                                 # and what it reaches is not hidden
         bad = {"k": o, "v": o, "q": o, "dout": dv}[name]
         assert bad[60].isnan().any() and (name not in ("k", "v") or bad[139].isnan().any())
