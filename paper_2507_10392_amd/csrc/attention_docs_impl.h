@@ -54,17 +54,16 @@ __device__ __attribute__((noinline)) void redo_fwd(DocRedo<NW>* redo, int groups
 // ------------------------------------------------------------------------------------------ forward
 // Four waves.  KS = 1: each has 32 rows of its own and walks all keys of a tile, two workgroups to a CU.  KS = 4: the four share 32 rows, each takes
 // 32 keys of a tile, and their sums meet at the end: for few rows.
-template <typename E, int D, int KS, int ROWS, int NBUF>
+template <typename E, int D, int MODE, int KS, int ROWS, int NBUF>
 __global__ __launch_bounds__(256, KS == 1 ? 2 : 1) void doc_fwd_kernel(DocAttn a, int heads) {
   typedef Tile<E, D> TL;
   typedef Mat<E> M;
-  constexpr int NW = 4, GROUPS = NW / KS, SUB = ROWS / 32 / KS, TILE = ROWS * TL::LD;
+  constexpr int NW = 4, GROUPS = NW / KS, SUB = ROWS / 32 / KS, TILE = TL::bytes(ROWS);
   constexpr float LAG = P_LAG<E>;
-  constexpr size_t LOOP = NBUF * 2 * TILE * sizeof(E), END = sizeof(DocRedo<NW>) + 16 + GROUPS * 32 * TL::LD * sizeof(E);
+  constexpr size_t LOOP = NBUF * 2 * TILE, END = sizeof(DocRedo<NW>) + 16 + GROUPS * TL::STORE;   // [NBUF][keys | values]
   __shared__ __align__(16) char smem_raw[LOOP > END ? LOOP : END];
   static_assert(LOOP >= (size_t)(KS - 1) * GROUPS * TL::BLOCKS * 4 * 64 * 16, "");
-  E* smem = reinterpret_cast<E*>(smem_raw);                                                       // [NBUF][keys | values]
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ks = wave / GROUPS, grp = wave % GROUPS, row_groups = GROUPS / heads, h_in = grp / row_groups, dd = a.d;
   const DocBlock blk = row_block(a, heads, 32 * row_groups);
   const int t0 = blk.block * 32 * row_groups, w0 = t0 + 32 * (grp % row_groups), my_q = w0 + (lane & 31), h = blk.h + h_in;
@@ -74,38 +73,35 @@ __global__ __launch_bounds__(256, KS == 1 ? 2 : 1) void doc_fwd_kernel(DocAttn a
   const int4 range = my_q < a.T ? doc_range((const int4*)a.ranges, my_q, a.T) : make_int4(0, 0, 0, 0);
   typename M::vec qf[TL::FRAGS];
   TL::load_frags(qf, qh, a.ldq, my_q, a.T, lane, dd);
-  const DocScale sc = doc_scale<E>(a, h);
+  const DocScale sc = doc_scale<E, MODE>(a, h);
   const int lo = range.x, seen = max(range.y - range.x, 0);   // keys
   const Span mine = span_of(range.x, range.y);
   const int tiles = (all.hi - all.lo + ROWS - 1) / ROWS;
 
-  TileLoad<E, D, ROWS, 256> kr, vr;
+  const unsigned smem = lds_address(smem_raw);
+  const TileLoad<E, D, ROWS, NW> load(a.ldkv, lane, dd);
+  auto fetch = [&](unsigned to, int row0) {
+    load.fetch(to, kh, row0, all.hi, wave);
+    load.fetch(to + TILE, vh, row0, all.hi, wave);
+  };
+  typename TL::Lane at(smem + TL::bytes(ks * 32 * SUB), lane);
   f32x16 oacc[TL::BLOCKS];
 #pragma unroll
   for (int i = 0; i < TL::BLOCKS; ++i) oacc[i] = f32x16{};
   float m = -INFINITY, l = 0.f;   // the reference of the weights, and their sum
-  if (tiles > 0) {
-    kr.fetch(kh, a.ldkv, all.lo, all.hi, tid, dd);
-    vr.fetch(vh, a.ldkv, all.lo, all.hi, tid, dd);
-    if (NBUF == 2) {
-      kr.put(smem, tid);
-      vr.put(smem + TILE, tid);
-      __syncthreads();
-    }
+  if (NBUF == 2 && tiles > 0) {
+    fetch(smem, all.lo);
+    tile_wait();
+    __syncthreads();
   }
-  const float f = sc.factor();
+  const float f = MODE == DOC_PLAIN ? sc.log2 : 1.f;
   for (int t = 0; t < tiles; ++t) {
-    const int key0 = all.lo + t * ROWS, at = NBUF == 2 ? (t & 1) * 2 * TILE : 0;
+    const int key0 = all.lo + t * ROWS;
     if (NBUF == 1) {
-      kr.put(smem, tid);
-      vr.put(smem + TILE, tid);
+      fetch(smem, key0);
+      tile_wait();
       __syncthreads();
-    }
-    if (t + 1 < tiles) {
-      kr.fetch(kh, a.ldkv, key0 + ROWS, all.hi, tid, dd);
-      vr.fetch(vh, a.ldkv, key0 + ROWS, all.hi, tid, dd);
-    }
-    const E *Kt = smem + at + ks * 32 * SUB * TL::LD, *Vt = Kt + TILE;
+    } else if (t + 1 < tiles) fetch(smem + ((t + 1) & 1) * 2 * TILE, key0 + ROWS);   // that buffer was last read before the barrier that ended the iteration before
     const int kb = key0 + ks * 32 * SUB;
     if (kb < mine.hi && kb + 32 * SUB > mine.lo) {
       f32x16 s[SUB];
@@ -113,10 +109,10 @@ __global__ __launch_bounds__(256, KS == 1 ? 2 : 1) void doc_fwd_kernel(DocAttn a
       for (int j = 0; j < SUB; ++j) {
         s[j] = f32x16{};
 #pragma unroll
-        for (int c = 0; c < TL::FRAGS; ++c) s[j] = M::rows(TL::frag(Kt, 32 * j, c, lane), qf[c], s[j]);
+        for (int c = 0; c < TL::FRAGS; ++c) s[j] = M::rows(at.frag(0, 32 * j, c), qf[c], s[j]);
       }
 #pragma unroll
-      for (int j = 0; j < SUB; ++j) doc_scores<E>(s[j], sc, (float)(kb + 32 * j + 4 * (lane >> 5) - my_q));
+      for (int j = 0; j < SUB; ++j) doc_scores<E, MODE>(s[j], sc, (float)(kb + 32 * j + 4 * (lane >> 5) - my_q));
       if (kb < mine.all_lo || kb + 32 * SUB > mine.all_hi) {   // not every row sees every key
 #pragma unroll
         for (int j = 0; j < SUB; ++j) {
@@ -159,19 +155,19 @@ __global__ __launch_bounds__(256, KS == 1 ? 2 : 1) void doc_fwd_kernel(DocAttn a
       for (int j = 0; j < SUB; ++j)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const typename M::col8 pf = M::pack(s[j], u);
+          const typename M::col8 pf = pack<E>(s[j], u);
 #pragma unroll
-          for (int b = 0; b < TL::BLOCKS; ++b) oacc[b] = M::cols(M::template col<TL::LD>(Vt, 32 * j + 16 * u, 32 * b, lane), pf, oacc[b]);
+          for (int b = 0; b < TL::BLOCKS; ++b) oacc[b] = M::cols(at.column(TILE, 32 * j + 16 * u, b), pf, oacc[b]);
         }
     }
-    if (NBUF == 2 && t + 1 < tiles) {   // the other buffer was last read before the barrier that ended the iteration before
-      kr.put(smem + ((t + 1) & 1) * 2 * TILE, tid);
-      vr.put(smem + ((t + 1) & 1) * 2 * TILE + TILE, tid);
+    if (NBUF == 2) {
+      tile_wait();
+      at.move(t & 1 ? -2 * TILE : 2 * TILE);
     }
     __syncthreads();
   }
   if constexpr (KS > 1) {
-    float* stat = reinterpret_cast<float*>(smem_raw);   // [KS][m | l][32]
+    float* stat = reinterpret_cast<float*>(smem_raw) + grp * KS * 64;   // [GROUPS][KS][m | l][32]
     if (lane < 32) {
       stat[ks * 64 + lane] = m;
       stat[ks * 64 + 32 + lane] = l;
@@ -190,7 +186,7 @@ __global__ __launch_bounds__(256, KS == 1 ? 2 : 1) void doc_fwd_kernel(DocAttn a
 #pragma unroll
       for (int r = 0; r < 16; ++r) oacc[i][r] *= alpha;
     __syncthreads();
-    merge_waves<TL::BLOCKS>(oacc, reinterpret_cast<f32x4*>(smem_raw), ks, KS, lane);
+    merge_waves<TL::BLOCKS>(oacc, reinterpret_cast<f32x4*>(smem_raw) + grp * (KS - 1) * TL::BLOCKS * 4 * 64, ks, KS, lane);
   }
   const bool live = seen > 0 && my_q < a.T;
   DocRedo<NW>& redo = *reinterpret_cast<DocRedo<NW>*>(smem_raw);
@@ -200,7 +196,7 @@ __global__ __launch_bounds__(256, KS == 1 ? 2 : 1) void doc_fwd_kernel(DocAttn a
 #pragma unroll
       for (int i = 0; i < TL::BLOCKS; ++i) oacc[i] = f32x16{};
     }
-    TL::store(oacc, live ? 1.f / l : 0.f, reinterpret_cast<E*>(smem_raw + (sizeof(redo) + 15) / 16 * 16) + grp * 32 * TL::LD, (E*)a.o + h * dd, a.ldo, w0, a.T,
+    TL::store(oacc, live ? 1.f / l : 0.f, smem_raw + (sizeof(redo) + 15) / 16 * 16 + grp * TL::STORE, (E*)a.o + h * dd, a.ldo, w0, a.T,
               lane, dd, again);
     if (lane < 32 && my_q < a.T)
       a.lse[(int64_t)h * a.T + my_q] = live ? (float)((double)m * 0.6931471805599453 + (double)logf(l)) : -INFINITY;
@@ -227,16 +223,15 @@ __device__ __attribute__((noinline)) void redo_dq(DocRedo<NW>* redo, int groups,
   });
 }
 
-template <typename E, int D, int KS, int ROWS, int NBUF>
+template <typename E, int D, int MODE, int KS, int ROWS, int NBUF>
 __global__ __launch_bounds__(256, KS == 1 && sizeof(E) == 2 ? 2 : 1) void doc_dq_kernel(DocAttn a, int heads) {
   typedef Tile<E, D> TL;
   typedef Mat<E> M;
-  constexpr int NW = 4, GROUPS = NW / KS, SUB = ROWS / 32 / KS, TILE = ROWS * TL::LD;
-  constexpr size_t LOOP = NBUF * 2 * TILE * sizeof(E), END = sizeof(DocRedo<NW>) + 16 + GROUPS * 32 * TL::LD * sizeof(E);
+  constexpr int NW = 4, GROUPS = NW / KS, SUB = ROWS / 32 / KS, TILE = TL::bytes(ROWS);
+  constexpr size_t LOOP = NBUF * 2 * TILE, END = sizeof(DocRedo<NW>) + 16 + GROUPS * TL::STORE;   // [NBUF][keys | values]
   __shared__ __align__(16) char smem_raw[LOOP > END ? LOOP : END];
   static_assert(LOOP >= (size_t)(KS - 1) * GROUPS * TL::BLOCKS * 4 * 64 * 16, "");
-  E* smem = reinterpret_cast<E*>(smem_raw);
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ks = wave / GROUPS, grp = wave % GROUPS, row_groups = GROUPS / heads, h_in = grp / row_groups, dd = a.d;
   const DocBlock blk = row_block(a, heads, 32 * row_groups);
   const int t0 = blk.block * 32 * row_groups, w0 = t0 + 32 * (grp % row_groups), my_q = w0 + (lane & 31), h = blk.h + h_in;
@@ -250,14 +245,17 @@ __global__ __launch_bounds__(256, KS == 1 && sizeof(E) == 2 ? 2 : 1) void doc_dq
   TL::load_frags(dof, (const E*)a.dout + h * dd, a.ldo, my_q, a.T, lane, dd);
   const int64_t stat = (int64_t)h * a.T + min(my_q, a.T - 1);
   const float lse2 = live ? a.lse[stat] * DOC_LOG2E : 0.f;
-  const DocScale sc = doc_scale<E>(a, h);
+  const DocScale sc = doc_scale<E, MODE>(a, h);
   const Span mine = span_of(range.x, range.y);
   const int tiles = (all.hi - all.lo + ROWS - 1) / ROWS;
-  TileLoad<E, D, ROWS, 256> kr, vr;
-  if (tiles > 0) {   // in flight while delta is formed
-    kr.fetch(kh, a.ldkv, all.lo, all.hi, tid, dd);
-    vr.fetch(vh, a.ldkv, all.lo, all.hi, tid, dd);
-  }
+  const unsigned smem = lds_address(smem_raw);
+  const TileLoad<E, D, ROWS, NW> load(a.ldkv, lane, dd);
+  auto fetch = [&](unsigned to, int row0) {
+    load.fetch(to, kh, row0, all.hi, wave);
+    load.fetch(to + TILE, vh, row0, all.hi, wave);
+  };
+  typename TL::Lane at(smem + TL::bytes(ks * 32 * SUB), lane);
+  if (NBUF == 2 && tiles > 0) fetch(smem, all.lo);   // in flight while delta is formed
   float delta = 0.f, largest = 0.f;
   {
     typename M::vec of[TL::FRAGS];
@@ -281,22 +279,16 @@ __global__ __launch_bounds__(256, KS == 1 && sizeof(E) == 2 ? 2 : 1) void doc_dq
 #pragma unroll
   for (int i = 0; i < TL::BLOCKS; ++i) acc[i] = f32x16{};
   if (NBUF == 2 && tiles > 0) {
-    kr.put(smem, tid);
-    vr.put(smem + TILE, tid);
+    tile_wait();
     __syncthreads();
   }
   for (int t = 0; t < tiles; ++t) {
-    const int key0 = all.lo + t * ROWS, at = NBUF == 2 ? (t & 1) * 2 * TILE : 0;
+    const int key0 = all.lo + t * ROWS;
     if (NBUF == 1) {
-      kr.put(smem, tid);
-      vr.put(smem + TILE, tid);
+      fetch(smem, key0);
+      tile_wait();
       __syncthreads();
-    }
-    if (t + 1 < tiles) {
-      kr.fetch(kh, a.ldkv, key0 + ROWS, all.hi, tid, dd);
-      vr.fetch(vh, a.ldkv, key0 + ROWS, all.hi, tid, dd);
-    }
-    const E *Kt = smem + at + ks * 32 * SUB * TL::LD, *Vt = Kt + TILE;
+    } else if (t + 1 < tiles) fetch(smem + ((t + 1) & 1) * 2 * TILE, key0 + ROWS);   // that buffer was last read before the barrier that ended the iteration before
     const int kb0 = key0 + ks * 32 * SUB;
     if (kb0 < mine.hi && kb0 + 32 * SUB > mine.lo) {
       const bool part = kb0 < mine.all_lo || kb0 + 32 * SUB > mine.all_hi;
@@ -306,10 +298,10 @@ __global__ __launch_bounds__(256, KS == 1 && sizeof(E) == 2 ? 2 : 1) void doc_dq
         f32x16 s = f32x16{}, dp = f32x16{};
 #pragma unroll
         for (int c = 0; c < TL::FRAGS; ++c) {
-          s = M::rows(TL::frag(Kt, 32 * j, c, lane), qf[c], s);
-          dp = M::rows(TL::frag(Vt, 32 * j, c, lane), dof[c], dp);
+          s = M::rows(at.frag(0, 32 * j, c), qf[c], s);
+          dp = M::rows(at.frag(TILE, 32 * j, c), dof[c], dp);
         }
-        doc_weights<E>(s, dp, sc, (float)(kb + 4 * (lane >> 5) - my_q), 0.f, unit, [&](int) { return lse2; }, [&](int) { return delta; });
+        doc_weights<E, MODE>(s, dp, sc, (float)(kb + 4 * (lane >> 5) - my_q), unit, [&](int) { return f32x4{lse2, lse2, lse2, lse2}; }, [&](int) { return f32x4{delta, delta, delta, delta}; });
         if (part) {
           const int from = kb + 4 * (lane >> 5) - lo;
 #pragma unroll
@@ -318,19 +310,19 @@ __global__ __launch_bounds__(256, KS == 1 && sizeof(E) == 2 ? 2 : 1) void doc_dq
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const typename M::col8 df = M::pack(dp, u);
+          const typename M::col8 df = pack<E>(dp, u);
 #pragma unroll
-          for (int b = 0; b < TL::BLOCKS; ++b) acc[b] = M::cols(M::template col<TL::LD>(Kt, 32 * j + 16 * u, 32 * b, lane), df, acc[b]);
+          for (int b = 0; b < TL::BLOCKS; ++b) acc[b] = M::cols(at.column(0, 32 * j + 16 * u, b), df, acc[b]);
         }
       }
     }
-    if (NBUF == 2 && t + 1 < tiles) {
-      kr.put(smem + ((t + 1) & 1) * 2 * TILE, tid);
-      vr.put(smem + ((t + 1) & 1) * 2 * TILE + TILE, tid);
+    if (NBUF == 2) {
+      tile_wait();
+      at.move(t & 1 ? -2 * TILE : 2 * TILE);
     }
     __syncthreads();
   }
-  if constexpr (KS > 1) merge_waves<TL::BLOCKS>(acc, reinterpret_cast<f32x4*>(smem_raw), ks, KS, lane);
+  if constexpr (KS > 1) merge_waves<TL::BLOCKS>(acc, reinterpret_cast<f32x4*>(smem_raw) + grp * (KS - 1) * TL::BLOCKS * 4 * 64, ks, KS, lane);
   DocRedo<NW>& redo = *reinterpret_cast<DocRedo<NW>*>(smem_raw);
   const unsigned again = redo_rows<NW>(redo, grp, ks == 0, ks == 0 && live && !(mark_of(acc) == 0.f));
   if (ks == 0) {
@@ -338,7 +330,7 @@ __global__ __launch_bounds__(256, KS == 1 && sizeof(E) == 2 ? 2 : 1) void doc_dq
 #pragma unroll
       for (int i = 0; i < TL::BLOCKS; ++i) acc[i] = f32x16{};
     }
-    TL::store(acc, a.scale / unit, reinterpret_cast<E*>(smem_raw + (sizeof(redo) + 15) / 16 * 16) + grp * 32 * TL::LD, (E*)a.dq + h * dd, a.lddq, w0, a.T,
+    TL::store(acc, a.scale / unit, smem_raw + (sizeof(redo) + 15) / 16 * 16 + grp * TL::STORE, (E*)a.dq + h * dd, a.lddq, w0, a.T,
               lane, dd, again);
   }
   if (__builtin_expect(any_row(redo.masks, GROUPS, lane), 0))   // the rows' delta: written by this workgroup, before its barrier
@@ -375,26 +367,23 @@ __device__ __attribute__((noinline)) void redo_dkv(DocRedo<NW>* redo, int groups
   });
 }
 
-template <typename E, int D, int KG, int QS, int ROWS, int NBUF>
+template <typename E, int D, int MODE, int KG, int QS, int ROWS, int NBUF>
 __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __launch_bounds__(64 * KG * QS) void doc_dkv_kernel(DocAttn a) {
   typedef Tile<E, D> TL;
   typedef Mat<E> M;
-  constexpr int NW = KG * QS, NT = 64 * NW, SUB = ROWS / 32 / QS, TILE = ROWS * TL::LD, STATS = HALF<E> ? 3 : 2;
-  struct Lds {
-    E tile[NBUF][2][TILE];          // Q, dO
-    float stat[NBUF][STATS][ROWS];  // log-sum-exp in powers of two, delta, (half) largest |dO|
-    E v[KG * 32 * TL::LD];
-  };
-  static_assert(ROWS <= NT, "");
-  __shared__ __align__(16) char smem_raw[sizeof(Lds)];
-  static_assert(sizeof(smem_raw) >= sizeof(DocRedo<NW>) + 16 + KG * 32 * TL::LD * sizeof(E), "");
-  static_assert(sizeof(smem_raw) >= (size_t)(QS - 1) * KG * TL::BLOCKS * 4 * 64 * 16, "");
-  Lds& lds = *reinterpret_cast<Lds*>(smem_raw);
+  constexpr int NW = KG * QS, SUB = ROWS / 32 / QS, TILE = TL::bytes(ROWS), STATS = HALF<E> ? 3 : 2;
+  constexpr int STAT = STATS * ROWS * 4;             // log-sum-exp in powers of two less P_SHIFT, delta, (half) largest |dO|
+  constexpr int V = NBUF * (2 * TILE + STAT);        // [NBUF][Q | dO], [NBUF][stats], [KG][V rows]
+  constexpr size_t LOOP = V + KG * TL::bytes(32), END = sizeof(DocRedo<NW>) + 16 + KG * TL::STORE, MERGE = (size_t)(QS - 1) * KG * TL::BLOCKS * 4 * 64 * 16;
+  static_assert(ROWS <= 64 * NW, "");
+  __shared__ __align__(16) char smem_raw[LOOP > END ? LOOP : END];
+  static_assert(sizeof(smem_raw) >= MERGE, "");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int qs = wave / KG, kg = wave % KG, dd = a.d, group = a.nh / a.nkv;
   const int kv = (int)blockIdx.x % a.nkv, t0 = (int)blockIdx.x / a.nkv * 32 * KG;   // early keys, under a causal mask seen by the most rows, first
   const int w0 = t0 + 32 * kg, my_k = w0 + (lane & 31);
   const E *kh = (const E*)a.k + kv * dd, *vh = (const E*)a.v + kv * dd;
+  const unsigned smem = lds_address(smem_raw);
   const Span all = block_span<true>(a.ranges, t0, 32 * KG, a.T, lane);
   const int4 range = my_k < a.T ? doc_range((const int4*)a.ranges, my_k, a.T) : make_int4(0, 0, 0, 0);
   const int lo = range.z, seen = max(range.w - range.z, 0);
@@ -402,42 +391,29 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
   TL::load_frags(kf, kh, a.ldkv, my_k, a.T, lane, dd);
   const Span mine = span_of(range.z, range.w);
   const int tiles = (all.hi - all.lo + ROWS - 1) / ROWS, total = tiles * group;
-  E* Vw = lds.v + kg * 32 * TL::LD;
   if (qs == 0) {
-    typename M::vec vf[TL::FRAGS];
-    constexpr int P = D / TL::VN;
-#pragma unroll
-    for (int i = 0; i < TL::FRAGS; ++i) {
-      const int p = lane + 64 * i, r = p / P, c = p % P * TL::VN;
-      vf[i] = typename M::vec{};
-      if (w0 + r < a.T && c < dd) vf[i] = *reinterpret_cast<const typename M::vec*>(vh + (w0 + r) * a.ldkv + c);
-    }
-#pragma unroll
-    for (int i = 0; i < TL::FRAGS; ++i) {
-      const int p = lane + 64 * i;
-      *reinterpret_cast<typename M::vec*>(Vw + p / P * TL::LD + p % P * TL::VN) = vf[i];
-    }
+    const TileLoad<E, D, 32, 1> load(a.ldkv, lane, dd);
+    load.fetch(smem + V + kg * TL::bytes(32), vh, w0, a.T, 0);
   }
-  TileLoad<E, D, ROWS, NT> qr, dr;
+  const TileLoad<E, D, ROWS, NW> load_q(a.ldq, lane, dd), load_d(a.ldo, lane, dd);
   float sr[STATS];
-  auto fetch = [&](int h, int row0) {
-    qr.fetch((const E*)a.q + h * dd, a.ldq, row0, all.hi, tid, dd);
-    dr.fetch((const E*)a.dout + h * dd, a.ldo, row0, all.hi, tid, dd);
+  auto fetch = [&](int buf, int h, int row0) {
+    load_q.fetch(smem + buf * 2 * TILE, (const E*)a.q + h * dd, row0, all.hi, wave);
+    load_d.fetch(smem + buf * 2 * TILE + TILE, (const E*)a.dout + h * dd, row0, all.hi, wave);
     if (tid < ROWS) {
-      const int64_t at = (int64_t)h * a.T + min(row0 + tid, a.T - 1);
-      sr[0] = a.lse[at];
-      sr[1] = a.delta[at];
-      if constexpr (HALF<E>) sr[2] = a.delta[(int64_t)a.nh * a.T + at];
+      const int64_t from = (int64_t)h * a.T + min(row0 + tid, a.T - 1);
+      sr[0] = a.lse[from];
+      sr[1] = a.delta[from];
+      if constexpr (HALF<E>) sr[2] = a.delta[(int64_t)a.nh * a.T + from];
     }
   };
-  auto put = [&](int buf, int row0) {
-    qr.put(lds.tile[buf][0], tid);
-    dr.put(lds.tile[buf][1], tid);
+  auto put_stats = [&](int buf, int row0) {
+    float* st = reinterpret_cast<float*>(smem_raw + NBUF * 2 * TILE + buf * STAT);
     if (tid < ROWS) {   // rows past the end: zeros, whose weights 1 meet rows of zeros
       const bool in = row0 + tid < all.hi;
-      lds.stat[buf][0][tid] = in ? sr[0] * DOC_LOG2E : 0.f;
-      lds.stat[buf][1][tid] = in ? sr[1] : 0.f;
-      if constexpr (HALF<E>) lds.stat[buf][2][tid] = in ? sr[2] : 0.f;
+      st[tid] = in ? fmaf(sr[0], DOC_LOG2E, -P_SHIFT<E>) : 0.f;
+      st[ROWS + tid] = in ? sr[1] : 0.f;
+      if constexpr (HALF<E>) st[2 * ROWS + tid] = in ? sr[2] : 0.f;
     }
   };
   f32x16 dk[TL::BLOCKS], dv[TL::BLOCKS];
@@ -445,36 +421,39 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
   for (int i = 0; i < TL::BLOCKS; ++i) dk[i] = dv[i] = f32x16{};
   float unit = 0.f;   // half: of the score gradients, none yet
   int h = kv * group, t = 0;
-  if (total > 0) {
-    fetch(h, all.lo);
-    if (NBUF == 2) put(0, all.lo);
+  if (NBUF == 2 && total > 0) {
+    fetch(0, h, all.lo);
+    put_stats(0, all.lo);
   }
+  tile_wait();
   __syncthreads();
-  DocScale sc = doc_scale<E>(a, h);
+  typename TL::Lane at(smem + TL::bytes(qs * 32 * SUB), lane);
+  const typename TL::Lane at_v(smem + V + kg * TL::bytes(32), lane);
+  unsigned stat_at = smem + NBUF * 2 * TILE + 4 * (qs * 32 * SUB + 4 * (lane >> 5));
+  DocScale sc = doc_scale<E, MODE>(a, h);
   for (int it = 0; it < total; ++it) {
     const int row0 = all.lo + t * ROWS, buf = NBUF == 2 ? it & 1 : 0;
     const int tn = t + 1 < tiles ? t + 1 : 0, hn = tn ? h : h + 1, rown = all.lo + tn * ROWS;
     if (NBUF == 1) {
-      put(0, row0);
+      fetch(0, h, row0);
+      put_stats(0, row0);
+      tile_wait();
       __syncthreads();
-    }
-    if (it + 1 < total) fetch(hn, rown);
-    const E *Qt = lds.tile[buf][0] + qs * 32 * SUB * TL::LD, *Dt = lds.tile[buf][1] + qs * 32 * SUB * TL::LD;
+    } else if (it + 1 < total) fetch(buf ^ 1, hn, rown);
     const int rb0 = row0 + qs * 32 * SUB;
     if (rb0 < mine.hi && rb0 + 32 * SUB > mine.lo) {
       const bool part = rb0 < mine.all_lo || rb0 + 32 * SUB > mine.all_hi;
 #pragma unroll
       for (int j = 0; j < SUB; ++j) {
         const int rb = rb0 + 32 * j;
-        const float* st = lds.stat[buf][0] + qs * 32 * SUB + 32 * j;
         f32x16 s = f32x16{}, dp = f32x16{};
 #pragma unroll
         for (int c = 0; c < TL::FRAGS; ++c) {
-          s = M::rows(TL::frag(Qt, 32 * j, c, lane), kf[c], s);
-          dp = M::rows(TL::frag(Dt, 32 * j, c, lane), TL::frag(Vw, 0, c, lane), dp);
+          s = M::rows(at.frag(0, 32 * j, c), kf[c], s);
+          dp = M::rows(at.frag(TILE, 32 * j, c), at_v.frag(0, 0, c), dp);
         }
         if constexpr (HALF<E>) {   // the unit follows the largest |dO| so far
-          const float top = wave_max(st[2 * ROWS + (lane & 31)]), now = unit_of(top);
+          const float top = wave_max(lds_read<float>(stat_at - 16 * (lane >> 5) + 4 * (2 * ROWS + 32 * j + (lane & 31)))), now = unit_of(top);
           if (top > 0.f && (unit == 0.f || now < unit)) {
             const float f = unit == 0.f ? 1.f : now / unit;
             unit = now;
@@ -484,14 +463,12 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
               for (int r = 0; r < 16; ++r) dk[b][r] *= f;
           }
         }
-        f32x4 lse2[4], delta[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          lse2[c] = *reinterpret_cast<const f32x4*>(st + 8 * c + 4 * (lane >> 5));
-          delta[c] = *reinterpret_cast<const f32x4*>(st + ROWS + 8 * c + 4 * (lane >> 5));
-        }
-        doc_weights<E>(s, dp, sc, (float)(rb + 4 * (lane >> 5) - my_k), P_SHIFT<E>, HALF<E> ? unit / 16384.f : 1.f,
-                       [&](int r) { return lse2[r >> 2][r & 3]; }, [&](int r) { return delta[r >> 2][r & 3]; });
+        // Two waves per SIMD have 256 registers each, of which 192 hold K, dK, dV and the scores: the phases are kept apart, or the compiler
+        // spills accumulators to read ahead.
+        if constexpr (NW == 8) __builtin_amdgcn_sched_barrier(0);
+        doc_weights<E, MODE>(s, dp, sc, (float)(rb + 4 * (lane >> 5) - my_k), HALF<E> ? unit / 16384.f : 1.f,
+                       [&](int c) { return lds_read<f32x4>(stat_at + 4 * (32 * j + 8 * c)); },
+                       [&](int c) { return lds_read<f32x4>(stat_at + 4 * (ROWS + 32 * j + 8 * c)); });
         if (part) {
           const int from = rb + 4 * (lane >> 5) - lo;
 #pragma unroll
@@ -500,18 +477,24 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const typename M::col8 pf = M::pack(s, u), df = M::pack(dp, u);
+          if constexpr (NW == 8) __builtin_amdgcn_sched_barrier(0);
+          const typename M::col8 pf = pack<E>(s, u), df = pack<E>(dp, u);
 #pragma unroll
           for (int b = 0; b < TL::BLOCKS; ++b) {
-            dv[b] = M::cols(M::template col<TL::LD>(Dt, 32 * j + 16 * u, 32 * b, lane), pf, dv[b]);
-            dk[b] = M::cols(M::template col<TL::LD>(Qt, 32 * j + 16 * u, 32 * b, lane), df, dk[b]);
+            dv[b] = M::cols(at.column(TILE, 32 * j + 16 * u, b), pf, dv[b]);
+            dk[b] = M::cols(at.column(0, 32 * j + 16 * u, b), df, dk[b]);
           }
         }
       }
     }
-    if (NBUF == 2 && it + 1 < total) put(buf ^ 1, rown);
+    if (NBUF == 2) {
+      if (it + 1 < total) put_stats(buf ^ 1, rown);
+      tile_wait();
+      at.move(buf ? -2 * TILE : 2 * TILE);
+      stat_at += buf ? -STAT : STAT;
+    }
     __syncthreads();
-    if (hn != h && it + 1 < total) sc = doc_scale<E>(a, hn);
+    if (hn != h && it + 1 < total) sc = doc_scale<E, MODE>(a, hn);
     t = tn;
     h = hn;
   }
@@ -538,7 +521,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
 #pragma unroll
       for (int i = 0; i < TL::BLOCKS; ++i) dk[i] = dv[i] = f32x16{};
     }
-    E* to = reinterpret_cast<E*>(smem_raw + (sizeof(redo) + 15) / 16 * 16) + kg * 32 * TL::LD;
+    char* to = smem_raw + (sizeof(redo) + 15) / 16 * 16 + kg * TL::STORE;
     TL::store(dv, HALF<E> ? 1.f / 16384.f : 1.f, to, (E*)a.dv + kv * dd, a.lddkv, w0, a.T, lane, dd, again);
     TL::store(dk, HALF<E> && unit != 0.f ? a.scale / unit : a.scale, to, (E*)a.dk + kv * dd, a.lddkv, w0, a.T, lane, dd, again);
   }
@@ -556,41 +539,52 @@ inline int doc_heads(const DocAttn& a, int groups) {
 // Few blocks of 128 rows: waves share 32 rows, so that there are four times as many workgroups.
 inline bool doc_few(int64_t rows_times_heads) { return cdiv(rows_times_heads, 128) < 256; }
 
-template <typename E, int D> hipError_t doc_fwd(hipStream_t st, const DocAttn& a) {
+// Waves that share rows, and rows of the tiles that they share out, as far as two buffers fit in LDS.
+template <typename E, int D> constexpr int SHARE = sizeof(E) == 4 && D > 64 ? 2 : 4;
+template <typename E, int D, int MODE> hipError_t doc_fwd(hipStream_t st, const DocAttn& a) {
   if (doc_few((int64_t)a.T * a.nh)) {
-    hipLaunchKernelGGL((doc_fwd_kernel<E, D, 4, 128, sizeof(E) == 4 ? 1 : 2>), dim3((unsigned)(cdiv(a.T, 32) * a.nh)), dim3(256), 0, st, a, 1);
+    constexpr int S = SHARE<E, D>;
+    hipLaunchKernelGGL((doc_fwd_kernel<E, D, MODE, S, 32 * S, 2>), dim3((unsigned)(cdiv(a.T, 128 / S) * a.nh)), dim3(256), 0, st, a, 1);
   } else {
     const int heads = doc_heads(a, 4);
-    hipLaunchKernelGGL((doc_fwd_kernel<E, D, 1, ROWS_LONG<E>, 2>), dim3((unsigned)(cdiv(a.T, 128 / heads) * (a.nh / heads))), dim3(256), 0, st, a, heads);
+    hipLaunchKernelGGL((doc_fwd_kernel<E, D, MODE, 1, ROWS_LONG<E>, 2>), dim3((unsigned)(cdiv(a.T, 128 / heads) * (a.nh / heads))), dim3(256), 0, st, a, heads);
   }
   return hipGetLastError();
 }
-template <typename E, int D> hipError_t doc_bwd(hipStream_t st, const DocAttn& a) {
+template <typename E, int D, int MODE> hipError_t doc_bwd(hipStream_t st, const DocAttn& a) {
   if (doc_few((int64_t)a.T * a.nh)) {
-    hipLaunchKernelGGL((doc_dq_kernel<E, D, 4, 128, sizeof(E) == 4 ? 1 : 2>), dim3((unsigned)(cdiv(a.T, 32) * a.nh)), dim3(256), 0, st, a, 1);
+    constexpr int S = SHARE<E, D>;
+    hipLaunchKernelGGL((doc_dq_kernel<E, D, MODE, S, 32 * S, 2>), dim3((unsigned)(cdiv(a.T, 128 / S) * a.nh)), dim3(256), 0, st, a, 1);
   } else {
     const int heads = doc_heads(a, 4);
-    hipLaunchKernelGGL((doc_dq_kernel<E, D, 1, ROWS_LONG<E>, 2>), dim3((unsigned)(cdiv(a.T, 128 / heads) * (a.nh / heads))), dim3(256), 0, st, a, heads);
+    hipLaunchKernelGGL((doc_dq_kernel<E, D, MODE, 1, ROWS_LONG<E>, 2>), dim3((unsigned)(cdiv(a.T, 128 / heads) * (a.nh / heads))), dim3(256), 0, st, a, heads);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (doc_few((int64_t)a.T * a.nkv)) {
-    hipLaunchKernelGGL((doc_dkv_kernel<E, D, 1, 4, 128, 1>), dim3((unsigned)(cdiv(a.T, 32) * a.nkv)), dim3(256), 0, st, a);
+    constexpr int BUFFERS = sizeof(E) == 4 && D > 64 ? 1 : 2;
+    hipLaunchKernelGGL((doc_dkv_kernel<E, D, MODE, 1, 4, 128, BUFFERS>), dim3((unsigned)(cdiv(a.T, 32) * a.nkv)), dim3(256), 0, st, a);
   } else if constexpr (sizeof(E) == 4) {
-    hipLaunchKernelGGL((doc_dkv_kernel<E, D, 4, 1, 32, 2>), dim3((unsigned)(cdiv(a.T, 128) * a.nkv)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((doc_dkv_kernel<E, D, MODE, 4, 1, 32, 2>), dim3((unsigned)(cdiv(a.T, 128) * a.nkv)), dim3(256), 0, st, a);
   } else {
-    hipLaunchKernelGGL((doc_dkv_kernel<E, D, 4, 2, 64, 2>), dim3((unsigned)(cdiv(a.T, 128) * a.nkv)), dim3(512), 0, st, a);
+    hipLaunchKernelGGL((doc_dkv_kernel<E, D, MODE, 4, 2, 64, 2>), dim3((unsigned)(cdiv(a.T, 128) * a.nkv)), dim3(512), 0, st, a);
   }
   return hipGetLastError();
+}
+template <typename E, int D, int MODE> hipError_t doc_either(hipStream_t st, const DocAttn& a, bool backward) {
+  return backward ? doc_bwd<E, D, MODE>(st, a) : doc_fwd<E, D, MODE>(st, a);
+}
+template <typename E, int D> hipError_t doc_mode(hipStream_t st, const DocAttn& a, bool backward) {
+  const bool cap = a.softcap > 0.f;
+  return cap ? (a.slopes ? doc_either<E, D, DOC_CAP | DOC_BIAS>(st, a, backward) : doc_either<E, D, DOC_CAP>(st, a, backward))
+             : (a.slopes ? doc_either<E, D, DOC_BIAS>(st, a, backward) : doc_either<E, D, DOC_PLAIN>(st, a, backward));
 }
 
 }  // namespace
 
 // Heads are padded with zeros to D = 64, 96 or 128.
 template <typename E> hipError_t doc_attention(hipStream_t st, const DocAttn& a, bool backward) {
-  if (a.d <= 64) return backward ? doc_bwd<E, 64>(st, a) : doc_fwd<E, 64>(st, a);
-  if (a.d <= 96) return backward ? doc_bwd<E, 96>(st, a) : doc_fwd<E, 96>(st, a);
-  return backward ? doc_bwd<E, 128>(st, a) : doc_fwd<E, 128>(st, a);
+  return a.d <= 64 ? doc_mode<E, 64>(st, a, backward) : a.d <= 96 ? doc_mode<E, 96>(st, a, backward) : doc_mode<E, 128>(st, a, backward);
 }
 
 }  // namespace zs

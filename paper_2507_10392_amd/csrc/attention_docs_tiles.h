@@ -12,37 +12,18 @@ namespace {
 
 constexpr float DOC_LOG2E = 1.4426950408889634f;
 typedef float f32x8 __attribute__((ext_vector_type(8)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-__device__ __forceinline__ int acc_row(int r, int lane) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
-
-// A type's 16 bytes along a row (vec), and 8 rows of a column (col8): of the rows 16 s + 4 (lane/32) + {0 .. 3, 8 .. 11}, in the order
+// What a lane reads 16 bytes at a time (vec), and 8 rows of a column (col8): of the rows 16 s + 4 (lane/32) + {0 .. 3, 8 .. 11}, in the order
 // of the accumulators 8 s .. 8 s + 7.
 template <typename E> struct Mat {
   typedef typename Vec<E>::type vec;
   typedef vec col8;
   static __device__ __forceinline__ f32x16 mma(vec a, vec b, f32x16 c) {
-    if constexpr (sizeof(E) == 2 && __is_same(E, bf16)) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    if constexpr (__is_same(E, bf16)) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
   static __device__ __forceinline__ f32x16 rows(vec a, vec b, f32x16 c) { return mma(a, b, c); }
   static __device__ __forceinline__ f32x16 cols(col8 a, col8 b, f32x16 c) { return mma(a, b, c); }
-  static __device__ __forceinline__ col8 pack(const f32x16& x, int s) {
-    col8 o;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = (E)x[8 * s + e];
-    return o;
-  }
-  // ds_read_b64_tr_b16 hands a lane 4 values that are consecutive along the rows
-  template <int LD> static __device__ __forceinline__ col8 col(const E* tile, int k0, int n0, int lane) {
-    const int r = lane & 15, gi = lane >> 4;
-    const E* p = tile + (k0 + 4 * (gi >> 1) + (r >> 2)) * LD + n0 + 16 * (gi & 1) + 4 * (r & 3);
-    union { struct { s16x4 a, b; } s; col8 v; } u;
-    u.s.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p);
-    u.s.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * LD));
-    return u.v;
-  }
 };
 template <> struct Mat<float> {
   typedef f32x4 vec;
@@ -57,30 +38,73 @@ template <> struct Mat<float> {
     for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
     return c;
   }
-  static __device__ __forceinline__ col8 pack(const f32x16& x, int s) {
-    col8 o;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = x[8 * s + e];
-    return o;
-  }
-  template <int LD> static __device__ __forceinline__ col8 col(const float* tile, int k0, int n0, int lane) {
-    col8 o;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = tile[(k0 + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)) * LD + n0 + (lane & 31)];
-    return o;
-  }
 };
+template <typename E> __device__ __forceinline__ typename Mat<E>::col8 pack(const f32x16& x, int s) {
+  typename Mat<E>::col8 o;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) o[e] = from_f<E>(x[8 * s + e]);
+  return o;
+}
 
-// Rows of D columns in LDS.  The padding spreads rows over the banks: 16-bit rows of 304, 240 and 176 bytes start in different groups
-// of 4 banks; fp32 rows are 8 (mod 16) floats apart, so that the two halves of a column read, 4 rows apart, take 32 banks each.
+typedef __attribute__((address_space(3))) char lds_char;
+__device__ __forceinline__ unsigned lds_address(const void* p) { return (unsigned)(uintptr_t)(const lds_char*)p; }
+template <typename T> __device__ __forceinline__ T lds_read(unsigned at) { return *(const __attribute__((address_space(3))) T*)(uintptr_t)at; }
+
+// Tiles of rows in LDS, D columns wide.  They come straight from memory (buffer loads into LDS), a wave's load bringing 1 KB: 8 rows by 128
+// bytes, lane l the piece of 16 bytes that belongs at 16 l.  Piece p of row r of such a square sits at position p ^ turn(r) of the row, which
+// the lanes arrange by what they load; squares of 8 rows are followed by a gap of 128 bytes.  Then the 16 rows that one cycle of a fragment
+// read touches lie in 16 different groups of 4 banks, and so do the 4 rows x 64 bytes of half a transposing read.  Of a fragment's
+// address only the place inside a square depends on the lane: four values for row fragments and two (fp32: four) for columns.
 template <typename E, int D> struct Tile {
-  static constexpr int VN = 16 / (int)sizeof(E), LD = D + (sizeof(E) == 2 ? 24 : 8), FRAGS = D / (2 * VN), BLOCKS = D / 32;
+  static constexpr int SZ = (int)sizeof(E), VN = 16 / SZ, FRAGS = D / (2 * VN), BLOCKS = D / 32, SQUARES = (D * SZ + 127) / 128;
+  static constexpr int OCTET = SQUARES * 1024 + 128;   // bytes of 8 rows
+  static constexpr int bytes(int rows) { return rows / 8 * OCTET; }
+  static constexpr int COLS = SZ == 4 ? 4 : 2;
   typedef typename Mat<E>::vec vec;
-  // columns 2 VN s + VN (lane/32) .. of row row0 + lane%32: an operand of the products over the columns
-  static __device__ __forceinline__ vec frag(const E* tile, int row0, int s, int lane) {
-    return *reinterpret_cast<const vec*>(tile + (row0 + (lane & 31)) * LD + 2 * VN * s + VN * (lane >> 5));
-  }
-  // The same of rows in memory; rows at or past `end` and columns past dd are zeros.
+  typedef typename Mat<E>::col8 col8;
+
+  static __device__ __forceinline__ unsigned turn(unsigned r) { return (r & 1) | (r & 2) << 1 | (r & 4) >> 1; }
+  static __device__ __forceinline__ unsigned place(unsigned row, unsigned piece) { return row * 128 + ((piece ^ turn(row)) << 4); }
+
+  // A lane's places, on top of an address in LDS.
+  struct Lane {
+    unsigned row[4], col[COLS];
+    __device__ __forceinline__ Lane(unsigned base, int lane) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) row[s] = base + (lane & 31) / 8 * OCTET + place(lane & 7, 2 * s + (lane >> 5));
+#pragma unroll
+      for (int i = 0; i < COLS; ++i)
+        col[i] = base + (SZ == 4 ? place(4 * (lane >> 5) + i, (lane & 31) >> 2) + 4 * (lane & 3)
+                                 : place(4 * (lane >> 5) + (lane & 15) / 4, 4 * i + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + 8 * (lane & 1));
+    }
+    __device__ __forceinline__ void move(int by) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) row[s] += by;
+#pragma unroll
+      for (int i = 0; i < COLS; ++i) col[i] += by;
+    }
+    // columns 2 VN s + VN (lane/32) .. of row row0 + lane%32: an operand of the products over the columns
+    __device__ __forceinline__ vec frag(int tile, int row0, int s) const { return lds_read<vec>(row[s & 3] + (tile + row0 / 8 * OCTET + (s >> 2) * 1024)); }
+    // column 32 b + lane%32 of 16 rows from row0 on: an operand of the products over the rows
+    __device__ __forceinline__ col8 column(int tile, int row0, int b) const {
+      if constexpr (SZ == 4) {
+        col8 o;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = lds_read<float>(col[e & 3] + (tile + (row0 / 8 + (e >> 2)) * OCTET + b * 1024));
+        return o;
+      } else {   // ds_read_b64_tr_b16 hands a lane 4 values that are consecutive along the rows
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        const unsigned at = col[b & 1] + (tile + row0 / 8 * OCTET + (b >> 1) * 1024);
+        union { struct { s16x4 a, b; } s; col8 v; } u;
+        u.s.a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)at);
+        u.s.b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(at + OCTET));
+        return u.v;
+      }
+    }
+  };
+
+  // Row fragments from memory; rows at or past `end` and columns past dd are zeros.
   static __device__ __forceinline__ void load_frags(vec (&f)[FRAGS], const E* __restrict__ head, int64_t ld, int row, int end, int lane, int dd) {
 #pragma unroll
     for (int s = 0; s < FRAGS; ++s) {
@@ -89,11 +113,13 @@ template <typename E, int D> struct Tile {
       if (row < end && c < dd) f[s] = *reinterpret_cast<const vec*>(head + row * ld + c);
     }
   }
-  // A wave's accumulators, block by block of 32 columns, into the rows row0 + lane%32 below `end` by way of its own part of the LDS, so
-  // that they leave as whole lines.
-  static __device__ __forceinline__ void store(const f32x16 (&acc)[BLOCKS], float factor, E* lds, E* head, int64_t ld, int row0, int end, int lane, int dd,
-                                               unsigned skip) {
+  // A wave's accumulators, block by block of 32 columns, into the rows row0 + lane%32 below `end` by way of its own part of the LDS (STORE
+  // bytes), so that they leave as whole lines.  skip: rows that stay as they are.
+  static constexpr int LD = D + (SZ == 2 ? 24 : 8), STORE = 32 * LD * SZ;
+  static __device__ __forceinline__ void store(const f32x16 (&acc)[BLOCKS], float factor, char* lds, E* head, int64_t ld, int row0, int end, int lane,
+                                               int dd, unsigned skip) {
     typedef E quad __attribute__((ext_vector_type(4)));
+    E* rows = reinterpret_cast<E*>(lds);
     wave_lds_order();
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b)
@@ -102,43 +128,55 @@ template <typename E, int D> struct Tile {
         quad w;
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = from_f<E>(acc[b][4 * c + e] * factor);
-        *reinterpret_cast<quad*>(lds + (lane & 31) * LD + 32 * b + 8 * c + 4 * (lane >> 5)) = w;
+        *reinterpret_cast<quad*>(rows + (lane & 31) * LD + 32 * b + 8 * c + 4 * (lane >> 5)) = w;
       }
     wave_lds_order();
     constexpr int P = D / VN;
 #pragma unroll
     for (int i = 0; i < 32 * P / 64; ++i) {
       const int v = lane + 64 * i, r = v / P, c = v % P * VN;
-      const vec w = *reinterpret_cast<const vec*>(lds + r * LD + c);
+      const vec w = *reinterpret_cast<const vec*>(rows + r * LD + c);
       if (row0 + r < end && c < dd && !(skip >> r & 1)) *reinterpret_cast<vec*>(head + (row0 + r) * ld + c) = w;
     }
   }
 };
 
-// ROWS rows on their way from memory to LDS through the registers of NT threads: fetch is issued before the products of the tile before, put
-// comes after them.  Rows are read through a buffer descriptor of the tile's own, so that offsets inside it are 32 bits wide however far the
-// rows lie apart; rows past the last one wanted and the columns past dd lie behind the descriptor's end and read as zeros.
-template <typename E, int D, int ROWS, int NT> struct TileLoad {
-  static constexpr int VN = Tile<E, D>::VN, P = D / VN, N = ROWS * P, NV = (N + NT - 1) / NT;
-  u32x4 v[NV];
-  __device__ __forceinline__ void fetch(const E* head, int64_t ld, int row0, int end, unsigned tid, int dd) {
-    const int rows = min(end - row0, ROWS);
-    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<E*>(head + row0 * ld), 0,
-                                                                        rows > 0 ? (int)(((rows - 1) * ld + dd) * sizeof(E)) : 0, 0x00020000);
+// Brings ROWS rows into LDS by NW waves.  The rows are read through a buffer descriptor of the tile's own, so that offsets inside it are 32 bits wide however
+// far the rows lie apart; rows at or past `end` and the columns past dd lie behind the descriptor's end and arrive as zeros.  tile_wait, before the
+// barrier that publishes a tile, waits for what a wave has under way.
+template <typename E, int D, int ROWS, int NW> struct TileLoad {
+  typedef Tile<E, D> TL;
+  static constexpr int N = ROWS / 8 * TL::SQUARES / NW;
+  static_assert(N * NW * 8 == ROWS * TL::SQUARES, "");
+  unsigned at[TL::SQUARES];   // of a lane's piece in the first 8 rows
+  int ld, width;              // elements of a row, bytes of a head's part of it
+  __device__ __forceinline__ TileLoad(int64_t stride, int lane, int dd) : ld((int)stride), width(dd * TL::SZ) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int p = (int)tid + NT * i, r = p / P, c = p % P * VN;
-      v[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, c < dd && (N % NT == 0 || p < N) ? (int)((r * (int)ld + c) * sizeof(E)) : (int)0x80000000, 0, 0);
+    for (int q = 0; q < TL::SQUARES; ++q) {
+      const int c = (8 * q + (int)((lane & 7) ^ TL::turn(lane >> 3))) * TL::VN;
+      at[q] = c < dd ? (unsigned)((lane >> 3) * ld + c) * TL::SZ : 0x80000000u;
     }
   }
-  __device__ __forceinline__ void put(E* tile, unsigned tid) const {
+  __device__ __forceinline__ void fetch(unsigned lds, const E* head, int row0, int end, int wave) const {
+    const int rows = min(end - row0, ROWS);
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<E*>(head + (int64_t)row0 * ld), 0,
+                                                                        rows > 0 ? (rows - 1) * ld * TL::SZ + width : 0, 0x00020000);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int p = (int)tid + NT * i;
-      if (N % NT == 0 || p < N) *reinterpret_cast<u32x4*>(tile + p / P * Tile<E, D>::LD + p % P * VN) = v[i];
+    for (int i = 0; i < N; ++i) {
+      // a wave's loads lie in one column of squares where the waves are as many as these columns, or a multiple
+      const int sq = wave + NW * i, oct = sq / TL::SQUARES, q = sq % TL::SQUARES;
+      unsigned from = at[0];
+#pragma unroll
+      for (int k = 1; k < TL::SQUARES; ++k) from = q == k ? at[k] : from;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(uintptr_t)(lds + oct * TL::OCTET + q * 1024), 16,
+                                               from + (unsigned)(8 * oct * ld * TL::SZ), 0, 0, 0);
     }
   }
 };
+__device__ __forceinline__ void tile_wait() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
+}
 
 // First and last of a wave's (or block's) tokens that have a range.  Ranges grow from token to token, so theirs are its union's ends (lo,
 // hi) and what all of them share (all_lo, all_hi).
@@ -164,72 +202,61 @@ template <bool ROWS> __device__ __forceinline__ Span block_span(const int32_t* r
   return span_join(span_of(lo[0], hi[0]), span_of(lo[1], hi[1]));
 }
 
-// The scores of a block, in powers of two.  factor: what turns an entry of `s` into that: scale * log2 e where there is neither cap nor bias
-// and s stays as the product left it, else 1.
+// The scores of a block, in powers of two.  MODE says which of cap and bias a call has.
 //   capped: softcap tanh(u / softcap) = softcap - 2 softcap / (1 + exp(2 u / softcap)); 16-bit types take it so, with the hardware's
 //   exp2 and reciprocal (absolute error softcap 2^-22, of weights that are then rounded to 2^-9 or 2^-12 of themselves); fp32 takes tanhf.
+enum DocMode { DOC_PLAIN = 0, DOC_CAP = 1, DOC_BIAS = 2 };   // or-ed
 struct DocScale {
-  float log2, cap, cap_log2, into_tanh, slope_log2;   // scale log2 e; softcap; softcap log2 e; 2 scale log2 e / softcap, or (fp32) scale / softcap; slope log2 e
-  bool capped, biased;
-  __device__ __forceinline__ float factor() const { return capped || biased ? 1.f : log2; }
+  float log2, cap_log2, into_tanh, slope_log2;   // scale log2 e; softcap log2 e; 2 scale log2 e / softcap, or (fp32) scale / softcap; slope log2 e
 };
-template <typename E> __device__ __forceinline__ DocScale doc_scale(const DocAttn& a, int h) {
-  const float slope = a.slopes ? a.slopes[h] : 0.f;
-  const bool capped = a.softcap > 0.f;
-  return DocScale{a.scale * DOC_LOG2E, a.softcap, a.softcap * DOC_LOG2E, capped ? (sizeof(E) == 4 ? a.scale : 2.f * DOC_LOG2E * a.scale) / a.softcap : 0.f,
-                  slope * DOC_LOG2E, capped, a.slopes != nullptr};
+template <typename E, int MODE> __device__ __forceinline__ DocScale doc_scale(const DocAttn& a, int h) {
+  return DocScale{a.scale * DOC_LOG2E, a.softcap * DOC_LOG2E, MODE & DOC_CAP ? (sizeof(E) == 4 ? a.scale : 2.f * DOC_LOG2E * a.scale) / a.softcap : 0.f,
+                  MODE & DOC_BIAS ? a.slopes[h] * DOC_LOG2E : 0.f};
 }
-// tanh(u / softcap) of a product, as (1 - tanh) / 2 in 16-bit types
+// tanh(u / softcap) of a product, as (1 - tanh) / 2 in 16-bit types; the score from it, and its slope 1 - tanh^2
 template <typename E> __device__ __forceinline__ float cap_part(const DocScale& c, float product) {
   if constexpr (sizeof(E) == 4) return tanhf(product * c.into_tanh);
   else return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(product * c.into_tanh));
 }
-template <typename E> __device__ __forceinline__ float cap_score(const DocScale& c, float part) {
-  return sizeof(E) == 4 ? c.cap_log2 * part : fmaf(-2.f * c.cap_log2, part, c.cap_log2);
+template <typename E> __device__ __forceinline__ float cap_score(const DocScale& c, float part, float plus) {
+  return sizeof(E) == 4 ? fmaf(c.cap_log2, part, plus) : fmaf(-2.f * c.cap_log2, part, c.cap_log2 + plus);
 }
 template <typename E> __device__ __forceinline__ float cap_slope(float part) {
-  return sizeof(E) == 4 ? (1.f - part) * (1.f + part) : 4.f * part * (1.f - part);
+  return sizeof(E) == 4 ? (1.f - part) * (1.f + part) : part * fmaf(part, -4.f, 4.f);
 }
 // apart: of the lane's own token and the one that its register 0 stands for
-__device__ __forceinline__ float bias_score(const DocScale& c, float apart, int r) { return -c.slope_log2 * fabsf(apart + (float)(8 * (r >> 2) + (r & 3))); }
-
-template <typename E> __device__ __forceinline__ void doc_scores(f32x16& s, const DocScale& c, float apart) {
-  if (c.capped) {
+__device__ __forceinline__ float bias_score(const DocScale& c, float apart, int r, float plus) {
+  return fmaf(-c.slope_log2, fabsf(apart + (float)(8 * (r >> 2) + (r & 3))), plus);
+}
+// Scores into s; a plain one stays as the product left it, to be taken times log2.
+template <typename E, int MODE> __device__ __forceinline__ void doc_scores(f32x16& s, const DocScale& c, float apart) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] = cap_score<E>(c, cap_part<E>(c, s[r]));
-  } else if (c.biased) {
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] *= c.log2;
-  }
-  if (c.biased) {
-#pragma unroll
-    for (int r = 0; r < 16; ++r) s[r] += bias_score(c, apart, r);
+  for (int r = 0; r < 16; ++r) {
+    if constexpr (MODE & DOC_CAP) s[r] = cap_score<E>(c, cap_part<E>(c, s[r]), 0.f);
+    else if constexpr (MODE & DOC_BIAS) s[r] *= c.log2;
+    if constexpr (MODE & DOC_BIAS) s[r] = bias_score(c, apart, r, s[r]);
   }
 }
-// Weights p = exp2(score - lse2[r]) into s, and p * (dp - delta[r]) * (the cap's slope) * factor into dp.  lse2 and delta: of the row that a register
-// (dK/dV) or the lane (dQ) stands for.
-template <typename E, typename F, typename G>
-__device__ __forceinline__ void doc_weights(f32x16& s, f32x16& dp, const DocScale& c, float apart, float p_shift, float factor, F&& lse2, G&& delta) {
-  if (!c.capped && !c.biased) {
+// Weights p = exp2(score - lse2) into s, and p * (dp - delta) * (the cap's slope) * factor into dp.  lse2(c) and delta(c): of the rows (dK/dV) that the
+// registers 4 c .. 4 c + 3 stand for, or of the lane's own (dQ); lse2 holds what else is added to the exponent, negated.
+template <typename E, int MODE, typename F, typename G>
+__device__ __forceinline__ void doc_weights(f32x16& s, f32x16& dp, const DocScale& c, float apart, float factor, F&& lse2, G&& delta) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c.log2, p_shift - lse2(r)));
-      dp[r] = s[r] * ((dp[r] - delta(r)) * factor);
-    }
-  } else if (!c.capped) {
+  for (int g = 0; g < 4; ++g) {
+    const f32x4 l = lse2(g), d = delta(g);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], c.log2, p_shift - lse2(r)) + bias_score(c, apart, r));
-      dp[r] = s[r] * ((dp[r] - delta(r)) * factor);
-    }
-  } else {
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float part = cap_part<E>(c, s[r]);
-      float x = cap_score<E>(c, part) + (p_shift - lse2(r));
-      if (c.biased) x += bias_score(c, apart, r);
+    for (int e = 0; e < 4; ++e) {
+      const int r = 4 * g + e;
+      float part = 0.f, x;
+      if constexpr (MODE & DOC_CAP) {
+        part = cap_part<E>(c, s[r]);
+        x = cap_score<E>(c, part, -l[e]);
+      } else x = fmaf(s[r], c.log2, -l[e]);
+      if constexpr (MODE & DOC_BIAS) x = bias_score(c, apart, r, x);
       s[r] = __builtin_amdgcn_exp2f(x);
-      dp[r] = s[r] * ((dp[r] - delta(r)) * factor) * cap_slope<E>(part);
+      float ds = s[r] * (dp[r] - d[e]);
+      if constexpr (MODE & DOC_CAP) ds *= cap_slope<E>(part);
+      dp[r] = __is_same(E, f16) ? ds * factor : ds;
     }
   }
 }
