@@ -334,10 +334,10 @@ class _Ops:
         fn = getattr(lib(), "stage_op_" + name)
 
         def call(*args):
-            conv = [(_ptr(a) if hasattr(a, "data_ptr") else a) for a in args]
-            code = fn(*conv)
+            code = fn(*[a.data_ptr() if hasattr(a, "data_ptr") else a for a in args])
             if code != STAGE_OK:
                 raise StageError(code, f"stage_op_{name}")
+        self.__dict__[name] = call   # found without this function from now on
         return call
 
 
@@ -377,10 +377,8 @@ def wgrad_parts(stream, dtype, M, N, K_each, K_last, A_parts, lda, B_parts, ldb,
 def rope_axes(stream, dtype, T, nq, nk, d, q, ldq, k, ldk, positions, sections, own_spectrum, base, sign, q_out, ldq_out, k_out, ldk_out):
     """stage_op_rope_axes with a list of the sections' pairs."""
     n = len(sections)
-    code = lib().stage_op_rope_axes(stream, dtype, T, nq, nk, d, _ptr(q), ldq, _ptr(k), ldk, _ptr(positions), n, (C.c_int32 * n)(*sections),
-                                    int(own_spectrum), base, sign, _ptr(q_out), ldq_out, _ptr(k_out), ldk_out)
-    if code != STAGE_OK:
-        raise StageError(code, "stage_op_rope_axes")
+    ops.rope_axes(stream, dtype, T, nq, nk, d, q, ldq, k, ldk, positions, n, (C.c_int32 * n)(*sections), int(own_spectrum), base, sign, q_out, ldq_out,
+                  k_out, ldk_out)
 
 
 def attention_docs_bwd_scratch_bytes(dtype, T, nh, nkv, d):

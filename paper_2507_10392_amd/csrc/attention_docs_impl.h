@@ -28,13 +28,14 @@ __device__ __forceinline__ float unit_of(float x) {
   return e > 60 || e < -60 ? 1.f : __uint_as_float((unsigned)(127 - e) << 23);
 }
 
-// Blocks of rows behind one another, the last (under a causal mask the longest) first, all heads of a block before the next one; key heads in
-// the fastest place, so that the blocks of a key head stay on an XCD where there are 8 of them and find its keys in its L2.
+// Blocks of rows, all heads of a block before the next one; key heads in the fastest place, so that the blocks of a key head stay on an XCD where
+// there are 8 of them and find its keys in its L2.  The longest blocks come first: by their ranges (a.sorted), or the last ones, which
+// under a causal mask are the longest of a document.
 struct DocBlock { int block, kv, h; };
-__device__ __forceinline__ DocBlock row_block(const DocAttn& a, int heads, int rows) {   // heads of a key head in a workgroup, rows of a block
+__device__ __forceinline__ DocBlock row_block(const DocAttn& a, int heads, int rows, int lane) {   // heads of a key head in a workgroup, rows of a block
   const int group = a.nh / a.nkv, sets = a.nkv * (group / heads), blocks = (a.T + rows - 1) / rows;
-  const int set = (int)blockIdx.x % sets, kv = set % a.nkv;
-  return DocBlock{blocks - 1 - (int)blockIdx.x / sets, kv, kv * group + set / a.nkv * heads};
+  const int set = (int)blockIdx.x % sets, kv = set % a.nkv, rank = (int)blockIdx.x / sets;
+  return DocBlock{a.sorted ? heavy_block<false>(a.ranges, a.T, rows, blocks, rank, lane) : blocks - 1 - rank, kv, kv * group + set / a.nkv * heads};
 }
 
 // Calls of their own, not inlined, so that the registers of the kernels' loops are not planned around them.
@@ -65,7 +66,7 @@ __global__ __launch_bounds__(256, KS == 1 ? 2 : 1) void doc_fwd_kernel(DocAttn a
   static_assert(LOOP >= (size_t)(KS - 1) * GROUPS * TL::BLOCKS * 4 * 64 * 16, "");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ks = wave / GROUPS, grp = wave % GROUPS, row_groups = GROUPS / heads, h_in = grp / row_groups, dd = a.d;
-  const DocBlock blk = row_block(a, heads, 32 * row_groups);
+  const DocBlock blk = row_block(a, heads, 32 * row_groups, lane);
   const int t0 = blk.block * 32 * row_groups, w0 = t0 + 32 * (grp % row_groups), my_q = w0 + (lane & 31), h = blk.h + h_in;
   const E* qh = (const E*)a.q + h * dd;
   const E *kh = (const E*)a.k + blk.kv * dd, *vh = (const E*)a.v + blk.kv * dd;
@@ -233,7 +234,7 @@ __global__ __launch_bounds__(256, KS == 1 && sizeof(E) == 2 ? 2 : 1) void doc_dq
   static_assert(LOOP >= (size_t)(KS - 1) * GROUPS * TL::BLOCKS * 4 * 64 * 16, "");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ks = wave / GROUPS, grp = wave % GROUPS, row_groups = GROUPS / heads, h_in = grp / row_groups, dd = a.d;
-  const DocBlock blk = row_block(a, heads, 32 * row_groups);
+  const DocBlock blk = row_block(a, heads, 32 * row_groups, lane);
   const int t0 = blk.block * 32 * row_groups, w0 = t0 + 32 * (grp % row_groups), my_q = w0 + (lane & 31), h = blk.h + h_in;
   const E *kh = (const E*)a.k + blk.kv * dd, *vh = (const E*)a.v + blk.kv * dd;
   const Span all = block_span<false>(a.ranges, t0, 32 * row_groups, a.T, lane);
@@ -345,7 +346,8 @@ __global__ __launch_bounds__(256, KS == 1 && sizeof(E) == 2 ? 2 : 1) void doc_dq
 template <typename E, int NW>
 __device__ __attribute__((noinline)) void redo_dkv(DocRedo<NW>* redo, int groups, int t0, const int32_t* ranges, int T, int d, int group, const E* q,
                                                    int64_t ldq, const E* k, const E* v, int64_t ldkv, const E* dout, int64_t ldo, const float* lse,
-                                                   const float* delta, float scale, float softcap, const float* slopes, E* dk, E* dv, int64_t lddkv) {
+                                                   const float* delta, float scale, float softcap, const float* slopes, E* dk, E* dv, int64_t lddkv,
+                                                   float* part_k, float* part_v, int64_t ld_part) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for_dealt_rows(redo->masks, groups, NW, wave, [&](int g, int r) {
     const int j = t0 + 32 * g + r;
@@ -361,8 +363,13 @@ __device__ __attribute__((noinline)) void redo_dkv(DocRedo<NW>* redo, int groups
 #pragma unroll
     for (int c = 0; c < 2; ++c)
       if (64 * c + lane < d) {
-        dk[j * lddkv + 64 * c + lane] = from_f<E>(xk[c] * scale);
-        dv[j * lddkv + 64 * c + lane] = from_f<E>(xv[c]);
+        if (part_k) {
+          part_k[j * ld_part + 64 * c + lane] = xk[c] * scale;
+          part_v[j * ld_part + 64 * c + lane] = xv[c];
+        } else {
+          dk[j * lddkv + 64 * c + lane] = from_f<E>(xk[c] * scale);
+          dv[j * lddkv + 64 * c + lane] = from_f<E>(xv[c]);
+        }
       }
   });
 }
@@ -374,13 +381,15 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
   constexpr int NW = KG * QS, SUB = ROWS / 32 / QS, TILE = TL::bytes(ROWS), STATS = HALF<E> ? 3 : 2;
   constexpr int STAT = STATS * ROWS * 4;             // log-sum-exp in powers of two less P_SHIFT, delta, (half) largest |dO|
   constexpr int V = NBUF * (2 * TILE + STAT);        // [NBUF][Q | dO], [NBUF][stats], [KG][V rows]
-  constexpr size_t LOOP = V + KG * TL::bytes(32), END = sizeof(DocRedo<NW>) + 16 + KG * TL::STORE, MERGE = (size_t)(QS - 1) * KG * TL::BLOCKS * 4 * 64 * 16;
+  constexpr size_t LOOP = V + KG * TL::bytes(32), END = sizeof(DocRedo<NW>) + 16 + KG * Tile<float, D>::STORE, MERGE = (size_t)(QS - 1) * KG * TL::BLOCKS * 4 * 64 * 16;
   static_assert(ROWS <= 64 * NW, "");
   __shared__ __align__(16) char smem_raw[LOOP > END ? LOOP : END];
   static_assert(sizeof(smem_raw) >= MERGE, "");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int qs = wave / KG, kg = wave % KG, dd = a.d, group = a.nh / a.nkv;
-  const int kv = (int)blockIdx.x % a.nkv, t0 = (int)blockIdx.x / a.nkv * 32 * KG;   // early keys, under a causal mask seen by the most rows, first
+  const int qs = wave / KG, kg = wave % KG, dd = a.d, group = a.nh / a.nkv / a.parts;
+  const int set = (int)blockIdx.x % (a.nkv * a.parts), kv = set % a.nkv, which = set / a.nkv, h0 = kv * (a.nh / a.nkv) + which * group;
+  const int rank = (int)blockIdx.x / (a.nkv * a.parts);
+  const int t0 = 32 * KG * (a.sorted ? heavy_block<true>(a.ranges, a.T, 32 * KG, (a.T + 32 * KG - 1) / (32 * KG), rank, lane) : rank);   // the longest first, in a document the early ones
   const int w0 = t0 + 32 * kg, my_k = w0 + (lane & 31);
   const E *kh = (const E*)a.k + kv * dd, *vh = (const E*)a.v + kv * dd;
   const unsigned smem = lds_address(smem_raw);
@@ -420,7 +429,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
 #pragma unroll
   for (int i = 0; i < TL::BLOCKS; ++i) dk[i] = dv[i] = f32x16{};
   float unit = 0.f;   // half: of the score gradients, none yet
-  int h = kv * group, t = 0;
+  int h = h0, t = 0;
   if (NBUF == 2 && total > 0) {
     fetch(0, h, all.lo);
     put_stats(0, all.lo);
@@ -514,6 +523,8 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
     merge_waves<TL::BLOCKS>(dk, red, qs, QS, lane);
   }
   const bool live = seen > 0 && my_k < a.T;
+  const int64_t ld_part = a.nkv * dd;
+  float *part_k = a.partial + (int64_t)which * a.T * ld_part + kv * dd, *part_v = part_k + (int64_t)a.parts * a.T * ld_part;
   DocRedo<NW>& redo = *reinterpret_cast<DocRedo<NW>*>(smem_raw);
   const unsigned again = redo_rows<NW>(redo, kg, qs == 0, qs == 0 && live && !(mark_of(dk) + mark_of(dv) == 0.f));
   if (qs == 0) {
@@ -521,14 +532,46 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
 #pragma unroll
       for (int i = 0; i < TL::BLOCKS; ++i) dk[i] = dv[i] = f32x16{};
     }
-    char* to = smem_raw + (sizeof(redo) + 15) / 16 * 16 + kg * TL::STORE;
-    TL::store(dv, HALF<E> ? 1.f / 16384.f : 1.f, to, (E*)a.dv + kv * dd, a.lddkv, w0, a.T, lane, dd, again);
-    TL::store(dk, HALF<E> && unit != 0.f ? a.scale / unit : a.scale, to, (E*)a.dk + kv * dd, a.lddkv, w0, a.T, lane, dd, again);
+    char* to = smem_raw + (sizeof(redo) + 15) / 16 * 16 + kg * Tile<float, D>::STORE;
+    const float fv = HALF<E> ? 1.f / 16384.f : 1.f, fk = HALF<E> && unit != 0.f ? a.scale / unit : a.scale;
+    if (a.parts > 1) {
+      Tile<float, D>::store(dv, fv, to, part_v, ld_part, w0, a.T, lane, dd, again);
+      Tile<float, D>::store(dk, fk, to, part_k, ld_part, w0, a.T, lane, dd, again);
+    } else {
+      TL::store(dv, fv, to, (E*)a.dv + kv * dd, a.lddkv, w0, a.T, lane, dd, again);
+      TL::store(dk, fk, to, (E*)a.dk + kv * dd, a.lddkv, w0, a.T, lane, dd, again);
+    }
   }
   if (__builtin_expect(any_row(redo.masks, KG, lane), 0))
-    redo_dkv<E, NW>(&redo, KG, t0, a.ranges, a.T, dd, group, (const E*)a.q + kv * group * dd, a.ldq, kh, vh, a.ldkv, (const E*)a.dout + kv * group * dd,
-                    a.ldo, a.lse + (int64_t)kv * group * a.T, a.delta + (int64_t)kv * group * a.T, a.scale, a.softcap,
-                    a.slopes ? a.slopes + kv * group : nullptr, (E*)a.dk + kv * dd, (E*)a.dv + kv * dd, a.lddkv);
+    redo_dkv<E, NW>(&redo, KG, t0, a.ranges, a.T, dd, group, (const E*)a.q + h0 * dd, a.ldq, kh, vh, a.ldkv, (const E*)a.dout + h0 * dd, a.ldo,
+                    a.lse + (int64_t)h0 * a.T, a.delta + (int64_t)h0 * a.T, a.scale, a.softcap, a.slopes ? a.slopes + h0 : nullptr, (E*)a.dk + kv * dd,
+                    (E*)a.dv + kv * dd, a.lddkv, a.parts > 1 ? part_k : nullptr, part_v, ld_part);
+}
+
+// Where the query heads of a key head are shared out over `parts` workgroups, these leave their sums in fp32; they meet here, in the order of the parts.
+template <typename E> __global__ __launch_bounds__(256) void doc_join_kernel(DocAttn a) {
+  constexpr int VN = 16 / sizeof(E);
+  typedef typename Vec<E>::type vec;
+  const int row = a.nkv * a.d / VN;   // vectors of a token
+  const int64_t n = (int64_t)a.T * row, at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (at >= 2 * n) return;
+  const bool is_v = at >= n;
+  const int64_t i = is_v ? at - n : at, t = i / row;
+  const int c = (int)(i - t * row) * VN;
+  float sum[VN] = {};
+  for (int p = 0; p < a.parts; ++p) {
+    const float* from = a.partial + (((int64_t)(is_v ? a.parts : 0) + p) * a.T + t) * (a.nkv * a.d) + c;
+#pragma unroll
+    for (int e = 0; e < VN; e += 4) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(from + e);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum[e + k] += x[k];
+    }
+  }
+  vec o;
+#pragma unroll
+  for (int e = 0; e < VN; ++e) o[e] = from_f<E>(sum[e]);
+  *reinterpret_cast<vec*>((E*)(is_v ? a.dv : a.dk) + t * a.lddkv + c) = o;
 }
 
 // Heads of a key head that share a workgroup of `groups` waves.
@@ -538,38 +581,47 @@ inline int doc_heads(const DocAttn& a, int groups) {
 }
 // Few blocks of 128 rows: waves share 32 rows, so that there are four times as many workgroups.
 inline bool doc_few(int64_t rows_times_heads) { return cdiv(rows_times_heads, 128) < 256; }
+// The longest blocks first by their ranges: where the workgroups are more than the chip holds at a time, and the blocks few enough to be ordered.
+inline bool doc_sorted(int64_t blocks, int64_t workgroups, int per_cu) { return blocks <= 256 && workgroups > 256 * per_cu; }
 
 // Waves that share rows, and rows of the tiles that they share out, as far as two buffers fit in LDS.
 template <typename E, int D> constexpr int SHARE = sizeof(E) == 4 && D > 64 ? 2 : 4;
-template <typename E, int D, int MODE> hipError_t doc_fwd(hipStream_t st, const DocAttn& a) {
+template <typename E, int D, int MODE> hipError_t doc_fwd(hipStream_t st, DocAttn a) {
   if (doc_few((int64_t)a.T * a.nh)) {
     constexpr int S = SHARE<E, D>;
     hipLaunchKernelGGL((doc_fwd_kernel<E, D, MODE, S, 32 * S, 2>), dim3((unsigned)(cdiv(a.T, 128 / S) * a.nh)), dim3(256), 0, st, a, 1);
   } else {
     const int heads = doc_heads(a, 4);
-    hipLaunchKernelGGL((doc_fwd_kernel<E, D, MODE, 1, ROWS_LONG<E>, 2>), dim3((unsigned)(cdiv(a.T, 128 / heads) * (a.nh / heads))), dim3(256), 0, st, a, heads);
+    const int64_t blocks = cdiv(a.T, 128 / heads), wgs = blocks * (a.nh / heads);
+    a.sorted = doc_sorted(blocks, wgs, 2);
+    hipLaunchKernelGGL((doc_fwd_kernel<E, D, MODE, 1, ROWS_LONG<E>, 2>), dim3((unsigned)wgs), dim3(256), 0, st, a, heads);
   }
   return hipGetLastError();
 }
-template <typename E, int D, int MODE> hipError_t doc_bwd(hipStream_t st, const DocAttn& a) {
+template <typename E, int D, int MODE, int KG, int QS, int ROWS, int NBUF> hipError_t doc_dkv(hipStream_t st, DocAttn a) {
+  const int64_t blocks = cdiv(a.T, 32 * KG), wgs = blocks * a.nkv * a.parts;
+  a.sorted = doc_sorted(blocks, wgs, 1);
+  hipLaunchKernelGGL((doc_dkv_kernel<E, D, MODE, KG, QS, ROWS, NBUF>), dim3((unsigned)wgs), dim3(64 * KG * QS), 0, st, a);
+  if (a.parts > 1) hipLaunchKernelGGL(doc_join_kernel<E>, dim3((unsigned)cdiv(2 * (int64_t)a.T * (a.nkv * a.d / (16 / (int)sizeof(E))), 256)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+template <typename E, int D, int MODE> hipError_t doc_bwd(hipStream_t st, DocAttn a) {
   if (doc_few((int64_t)a.T * a.nh)) {
     constexpr int S = SHARE<E, D>;
     hipLaunchKernelGGL((doc_dq_kernel<E, D, MODE, S, 32 * S, 2>), dim3((unsigned)(cdiv(a.T, 128 / S) * a.nh)), dim3(256), 0, st, a, 1);
   } else {
     const int heads = doc_heads(a, 4);
-    hipLaunchKernelGGL((doc_dq_kernel<E, D, MODE, 1, ROWS_LONG<E>, 2>), dim3((unsigned)(cdiv(a.T, 128 / heads) * (a.nh / heads))), dim3(256), 0, st, a, heads);
+    const int64_t blocks = cdiv(a.T, 128 / heads), wgs = blocks * (a.nh / heads);
+    a.sorted = doc_sorted(blocks, wgs, 2);
+    hipLaunchKernelGGL((doc_dq_kernel<E, D, MODE, 1, ROWS_LONG<E>, 2>), dim3((unsigned)wgs), dim3(256), 0, st, a, heads);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (doc_few((int64_t)a.T * a.nkv)) {
-    constexpr int BUFFERS = sizeof(E) == 4 && D > 64 ? 1 : 2;
-    hipLaunchKernelGGL((doc_dkv_kernel<E, D, MODE, 1, 4, 128, BUFFERS>), dim3((unsigned)(cdiv(a.T, 32) * a.nkv)), dim3(256), 0, st, a);
-  } else if constexpr (sizeof(E) == 4) {
-    hipLaunchKernelGGL((doc_dkv_kernel<E, D, MODE, 4, 1, 32, 2>), dim3((unsigned)(cdiv(a.T, 128) * a.nkv)), dim3(256), 0, st, a);
-  } else {
-    hipLaunchKernelGGL((doc_dkv_kernel<E, D, MODE, 4, 2, 64, 2>), dim3((unsigned)(cdiv(a.T, 128) * a.nkv)), dim3(512), 0, st, a);
-  }
-  return hipGetLastError();
+  constexpr int BUFFERS = sizeof(E) == 4 && D > 64 ? 1 : 2;
+  const int keys = doc_dkv_keys((DType)(sizeof(E) == 4 ? F32 : BF16), a.T, a.nh, a.nkv);
+  if (keys == 32) return doc_dkv<E, D, MODE, 1, 4, 128, BUFFERS>(st, a);
+  if constexpr (sizeof(E) == 4) return doc_dkv<E, D, MODE, 4, 1, 32, 2>(st, a);
+  else return keys == 64 ? doc_dkv<E, D, MODE, 2, 4, 128, 2>(st, a) : doc_dkv<E, D, MODE, 4, 2, 64, 2>(st, a);
 }
 template <typename E, int D, int MODE> hipError_t doc_either(hipStream_t st, const DocAttn& a, bool backward) {
   return backward ? doc_bwd<E, D, MODE>(st, a) : doc_fwd<E, D, MODE>(st, a);

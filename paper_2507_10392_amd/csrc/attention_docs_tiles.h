@@ -202,9 +202,35 @@ template <bool ROWS> __device__ __forceinline__ Span block_span(const int32_t* r
   return span_join(span_of(lo[0], hi[0]), span_of(lo[1], hi[1]));
 }
 
+// The rank-th longest of `blocks` (at most 256) blocks of `rows` tokens, by the keys that they see or the rows that see them, in steps of 128 and, where
+// equal, the earlier one first.  Which tokens begin a document is known on the device only, so each workgroup finds its block by itself: the blocks'
+// numbers (length, then place) lie four to a lane, and the one with `rank` larger ones is found bit by bit, by counting.
+template <bool ROWS> __device__ __forceinline__ int heavy_block(const int32_t* ranges, int T, int rows, int blocks, int rank, int lane) {
+  int number[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int b = lane + 64 * i;
+    number[i] = -1;
+    if (b < blocks) {
+      const int4 first = doc_range((const int4*)ranges, b * rows, T), last = doc_range((const int4*)ranges, min(b * rows + rows, T) - 1, T);
+      const int span = ROWS ? last.w - first.z : last.y - first.x;
+      number[i] = min(max((span + 127) >> 7, 0), 127) << 8 | (255 - b);
+    }
+  }
+  int found = 0;
+  for (int bit = 1 << 14; bit; bit >>= 1) {
+    const int above = found | bit;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n += __popcll(__ballot(number[i] >= above));
+    if (n > rank) found = above;
+  }
+  return 255 - (found & 255);
+}
+
 // The scores of a block, in powers of two.  MODE says which of cap and bias a call has.
 //   capped: softcap tanh(u / softcap) = softcap - 2 softcap / (1 + exp(2 u / softcap)); 16-bit types take it so, with the hardware's
-//   exp2 and reciprocal (absolute error softcap 2^-22, of weights that are then rounded to 2^-9 or 2^-12 of themselves); fp32 takes tanhf.
+//   exp2 and reciprocal (absolute error softcap 2^-22, of weights that are then rounded to 2^-9 or 2^-12 of themselves).  fp32 takes tanh_f.
 enum DocMode { DOC_PLAIN = 0, DOC_CAP = 1, DOC_BIAS = 2 };   // or-ed
 struct DocScale {
   float log2, cap_log2, into_tanh, slope_log2;   // scale log2 e; softcap log2 e; 2 scale log2 e / softcap, or (fp32) scale / softcap; slope log2 e
@@ -213,9 +239,23 @@ template <typename E, int MODE> __device__ __forceinline__ DocScale doc_scale(co
   return DocScale{a.scale * DOC_LOG2E, a.softcap * DOC_LOG2E, MODE & DOC_CAP ? (sizeof(E) == 4 ? a.scale : 2.f * DOC_LOG2E * a.scale) / a.softcap : 0.f,
                   MODE & DOC_BIAS ? a.slopes[h] * DOC_LOG2E : 0.f};
 }
+// tanh within 1.5e-7 of itself: below 0.6 an odd polynomial (least squares in the relative error, which is 1e-10), above from the exponential, whose
+// cancellation is harmless there.  tanhf's branches and division took most of the fp32 kernels' time (capped forward, 1000 tokens, 8 heads of
+// 64: see the launch).
+__device__ __forceinline__ float tanh_f(float u) {
+  const float z = u * u;
+  float p = 0.0022269718f;
+  p = fmaf(p, z, -0.0082627423f);
+  p = fmaf(p, z, 0.021732720f);
+  p = fmaf(p, z, -0.053952165f);
+  p = fmaf(p, z, 0.13333246f);
+  p = fmaf(p, z, -0.33333331f);
+  const float t = fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.f * DOC_LOG2E * fabsf(u))), 1.f);
+  return fabsf(u) < 0.6f ? fmaf(u * z, p, u) : copysignf(t, u);
+}
 // tanh(u / softcap) of a product, as (1 - tanh) / 2 in 16-bit types; the score from it, and its slope 1 - tanh^2
 template <typename E> __device__ __forceinline__ float cap_part(const DocScale& c, float product) {
-  if constexpr (sizeof(E) == 4) return tanhf(product * c.into_tanh);
+  if constexpr (sizeof(E) == 4) return tanh_f(product * c.into_tanh);
   else return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(product * c.into_tanh));
 }
 template <typename E> __device__ __forceinline__ float cap_score(const DocScale& c, float part, float plus) {

@@ -228,8 +228,13 @@ struct DocAttn {
   float scale, softcap; const float* slopes;
   const void* dout; void* o; int64_t ldo; float* lse;      // o, lse: results of the forward, inputs of the backward
   void* dq; int64_t lddq; void *dk, *dv; int64_t lddkv;
-  float* delta;                                            // backward: [nh, T], dO_i . O_i
+  float* delta;                                            // backward: [nh, T], dO_i . O_i, and in half [nh, T], the largest |dO_i|
+  float* partial; int parts;                               // parts > 1: float[2][parts][T][nkv * d], dK and dV by part of the query heads of a key head
+  int sorted;                                              // set by the launches: the longest blocks first
 };
+// Keys of a workgroup of the dK/dV kernel, and the parts in which the query heads of a key head are shared out over workgroups.
+int doc_dkv_keys(DType dt, int T, int nh, int nkv);
+int doc_dkv_parts(DType dt, int T, int nh, int nkv);
 hipError_t attn_docs_fwd(hipStream_t st, DType dt, const DocAttn& a);
 int64_t attn_docs_bwd_scratch(DType dt, int T, int nh, int nkv, int d);   // bytes
 hipError_t attn_docs_bwd(hipStream_t st, DType dt, const DocAttn& a, void* scratch);
