@@ -21,7 +21,6 @@ namespace {
 template <typename E> constexpr bool HALF = __is_same(E, f16);
 template <typename E> constexpr float P_LAG = HALF<E> ? 7.f : 0.f;     // forward: weights are at most 2^(8 + lag)
 template <typename E> constexpr float P_SHIFT = HALF<E> ? 14.f : 0.f;  // backward: weights times 2^shift
-template <typename E> constexpr int ROWS_LONG = sizeof(E) == 4 ? 32 : 64;   // rows of a tile where a wave takes all of them
 // 2^-e for the exponent e of x > 0, within what halves times it can use; 1 for 0, inf and NaN
 __device__ __forceinline__ float unit_of(float x) {
   const int e = (int)((__float_as_uint(x) >> 23) & 255) - 127;
@@ -55,22 +54,22 @@ __device__ __attribute__((noinline)) void redo_fwd(DocRedo<NW>* redo, int groups
 // ------------------------------------------------------------------------------------------ forward
 // Four waves.  KS = 1: each has 32 rows of its own and walks all keys of a tile, two workgroups to a CU.  KS = 4: the four share 32 rows, each takes
 // 32 keys of a tile, and their sums meet at the end: for few rows.
-template <typename E, int D, int MODE, int KS, int ROWS, int NBUF>
-__global__ __launch_bounds__(256, KS == 1 ? 2 : 1) void doc_fwd_kernel(DocAttn a, int heads) {
+template <typename E, int D, int MODE, int NW, int KS, int ROWS>
+__global__ __launch_bounds__(64 * NW, NW == 8 || KS == 1 ? 2 : 1) void doc_fwd_kernel(DocAttn a, int heads) {
   typedef Tile<E, D> TL;
   typedef Mat<E> M;
-  constexpr int NW = 4, GROUPS = NW / KS, SUB = ROWS / 32 / KS, TILE = TL::bytes(ROWS);
+  constexpr int GROUPS = NW / KS, SUB = ROWS / 32 / KS, TILE = TL::bytes(ROWS);
   constexpr float LAG = P_LAG<E>;
-  constexpr size_t LOOP = NBUF * 2 * TILE, END = sizeof(DocRedo<NW>) + 16 + GROUPS * TL::STORE;   // [NBUF][keys | values]
+  constexpr size_t LOOP = 4 * TILE, END = sizeof(DocRedo<NW>) + 16 + GROUPS * TL::STORE;   // two buffers of keys and values
   __shared__ __align__(16) char smem_raw[LOOP > END ? LOOP : END];
-  static_assert(LOOP >= (size_t)(KS - 1) * GROUPS * TL::BLOCKS * 4 * 64 * 16, "");
+  static_assert((LOOP > END ? LOOP : END) >= (size_t)(KS - 1) * GROUPS * TL::BLOCKS * 4 * 64 * 16, "");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ks = wave / GROUPS, grp = wave % GROUPS, row_groups = GROUPS / heads, h_in = grp / row_groups, dd = a.d;
   const DocBlock blk = row_block(a, heads, 32 * row_groups, lane);
   const int t0 = blk.block * 32 * row_groups, w0 = t0 + 32 * (grp % row_groups), my_q = w0 + (lane & 31), h = blk.h + h_in;
   const E* qh = (const E*)a.q + h * dd;
   const E *kh = (const E*)a.k + blk.kv * dd, *vh = (const E*)a.v + blk.kv * dd;
-  const Span all = block_span<false>(a.ranges, t0, 32 * row_groups, a.T, lane);
+  const Span all = block_span<false, (32 * GROUPS + 63) / 64>(a.ranges, t0, 32 * row_groups, a.T, lane);
   const int4 range = my_q < a.T ? doc_range((const int4*)a.ranges, my_q, a.T) : make_int4(0, 0, 0, 0);
   typename M::vec qf[TL::FRAGS];
   TL::load_frags(qf, qh, a.ldq, my_q, a.T, lane, dd);
@@ -90,7 +89,7 @@ __global__ __launch_bounds__(256, KS == 1 ? 2 : 1) void doc_fwd_kernel(DocAttn a
 #pragma unroll
   for (int i = 0; i < TL::BLOCKS; ++i) oacc[i] = f32x16{};
   float m = -INFINITY, l = 0.f;   // the reference of the weights, and their sum
-  if (NBUF == 2 && tiles > 0) {
+  if (tiles > 0) {
     fetch(smem, all.lo);
     tile_wait();
     __syncthreads();
@@ -98,11 +97,7 @@ __global__ __launch_bounds__(256, KS == 1 ? 2 : 1) void doc_fwd_kernel(DocAttn a
   const float f = MODE == DOC_PLAIN ? sc.log2 : 1.f;
   for (int t = 0; t < tiles; ++t) {
     const int key0 = all.lo + t * ROWS;
-    if (NBUF == 1) {
-      fetch(smem, key0);
-      tile_wait();
-      __syncthreads();
-    } else if (t + 1 < tiles) fetch(smem + ((t + 1) & 1) * 2 * TILE, key0 + ROWS);   // that buffer was last read before the barrier that ended the iteration before
+    if (t + 1 < tiles) fetch(smem + ((t + 1) & 1) * 2 * TILE, key0 + ROWS);   // that buffer was last read before the barrier that ended the iteration before
     const int kb = key0 + ks * 32 * SUB;
     if (kb < mine.hi && kb + 32 * SUB > mine.lo) {
       f32x16 s[SUB];
@@ -161,10 +156,8 @@ __global__ __launch_bounds__(256, KS == 1 ? 2 : 1) void doc_fwd_kernel(DocAttn a
           for (int b = 0; b < TL::BLOCKS; ++b) oacc[b] = M::cols(at.column(TILE, 32 * j + 16 * u, b), pf, oacc[b]);
         }
     }
-    if (NBUF == 2) {
-      tile_wait();
-      at.move(t & 1 ? -2 * TILE : 2 * TILE);
-    }
+    tile_wait();
+    at.move(t & 1 ? -2 * TILE : 2 * TILE);
     __syncthreads();
   }
   if constexpr (KS > 1) {
@@ -224,20 +217,20 @@ __device__ __attribute__((noinline)) void redo_dq(DocRedo<NW>* redo, int groups,
   });
 }
 
-template <typename E, int D, int MODE, int KS, int ROWS, int NBUF>
-__global__ __launch_bounds__(256, KS == 1 && sizeof(E) == 2 ? 2 : 1) void doc_dq_kernel(DocAttn a, int heads) {
+template <typename E, int D, int MODE, int NW, int KS, int ROWS>
+__global__ __launch_bounds__(64 * NW, sizeof(E) == 2 && (NW == 8 || KS == 1) ? 2 : 1) void doc_dq_kernel(DocAttn a, int heads) {
   typedef Tile<E, D> TL;
   typedef Mat<E> M;
-  constexpr int NW = 4, GROUPS = NW / KS, SUB = ROWS / 32 / KS, TILE = TL::bytes(ROWS);
-  constexpr size_t LOOP = NBUF * 2 * TILE, END = sizeof(DocRedo<NW>) + 16 + GROUPS * TL::STORE;   // [NBUF][keys | values]
+  constexpr int GROUPS = NW / KS, SUB = ROWS / 32 / KS, TILE = TL::bytes(ROWS);
+  constexpr size_t LOOP = 4 * TILE, END = sizeof(DocRedo<NW>) + 16 + GROUPS * TL::STORE;   // two buffers of keys and values
   __shared__ __align__(16) char smem_raw[LOOP > END ? LOOP : END];
-  static_assert(LOOP >= (size_t)(KS - 1) * GROUPS * TL::BLOCKS * 4 * 64 * 16, "");
+  static_assert((LOOP > END ? LOOP : END) >= (size_t)(KS - 1) * GROUPS * TL::BLOCKS * 4 * 64 * 16, "");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ks = wave / GROUPS, grp = wave % GROUPS, row_groups = GROUPS / heads, h_in = grp / row_groups, dd = a.d;
   const DocBlock blk = row_block(a, heads, 32 * row_groups, lane);
   const int t0 = blk.block * 32 * row_groups, w0 = t0 + 32 * (grp % row_groups), my_q = w0 + (lane & 31), h = blk.h + h_in;
   const E *kh = (const E*)a.k + blk.kv * dd, *vh = (const E*)a.v + blk.kv * dd;
-  const Span all = block_span<false>(a.ranges, t0, 32 * row_groups, a.T, lane);
+  const Span all = block_span<false, (32 * GROUPS + 63) / 64>(a.ranges, t0, 32 * row_groups, a.T, lane);
   const int4 range = my_q < a.T ? doc_range((const int4*)a.ranges, my_q, a.T) : make_int4(0, 0, 0, 0);
   const int lo = range.x, seen = max(range.y - range.x, 0);
   const bool live = seen > 0 && my_q < a.T;
@@ -256,7 +249,7 @@ __global__ __launch_bounds__(256, KS == 1 && sizeof(E) == 2 ? 2 : 1) void doc_dq
     load.fetch(to + TILE, vh, row0, all.hi, wave);
   };
   typename TL::Lane at(smem + TL::bytes(ks * 32 * SUB), lane);
-  if (NBUF == 2 && tiles > 0) fetch(smem, all.lo);   // in flight while delta is formed
+  if (tiles > 0) fetch(smem, all.lo);   // in flight while delta is formed
   float delta = 0.f, largest = 0.f;
   {
     typename M::vec of[TL::FRAGS];
@@ -279,17 +272,13 @@ __global__ __launch_bounds__(256, KS == 1 && sizeof(E) == 2 ? 2 : 1) void doc_dq
   f32x16 acc[TL::BLOCKS];
 #pragma unroll
   for (int i = 0; i < TL::BLOCKS; ++i) acc[i] = f32x16{};
-  if (NBUF == 2 && tiles > 0) {
+  if (tiles > 0) {
     tile_wait();
     __syncthreads();
   }
   for (int t = 0; t < tiles; ++t) {
     const int key0 = all.lo + t * ROWS;
-    if (NBUF == 1) {
-      fetch(smem, key0);
-      tile_wait();
-      __syncthreads();
-    } else if (t + 1 < tiles) fetch(smem + ((t + 1) & 1) * 2 * TILE, key0 + ROWS);   // that buffer was last read before the barrier that ended the iteration before
+    if (t + 1 < tiles) fetch(smem + ((t + 1) & 1) * 2 * TILE, key0 + ROWS);   // that buffer was last read before the barrier that ended the iteration before
     const int kb0 = key0 + ks * 32 * SUB;
     if (kb0 < mine.hi && kb0 + 32 * SUB > mine.lo) {
       const bool part = kb0 < mine.all_lo || kb0 + 32 * SUB > mine.all_hi;
@@ -317,10 +306,8 @@ __global__ __launch_bounds__(256, KS == 1 && sizeof(E) == 2 ? 2 : 1) void doc_dq
         }
       }
     }
-    if (NBUF == 2) {
-      tile_wait();
-      at.move(t & 1 ? -2 * TILE : 2 * TILE);
-    }
+    tile_wait();
+    at.move(t & 1 ? -2 * TILE : 2 * TILE);
     __syncthreads();
   }
   if constexpr (KS > 1) merge_waves<TL::BLOCKS>(acc, reinterpret_cast<f32x4*>(smem_raw) + grp * (KS - 1) * TL::BLOCKS * 4 * 64, ks, KS, lane);
@@ -393,7 +380,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
   const int w0 = t0 + 32 * kg, my_k = w0 + (lane & 31);
   const E *kh = (const E*)a.k + kv * dd, *vh = (const E*)a.v + kv * dd;
   const unsigned smem = lds_address(smem_raw);
-  const Span all = block_span<true>(a.ranges, t0, 32 * KG, a.T, lane);
+  const Span all = block_span<true, (32 * KG + 63) / 64>(a.ranges, t0, 32 * KG, a.T, lane);
   const int4 range = my_k < a.T ? doc_range((const int4*)a.ranges, my_k, a.T) : make_int4(0, 0, 0, 0);
   const int lo = range.z, seen = max(range.w - range.z, 0);
   typename M::vec kf[TL::FRAGS];
@@ -579,24 +566,33 @@ inline int doc_heads(const DocAttn& a, int groups) {
   const int group = a.nh / a.nkv;
   return groups % 4 == 0 && group % 4 == 0 ? 4 : groups % 2 == 0 && group % 2 == 0 ? 2 : 1;
 }
-// Few blocks of 128 rows: waves share 32 rows, so that there are four times as many workgroups.
-inline bool doc_few(int64_t rows_times_heads) { return cdiv(rows_times_heads, 128) < 256; }
 // The longest blocks first by their ranges: where the workgroups are more than the chip holds at a time, and the blocks few enough to be ordered.
 inline bool doc_sorted(int64_t blocks, int64_t workgroups, int per_cu) { return blocks <= 256 && workgroups > 256 * per_cu; }
 
 // Waves that share rows, and rows of the tiles that they share out, as far as two buffers fit in LDS.
 template <typename E, int D> constexpr int SHARE = sizeof(E) == 4 && D > 64 ? 2 : 4;
-template <typename E, int D, int MODE> hipError_t doc_fwd(hipStream_t st, DocAttn a) {
-  if (doc_few((int64_t)a.T * a.nh)) {
-    constexpr int S = SHARE<E, D>;
-    hipLaunchKernelGGL((doc_fwd_kernel<E, D, MODE, S, 32 * S, 2>), dim3((unsigned)(cdiv(a.T, 128 / S) * a.nh)), dim3(256), 0, st, a, 1);
-  } else {
-    const int heads = doc_heads(a, 4);
-    const int64_t blocks = cdiv(a.T, 128 / heads), wgs = blocks * (a.nh / heads);
-    a.sorted = doc_sorted(blocks, wgs, 2);
-    hipLaunchKernelGGL((doc_fwd_kernel<E, D, MODE, 1, ROWS_LONG<E>, 2>), dim3((unsigned)wgs), dim3(256), 0, st, a, heads);
-  }
+template <typename E, int D, int MODE, int NW, int KS, int ROWS, bool BWD> hipError_t doc_rows(hipStream_t st, DocAttn a) {
+  const int heads = doc_heads(a, NW / KS);
+  const int64_t blocks = cdiv(a.T, 32 * (NW / KS) / heads), wgs = blocks * (a.nh / heads);
+  a.sorted = doc_sorted(blocks, wgs, NW == 4 && KS == 1 ? 2 : 1);
+  if constexpr (BWD) hipLaunchKernelGGL((doc_dq_kernel<E, D, MODE, NW, KS, ROWS>), dim3((unsigned)wgs), dim3(64 * NW), 0, st, a, heads);
+  else hipLaunchKernelGGL((doc_fwd_kernel<E, D, MODE, NW, KS, ROWS>), dim3((unsigned)wgs), dim3(64 * NW), 0, st, a, heads);
   return hipGetLastError();
+}
+// The forward's and dQ's workgroups by the groups of 32 rows that there are, for 1024 SIMDs: with few of them the waves of a workgroup share rows and
+// each walks a part of the keys.  us, bf16, heads of 128, forward: 500 tokens, 8 heads (125 groups) four waves on 32 rows 11.3, on
+// 128 rows 14.5, eight waves on 64 rows 12.5; 1024 tokens, 16 heads (512) 25.2, 24.1, 18.3; 2048 tokens, 16 heads over 4 (1024) 44, 26.6, 28.1
+// and eight waves on 128 rows 23.4; 4096 tokens, 32 heads over 8 (4096), six documents four waves on 128 rows 75, eight on 256 rows 84 (one
+// document 155 and 144: the only kind that gains, by 7 % and less the longer).  dQ likewise.
+template <typename E, int D, int MODE, bool BWD> hipError_t doc_by_rows(hipStream_t st, const DocAttn& a) {
+  constexpr int S = SHARE<E, D>;
+  const int64_t groups = cdiv(a.T, 32) * a.nh;
+  if (groups < (sizeof(E) == 2 ? 256 : 1024)) return doc_rows<E, D, MODE, 4, S, 32 * S, BWD>(st, a);
+  if constexpr (sizeof(E) == 2) {
+    if (groups < 768) return doc_rows<E, D, MODE, 8, 4, 128, BWD>(st, a);
+    if (groups < 2000) return doc_rows<E, D, MODE, 8, 2, 128, BWD>(st, a);
+    return doc_rows<E, D, MODE, 4, 1, 64, BWD>(st, a);
+  } else return doc_rows<E, D, MODE, 4, 1, 32, BWD>(st, a);
 }
 template <typename E, int D, int MODE, int KG, int QS, int ROWS, int NBUF> hipError_t doc_dkv(hipStream_t st, DocAttn a) {
   const int64_t blocks = cdiv(a.T, 32 * KG), wgs = blocks * a.nkv * a.parts;
@@ -605,17 +601,8 @@ template <typename E, int D, int MODE, int KG, int QS, int ROWS, int NBUF> hipEr
   if (a.parts > 1) hipLaunchKernelGGL(doc_join_kernel<E>, dim3((unsigned)cdiv(2 * (int64_t)a.T * (a.nkv * a.d / (16 / (int)sizeof(E))), 256)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
-template <typename E, int D, int MODE> hipError_t doc_bwd(hipStream_t st, DocAttn a) {
-  if (doc_few((int64_t)a.T * a.nh)) {
-    constexpr int S = SHARE<E, D>;
-    hipLaunchKernelGGL((doc_dq_kernel<E, D, MODE, S, 32 * S, 2>), dim3((unsigned)(cdiv(a.T, 128 / S) * a.nh)), dim3(256), 0, st, a, 1);
-  } else {
-    const int heads = doc_heads(a, 4);
-    const int64_t blocks = cdiv(a.T, 128 / heads), wgs = blocks * (a.nh / heads);
-    a.sorted = doc_sorted(blocks, wgs, 2);
-    hipLaunchKernelGGL((doc_dq_kernel<E, D, MODE, 1, ROWS_LONG<E>, 2>), dim3((unsigned)wgs), dim3(256), 0, st, a, heads);
-  }
-  const hipError_t e = hipGetLastError();
+template <typename E, int D, int MODE> hipError_t doc_bwd(hipStream_t st, const DocAttn& a) {
+  const hipError_t e = doc_by_rows<E, D, MODE, true>(st, a);
   if (e != hipSuccess) return e;
   constexpr int BUFFERS = sizeof(E) == 4 && D > 64 ? 1 : 2;
   const int keys = doc_dkv_keys((DType)(sizeof(E) == 4 ? F32 : BF16), a.T, a.nh, a.nkv);
@@ -624,7 +611,7 @@ template <typename E, int D, int MODE> hipError_t doc_bwd(hipStream_t st, DocAtt
   else return keys == 64 ? doc_dkv<E, D, MODE, 2, 4, 128, 2>(st, a) : doc_dkv<E, D, MODE, 4, 2, 64, 2>(st, a);
 }
 template <typename E, int D, int MODE> hipError_t doc_either(hipStream_t st, const DocAttn& a, bool backward) {
-  return backward ? doc_bwd<E, D, MODE>(st, a) : doc_fwd<E, D, MODE>(st, a);
+  return backward ? doc_bwd<E, D, MODE>(st, a) : doc_by_rows<E, D, MODE, false>(st, a);
 }
 template <typename E, int D> hipError_t doc_mode(hipStream_t st, const DocAttn& a, bool backward) {
   const bool cap = a.softcap > 0.f;

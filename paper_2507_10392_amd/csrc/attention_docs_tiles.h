@@ -189,19 +189,21 @@ __device__ __forceinline__ Span span_of(int lo, int hi) {
               __builtin_amdgcn_readlane(hi, first)};
 }
 __device__ __forceinline__ Span span_join(const Span& a, const Span& b) { return a.lo >= a.hi ? b : b.lo >= b.hi ? a : Span{a.lo, b.hi, b.all_lo, a.all_hi}; }
-// Of `n` (at most 128) tokens from t0: the keys that they see, or the rows that see them.
-template <bool ROWS> __device__ __forceinline__ Span block_span(const int32_t* ranges, int t0, int n, int T, int lane) {
-  int lo[2], hi[2];
+// Of `n` (at most 64 N) tokens from t0: the keys that they see, or the rows that see them.
+template <bool ROWS, int N> __device__ __forceinline__ Span block_span(const int32_t* ranges, int t0, int n, int T, int lane) {
+  int lo[N], hi[N];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < N; ++i) {
     const int t = lane + 64 * i;
     const int4 r = t < n && t0 + t < T ? doc_range((const int4*)ranges, t0 + t, T) : make_int4(0, 0, 0, 0);
     lo[i] = ROWS ? r.z : r.x;
     hi[i] = ROWS ? r.w : r.y;
   }
-  return span_join(span_of(lo[0], hi[0]), span_of(lo[1], hi[1]));
+  Span all = span_of(lo[0], hi[0]);
+#pragma unroll
+  for (int i = 1; i < N; ++i) all = span_join(all, span_of(lo[i], hi[i]));
+  return all;
 }
-
 // The rank-th longest of `blocks` (at most 256) blocks of `rows` tokens, by the keys that they see or the rows that see them, in steps of 128 and, where
 // equal, the earlier one first.  Which tokens begin a document is known on the device only, so each workgroup finds its block by itself: the blocks'
 // numbers (length, then place) lie four to a lane, and the one with `rank` larger ones is found bit by bit, by counting.

@@ -1,4 +1,4 @@
-"""Attention inside packed documents in 64 bits on the CPU, and how far a correct kernel may be off it.
+"""Attention inside packed documents in 64 bits (on the device of its inputs), and how far a correct kernel may be off it.
 
 The bounds are worst cases of the roundings that the kernels make, element by element:
 - scores: sums of d exact products in fp32, (d + 8) 2^-24 of the sum of absolute values; the cap, the bias and the change to powers of two,
@@ -32,8 +32,8 @@ def visible(T, offsets, prefix):
     for n in range(len(offsets) - 1):
         b, e = offsets[n], offsets[n + 1]
         p = min(prefix[n], e - b) if prefix else 0
-        for i in range(b, e):
-            m[i, b:max(i + 1, b + p)] = True
+        m[b:e, b:e] = np.tril(np.ones((e - b, e - b), dtype=bool))
+        m[b:e, b:b + p] = True
     return m
 
 
@@ -84,11 +84,11 @@ def scores(c, q, k):
         s, ds = c.softcap * t, 1 - t * t
         err = err + 16 * c.softcap * E24
     if c.slopes:
-        at = torch.arange(c.T).double()
-        bias = torch.tensor(c.slopes, dtype=torch.float64)[:, None, None] * (at[:, None] - at[None, :]).abs()
+        at = torch.arange(c.T, device=q.device).double()
+        bias = torch.tensor(c.slopes, dtype=torch.float64, device=q.device)[:, None, None] * (at[:, None] - at[None, :]).abs()
         s = s - bias
         err = err + 4 * bias * E24
-    return s, ds, err + 8 * (s.abs() + 8) * E24, torch.from_numpy(visible(c.T, c.offsets, c.prefix))
+    return s, ds, err + 8 * (s.abs() + 8) * E24, torch.from_numpy(visible(c.T, c.offsets, c.prefix)).to(q.device)
 
 
 def forward(c, q, k, v):
@@ -149,7 +149,7 @@ def _backward(c, dtype, q, k, v, o, lse, dout):
     n = float(max(c.lengths, default=0))
     sums = lambda terms, errs: errs + terms * (up + (n + 8) * E24)
     # in half, ds is rounded in steps that may be as coarse as 2^-25 of the largest magnitude that its rows' gradient has
-    ds_t = t * torch.maximum(D.abs().amax(), torch.tensor(1.0))
+    ds_t = t * D.abs().amax().clamp(min=1.0)
     bq = (sums(ds.abs() @ K.abs(), dds @ K.abs()) + ds_t * m.double() @ K.abs()) * c.scale
     mt = m.double().t()
     bk = (sums(ds.abs().transpose(1, 2) @ Q.abs(), dds.transpose(1, 2) @ Q.abs()) + ds_t * mt @ Q.abs()) * c.scale
@@ -162,7 +162,7 @@ def _backward(c, dtype, q, k, v, o, lse, dout):
 
 def within(got, want, bound, what):
     """got may be off want by bound, element by element."""
-    got, want = got.double().cpu(), want.double()
+    got, want = got.double().to(want.device), want.double()
     same = (got == want) | (got.isnan() & want.isnan())   # infinities
     off = torch.where(same, 0.0, (got - want).abs() / bound)
     assert not off.isnan().any() and off.max() <= 1.0, "%s: %.2f of its bound, at %s" % (what, off.nan_to_num(math.inf).max(), tuple(np.unravel_index(int(off.nan_to_num(math.inf).argmax()), off.shape)))

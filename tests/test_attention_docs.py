@@ -94,7 +94,7 @@ class Run:
         bo, bl = ref.forward_bounds(c, self.dtype, q, k, v)
         ref.within(self.go, o, bo, "o")
         ref.within(self.lse, lse, bl, "lse")
-        saved = (self.go.double().cpu(), self.lse.double().cpu())
+        saved = (self.go.double().to(q.device), self.lse.double().to(q.device))
         want = ref.backward(c, q, k, v, *saved, dout)
         bounds = ref.backward_bounds(c, self.dtype, q, k, v, *saved, dout)
         for name, got, w, b in zip(("dq", "dk", "dv"), (self.dq, self.dk, self.dv), want, bounds):
@@ -126,6 +126,66 @@ def test_forward_and_gradients_match_64_bits(gpu_device, c, dtype):
     again = r.all()
     for a, b in zip(first, again):                    # and the same bits from a second call
         assert torch.equal(a, b)
+
+
+DOCS = [200, 1, 350, 64, 30, 410]   # 1055 tokens
+LARGE = [Case(500, 32, 8, 128, [100, 300, 90], slopes=True), Case(500, 32, 32, 64, [480], prefix=[70], softcap=20.0),     # 512 groups of 32 rows
+         Case(1000, 32, 8, 80, DOCS[:4] + [300]), Case(1000, 32, 16, 128, [1000], softcap=10.0, slopes=True),             # 1024
+         Case(1100, 64, 16, 128, DOCS, prefix=[50, 1, 0, 64, 0, 100], softcap=30.0), Case(1100, 64, 64, 128, DOCS, first=17),   # 2240
+         Case(1100, 64, 32, 64, [1090], slopes=True), Case(1100, 64, 64, 96, DOCS, prefix=[0, 0, 350, 0, 0, 0], softcap=30.0, slopes=True),
+         Case(1500, 64, 1, 128, [700, 33, 600]),                                                                          # one key head, its query heads in parts
+         Case(9000, 8, 1, 64, [60, 3000, 900] + [500] * 10), Case(9001, 8, 8, 128, [2900] + [100] * 61)]                   # more than 256 blocks of rows
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+@pytest.mark.parametrize("c", LARGE, ids=str)
+def test_larger_launches_match_64_bits(gpu_device, c, dtype):
+    """Launches of hundreds and thousands of groups of rows; the 64-bit side on the GPU, head by head."""
+    say(c, dtype)
+    r = Run(c, dtype)
+    first = r.all()
+    group = c.nh // c.nkv
+    for kv in sorted({0, c.nkv // 2, c.nkv - 1}):        # three key heads with their query heads
+        h = slice(kv * group, (kv + 1) * group)
+        part = Case(c.T, group, 1, c.d, c.lengths, c.prefix, c.first, c.softcap, scale=c.scale)
+        part.slopes = c.slopes[h] if c.slopes else None
+        cols, key = slice(h.start * c.d, h.stop * c.d), slice(kv * c.d, (kv + 1) * c.d)
+        q, k, v, dout = r.q[:, cols].cuda(), r.k[:, key].cuda(), r.v[:, key].cuda(), r.dout[:, cols].cuda()
+        for rows in chunks(part):
+            check_part(part, dtype, rows, q, k, v, dout, r.go[:, cols], r.lse[h], r.dq[:, cols], r.dk[:, key], r.dv[:, key])
+    for a, b in zip(first, r.all()):
+        assert torch.equal(a, b)
+
+
+def chunks(c):
+    """Runs of whole documents of up to 3000 tokens: (first token, end, lengths, prefix)."""
+    runs, at = [], c.first
+    for n, length in enumerate(c.lengths):
+        p = c.prefix[n] if c.prefix else 0
+        if not runs or runs[-1][1] - runs[-1][0] + length > 3000:
+            runs.append([at, at, [], []])
+        runs[-1][1] += length
+        runs[-1][2].append(length)
+        runs[-1][3].append(p)
+        at += length
+    return runs
+
+
+def check_part(c, dtype, run, q, k, v, dout, o, lse, dq, dk, dv):
+    first, end, lengths, prefix = run
+    t = slice(first, end)
+    part = Case(end - first, c.nh, 1, c.d, lengths, prefix, 0, c.softcap, scale=c.scale)
+    part.slopes = c.slopes
+    x = (q[t], k[t], v[t])
+    want, wl = ref.forward(part, *x)
+    bo, bl = ref.forward_bounds(part, dtype, *x)
+    ref.within(o[t], want, bo, "o")
+    ref.within(lse[:, t], wl, bl, "lse")
+    saved = (o[t].double(), lse[:, t].double())
+    want = ref.backward(part, *x, *saved, dout[t])
+    for name, got, w, b in zip(("dq", "dk", "dv"), (dq[t], dk[t], dv[t]), want, ref.backward_bounds(part, dtype, *x, *saved, dout[t])):
+        ref.within(got, w, b, name)
 
 
 @gpu
