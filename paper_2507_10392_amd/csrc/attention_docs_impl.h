@@ -31,9 +31,9 @@ __device__ __forceinline__ float unit_of(float x) {
 // there are 8 of them and find its keys in its L2.  The longest blocks come first: by their ranges (a.sorted), or the last ones, which
 // under a causal mask are the longest of a document.
 struct DocBlock { int block, kv, h; };
-__device__ __forceinline__ DocBlock row_block(const DocAttn& a, int heads, int rows, int lane) {   // heads of a key head in a workgroup, rows of a block
+__device__ __forceinline__ DocBlock row_block(const DocAttn& a, int workgroup, int heads, int rows, int lane) {   // heads of a key head in a workgroup, rows of a block
   const int group = a.nh / a.nkv, sets = a.nkv * (group / heads), blocks = (a.T + rows - 1) / rows;
-  const int set = (int)blockIdx.x % sets, kv = set % a.nkv, rank = (int)blockIdx.x / sets;
+  const int set = workgroup % sets, kv = set % a.nkv, rank = workgroup / sets;
   return DocBlock{a.sorted ? heavy_block<false>(a.ranges, a.T, rows, blocks, rank, lane) : blocks - 1 - rank, kv, kv * group + set / a.nkv * heads};
 }
 
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || KS == 1 ? 2 : 1) void doc_fwd_k
   static_assert((LOOP > END ? LOOP : END) >= (size_t)(KS - 1) * GROUPS * TL::BLOCKS * 4 * 64 * 16, "");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ks = wave / GROUPS, grp = wave % GROUPS, row_groups = GROUPS / heads, h_in = grp / row_groups, dd = a.d;
-  const DocBlock blk = row_block(a, heads, 32 * row_groups, lane);
+  const DocBlock blk = row_block(a, blockIdx.x, heads, 32 * row_groups, lane);
   const int t0 = blk.block * 32 * row_groups, w0 = t0 + 32 * (grp % row_groups), my_q = w0 + (lane & 31), h = blk.h + h_in;
   const E* qh = (const E*)a.q + h * dd;
   const E *kh = (const E*)a.k + blk.kv * dd, *vh = (const E*)a.v + blk.kv * dd;
@@ -217,17 +217,20 @@ __device__ __attribute__((noinline)) void redo_dq(DocRedo<NW>* redo, int groups,
   });
 }
 
-template <typename E, int D, int MODE, int NW, int KS, int ROWS>
-__global__ __launch_bounds__(64 * NW, sizeof(E) == 2 && (NW == 8 || KS == 1) ? 2 : 1) void doc_dq_kernel(DocAttn a, int heads) {
+template <typename E, int D, int NW, int KS, int ROWS, int NBUF> constexpr size_t dq_lds() {
+  typedef Tile<E, D> TL;
+  constexpr size_t LOOP = 2 * NBUF * TL::bytes(ROWS), END = sizeof(DocRedo<NW>) + 16 + NW / KS * TL::STORE,   // [NBUF][keys | values]
+                   MERGE = (size_t)(KS - 1) * (NW / KS) * TL::BLOCKS * 4 * 64 * 16;
+  return LOOP > END ? (LOOP > MERGE ? LOOP : MERGE) : END > MERGE ? END : MERGE;
+}
+template <typename E, int D, int MODE, int NW, int KS, int ROWS, int NBUF>
+__device__ __forceinline__ void dq_block(char* smem_raw, const DocAttn& a, int workgroup, int heads) {
   typedef Tile<E, D> TL;
   typedef Mat<E> M;
   constexpr int GROUPS = NW / KS, SUB = ROWS / 32 / KS, TILE = TL::bytes(ROWS);
-  constexpr size_t LOOP = 4 * TILE, END = sizeof(DocRedo<NW>) + 16 + GROUPS * TL::STORE;   // two buffers of keys and values
-  __shared__ __align__(16) char smem_raw[LOOP > END ? LOOP : END];
-  static_assert((LOOP > END ? LOOP : END) >= (size_t)(KS - 1) * GROUPS * TL::BLOCKS * 4 * 64 * 16, "");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ks = wave / GROUPS, grp = wave % GROUPS, row_groups = GROUPS / heads, h_in = grp / row_groups, dd = a.d;
-  const DocBlock blk = row_block(a, heads, 32 * row_groups, lane);
+  const DocBlock blk = row_block(a, workgroup, heads, 32 * row_groups, lane);
   const int t0 = blk.block * 32 * row_groups, w0 = t0 + 32 * (grp % row_groups), my_q = w0 + (lane & 31), h = blk.h + h_in;
   const E *kh = (const E*)a.k + blk.kv * dd, *vh = (const E*)a.v + blk.kv * dd;
   const Span all = block_span<false, (32 * GROUPS + 63) / 64>(a.ranges, t0, 32 * row_groups, a.T, lane);
@@ -249,7 +252,7 @@ __global__ __launch_bounds__(64 * NW, sizeof(E) == 2 && (NW == 8 || KS == 1) ? 2
     load.fetch(to + TILE, vh, row0, all.hi, wave);
   };
   typename TL::Lane at(smem + TL::bytes(ks * 32 * SUB), lane);
-  if (tiles > 0) fetch(smem, all.lo);   // in flight while delta is formed
+  if (NBUF == 2 && tiles > 0) fetch(smem, all.lo);   // in flight while delta is formed
   float delta = 0.f, largest = 0.f;
   {
     typename M::vec of[TL::FRAGS];
@@ -272,13 +275,17 @@ __global__ __launch_bounds__(64 * NW, sizeof(E) == 2 && (NW == 8 || KS == 1) ? 2
   f32x16 acc[TL::BLOCKS];
 #pragma unroll
   for (int i = 0; i < TL::BLOCKS; ++i) acc[i] = f32x16{};
-  if (tiles > 0) {
+  if (NBUF == 2 && tiles > 0) {
     tile_wait();
     __syncthreads();
   }
   for (int t = 0; t < tiles; ++t) {
     const int key0 = all.lo + t * ROWS;
-    if (t + 1 < tiles) fetch(smem + ((t + 1) & 1) * 2 * TILE, key0 + ROWS);   // that buffer was last read before the barrier that ended the iteration before
+    if (NBUF == 1) {
+      fetch(smem, key0);
+      tile_wait();
+      __syncthreads();
+    } else if (t + 1 < tiles) fetch(smem + ((t + 1) & 1) * 2 * TILE, key0 + ROWS);   // that buffer was last read before the barrier that ended the iteration before
     const int kb0 = key0 + ks * 32 * SUB;
     if (kb0 < mine.hi && kb0 + 32 * SUB > mine.lo) {
       const bool part = kb0 < mine.all_lo || kb0 + 32 * SUB > mine.all_hi;
@@ -306,8 +313,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(E) == 2 && (NW == 8 || KS == 1) ? 2
         }
       }
     }
-    tile_wait();
-    at.move(t & 1 ? -2 * TILE : 2 * TILE);
+    if (NBUF == 2) {
+      tile_wait();
+      at.move(t & 1 ? -2 * TILE : 2 * TILE);
+    }
     __syncthreads();
   }
   if constexpr (KS > 1) merge_waves<TL::BLOCKS>(acc, reinterpret_cast<f32x4*>(smem_raw) + grp * (KS - 1) * TL::BLOCKS * 4 * 64, ks, KS, lane);
@@ -327,13 +336,19 @@ __global__ __launch_bounds__(64 * NW, sizeof(E) == 2 && (NW == 8 || KS == 1) ? 2
                    (E*)a.dq + blk.h * dd, a.lddq);
 }
 
+template <typename E, int D, int MODE, int NW, int KS, int ROWS>
+__global__ __launch_bounds__(64 * NW, sizeof(E) == 2 && (NW == 8 || KS == 1) ? 2 : 1) void doc_dq_kernel(DocAttn a, int heads) {
+  __shared__ __align__(16) char smem[dq_lds<E, D, NW, KS, ROWS, 2>()];
+  dq_block<E, D, MODE, NW, KS, ROWS, 2>(smem, a, blockIdx.x, heads);
+}
+
 // ------------------------------------------------------------------------------------------ dK, dV
 // dV^T += dO^T P, dK^T += Q^T dS with S = Q K^T: lanes are keys, registers rows.  KG groups of 32 keys, each with QS waves, which share out the rows of a
 // tile; a wave's V rows sit in LDS, which leaves registers for two waves per SIMD.
 template <typename E, int NW>
 __device__ __attribute__((noinline)) void redo_dkv(DocRedo<NW>* redo, int groups, int t0, const int32_t* ranges, int T, int d, int group, const E* q,
-                                                   int64_t ldq, const E* k, const E* v, int64_t ldkv, const E* dout, int64_t ldo, const float* lse,
-                                                   const float* delta, float scale, float softcap, const float* slopes, E* dk, E* dv, int64_t lddkv,
+                                                   int64_t ldq, const E* k, const E* v, int64_t ldkv, const E* dout, const E* o, int64_t ldo,
+                                                   const float* lse, const float* delta, float scale, float softcap, const float* slopes, E* dk, E* dv, int64_t lddkv,
                                                    float* part_k, float* part_v, int64_t ld_part) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   for_dealt_rows(redo->masks, groups, NW, wave, [&](int g, int r) {
@@ -345,8 +360,8 @@ __device__ __attribute__((noinline)) void redo_dkv(DocRedo<NW>* redo, int groups
     wave_lds_order();
     float xk[2] = {0.f, 0.f}, xv[2] = {0.f, 0.f};
     for (int h = 0; h < group; ++h)
-      doc_dkv_head<E>(redo->rows[wave], j, range.z, range.w, d, DocRows<E>{q + h * d, ldq}, DocRows<E>{dout + h * d, ldo}, lse + (int64_t)h * T,
-                      delta + (int64_t)h * T, scale, DocScore{softcap, slopes ? slopes[h] : 0.f}, lane, xk, xv);
+      doc_dkv_head<E>(redo->rows[wave], j, range.z, range.w, d, DocRows<E>{q + h * d, ldq}, DocRows<E>{dout + h * d, ldo}, DocRows<E>{o + h * d, ldo},
+                      lse + (int64_t)h * T, delta ? delta + (int64_t)h * T : nullptr, scale, DocScore{softcap, slopes ? slopes[h] : 0.f}, lane, xk, xv);
 #pragma unroll
     for (int c = 0; c < 2; ++c)
       if (64 * c + lane < d) {
@@ -361,21 +376,26 @@ __device__ __attribute__((noinline)) void redo_dkv(DocRedo<NW>* redo, int groups
   });
 }
 
-template <typename E, int D, int MODE, int KG, int QS, int ROWS, int NBUF>
-__global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __launch_bounds__(64 * KG * QS) void doc_dkv_kernel(DocAttn a) {
+template <typename E, int D, int KG, int QS, int ROWS, int NBUF> struct DkvLds {   // [NBUF][Q | dO], [NBUF][stats], [KG][V rows]
+  typedef Tile<E, D> TL;
+  static constexpr int STATS = HALF<E> ? 3 : 2, STAT = STATS * ROWS * 4;   // log-sum-exp in powers of two less P_SHIFT, delta, (half) largest |dO|
+  static constexpr int V = NBUF * (2 * TL::bytes(ROWS) + STAT);
+  static constexpr size_t LOOP = V + KG * TL::bytes(32), END = sizeof(DocRedo<KG * QS>) + 16 + KG * Tile<float, D>::STORE,
+                          MERGE = (size_t)(QS - 1) * KG * TL::BLOCKS * 4 * 64 * 16;
+  static constexpr size_t bytes = LOOP > END ? (LOOP > MERGE ? LOOP : MERGE) : END > MERGE ? END : MERGE;
+};
+// OWN: delta is formed here, from dO and the rows of o, by the wave that works on a row, instead of read.
+template <typename E, int D, int MODE, int KG, int QS, int ROWS, int NBUF, bool OWN>
+__device__ __forceinline__ void dkv_block(char* smem_raw, const DocAttn& a, int workgroup) {
   typedef Tile<E, D> TL;
   typedef Mat<E> M;
-  constexpr int NW = KG * QS, SUB = ROWS / 32 / QS, TILE = TL::bytes(ROWS), STATS = HALF<E> ? 3 : 2;
-  constexpr int STAT = STATS * ROWS * 4;             // log-sum-exp in powers of two less P_SHIFT, delta, (half) largest |dO|
-  constexpr int V = NBUF * (2 * TILE + STAT);        // [NBUF][Q | dO], [NBUF][stats], [KG][V rows]
-  constexpr size_t LOOP = V + KG * TL::bytes(32), END = sizeof(DocRedo<NW>) + 16 + KG * Tile<float, D>::STORE, MERGE = (size_t)(QS - 1) * KG * TL::BLOCKS * 4 * 64 * 16;
-  static_assert(ROWS <= 64 * NW, "");
-  __shared__ __align__(16) char smem_raw[LOOP > END ? LOOP : END];
-  static_assert(sizeof(smem_raw) >= MERGE, "");
+  typedef DkvLds<E, D, KG, QS, ROWS, NBUF> L;
+  constexpr int NW = KG * QS, SUB = ROWS / 32 / QS, TILE = TL::bytes(ROWS), STATS = L::STATS, STAT = L::STAT, V = L::V;
+  static_assert(ROWS <= 64 * NW && (!OWN || (KG == 1 && SUB == 1)), "");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int qs = wave / KG, kg = wave % KG, dd = a.d, group = a.nh / a.nkv / a.parts;
-  const int set = (int)blockIdx.x % (a.nkv * a.parts), kv = set % a.nkv, which = set / a.nkv, h0 = kv * (a.nh / a.nkv) + which * group;
-  const int rank = (int)blockIdx.x / (a.nkv * a.parts);
+  const int set = workgroup % (a.nkv * a.parts), kv = set % a.nkv, which = set / a.nkv, h0 = kv * (a.nh / a.nkv) + which * group;
+  const int rank = workgroup / (a.nkv * a.parts);
   const int t0 = 32 * KG * (a.sorted ? heavy_block<true>(a.ranges, a.T, 32 * KG, (a.T + 32 * KG - 1) / (32 * KG), rank, lane) : rank);   // the longest first, in a document the early ones
   const int w0 = t0 + 32 * kg, my_k = w0 + (lane & 31);
   const E *kh = (const E*)a.k + kv * dd, *vh = (const E*)a.v + kv * dd;
@@ -393,14 +413,16 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
   }
   const TileLoad<E, D, ROWS, NW> load_q(a.ldq, lane, dd), load_d(a.ldo, lane, dd);
   float sr[STATS];
+  typename M::vec of[OWN ? TL::FRAGS : 1];
   auto fetch = [&](int buf, int h, int row0) {
+    if constexpr (OWN) TL::load_frags(of, (const E*)a.o + h * dd, a.ldo, row0 + 32 * qs + (lane & 31), a.T, lane, dd);
     load_q.fetch(smem + buf * 2 * TILE, (const E*)a.q + h * dd, row0, all.hi, wave);
     load_d.fetch(smem + buf * 2 * TILE + TILE, (const E*)a.dout + h * dd, row0, all.hi, wave);
     if (tid < ROWS) {
       const int64_t from = (int64_t)h * a.T + min(row0 + tid, a.T - 1);
       sr[0] = a.lse[from];
-      sr[1] = a.delta[from];
-      if constexpr (HALF<E>) sr[2] = a.delta[(int64_t)a.nh * a.T + from];
+      if constexpr (!OWN) sr[1] = a.delta[from];
+      if constexpr (HALF<E> && !OWN) sr[2] = a.delta[(int64_t)a.nh * a.T + from];
     }
   };
   auto put_stats = [&](int buf, int row0) {
@@ -408,8 +430,8 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
     if (tid < ROWS) {   // rows past the end: zeros, whose weights 1 meet rows of zeros
       const bool in = row0 + tid < all.hi;
       st[tid] = in ? fmaf(sr[0], DOC_LOG2E, -P_SHIFT<E>) : 0.f;
-      st[ROWS + tid] = in ? sr[1] : 0.f;
-      if constexpr (HALF<E>) st[2 * ROWS + tid] = in ? sr[2] : 0.f;
+      if constexpr (!OWN) st[ROWS + tid] = in ? sr[1] : 0.f;
+      if constexpr (HALF<E> && !OWN) st[2 * ROWS + tid] = in ? sr[2] : 0.f;
     }
   };
   f32x16 dk[TL::BLOCKS], dv[TL::BLOCKS];
@@ -435,7 +457,24 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
       put_stats(0, row0);
       tile_wait();
       __syncthreads();
-    } else if (it + 1 < total) fetch(buf ^ 1, hn, rown);
+    }
+    float own_largest = 0.f;
+    if constexpr (OWN) {   // lane and lane ^ 32 hold a row
+      float x = 0.f;
+#pragma unroll
+      for (int c = 0; c < TL::FRAGS; ++c) {
+        const typename M::vec d = at.frag(TILE, 0, c);
+#pragma unroll
+        for (int e = 0; e < TL::VN; ++e) {
+          x = fmaf((float)d[e], (float)of[c][e], x);
+          if constexpr (HALF<E>) own_largest = fmaxf(own_largest, fabsf((float)d[e]));
+        }
+      }
+      x += __shfl_xor(x, 32, 64);
+      *(__attribute__((address_space(3))) float*)(uintptr_t)(stat_at - 16 * (lane >> 5) + 4 * (ROWS + (lane & 31))) = x;
+      wave_lds_order();
+    }
+    if (NBUF == 2 && it + 1 < total) fetch(buf ^ 1, hn, rown);
     const int rb0 = row0 + qs * 32 * SUB;
     if (rb0 < mine.hi && rb0 + 32 * SUB > mine.lo) {
       const bool part = rb0 < mine.all_lo || rb0 + 32 * SUB > mine.all_hi;
@@ -449,7 +488,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
           dp = M::rows(at.frag(TILE, 32 * j, c), at_v.frag(0, 0, c), dp);
         }
         if constexpr (HALF<E>) {   // the unit follows the largest |dO| so far
-          const float top = wave_max(lds_read<float>(stat_at - 16 * (lane >> 5) + 4 * (2 * ROWS + 32 * j + (lane & 31)))), now = unit_of(top);
+          const float top = wave_max(OWN ? own_largest : lds_read<float>(stat_at - 16 * (lane >> 5) + 4 * (2 * ROWS + 32 * j + (lane & 31)))), now = unit_of(top);
           if (top > 0.f && (unit == 0.f || now < unit)) {
             const float f = unit == 0.f ? 1.f : now / unit;
             unit = now;
@@ -461,7 +500,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
         }
         // Two waves per SIMD have 256 registers each, of which 192 hold K, dK, dV and the scores: the phases are kept apart, or the compiler
         // spills accumulators to read ahead.
-        if constexpr (NW == 8) __builtin_amdgcn_sched_barrier(0);
+        if constexpr (NW == 8 || OWN) __builtin_amdgcn_sched_barrier(0);
         doc_weights<E, MODE>(s, dp, sc, (float)(rb + 4 * (lane >> 5) - my_k), HALF<E> ? unit / 16384.f : 1.f,
                        [&](int c) { return lds_read<f32x4>(stat_at + 4 * (32 * j + 8 * c)); },
                        [&](int c) { return lds_read<f32x4>(stat_at + 4 * (ROWS + 32 * j + 8 * c)); });
@@ -473,7 +512,7 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          if constexpr (NW == 8) __builtin_amdgcn_sched_barrier(0);
+          if constexpr (NW == 8 || OWN) __builtin_amdgcn_sched_barrier(0);
           const typename M::col8 pf = pack<E>(s, u), df = pack<E>(dp, u);
 #pragma unroll
           for (int b = 0; b < TL::BLOCKS; ++b) {
@@ -530,9 +569,28 @@ __global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __laun
     }
   }
   if (__builtin_expect(any_row(redo.masks, KG, lane), 0))
-    redo_dkv<E, NW>(&redo, KG, t0, a.ranges, a.T, dd, group, (const E*)a.q + h0 * dd, a.ldq, kh, vh, a.ldkv, (const E*)a.dout + h0 * dd, a.ldo,
-                    a.lse + (int64_t)h0 * a.T, a.delta + (int64_t)h0 * a.T, a.scale, a.softcap, a.slopes ? a.slopes + h0 : nullptr, (E*)a.dk + kv * dd,
+    redo_dkv<E, NW>(&redo, KG, t0, a.ranges, a.T, dd, group, (const E*)a.q + h0 * dd, a.ldq, kh, vh, a.ldkv, (const E*)a.dout + h0 * dd,
+                    (const E*)a.o + h0 * dd, a.ldo, a.lse + (int64_t)h0 * a.T, OWN ? nullptr : a.delta + (int64_t)h0 * a.T, a.scale, a.softcap, a.slopes ? a.slopes + h0 : nullptr, (E*)a.dk + kv * dd,
                     (E*)a.dv + kv * dd, a.lddkv, a.parts > 1 ? part_k : nullptr, part_v, ld_part);
+}
+
+template <typename E, int D, int MODE, int KG, int QS, int ROWS, int NBUF>
+__global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __launch_bounds__(64 * KG * QS) void doc_dkv_kernel(DocAttn a) {
+  __shared__ __align__(16) char smem[DkvLds<E, D, KG, QS, ROWS, NBUF>::bytes];
+  dkv_block<E, D, MODE, KG, QS, ROWS, NBUF, false>(smem, a, blockIdx.x);
+}
+
+// Both in one launch, for few rows, where one after the other would leave most of the chip idle twice: no block reads what another one writes.  One buffer
+// where two workgroups then fit a CU, whose waits overlap (fp32 heads over 64: one workgroup in any case).
+template <typename E, int D> constexpr int FEW_BUFFERS = sizeof(E) == 2 && D == 64 ? 2 : 1;
+template <typename E, int D> constexpr int FEW_WAVES = sizeof(E) == 4 && D > 64 ? 1 : 2;   // per SIMD
+template <typename E, int D, int MODE>
+__global__ __attribute__((amdgpu_waves_per_eu(FEW_WAVES<E, D>, FEW_WAVES<E, D>))) __launch_bounds__(256) void doc_bwd_kernel(DocAttn a, int dkv_workgroups) {
+  constexpr int N = FEW_BUFFERS<E, D>;
+  constexpr size_t A = DkvLds<E, D, 1, 4, 128, N>::bytes, B = dq_lds<E, D, 4, 4, 128, N>();
+  __shared__ __align__(16) char smem[A > B ? A : B];
+  if ((int)blockIdx.x < dkv_workgroups) dkv_block<E, D, MODE, 1, 4, 128, N, true>(smem, a, blockIdx.x);
+  else dq_block<E, D, MODE, 4, 4, 128, N>(smem, a, blockIdx.x - dkv_workgroups, 1);
 }
 
 // Where the query heads of a key head are shared out over `parts` workgroups, these leave their sums in fp32; they meet here, in the order of the parts.
@@ -587,28 +645,37 @@ template <typename E, int D, int MODE, int NW, int KS, int ROWS, bool BWD> hipEr
 template <typename E, int D, int MODE, bool BWD> hipError_t doc_by_rows(hipStream_t st, const DocAttn& a) {
   constexpr int S = SHARE<E, D>;
   const int64_t groups = cdiv(a.T, 32) * a.nh;
-  if (groups < (sizeof(E) == 2 ? 256 : 1024)) return doc_rows<E, D, MODE, 4, S, 32 * S, BWD>(st, a);
+  if constexpr (!BWD)   // the backward of so few rows takes doc_bwd_kernel
+    if (groups < (sizeof(E) == 2 ? 256 : 1024)) return doc_rows<E, D, MODE, 4, S, 32 * S, BWD>(st, a);
   if constexpr (sizeof(E) == 2) {
     if (groups < 768) return doc_rows<E, D, MODE, 8, 4, 128, BWD>(st, a);
     if (groups < 2000) return doc_rows<E, D, MODE, 8, 2, 128, BWD>(st, a);
     return doc_rows<E, D, MODE, 4, 1, 64, BWD>(st, a);
   } else return doc_rows<E, D, MODE, 4, 1, 32, BWD>(st, a);
 }
+template <typename E> hipError_t doc_join(hipStream_t st, const DocAttn& a) {
+  if (a.parts > 1) hipLaunchKernelGGL(doc_join_kernel<E>, dim3((unsigned)cdiv(2 * (int64_t)a.T * (a.nkv * a.d / (16 / (int)sizeof(E))), 256)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
 template <typename E, int D, int MODE, int KG, int QS, int ROWS, int NBUF> hipError_t doc_dkv(hipStream_t st, DocAttn a) {
   const int64_t blocks = cdiv(a.T, 32 * KG), wgs = blocks * a.nkv * a.parts;
   a.sorted = doc_sorted(blocks, wgs, 1);
   hipLaunchKernelGGL((doc_dkv_kernel<E, D, MODE, KG, QS, ROWS, NBUF>), dim3((unsigned)wgs), dim3(64 * KG * QS), 0, st, a);
-  if (a.parts > 1) hipLaunchKernelGGL(doc_join_kernel<E>, dim3((unsigned)cdiv(2 * (int64_t)a.T * (a.nkv * a.d / (16 / (int)sizeof(E))), 256)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 template <typename E, int D, int MODE> hipError_t doc_bwd(hipStream_t st, const DocAttn& a) {
-  const hipError_t e = doc_by_rows<E, D, MODE, true>(st, a);
-  if (e != hipSuccess) return e;
-  constexpr int BUFFERS = sizeof(E) == 4 && D > 64 ? 1 : 2;
   const int keys = doc_dkv_keys((DType)(sizeof(E) == 4 ? F32 : BF16), a.T, a.nh, a.nkv);
-  if (keys == 32) return doc_dkv<E, D, MODE, 1, 4, 128, BUFFERS>(st, a);
-  if constexpr (sizeof(E) == 4) return doc_dkv<E, D, MODE, 4, 1, 32, 2>(st, a);
-  else return keys == 64 ? doc_dkv<E, D, MODE, 2, 4, 128, 2>(st, a) : doc_dkv<E, D, MODE, 4, 2, 64, 2>(st, a);
+  if (keys == 32) {
+    const int64_t dkv = cdiv(a.T, 32) * a.nkv * a.parts, dq = cdiv(a.T, 32) * a.nh;
+    hipLaunchKernelGGL((doc_bwd_kernel<E, D, MODE>), dim3((unsigned)(dkv + dq)), dim3(256), 0, st, a, (int)dkv);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? e : doc_join<E>(st, a);
+  }
+  hipError_t e = doc_by_rows<E, D, MODE, true>(st, a);
+  if (e != hipSuccess) return e;
+  if constexpr (sizeof(E) == 4) e = doc_dkv<E, D, MODE, 4, 1, 32, 2>(st, a);
+  else e = keys == 64 ? doc_dkv<E, D, MODE, 2, 4, 128, 2>(st, a) : doc_dkv<E, D, MODE, 4, 2, 64, 2>(st, a);
+  return e != hipSuccess ? e : doc_join<E>(st, a);
 }
 template <typename E, int D, int MODE> hipError_t doc_either(hipStream_t st, const DocAttn& a, bool backward) {
   return backward ? doc_bwd<E, D, MODE>(st, a) : doc_by_rows<E, D, MODE, false>(st, a);

@@ -97,9 +97,9 @@ __device__ __forceinline__ void doc_dq_row(float* rows, int i, int lo, int hi, i
 }
 
 // Adds one query head's part of dk_j / scale and dv_j, from the rows lo .. hi - 1 that see key j, to dk[c] and dv[c] of the columns
-// lane + 64 c.  rows: LDS of the wave's own, 256 floats, which holds k_j and, from 128 on, v_j.
+// lane + 64 c.  rows: LDS of the wave's own, 256 floats, which holds k_j and, from 128 on, v_j.  delta: the rows' dO . o, or NULL: formed here.
 template <typename T>
-__device__ __forceinline__ void doc_dkv_head(const float* rows, int j, int lo, int hi, int d, DocRows<T> q, DocRows<T> dout, const float* lse,
+__device__ __forceinline__ void doc_dkv_head(const float* rows, int j, int lo, int hi, int d, DocRows<T> q, DocRows<T> dout, DocRows<T> o, const float* lse,
                                              const float* delta, float scale, DocScore score, int lane, float (&dk)[2], float (&dv)[2]) {
   for (int i0 = lo; i0 < hi; i0 += 64) {
     const int i = i0 + lane, n = min(64, hi - i0);
@@ -107,7 +107,11 @@ __device__ __forceinline__ void doc_dkv_head(const float* rows, int j, int lo, i
     if (i < hi) {
       float slope;
       p = expf(score(scale * dot_row(rows, q.row(i), d), i, j, slope) - lse[i]);
-      ds = p * (dot_row(rows + 128, dout.row(i), d) - delta[i]) * slope;
+      float di = 0.f;
+      if (delta) di = delta[i];
+      else
+        for (int c = 0; c < d; ++c) di = fmaf(to_f(dout.row(i)[c]), to_f(o.row(i)[c]), di);
+      ds = p * (dot_row(rows + 128, dout.row(i), d) - di) * slope;
     }
     for (int ii = 0; ii < n; ++ii) {
       const float pi = __shfl(p, ii, 64), dsi = __shfl(ds, ii, 64);
