@@ -88,13 +88,13 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || KS == 1 ? 2 : 1) void doc_fwd_k
   f32x16 oacc[TL::BLOCKS];
 #pragma unroll
   for (int i = 0; i < TL::BLOCKS; ++i) oacc[i] = f32x16{};
-  float m = -INFINITY, l = 0.f;   // the reference of the weights, and their sum
+  float m = -INFINITY, l = 0.f;   // the reference of the weights, less g, and their sum
   if (tiles > 0) {
     fetch(smem, all.lo);
     tile_wait();
     __syncthreads();
   }
-  const float f = MODE == DOC_PLAIN ? sc.log2 : 1.f;
+  const float f = sc.f<MODE>(), MASKED = DOC_FALLS<E, MODE> ? INFINITY : -INFINITY;
   for (int t = 0; t < tiles; ++t) {
     const int key0 = all.lo + t * ROWS;
     if (t + 1 < tiles) fetch(smem + ((t + 1) & 1) * 2 * TILE, key0 + ROWS);   // that buffer was last read before the barrier that ended the iteration before
@@ -115,15 +115,16 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || KS == 1 ? 2 : 1) void doc_fwd_k
           const int from = kb + 32 * j + 4 * (lane >> 5) - lo;
 #pragma unroll
           for (int r = 0; r < 16; ++r)
-            if ((unsigned)(from + 8 * (r >> 2) + (r & 3)) >= (unsigned)seen) s[j][r] = -INFINITY;
+            if ((unsigned)(from + 8 * (r >> 2) + (r & 3)) >= (unsigned)seen) s[j][r] = MASKED;
         }
       }
-      float mx = -INFINITY;
+      float mx = MASKED;   // of the registers; then the largest score, less g
 #pragma unroll
       for (int j = 0; j < SUB; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[j][r]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * f;   // f > 0
+        for (int r = 0; r < 16; ++r) mx = DOC_FALLS<E, MODE> ? fminf(mx, s[j][r]) : fmaxf(mx, s[j][r]);
+      mx *= f;
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
       // The reference moves only when some row's maximum has outgrown it by 2^8: weights are at most 2^(8 + LAG), the sums and the result refer to the
       // same reference whenever it moves.
       if (__any(mx > m + (8.f + LAG))) {
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || KS == 1 ? 2 : 1) void doc_fwd_k
     TL::store(oacc, live ? 1.f / l : 0.f, smem_raw + (sizeof(redo) + 15) / 16 * 16 + grp * TL::STORE, (E*)a.o + h * dd, a.ldo, w0, a.T,
               lane, dd, again);
     if (lane < 32 && my_q < a.T)
-      a.lse[(int64_t)h * a.T + my_q] = live ? (float)((double)m * 0.6931471805599453 + (double)logf(l)) : -INFINITY;
+      a.lse[(int64_t)h * a.T + my_q] = live ? (float)(((double)m + (double)sc.g) * 0.6931471805599453 + (double)logf(l)) : -INFINITY;
   }
   if (__builtin_expect(any_row(redo.masks, GROUPS, lane), 0))
     redo_fwd<E, NW>(&redo, GROUPS, row_groups, t0, a.ranges, a.T, dd, (const E*)a.q + blk.h * dd, a.ldq, kh, vh, a.ldkv, a.scale, a.softcap,
@@ -241,8 +242,8 @@ __device__ __forceinline__ void dq_block(char* smem_raw, const DocAttn& a, int w
   TL::load_frags(qf, (const E*)a.q + h * dd, a.ldq, my_q, a.T, lane, dd);
   TL::load_frags(dof, (const E*)a.dout + h * dd, a.ldo, my_q, a.T, lane, dd);
   const int64_t stat = (int64_t)h * a.T + min(my_q, a.T - 1);
-  const float lse2 = live ? a.lse[stat] * DOC_LOG2E : 0.f;
   const DocScale sc = doc_scale<E, MODE>(a, h);
+  const float lse2 = live ? fmaf(a.lse[stat], DOC_LOG2E, -sc.g) : 0.f;
   const Span mine = span_of(range.x, range.y);
   const int tiles = (all.hi - all.lo + ROWS - 1) / ROWS;
   const unsigned smem = lds_address(smem_raw);
@@ -327,7 +328,7 @@ __device__ __forceinline__ void dq_block(char* smem_raw, const DocAttn& a, int w
 #pragma unroll
       for (int i = 0; i < TL::BLOCKS; ++i) acc[i] = f32x16{};
     }
-    TL::store(acc, a.scale / unit, smem_raw + (sizeof(redo) + 15) / 16 * 16 + grp * TL::STORE, (E*)a.dq + h * dd, a.lddq, w0, a.T,
+    TL::store(acc, DOC_SLOPE<E, MODE> * a.scale / unit, smem_raw + (sizeof(redo) + 15) / 16 * 16 + grp * TL::STORE, (E*)a.dq + h * dd, a.lddq, w0, a.T,
               lane, dd, again);
   }
   if (__builtin_expect(any_row(redo.masks, GROUPS, lane), 0))   // the rows' delta: written by this workgroup, before its barrier
@@ -378,7 +379,7 @@ __device__ __attribute__((noinline)) void redo_dkv(DocRedo<NW>* redo, int groups
 
 template <typename E, int D, int KG, int QS, int ROWS, int NBUF> struct DkvLds {   // [NBUF][Q | dO], [NBUF][stats], [KG][V rows]
   typedef Tile<E, D> TL;
-  static constexpr int STATS = HALF<E> ? 3 : 2, STAT = STATS * ROWS * 4;   // log-sum-exp in powers of two less P_SHIFT, delta, (half) largest |dO|
+  static constexpr int STATS = HALF<E> ? 3 : 2, STAT = STATS * ROWS * 4;   // log-sum-exp in powers of two less P_SHIFT and g, delta, (half) largest |dO|
   static constexpr int V = NBUF * (2 * TL::bytes(ROWS) + STAT);
   static constexpr size_t LOOP = V + KG * TL::bytes(32), END = sizeof(DocRedo<KG * QS>) + 16 + KG * Tile<float, D>::STORE,
                           MERGE = (size_t)(QS - 1) * KG * TL::BLOCKS * 4 * 64 * 16;
@@ -425,11 +426,13 @@ __device__ __forceinline__ void dkv_block(char* smem_raw, const DocAttn& a, int 
       if constexpr (HALF<E> && !OWN) sr[2] = a.delta[(int64_t)a.nh * a.T + from];
     }
   };
+  DocScale sc = doc_scale<E, MODE>(a, h0);
+  const float minus = P_SHIFT<E> + sc.g;
   auto put_stats = [&](int buf, int row0) {
     float* st = reinterpret_cast<float*>(smem_raw + NBUF * 2 * TILE + buf * STAT);
     if (tid < ROWS) {   // rows past the end: zeros, whose weights 1 meet rows of zeros
       const bool in = row0 + tid < all.hi;
-      st[tid] = in ? fmaf(sr[0], DOC_LOG2E, -P_SHIFT<E>) : 0.f;
+      st[tid] = in ? fmaf(sr[0], DOC_LOG2E, -minus) : 0.f;
       if constexpr (!OWN) st[ROWS + tid] = in ? sr[1] : 0.f;
       if constexpr (HALF<E> && !OWN) st[2 * ROWS + tid] = in ? sr[2] : 0.f;
     }
@@ -448,7 +451,6 @@ __device__ __forceinline__ void dkv_block(char* smem_raw, const DocAttn& a, int 
   typename TL::Lane at(smem + TL::bytes(qs * 32 * SUB), lane);
   const typename TL::Lane at_v(smem + V + kg * TL::bytes(32), lane);
   unsigned stat_at = smem + NBUF * 2 * TILE + 4 * (qs * 32 * SUB + 4 * (lane >> 5));
-  DocScale sc = doc_scale<E, MODE>(a, h);
   for (int it = 0; it < total; ++it) {
     const int row0 = all.lo + t * ROWS, buf = NBUF == 2 ? it & 1 : 0;
     const int tn = t + 1 < tiles ? t + 1 : 0, hn = tn ? h : h + 1, rown = all.lo + tn * ROWS;
@@ -559,7 +561,7 @@ __device__ __forceinline__ void dkv_block(char* smem_raw, const DocAttn& a, int 
       for (int i = 0; i < TL::BLOCKS; ++i) dk[i] = dv[i] = f32x16{};
     }
     char* to = smem_raw + (sizeof(redo) + 15) / 16 * 16 + kg * Tile<float, D>::STORE;
-    const float fv = HALF<E> ? 1.f / 16384.f : 1.f, fk = HALF<E> && unit != 0.f ? a.scale / unit : a.scale;
+    const float fv = HALF<E> ? 1.f / 16384.f : 1.f, fk = DOC_SLOPE<E, MODE> * (HALF<E> && unit != 0.f ? a.scale / unit : a.scale);
     if (a.parts > 1) {
       Tile<float, D>::store(dv, fv, to, part_v, ld_part, w0, a.T, lane, dd, again);
       Tile<float, D>::store(dk, fk, to, part_k, ld_part, w0, a.T, lane, dd, again);

@@ -230,16 +230,26 @@ template <bool ROWS> __device__ __forceinline__ int heavy_block(const int32_t* r
   return 255 - (found & 255);
 }
 
-// The scores of a block, in powers of two.  MODE says which of cap and bias a call has.
-//   capped: softcap tanh(u / softcap) = softcap - 2 softcap / (1 + exp(2 u / softcap)); 16-bit types take it so, with the hardware's
-//   exp2 and reciprocal (absolute error softcap 2^-22, of weights that are then rounded to 2^-9 or 2^-12 of themselves).  fp32 takes tanh_f.
+// The scores of a block, in powers of two: what a register holds after doc_scores, times f, plus g.  MODE says which of cap and bias a call has.
+//   plain: the product as it is, f = scale log2 e.
+//   capped: softcap tanh(u / softcap) = softcap - 2 softcap r, r = 1 / (1 + exp(2 u / softcap)).  16-bit types keep r (so the largest score is the
+//   smallest register), from the hardware's exp2 and reciprocal: an absolute error of softcap 2^-22, of weights that are then rounded to 2^-9 or 2^-12
+//   of themselves.  fp32 keeps tanh_f.
+//   biased: with the bias in.
+// The vector units bound a capped kernel, so its additions are folded: g goes with the reference or the log-sum-exp that is subtracted anyway, and the
+// cap's slope 1 - tanh^2 = 4 (r - r^2) leaves its 4 to the gradients' last factor.
 enum DocMode { DOC_PLAIN = 0, DOC_CAP = 1, DOC_BIAS = 2 };   // or-ed
+template <typename E, int MODE> constexpr bool DOC_FALLS = MODE == DOC_CAP && sizeof(E) == 2;   // f < 0
+template <typename E, int MODE> constexpr float DOC_SLOPE = (MODE & DOC_CAP) && sizeof(E) == 2 ? 4.f : 1.f;
 struct DocScale {
-  float log2, cap_log2, into_tanh, slope_log2;   // scale log2 e; softcap log2 e; 2 scale log2 e / softcap, or (fp32) scale / softcap; slope log2 e
+  float log2, cap, into_tanh, slope, g;   // scale log2 e; of tanh or r; 2 scale log2 e / softcap, or (fp32) scale / softcap; slope log2 e; see above
+  template <int MODE> __device__ __forceinline__ float f() const { return MODE == DOC_PLAIN ? log2 : MODE == DOC_CAP ? cap : 1.f; }
 };
 template <typename E, int MODE> __device__ __forceinline__ DocScale doc_scale(const DocAttn& a, int h) {
-  return DocScale{a.scale * DOC_LOG2E, a.softcap * DOC_LOG2E, MODE & DOC_CAP ? (sizeof(E) == 4 ? a.scale : 2.f * DOC_LOG2E * a.scale) / a.softcap : 0.f,
-                  MODE & DOC_BIAS ? a.slopes[h] * DOC_LOG2E : 0.f};
+  constexpr bool CAP = MODE & DOC_CAP, HALF_SIZE = sizeof(E) == 2;
+  const float cap = a.softcap * DOC_LOG2E;
+  return DocScale{a.scale * DOC_LOG2E, HALF_SIZE ? -2.f * cap : cap, CAP ? (HALF_SIZE ? 2.f * DOC_LOG2E * a.scale : a.scale) / a.softcap : 0.f,
+                  MODE & DOC_BIAS ? a.slopes[h] * DOC_LOG2E : 0.f, CAP && HALF_SIZE ? cap : 0.f};
 }
 // tanh within 1.5e-7 of itself: below 0.6 an odd polynomial (least squares in the relative error, which is 1e-10), above from the exponential, whose
 // cancellation is harmless there.  tanhf's branches and division took most of the fp32 kernels' time (capped forward, 1000 tokens, 8 heads of
@@ -255,32 +265,22 @@ __device__ __forceinline__ float tanh_f(float u) {
   const float t = fmaf(-2.f, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(2.f * DOC_LOG2E * fabsf(u))), 1.f);
   return fabsf(u) < 0.6f ? fmaf(u * z, p, u) : copysignf(t, u);
 }
-// tanh(u / softcap) of a product, as (1 - tanh) / 2 in 16-bit types; the score from it, and its slope 1 - tanh^2
+// tanh(u / softcap) of a product, or r.
 template <typename E> __device__ __forceinline__ float cap_part(const DocScale& c, float product) {
   if constexpr (sizeof(E) == 4) return tanh_f(product * c.into_tanh);
   else return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(product * c.into_tanh));
 }
-template <typename E> __device__ __forceinline__ float cap_score(const DocScale& c, float part, float plus) {
-  return sizeof(E) == 4 ? fmaf(c.cap_log2, part, plus) : fmaf(-2.f * c.cap_log2, part, c.cap_log2 + plus);
-}
-template <typename E> __device__ __forceinline__ float cap_slope(float part) {
-  return sizeof(E) == 4 ? (1.f - part) * (1.f + part) : part * fmaf(part, -4.f, 4.f);
-}
-// apart: of the lane's own token and the one that its register 0 stands for
-__device__ __forceinline__ float bias_score(const DocScale& c, float apart, int r, float plus) {
-  return fmaf(-c.slope_log2, fabsf(apart + (float)(8 * (r >> 2) + (r & 3))), plus);
-}
-// Scores into s; a plain one stays as the product left it, to be taken times log2.
+// The bias.  apart: of the lane's own token and the one that its register 0 stands for
+__device__ __forceinline__ float bias_score(const DocScale& c, float apart, int r) { return -c.slope * fabsf(apart + (float)(8 * (r >> 2) + (r & 3))); }
 template <typename E, int MODE> __device__ __forceinline__ void doc_scores(f32x16& s, const DocScale& c, float apart) {
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
-    if constexpr (MODE & DOC_CAP) s[r] = cap_score<E>(c, cap_part<E>(c, s[r]), 0.f);
-    else if constexpr (MODE & DOC_BIAS) s[r] *= c.log2;
-    if constexpr (MODE & DOC_BIAS) s[r] = bias_score(c, apart, r, s[r]);
+    if constexpr (MODE & DOC_CAP) s[r] = cap_part<E>(c, s[r]);
+    if constexpr (MODE & DOC_BIAS) s[r] = fmaf(s[r], MODE & DOC_CAP ? c.cap : c.log2, bias_score(c, apart, r));
   }
 }
-// Weights p = exp2(score - lse2) into s, and p * (dp - delta) * (the cap's slope) * factor into dp.  lse2(c) and delta(c): of the rows (dK/dV) that the
-// registers 4 c .. 4 c + 3 stand for, or of the lane's own (dQ); lse2 holds what else is added to the exponent, negated.
+// Weights p = exp2(score - lse2) into s, and p * (dp - delta) * (the cap's slope / DOC_SLOPE) * factor into dp.  lse2(c), less g, and delta(c): of the rows
+// (dK/dV) that the registers 4 c .. 4 c + 3 stand for, or of the lane's own (dQ).
 template <typename E, int MODE, typename F, typename G>
 __device__ __forceinline__ void doc_weights(f32x16& s, f32x16& dp, const DocScale& c, float apart, float factor, F&& lse2, G&& delta) {
 #pragma unroll
@@ -289,15 +289,12 @@ __device__ __forceinline__ void doc_weights(f32x16& s, f32x16& dp, const DocScal
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int r = 4 * g + e;
-      float part = 0.f, x;
-      if constexpr (MODE & DOC_CAP) {
-        part = cap_part<E>(c, s[r]);
-        x = cap_score<E>(c, part, -l[e]);
-      } else x = fmaf(s[r], c.log2, -l[e]);
-      if constexpr (MODE & DOC_BIAS) x = bias_score(c, apart, r, x);
+      const float part = MODE & DOC_CAP ? cap_part<E>(c, s[r]) : s[r];
+      float x = fmaf(part, MODE & DOC_CAP ? c.cap : c.log2, -l[e]);
+      if constexpr (MODE & DOC_BIAS) x += bias_score(c, apart, r);
       s[r] = __builtin_amdgcn_exp2f(x);
       float ds = s[r] * (dp[r] - d[e]);
-      if constexpr (MODE & DOC_CAP) ds *= cap_slope<E>(part);
+      if constexpr (MODE & DOC_CAP) ds *= fmaf(-part, part, sizeof(E) == 4 ? 1.f : part);
       dp[r] = __is_same(E, f16) ? ds * factor : ds;
     }
   }
