@@ -16,7 +16,7 @@ hipError_t run(hipStream_t st, DType dt, const DocAttn& a, bool backward) {
 int doc_dkv_keys(DType dt, int T, int nh, int nkv) {
   const int most = dt == F32 ? 128 : 64;
   if (cdiv(T, most) * nh < 256) return 32;
-  return dt == F32 || cdiv(T, 128) * nkv >= 512 ? 128 : 64;
+  return dt == F32 || cdiv(T, 128) * nkv >= 1024 ? 128 : 64;
 }
 int doc_dkv_parts(DType dt, int T, int nh, int nkv) {
   const int group = nh / nkv;

@@ -502,7 +502,7 @@ __device__ __forceinline__ void dkv_block(char* smem_raw, const DocAttn& a, int 
         }
         // Two waves per SIMD have 256 registers each, of which 192 hold K, dK, dV and the scores: the phases are kept apart, or the compiler
         // spills accumulators to read ahead.
-        if constexpr (NW == 8 || OWN) __builtin_amdgcn_sched_barrier(0);
+        if constexpr (sizeof(E) == 2) __builtin_amdgcn_sched_barrier(0);
         doc_weights<E, MODE>(s, dp, sc, (float)(rb + 4 * (lane >> 5) - my_k), HALF<E> ? unit / 16384.f : 1.f,
                        [&](int c) { return lds_read<f32x4>(stat_at + 4 * (32 * j + 8 * c)); },
                        [&](int c) { return lds_read<f32x4>(stat_at + 4 * (ROWS + 32 * j + 8 * c)); });
@@ -514,7 +514,7 @@ __device__ __forceinline__ void dkv_block(char* smem_raw, const DocAttn& a, int 
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          if constexpr (NW == 8 || OWN) __builtin_amdgcn_sched_barrier(0);
+          if constexpr (sizeof(E) == 2) __builtin_amdgcn_sched_barrier(0);
           const typename M::col8 pf = pack<E>(s, u), df = pack<E>(dp, u);
 #pragma unroll
           for (int b = 0; b < TL::BLOCKS; ++b) {
@@ -577,7 +577,7 @@ __device__ __forceinline__ void dkv_block(char* smem_raw, const DocAttn& a, int 
 }
 
 template <typename E, int D, int MODE, int KG, int QS, int ROWS, int NBUF>
-__global__ __attribute__((amdgpu_waves_per_eu(KG * QS / 4, KG * QS / 4))) __launch_bounds__(64 * KG * QS) void doc_dkv_kernel(DocAttn a) {
+__global__ __attribute__((amdgpu_waves_per_eu(sizeof(E) == 2 ? 2 : 1, sizeof(E) == 2 ? 2 : 1))) __launch_bounds__(64 * KG * QS) void doc_dkv_kernel(DocAttn a) {
   __shared__ __align__(16) char smem[DkvLds<E, D, KG, QS, ROWS, NBUF>::bytes];
   dkv_block<E, D, MODE, KG, QS, ROWS, NBUF, false>(smem, a, blockIdx.x);
 }
@@ -661,10 +661,14 @@ template <typename E> hipError_t doc_join(hipStream_t st, const DocAttn& a) {
 }
 template <typename E, int D, int MODE, int KG, int QS, int ROWS, int NBUF> hipError_t doc_dkv(hipStream_t st, DocAttn a) {
   const int64_t blocks = cdiv(a.T, 32 * KG), wgs = blocks * a.nkv * a.parts;
-  a.sorted = doc_sorted(blocks, wgs, 1);
+  a.sorted = doc_sorted(blocks, wgs, sizeof(E) == 2 && KG * QS == 4 ? 2 : 1);
   hipLaunchKernelGGL((doc_dkv_kernel<E, D, MODE, KG, QS, ROWS, NBUF>), dim3((unsigned)wgs), dim3(64 * KG * QS), 0, st, a);
   return hipGetLastError();
 }
+// dK/dV's workgroups: with many key blocks, four waves on 128 keys, two workgroups to a CU, which hide one another's beginnings and ends; with fewer four
+// waves on 64 keys; below that eight waves on 64 keys, and then the query heads of a key head in parts (doc_dkv_parts).  us of the whole backward,
+// bf16, heads of 128, 4096 tokens: 32 key heads, packed 175, 189, 232; 16 key heads 205, 168, 185; 8 key heads, capped 369, 269,
+// 207, and with two parts 256, 216, 236.  Eight waves on 128 keys, which bring in half the rows, are never the fastest: 190, 178, 275.
 template <typename E, int D, int MODE> hipError_t doc_bwd(hipStream_t st, const DocAttn& a) {
   const int keys = doc_dkv_keys((DType)(sizeof(E) == 4 ? F32 : BF16), a.T, a.nh, a.nkv);
   if (keys == 32) {
@@ -676,7 +680,9 @@ template <typename E, int D, int MODE> hipError_t doc_bwd(hipStream_t st, const 
   hipError_t e = doc_by_rows<E, D, MODE, true>(st, a);
   if (e != hipSuccess) return e;
   if constexpr (sizeof(E) == 4) e = doc_dkv<E, D, MODE, 4, 1, 32, 2>(st, a);
-  else e = keys == 64 ? doc_dkv<E, D, MODE, 2, 4, 128, 2>(st, a) : doc_dkv<E, D, MODE, 4, 2, 64, 2>(st, a);
+  else if (keys == 128) e = doc_dkv<E, D, MODE, 4, 1, 32, 2>(st, a);
+  else if (cdiv(a.T, 128) * a.nkv >= 384) e = doc_dkv<E, D, MODE, 2, 2, 64, 1>(st, a);
+  else e = doc_dkv<E, D, MODE, 2, 4, 128, 2>(st, a);
   return e != hipSuccess ? e : doc_join<E>(st, a);
 }
 template <typename E, int D, int MODE> hipError_t doc_either(hipStream_t st, const DocAttn& a, bool backward) {

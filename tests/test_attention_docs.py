@@ -134,6 +134,7 @@ LARGE = [Case(500, 32, 8, 128, [100, 300, 90], slopes=True), Case(500, 32, 32, 6
          Case(1100, 64, 16, 128, DOCS, prefix=[50, 1, 0, 64, 0, 100], softcap=30.0), Case(1100, 64, 64, 128, DOCS, first=17),   # 2240
          Case(1100, 64, 32, 64, [1090], slopes=True), Case(1100, 64, 64, 96, DOCS, prefix=[0, 0, 350, 0, 0, 0], softcap=30.0, slopes=True),
          Case(1500, 64, 1, 128, [700, 33, 600]),                                                                          # one key head, its query heads in parts
+         Case(900, 132, 132, 128, [333, 66, 500], softcap=25.0), Case(2050, 64, 64, 64, [40] * 50, slopes=True),   # 1056 and 1088 blocks of 128 keys
          Case(9000, 8, 1, 64, [60, 3000, 900] + [500] * 10), Case(9001, 8, 8, 128, [2900] + [100] * 61)]                   # more than 256 blocks of rows
 
 
