@@ -143,7 +143,7 @@ int stage_op_attention_bwd_noalloc(void* stream, int32_t dtype, int32_t mb, int3
  * stage_op_doc_ranges writes the table that stage_op_attention_docs_* read: ranges[t] = int32 (first and end of the keys that token t
  * sees, first and end of the rows that see token t), zeros for tokens of no document.  It depends on the documents only: one call
  * per microbatch serves all layers, forward and backward.
- * offsets: device int32[ndocs+1], non-decreasing (a document may be empty) and in [0, T]; prefix: device int32[ndocs], cut to the
+ * T <= 2^30.  offsets: device int32[ndocs+1], non-decreasing (a document may be empty) and in [0, T]; prefix: device int32[ndocs], cut to the
  * document's length, or NULL for none; ranges: device int32[T, 4], 16-byte aligned.  The offsets live on the device and are not
  * checked: other values make documents of unspecified tokens, but never ranges outside [0, T]. */
 int stage_op_doc_ranges(void* stream, int32_t T, int32_t ndocs, const int32_t* offsets, const int32_t* prefix, int32_t* ranges);
@@ -154,8 +154,9 @@ int stage_op_doc_ranges(void* stream, int32_t T, int32_t ndocs, const int32_t* o
  * A token of no document gets o = 0 and lse = -inf; its q, k and v may hold anything.
  * Shared key heads: nh query heads, nkv key heads, nh a multiple of nkv; query head h reads key head h / (nh / nkv).  q and o: rows of nh
  * heads, d wide, strides ldq and ldo; k and v: rows of nkv heads, stride ldkv; lse: float[nh, T]; slopes: device float[nh].
- * d: a multiple of 8 up to 128.  Rows start at multiples of 16 bytes and strides are at most 2^22 elements; T * nh < 2^31.
- * scale > 0 and softcap >= 0 are finite.  No output overlaps an input or another output.  T = 0 does nothing.
+ * d: a multiple of 8 up to 128.  Rows start at multiples of 16 bytes, strides are multiples of 16 bytes and at most 2^22 elements;
+ * T <= 2^30 and T * nh < 2^31.  0 < scale <= 2^100; softcap is 0 or between 2^-100 and 2^100 with scale / softcap <= 2^100; slopes are finite.
+ * No output overlaps an input or another output.  T = 0 does nothing.  The GPU that owns `stream` must be the current device.
  * inf or NaN in a token's q, k, v or dout reaches only the rows that see the token, here and in the gradients below. */
 int stage_op_attention_docs_fwd(void* stream, int32_t dtype, int32_t T, int32_t nh, int32_t nkv, int32_t d, const void* q, int64_t ldq,
                                 const void* k, const void* v, int64_t ldkv, const int32_t* ranges, float scale, float softcap,
@@ -178,8 +179,8 @@ int stage_op_attention_docs_bwd(void* stream, int32_t dtype, int32_t T, int32_t 
  * Pair i of token t turns by the angle sign * positions[a, t] * f_i, (u, w) -> (u cos - w sin, u sin + w cos), with f_i = base^(-2i/d), or
  * (own_spectrum != 0) f_i = base^(-j/sections[a]) for the j-th pair of its axis.  Angles are formed in double precision.
  * sign = 1, or -1: the inverse rotation, which is also the gradient.  The results may take the place of the inputs (the same pointer and
- * stride); no other overlap.  d: a multiple of 8 up to 256.  Rows start at multiples of 16 bytes, strides are at most 2^22
- * elements. */
+ * stride); no other overlap.  d: a multiple of 8 up to 256.  Rows start at multiples of 16 bytes, strides are
+ * multiples of 16 bytes and at most 2^22 elements, and (nq + nk) * d is at most 2^24. */
 #define STAGE_OP_ROPE_MAX_AXES 4
 int stage_op_rope_axes(void* stream, int32_t dtype, int32_t T, int32_t nq, int32_t nk, int32_t d, const void* q, int64_t ldq,
                        const void* k, int64_t ldk, const int32_t* positions, int32_t naxes, const int32_t* sections,

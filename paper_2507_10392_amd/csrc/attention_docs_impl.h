@@ -52,8 +52,13 @@ __device__ __attribute__((noinline)) void redo_fwd(DocRedo<NW>* redo, int groups
 }
 
 // ------------------------------------------------------------------------------------------ forward
-// Four waves.  KS = 1: each has 32 rows of its own and walks all keys of a tile, two workgroups to a CU.  KS = 4: the four share 32 rows, each takes
-// 32 keys of a tile, and their sums meet at the end: for few rows.
+// NW waves in groups that have 32 rows of their own.  KS = 1: a wave to a group, which walks all keys of a tile; two workgroups of four waves to a CU.
+// KS = 2, 4: that many waves share a group's rows, each takes its part of a tile's keys, and their sums meet at the end: for few rows.
+// What bounds it: a long document's 32 x 32 blocks cost 16 matrix instructions of 32 cycles (heads of 128) and about as many vector cycles (exponentials,
+// maximum, sums, conversion; with a cap twice that), which two waves per SIMD overlap little: of 8192 tokens after a prefix, 32 heads, 49 % of the
+// SIMDs' cycles are matrix and 43 % vector instructions at 1.04 PFLOP/s (a library product of 8192^3: 1.11).  Two waves held half a step apart by
+// barriers, one at its products while the other forms weights, were slower (529 -> 639 us): the products' LDS reads, spread out otherwise, then fill
+// half of the time.  Raised wave priority around the products: no difference.
 template <typename E, int D, int MODE, int NW, int KS, int ROWS>
 __global__ __launch_bounds__(64 * NW, NW == 8 || KS == 1 ? 2 : 1) void doc_fwd_kernel(DocAttn a, int heads) {
   typedef Tile<E, D> TL;
@@ -127,7 +132,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || KS == 1 ? 2 : 1) void doc_fwd_k
       mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
       // The reference moves only when some row's maximum has outgrown it by 2^8: weights are at most 2^(8 + LAG), the sums and the result refer to the
       // same reference whenever it moves.
-      if (__any(mx > m + (8.f + LAG))) {
+      if (__any(seen > 0 && mx > m + (8.f + LAG))) {
         const float mn = fmaxf(m, mx - LAG), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
         l *= alpha;
         m = mn;
@@ -299,7 +304,8 @@ __device__ __forceinline__ void dq_block(char* smem_raw, const DocAttn& a, int w
           s = M::rows(at.frag(0, 32 * j, c), qf[c], s);
           dp = M::rows(at.frag(TILE, 32 * j, c), dof[c], dp);
         }
-        doc_weights<E, MODE>(s, dp, sc, (float)(kb + 4 * (lane >> 5) - my_q), unit, [&](int) { return f32x4{lse2, lse2, lse2, lse2}; }, [&](int) { return f32x4{delta, delta, delta, delta}; });
+        doc_weights<E, MODE>(s, dp, sc, (float)(kb + 4 * (lane >> 5) - my_q), unit, [&](int) { return f32x4{lse2, lse2, lse2, lse2}; },
+                             [&](int) { return f32x4{delta, delta, delta, delta}; });
         if (part) {
           const int from = kb + 4 * (lane >> 5) - lo;
 #pragma unroll
@@ -345,7 +351,8 @@ __global__ __launch_bounds__(64 * NW, sizeof(E) == 2 && (NW == 8 || KS == 1) ? 2
 
 // ------------------------------------------------------------------------------------------ dK, dV
 // dV^T += dO^T P, dK^T += Q^T dS with S = Q K^T: lanes are keys, registers rows.  KG groups of 32 keys, each with QS waves, which share out the rows of a
-// tile; a wave's V rows sit in LDS, which leaves registers for two waves per SIMD.
+// tile; a wave's V rows sit in LDS, which leaves registers for two waves per SIMD.  Bound like the forward, with 32 matrix instructions per block: 4096
+// tokens, 32 heads, one document 290 us (950 TFLOP/s of the 8 products' worth), capped 355; dQ, with 24, 200 (1030) and 242.
 template <typename E, int NW>
 __device__ __attribute__((noinline)) void redo_dkv(DocRedo<NW>* redo, int groups, int t0, const int32_t* ranges, int T, int d, int group, const E* q,
                                                    int64_t ldq, const E* k, const E* v, int64_t ldkv, const E* dout, const E* o, int64_t ldo,
@@ -504,8 +511,8 @@ __device__ __forceinline__ void dkv_block(char* smem_raw, const DocAttn& a, int 
         // spills accumulators to read ahead.
         if constexpr (sizeof(E) == 2) __builtin_amdgcn_sched_barrier(0);
         doc_weights<E, MODE>(s, dp, sc, (float)(rb + 4 * (lane >> 5) - my_k), HALF<E> ? unit / 16384.f : 1.f,
-                       [&](int c) { return lds_read<f32x4>(stat_at + 4 * (32 * j + 8 * c)); },
-                       [&](int c) { return lds_read<f32x4>(stat_at + 4 * (ROWS + 32 * j + 8 * c)); });
+                             [&](int c) { return lds_read<f32x4>(stat_at + 4 * (32 * j + 8 * c)); },
+                             [&](int c) { return lds_read<f32x4>(stat_at + 4 * (ROWS + 32 * j + 8 * c)); });
         if (part) {
           const int from = rb + 4 * (lane >> 5) - lo;
 #pragma unroll
@@ -572,8 +579,8 @@ __device__ __forceinline__ void dkv_block(char* smem_raw, const DocAttn& a, int 
   }
   if (__builtin_expect(any_row(redo.masks, KG, lane), 0))
     redo_dkv<E, NW>(&redo, KG, t0, a.ranges, a.T, dd, group, (const E*)a.q + h0 * dd, a.ldq, kh, vh, a.ldkv, (const E*)a.dout + h0 * dd,
-                    (const E*)a.o + h0 * dd, a.ldo, a.lse + (int64_t)h0 * a.T, OWN ? nullptr : a.delta + (int64_t)h0 * a.T, a.scale, a.softcap, a.slopes ? a.slopes + h0 : nullptr, (E*)a.dk + kv * dd,
-                    (E*)a.dv + kv * dd, a.lddkv, a.parts > 1 ? part_k : nullptr, part_v, ld_part);
+                    (const E*)a.o + h0 * dd, a.ldo, a.lse + (int64_t)h0 * a.T, OWN ? nullptr : a.delta + (int64_t)h0 * a.T, a.scale, a.softcap,
+                    a.slopes ? a.slopes + h0 : nullptr, (E*)a.dk + kv * dd, (E*)a.dv + kv * dd, a.lddkv, a.parts > 1 ? part_k : nullptr, part_v, ld_part);
 }
 
 template <typename E, int D, int MODE, int KG, int QS, int ROWS, int NBUF>
@@ -583,7 +590,8 @@ __global__ __attribute__((amdgpu_waves_per_eu(sizeof(E) == 2 ? 2 : 1, sizeof(E) 
 }
 
 // Both in one launch, for few rows, where one after the other would leave most of the chip idle twice: no block reads what another one writes.  One buffer
-// where two workgroups then fit a CU, whose waits overlap (fp32 heads over 64: one workgroup in any case).
+// where two workgroups then fit a CU, whose waits overlap (fp32 heads over 64: one workgroup in any case).  us, one after the other : together: 256
+// tokens, 4 heads of 128, bf16 24.4 : 16.7; 500 tokens, 8 heads 29.4 : 23.0; fp32, 1000 tokens, 8 heads of 64 over 2 74.5 : 53.2.
 template <typename E, int D> constexpr int FEW_BUFFERS = sizeof(E) == 2 && D == 64 ? 2 : 1;
 template <typename E, int D> constexpr int FEW_WAVES = sizeof(E) == 4 && D > 64 ? 1 : 2;   // per SIMD
 template <typename E, int D, int MODE>
@@ -626,7 +634,8 @@ inline int doc_heads(const DocAttn& a, int groups) {
   const int group = a.nh / a.nkv;
   return groups % 4 == 0 && group % 4 == 0 ? 4 : groups % 2 == 0 && group % 2 == 0 ? 2 : 1;
 }
-// The longest blocks first by their ranges: where the workgroups are more than the chip holds at a time, and the blocks few enough to be ordered.
+// The longest blocks first by their ranges: where the workgroups are more than the chip holds at a time, and the blocks few enough to be ordered (six
+// documents in 4096 tokens: forward 74 -> 66 us, dQ 107 -> 98, dK/dV 160 -> 144).
 inline bool doc_sorted(int64_t blocks, int64_t workgroups, int per_cu) { return blocks <= 256 && workgroups > 256 * per_cu; }
 
 // Waves that share rows, and rows of the tiles that they share out, as far as two buffers fit in LDS.

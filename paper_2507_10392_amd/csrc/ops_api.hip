@@ -12,14 +12,15 @@ namespace {
 int rc(hipError_t e) { return e == hipSuccess ? STAGE_OK : STAGE_ERR_DEVICE; }
 bool dt_ok(int d) { return d == 0 || d == 1 || d == 2; }
 int vec_of(int d) { return d == 0 ? 4 : 8; }
-// n heads, d wide, side by side in rows of stride ld that 16-byte accesses can walk.  Strides are bounded so that 64 rows stay within the 32-bit
+// n heads, d wide, side by side in rows of stride ld that 16-byte accesses can walk.  Strides are bounded so that 128 rows stay within the 32-bit
 // offsets of a buffer descriptor.
 bool rows_ok(int dtype, const void* p, int64_t ld, int n, int d) {
   return p && !((uintptr_t)p & 15) && ld >= (int64_t)n * d && ld % vec_of(dtype) == 0 && ld <= (1 << 22);
 }
 bool words_ok(const void* p) { return !((uintptr_t)p & 3); }   // floats or whole numbers, or nothing
+constexpr int DOCS_MAX_TOKENS = 1 << 30;   // a block's last token keeps a 32-bit number
 bool docs_shape_ok(int dtype, int T, int nh, int nkv, int d) {
-  return dt_ok(dtype) && T >= 0 && nh >= 1 && nkv >= 1 && nh % nkv == 0 && d >= 8 && d % 8 == 0 && d <= 128 && (int64_t)T * nh <= INT32_MAX;
+  return dt_ok(dtype) && T >= 0 && nh >= 1 && nkv >= 1 && nh % nkv == 0 && d >= 8 && d % 8 == 0 && d <= 128 && T <= DOCS_MAX_TOKENS && (int64_t)T * nh <= INT32_MAX;
 }
 
 // Scratch of stage_op_attention_bwd_noalloc: the row sums delta[mb, nh, S] that the dQ kernel leaves for the dK/dV
@@ -278,18 +279,19 @@ int stage_op_rope_axes(void* stream, int32_t dtype, int32_t T, int32_t nq, int32
 }
 
 int stage_op_doc_ranges(void* stream, int32_t T, int32_t ndocs, const int32_t* offsets, const int32_t* prefix, int32_t* ranges) {
-  if (T < 0 || ndocs < 0 || ndocs == INT32_MAX || !offsets || !ranges || ((uintptr_t)ranges & 15) || !words_ok(offsets) || !words_ok(prefix)) return STAGE_ERR_ARG;
+  if (T < 0 || T > DOCS_MAX_TOKENS || ndocs < 0 || ndocs == INT32_MAX || !offsets || !ranges || ((uintptr_t)ranges & 15) || !words_ok(offsets) || !words_ok(prefix)) return STAGE_ERR_ARG;
   if (T == 0) return STAGE_OK;
   return rc(doc_ranges((hipStream_t)stream, T, ndocs, offsets, prefix, ranges));
 }
 
 namespace {
-// The arguments that both directions of attention_docs share.
+// The arguments that both directions of attention_docs share.  The factors that the kernels make of scale and softcap stay finite.
+constexpr float MOST = 1.2676506e30f;   // 2^100
 bool docs_ok(int32_t dtype, int32_t T, int32_t nh, int32_t nkv, int32_t d, const void* q, int64_t ldq, const void* k, const void* v, int64_t ldkv,
              const int32_t* ranges, float scale, float softcap, const float* slopes, const void* o, int64_t ldo, const float* lse) {
   return docs_shape_ok(dtype, T, nh, nkv, d) && rows_ok(dtype, q, ldq, nh, d) && rows_ok(dtype, k, ldkv, nkv, d) && rows_ok(dtype, v, ldkv, nkv, d) &&
-         rows_ok(dtype, o, ldo, nh, d) && ranges && !((uintptr_t)ranges & 15) && scale > 0.f && !std::isinf(scale) && softcap >= 0.f &&
-         !std::isinf(softcap) && words_ok(slopes) && lse && words_ok(lse);
+         rows_ok(dtype, o, ldo, nh, d) && ranges && !((uintptr_t)ranges & 15) && words_ok(slopes) && lse && words_ok(lse) && scale > 0.f && scale <= MOST &&
+         (softcap == 0.f || (softcap <= MOST && scale / softcap <= MOST && softcap >= 1.f / MOST));
 }
 }  // namespace
 

@@ -357,7 +357,8 @@ BAD = [dict(dtype=3), dict(dtype=-1), dict(T=-1), dict(nh=0), dict(nkv=0), dict(
        dict(v=None), dict(ranges=None), dict(ranges=4100), dict(o=None), dict(lse=None), dict(lse=4098), dict(q=4104), dict(k=4098), dict(v=4104),
        dict(o=4104), dict(ldq=255), dict(ldq=248), dict(ldq=260), dict(ldkv=120), dict(ldkv=132), dict(ldo=248), dict(ldo=(1 << 22) + 8),
        dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf), dict(softcap=-1.0), dict(softcap=math.nan),
-       dict(softcap=math.inf), dict(slopes=4097), dict(T=1 << 29)]
+       dict(softcap=math.inf), dict(softcap=1e-31), dict(softcap=1e31), dict(scale=1e31), dict(scale=1e10, softcap=1e-25),
+       dict(slopes=4097), dict(T=1 << 29), dict(T=(1 << 30) + 1, nh=1, nkv=1)]
 
 
 def fwd_code(a):
@@ -400,6 +401,6 @@ def test_no_tokens():
 
 
 @pytest.mark.parametrize("args", [(-1, 1, 4096, None, 4096), (8, -1, 4096, None, 4096), (8, 1, None, None, 4096), (8, 1, 4096, None, None),
-                                  (8, 1, 4096, None, 4104), (8, 1, 4097, None, 4096), (8, 1, 4096, 4097, 4096)], ids=str)
+                                  (8, 1, 4096, None, 4104), ((1 << 30) + 1, 1, 4096, None, 4096), (8, 1, 4097, None, 4096), (8, 1, 4096, 4097, 4096)], ids=str)
 def test_refusals_of_ranges(args):
     assert zs.lib().stage_op_doc_ranges(None, *args) == zs.STAGE_ERR_ARG
