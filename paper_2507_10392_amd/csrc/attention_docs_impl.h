@@ -57,8 +57,8 @@ __device__ __attribute__((noinline)) void redo_fwd(DocRedo<NW>* redo, int groups
 // What bounds it: a long document's 32 x 32 blocks cost 16 matrix instructions of 32 cycles (heads of 128) and about as many vector cycles (exponentials,
 // maximum, sums, conversion; with a cap twice that), which two waves per SIMD overlap little: of 8192 tokens after a prefix, 32 heads, 49 % of the
 // SIMDs' cycles are matrix and 43 % vector instructions at 1.04 PFLOP/s (a library product of 8192^3: 1.11).  Two waves held half a step apart by
-// barriers, one at its products while the other forms weights, were slower (529 -> 639 us): the products' LDS reads, spread out otherwise, then fill
-// half of the time.  Raised wave priority around the products: no difference.
+// barriers, one at its products while the other forms weights, were slower (529 -> 639 us), and so were the next tile's scores issued between this one's
+// exponentials (531 -> 564).  Raised wave priority around the products: no difference.
 template <typename E, int D, int MODE, int NW, int KS, int ROWS>
 __global__ __launch_bounds__(64 * NW, NW == 8 || KS == 1 ? 2 : 1) void doc_fwd_kernel(DocAttn a, int heads) {
   typedef Tile<E, D> TL;

@@ -315,6 +315,39 @@ def test_side_stream_and_graph(gpu_device):
 
 
 @gpu
+def test_two_streams(gpu_device):
+    """Calls that run side by side, each with a scratch of its own."""
+    c = Case(500, 16, 4, 64, [300, 150], slopes=True)
+    runs = [Run(c, 2, seed=s) for s in (1, 2)]
+    want = [r.all() for r in runs]
+    streams = [torch.cuda.Stream() for _ in runs]
+    for _ in range(5):
+        for r in runs:
+            for x in (r.go, r.lse, r.dq, r.dk, r.dv):
+                x.zero_()
+        torch.cuda.synchronize()
+        for r, s in zip(runs, streams):
+            with torch.cuda.stream(s):
+                r.fwd()
+                r.bwd()
+        torch.cuda.synchronize()
+        for r, w in zip(runs, want):
+            for a, b in zip(w, (r.go, r.lse, r.dq, r.dk, r.dv)):
+                assert torch.equal(a, b)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+def test_every_length_around_the_blocks(gpu_device, dtype):
+    """One document of every length up to 70, and around 128, alone and behind another one."""
+    for n in list(range(1, 71)) + [95, 96, 97, 127, 128, 129, 130]:
+        for c in (Case(n, 2, 1, 32, [n]), Case(n + 33, 1, 1, 32, [n, 33], prefix=[n // 2, 5], softcap=8.0)):
+            r = Run(c, dtype)
+            r.all()
+            r.check()
+
+
+@gpu
 def test_gradients_against_differences(gpu_device):
     """sum(o * w) of the fp32 forward, differenced along random directions."""
     c = Case(24, 2, 1, 16, [10, 12], prefix=[4, 0], softcap=3.0, slopes=True)
