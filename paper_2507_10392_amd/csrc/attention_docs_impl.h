@@ -64,6 +64,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || KS == 1 ? 2 : 1) void doc_fwd_k
   typedef Tile<E, D> TL;
   typedef Mat<E> M;
   constexpr int GROUPS = NW / KS, SUB = ROWS / 32 / KS, TILE = TL::bytes(ROWS);
+  constexpr bool LINES = 2 * ROWS >= 32 * NW;   // q comes by whole lines through the second buffer, where that holds the waves' rows
   constexpr float LAG = P_LAG<E>;
   constexpr size_t LOOP = 4 * TILE, END = sizeof(DocRedo<NW>) + 16 + GROUPS * TL::STORE;   // two buffers of keys and values
   __shared__ __align__(16) char smem_raw[LOOP > END ? LOOP : END];
@@ -77,7 +78,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || KS == 1 ? 2 : 1) void doc_fwd_k
   const Span all = block_span<false, (32 * GROUPS + 63) / 64>(a.ranges, t0, 32 * row_groups, a.T, lane);
   const int4 range = my_q < a.T ? doc_range((const int4*)a.ranges, my_q, a.T) : make_int4(0, 0, 0, 0);
   typename M::vec qf[TL::FRAGS];
-  TL::load_frags(qf, qh, a.ldq, my_q, a.T, lane, dd);
+  if constexpr (!LINES) TL::load_frags(qf, qh, a.ldq, my_q, a.T, lane, dd);
   const DocScale sc = doc_scale<E, MODE>(a, h);
   const int lo = range.x, seen = max(range.y - range.x, 0);   // keys
   const Span mine = span_of(range.x, range.y);
@@ -96,6 +97,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || KS == 1 ? 2 : 1) void doc_fwd_k
   float m = -INFINITY, l = 0.f;   // the reference of the weights, less g, and their sum
   if (tiles > 0) {
     fetch(smem, all.lo);
+    if constexpr (LINES) load_frags_by_lines<E, D>(qf, smem + 2 * TILE + wave * TL::bytes(32), qh, a.ldq, w0, a.T, lane, dd);
     tile_wait();
     __syncthreads();
   }
@@ -234,6 +236,8 @@ __device__ __forceinline__ void dq_block(char* smem_raw, const DocAttn& a, int w
   typedef Tile<E, D> TL;
   typedef Mat<E> M;
   constexpr int GROUPS = NW / KS, SUB = ROWS / 32 / KS, TILE = TL::bytes(ROWS);
+  // q, dout and o come by whole lines through the second buffer, where there is one and it holds the waves' rows.
+  constexpr bool LINES = NBUF == 2 && 2 * ROWS >= 32 * NW;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int ks = wave / GROUPS, grp = wave % GROUPS, row_groups = GROUPS / heads, h_in = grp / row_groups, dd = a.d;
   const DocBlock blk = row_block(a, workgroup, heads, 32 * row_groups, lane);
@@ -244,8 +248,10 @@ __device__ __forceinline__ void dq_block(char* smem_raw, const DocAttn& a, int w
   const int lo = range.x, seen = max(range.y - range.x, 0);
   const bool live = seen > 0 && my_q < a.T;
   typename M::vec qf[TL::FRAGS], dof[TL::FRAGS];
-  TL::load_frags(qf, (const E*)a.q + h * dd, a.ldq, my_q, a.T, lane, dd);
-  TL::load_frags(dof, (const E*)a.dout + h * dd, a.ldo, my_q, a.T, lane, dd);
+  if constexpr (!LINES) {
+    TL::load_frags(qf, (const E*)a.q + h * dd, a.ldq, my_q, a.T, lane, dd);
+    TL::load_frags(dof, (const E*)a.dout + h * dd, a.ldo, my_q, a.T, lane, dd);
+  }
   const int64_t stat = (int64_t)h * a.T + min(my_q, a.T - 1);
   const DocScale sc = doc_scale<E, MODE>(a, h);
   const float lse2 = live ? fmaf(a.lse[stat], DOC_LOG2E, -sc.g) : 0.f;
@@ -262,7 +268,12 @@ __device__ __forceinline__ void dq_block(char* smem_raw, const DocAttn& a, int w
   float delta = 0.f, largest = 0.f;
   {
     typename M::vec of[TL::FRAGS];
-    TL::load_frags(of, (const E*)a.o + h * dd, a.ldo, my_q, a.T, lane, dd);
+    if constexpr (LINES) {
+      const unsigned rows = smem + 2 * TILE + wave * TL::bytes(32);
+      load_frags_by_lines<E, D>(qf, rows, (const E*)a.q + h * dd, a.ldq, w0, a.T, lane, dd);
+      load_frags_by_lines<E, D>(dof, rows, (const E*)a.dout + h * dd, a.ldo, w0, a.T, lane, dd);
+      load_frags_by_lines<E, D>(of, rows, (const E*)a.o + h * dd, a.ldo, w0, a.T, lane, dd);
+    } else TL::load_frags(of, (const E*)a.o + h * dd, a.ldo, my_q, a.T, lane, dd);
 #pragma unroll
     for (int c = 0; c < TL::FRAGS; ++c)
 #pragma unroll
@@ -281,7 +292,7 @@ __device__ __forceinline__ void dq_block(char* smem_raw, const DocAttn& a, int w
   f32x16 acc[TL::BLOCKS];
 #pragma unroll
   for (int i = 0; i < TL::BLOCKS; ++i) acc[i] = f32x16{};
-  if (NBUF == 2 && tiles > 0) {
+  if (NBUF == 2) {   // the second buffer's rows have been read, too
     tile_wait();
     __syncthreads();
   }
@@ -412,12 +423,15 @@ __device__ __forceinline__ void dkv_block(char* smem_raw, const DocAttn& a, int 
   const int4 range = my_k < a.T ? doc_range((const int4*)a.ranges, my_k, a.T) : make_int4(0, 0, 0, 0);
   const int lo = range.z, seen = max(range.w - range.z, 0);
   typename M::vec kf[TL::FRAGS];
-  TL::load_frags(kf, kh, a.ldkv, my_k, a.T, lane, dd);
+  constexpr bool LINES = ROWS >= 16 * KG;
+  const unsigned k_at = smem + (NBUF - 1) * 2 * TILE + kg * TL::bytes(32);   // k comes by whole lines through the last buffer, where that holds the rows
+  if constexpr (!LINES) TL::load_frags(kf, kh, a.ldkv, my_k, a.T, lane, dd);
   const Span mine = span_of(range.z, range.w);
   const int tiles = (all.hi - all.lo + ROWS - 1) / ROWS, total = tiles * group;
   if (qs == 0) {
     const TileLoad<E, D, 32, 1> load(a.ldkv, lane, dd);
     load.fetch(smem + V + kg * TL::bytes(32), vh, w0, a.T, 0);
+    if constexpr (LINES) load.fetch(k_at, kh, w0, a.T, 0);
   }
   const TileLoad<E, D, ROWS, NW> load_q(a.ldq, lane, dd), load_d(a.ldo, lane, dd);
   float sr[STATS];
@@ -455,6 +469,12 @@ __device__ __forceinline__ void dkv_block(char* smem_raw, const DocAttn& a, int 
   }
   tile_wait();
   __syncthreads();
+  if constexpr (LINES) {
+    const typename TL::Lane at_k(k_at, lane);
+#pragma unroll
+    for (int s = 0; s < TL::FRAGS; ++s) kf[s] = at_k.frag(0, 0, s);
+    __syncthreads();   // before that buffer's first tile
+  }
   typename TL::Lane at(smem + TL::bytes(qs * 32 * SUB), lane);
   const typename TL::Lane at_v(smem + V + kg * TL::bytes(32), lane);
   unsigned stat_at = smem + NBUF * 2 * TILE + 4 * (qs * 32 * SUB + 4 * (lane >> 5));
