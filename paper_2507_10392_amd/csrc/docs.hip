@@ -14,7 +14,7 @@ __global__ __launch_bounds__(256) void doc_ranges_kernel(int T, int ndocs, const
   if (t >= T) return;
   int lo = 0, hi = ndocs;   // the first document that ends behind t
   while (lo < hi) {
-    const int mid = (lo + hi) >> 1;
+    const int mid = lo + ((hi - lo) >> 1);
     if (offsets[mid + 1] > t) hi = mid;
     else lo = mid + 1;
   }

@@ -383,6 +383,17 @@ def test_documents_of_wrong_offsets_stay_inside(gpu_device):
         assert (r >= 0).all() and (r <= T).all() and (r[:, 0] <= r[:, 1]).all() and (r[:, 2] <= r[:, 3]).all()
 
 
+@gpu
+def test_more_documents_than_two_numbers_of_them_add_up_to(gpu_device):
+    """2^30 + 4 empty documents before the one that has the tokens: the sum of two documents' numbers passes 31 bits."""
+    n, T = (1 << 30) + 5, 5
+    o = torch.zeros(n + 1, dtype=torch.int32, device="cuda")
+    o[n] = T
+    r = torch.full((T, 4), -1, dtype=torch.int32, device="cuda")
+    zs.ops.doc_ranges(stream(), T, n, o, None, r)
+    assert r.cpu().tolist() == [[0, t + 1, t, T] for t in range(T)]
+
+
 # ---------------------------------------------------------------------------------------------- no GPU
 GOOD = dict(dtype=1, T=16, nh=4, nkv=2, d=64, q=4096, ldq=256, k=4096, v=4096, ldkv=128, ranges=4096, scale=0.125, softcap=0.0, slopes=None,
             o=4096, ldo=256, lse=4096)
