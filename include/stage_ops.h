@@ -155,8 +155,9 @@ int stage_op_doc_ranges(void* stream, int32_t T, int32_t ndocs, const int32_t* o
  * Shared key heads: nh query heads, nkv key heads, nh a multiple of nkv; query head h reads key head h / (nh / nkv).  q and o: rows of nh
  * heads, d wide, strides ldq and ldo; k and v: rows of nkv heads, stride ldkv; lse: float[nh, T]; slopes: device float[nh].
  * d: a multiple of 8 up to 128.  Rows start at multiples of 16 bytes, strides are multiples of 16 bytes and at most 2^22 elements;
- * T <= 2^30 and T * nh < 2^31.  0 < scale <= 2^100; softcap is 0 or between 2^-100 and 2^100 with scale / softcap <= 2^100; slopes are finite.
- * No output overlaps an input or another output.  T = 0 does nothing.  The GPU that owns `stream` must be the current device.
+ * T * nh <= 2^30.  0 < scale <= 2^100; softcap is 0 or between 2^-100 and 2^100 (bf16 and half: 2^10, their
+ * capped scores are off by up to 2^-22 softcap) with scale / softcap <= 2^100; slopes are finite.
+ * No output overlaps an input or another output.  T = 0 does nothing (the pointers may be NULL).  The GPU that owns `stream` must be the current device.
  * inf or NaN in a token's q, k, v or dout reaches only the rows that see the token, here and in the gradients below. */
 int stage_op_attention_docs_fwd(void* stream, int32_t dtype, int32_t T, int32_t nh, int32_t nkv, int32_t d, const void* q, int64_t ldq,
                                 const void* k, const void* v, int64_t ldkv, const int32_t* ranges, float scale, float softcap,
@@ -180,7 +181,8 @@ int stage_op_attention_docs_bwd(void* stream, int32_t dtype, int32_t T, int32_t 
  * (own_spectrum != 0) f_i = base^(-j/sections[a]) for the j-th pair of its axis.  Angles are formed in double precision.
  * sign = 1, or -1: the inverse rotation, which is also the gradient.  The results may take the place of the inputs (the same pointer and
  * stride); no other overlap.  d: a multiple of 8 up to 256.  Rows start at multiples of 16 bytes, strides are
- * multiples of 16 bytes and at most 2^22 elements, and (nq + nk) * d is at most 2^24. */
+ * multiples of 16 bytes and at most 2^22 elements, T is at most 2^26 and (nq + nk) * d at most 2^24.  T = 0 does nothing (the
+ * pointers may be NULL). */
 #define STAGE_OP_ROPE_MAX_AXES 4
 int stage_op_rope_axes(void* stream, int32_t dtype, int32_t T, int32_t nq, int32_t nk, int32_t d, const void* q, int64_t ldq,
                        const void* k, int64_t ldk, const int32_t* positions, int32_t naxes, const int32_t* sections,

@@ -19,8 +19,10 @@ bool rows_ok(int dtype, const void* p, int64_t ld, int n, int d) {
 }
 bool words_ok(const void* p) { return !((uintptr_t)p & 3); }   // floats or whole numbers, or nothing
 constexpr int DOCS_MAX_TOKENS = 1 << 30;   // a block's last token keeps a 32-bit number
+constexpr int64_t DOCS_MAX_ROWS = 1 << 30; // tokens times heads: a launch has less than 2^32 threads, which are 64 for 32 rows
+constexpr int ROPE_AXES_MAX_TOKENS = 1 << 26;   // 256 threads take up to 8 of them
 bool docs_shape_ok(int dtype, int T, int nh, int nkv, int d) {
-  return dt_ok(dtype) && T >= 0 && nh >= 1 && nkv >= 1 && nh % nkv == 0 && d >= 8 && d % 8 == 0 && d <= 128 && T <= DOCS_MAX_TOKENS && (int64_t)T * nh <= INT32_MAX;
+  return dt_ok(dtype) && T >= 0 && nh >= 1 && nkv >= 1 && nh % nkv == 0 && d >= 8 && d % 8 == 0 && d <= 128 && (int64_t)T * nh <= DOCS_MAX_ROWS;
 }
 
 // Scratch of stage_op_attention_bwd_noalloc: the row sums delta[mb, nh, S] that the dQ kernel leaves for the dK/dV
@@ -261,7 +263,7 @@ int stage_op_attention_bwd_noalloc(void* stream, int32_t dtype, int32_t mb, int3
 int stage_op_rope_axes(void* stream, int32_t dtype, int32_t T, int32_t nq, int32_t nk, int32_t d, const void* q, int64_t ldq, const void* k,
                        int64_t ldk, const int32_t* positions, int32_t naxes, const int32_t* sections, int32_t own_spectrum, float base,
                        int32_t sign, void* q_out, int64_t ldq_out, void* k_out, int64_t ldk_out) {
-  if (!dt_ok(dtype) || T < 0 || nq < 1 || nk < 0 || d < 8 || d % 8 || d > ROPE_AXES_MAX_D || naxes < 1 || naxes > STAGE_OP_ROPE_MAX_AXES ||
+  if (!dt_ok(dtype) || T < 0 || T > ROPE_AXES_MAX_TOKENS || nq < 1 || nk < 0 || d < 8 || d % 8 || d > ROPE_AXES_MAX_D || naxes < 1 || naxes > STAGE_OP_ROPE_MAX_AXES ||
       !sections || (sign != 1 && sign != -1) || !(base > 0.f) || std::isinf(base))
     return STAGE_ERR_ARG;
   int64_t pairs = 0;
@@ -269,37 +271,39 @@ int stage_op_rope_axes(void* stream, int32_t dtype, int32_t T, int32_t nq, int32
     if (sections[a] < 0) return STAGE_ERR_ARG;
     pairs += sections[a];
   }
-  if (pairs != d / 2) return STAGE_ERR_ARG;
+  if (pairs != d / 2 || ((int64_t)nq + nk) * d > (1 << 24)) return STAGE_ERR_ARG;   // the latter: the kernel's index inside a block of tokens
+  if (T == 0) return STAGE_OK;
   if (!rows_ok(dtype, q, ldq, nq, d) || !rows_ok(dtype, q_out, ldq_out, nq, d) || !positions || !words_ok(positions)) return STAGE_ERR_ARG;
   if (nk > 0 && (!rows_ok(dtype, k, ldk, nk, d) || !rows_ok(dtype, k_out, ldk_out, nk, d))) return STAGE_ERR_ARG;
-  if (((int64_t)nq + nk) * d > (1 << 24)) return STAGE_ERR_ARG;   // the kernel's index inside a block of tokens
-  if (T == 0) return STAGE_OK;
   return rc(rope_axes((hipStream_t)stream, (DType)dtype, T, d, RopeHeads{q, q_out, ldq, ldq_out, nq}, RopeHeads{k, k_out, ldk, ldk_out, nk}, positions,
                       naxes, sections, own_spectrum != 0, base, sign));
 }
 
 int stage_op_doc_ranges(void* stream, int32_t T, int32_t ndocs, const int32_t* offsets, const int32_t* prefix, int32_t* ranges) {
-  if (T < 0 || T > DOCS_MAX_TOKENS || ndocs < 0 || ndocs == INT32_MAX || !offsets || !ranges || ((uintptr_t)ranges & 15) || !words_ok(offsets) || !words_ok(prefix)) return STAGE_ERR_ARG;
+  if (T < 0 || T > DOCS_MAX_TOKENS || ndocs < 0 || ndocs == INT32_MAX) return STAGE_ERR_ARG;
   if (T == 0) return STAGE_OK;
+  if (!offsets || !ranges || ((uintptr_t)ranges & 15) || !words_ok(offsets) || !words_ok(prefix)) return STAGE_ERR_ARG;
   return rc(doc_ranges((hipStream_t)stream, T, ndocs, offsets, prefix, ranges));
 }
 
 namespace {
 // The arguments that both directions of attention_docs share.  The factors that the kernels make of scale and softcap stay finite.
 constexpr float MOST = 1.2676506e30f;   // 2^100
-bool docs_ok(int32_t dtype, int32_t T, int32_t nh, int32_t nkv, int32_t d, const void* q, int64_t ldq, const void* k, const void* v, int64_t ldkv,
+constexpr float MOST_CAP_16 = 1024.f;   // 16-bit kernels' capped scores are off by up to softcap 2^-22: half a step of half's weights
+bool docs_ok(int32_t dtype, int32_t nh, int32_t nkv, int32_t d, const void* q, int64_t ldq, const void* k, const void* v, int64_t ldkv,
              const int32_t* ranges, float scale, float softcap, const float* slopes, const void* o, int64_t ldo, const float* lse) {
-  return docs_shape_ok(dtype, T, nh, nkv, d) && rows_ok(dtype, q, ldq, nh, d) && rows_ok(dtype, k, ldkv, nkv, d) && rows_ok(dtype, v, ldkv, nkv, d) &&
+  return rows_ok(dtype, q, ldq, nh, d) && rows_ok(dtype, k, ldkv, nkv, d) && rows_ok(dtype, v, ldkv, nkv, d) &&
          rows_ok(dtype, o, ldo, nh, d) && ranges && !((uintptr_t)ranges & 15) && words_ok(slopes) && lse && words_ok(lse) && scale > 0.f && scale <= MOST &&
-         (softcap == 0.f || (softcap <= MOST && scale / softcap <= MOST && softcap >= 1.f / MOST));
+         (softcap == 0.f || (softcap <= (dtype == 0 ? MOST : MOST_CAP_16) && scale / softcap <= MOST && softcap >= 1.f / MOST));
 }
 }  // namespace
 
 int stage_op_attention_docs_fwd(void* stream, int32_t dtype, int32_t T, int32_t nh, int32_t nkv, int32_t d, const void* q, int64_t ldq, const void* k,
                                 const void* v, int64_t ldkv, const int32_t* ranges, float scale, float softcap, const float* slopes, void* o,
                                 int64_t ldo, float* lse) {
-  if (!docs_ok(dtype, T, nh, nkv, d, q, ldq, k, v, ldkv, ranges, scale, softcap, slopes, o, ldo, lse)) return STAGE_ERR_ARG;
+  if (!docs_shape_ok(dtype, T, nh, nkv, d)) return STAGE_ERR_ARG;
   if (T == 0) return STAGE_OK;
+  if (!docs_ok(dtype, nh, nkv, d, q, ldq, k, v, ldkv, ranges, scale, softcap, slopes, o, ldo, lse)) return STAGE_ERR_ARG;
   DocAttn a = {};
   a.T = T; a.nh = nh; a.nkv = nkv; a.d = d; a.q = q; a.ldq = ldq; a.k = k; a.v = v; a.ldkv = ldkv; a.ranges = ranges; a.scale = scale;
   a.softcap = softcap; a.slopes = slopes; a.o = o; a.ldo = ldo; a.lse = lse;
@@ -315,10 +319,11 @@ int stage_op_attention_docs_bwd(void* stream, int32_t dtype, int32_t T, int32_t 
                                 const void* v, int64_t ldkv, const int32_t* ranges, float scale, float softcap, const float* slopes, const void* o,
                                 const void* dout, int64_t ldo, const float* lse, void* dq, int64_t lddq, void* dk, void* dv, int64_t lddkv,
                                 void* scratch, int64_t scratch_bytes) {
-  if (!docs_ok(dtype, T, nh, nkv, d, q, ldq, k, v, ldkv, ranges, scale, softcap, slopes, o, ldo, lse) || !rows_ok(dtype, dout, ldo, nh, d) ||
+  if (!docs_shape_ok(dtype, T, nh, nkv, d)) return STAGE_ERR_ARG;
+  if (T == 0) return STAGE_OK;
+  if (!docs_ok(dtype, nh, nkv, d, q, ldq, k, v, ldkv, ranges, scale, softcap, slopes, o, ldo, lse) || !rows_ok(dtype, dout, ldo, nh, d) ||
       !rows_ok(dtype, dq, lddq, nh, d) || !rows_ok(dtype, dk, lddkv, nkv, d) || !rows_ok(dtype, dv, lddkv, nkv, d))
     return STAGE_ERR_ARG;
-  if (T == 0) return STAGE_OK;
   if (!scratch || ((uintptr_t)scratch & 255) || scratch_bytes < attn_docs_bwd_scratch((DType)dtype, T, nh, nkv, d)) return STAGE_ERR_WORKSPACE;
   DocAttn a = {};
   a.T = T; a.nh = nh; a.nkv = nkv; a.d = d; a.q = q; a.ldq = ldq; a.k = k; a.v = v; a.ldkv = ldkv; a.ranges = ranges; a.scale = scale;

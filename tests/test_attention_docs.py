@@ -272,6 +272,26 @@ def test_large_scores(gpu_device, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,softcap", [(0, 1e6), (0, 1024.0), (1, 1024.0), (2, 1024.0)])
+def test_caps_far_above_the_scores(gpu_device, dtype, softcap):
+    """Such a cap changes nothing that the type shows.  Scores of up to about 5 differ from uncapped ones by s^3 / (3 softcap^2) < 2^-14, and are off by
+    up to 2^-22 softcap = 2^-12 in 16 bits (fp32: 2^-21 of themselves): weights by twice that, relative, and so o, against the largest |v|; then the
+    roundings of P and o."""
+    say(dtype, softcap)
+    c = Case(200, 4, 2, 64, [150, 50], softcap=softcap)
+    r = Run(c, dtype)
+    r.all()
+    plain = Case(200, 4, 2, 64, [150, 50])
+    u = ref.scores(plain, r.q, r.k)[0].abs().max()
+    assert u < 6, u
+    o, lse = ref.forward(plain, r.q, r.k, r.v)
+    off = float(u) ** 3 / (3 * softcap ** 2) + (2.0 ** -21 * 6 if dtype == 0 else 2.0 ** -22 * softcap) + 72 * 2.0 ** -24 * 64
+    half = torch.finfo(ref.TD[dtype]).eps / 2
+    assert (r.lse.double().cpu() - lse).abs().max() <= off + 2.0 ** -16   # the sum: 158 x 2^-24
+    assert (r.go.double().cpu() - o).abs().max() <= (2 * off + (2 if dtype else 1) * half + 2.0 ** -16) * r.v.abs().max()
+
+
+@gpu
 def test_rows_that_are_far_apart(gpu_device):
     """Rows whose byte offsets pass 32 bits."""
     T, ld = 600, 1 << 22
@@ -401,8 +421,9 @@ BAD = [dict(dtype=3), dict(dtype=-1), dict(T=-1), dict(nh=0), dict(nkv=0), dict(
        dict(v=None), dict(ranges=None), dict(ranges=4100), dict(o=None), dict(lse=None), dict(lse=4098), dict(q=4104), dict(k=4098), dict(v=4104),
        dict(o=4104), dict(ldq=255), dict(ldq=248), dict(ldq=260), dict(ldkv=120), dict(ldkv=132), dict(ldo=248), dict(ldo=(1 << 22) + 8),
        dict(scale=0.0), dict(scale=-1.0), dict(scale=math.nan), dict(scale=math.inf), dict(softcap=-1.0), dict(softcap=math.nan),
-       dict(softcap=math.inf), dict(softcap=1e-31), dict(softcap=1e31), dict(scale=1e31), dict(scale=1e10, softcap=1e-25),
-       dict(slopes=4097), dict(T=1 << 29), dict(T=(1 << 30) + 1, nh=1, nkv=1)]
+       dict(softcap=math.inf), dict(softcap=1025.0), dict(dtype=2, softcap=2048.0), dict(softcap=1e-31), dict(softcap=1e31), dict(scale=1e31), dict(scale=1e10, softcap=1e-25),
+       dict(slopes=4097), dict(T=1 << 29), dict(T=(1 << 30) + 1, nh=1, nkv=1),
+       dict(T=(1 << 28) + 1)]
 
 
 def fwd_code(a):
@@ -442,6 +463,10 @@ def test_scratch_of_the_backward():
 def test_no_tokens():
     assert fwd_code(dict(GOOD, T=0)) == zs.STAGE_OK and bwd_code(dict(GOOD, T=0)) == zs.STAGE_OK
     assert zs.lib().stage_op_doc_ranges(None, 0, 1, 4096, None, 4096) == zs.STAGE_OK
+    empty = dict(GOOD, T=0, q=None, k=None, v=None, o=None, lse=None, ranges=None)   # an empty tensor's address
+    assert fwd_code(empty) == zs.STAGE_OK and bwd_code(empty, dout=None, dq=None, dk=None, dv=None, scratch=None, bytes=0) == zs.STAGE_OK
+    assert zs.lib().stage_op_doc_ranges(None, 0, 0, None, None, None) == zs.STAGE_OK
+    assert fwd_code(dict(GOOD, T=0, nh=5)) == zs.STAGE_ERR_ARG
 
 
 @pytest.mark.parametrize("args", [(-1, 1, 4096, None, 4096), (8, -1, 4096, None, 4096), (8, 1, None, None, 4096), (8, 1, 4096, None, None),

@@ -145,10 +145,11 @@ def code(**change):
                                  dict(k=None), dict(qo=None), dict(ko=None), dict(positions=None), dict(positions=4098), dict(q=4104), dict(k=4104),
                                  dict(qo=4098), dict(ko=4104), dict(ldq=120), dict(ldk=60), dict(ldqo=130), dict(ldko=56), dict(sections=[12, 21]),
                                  dict(sections=[-1, 33]), dict(sections=[]), dict(sections=[8, 8, 8, 4, 4]), dict(sections=None, naxes=1),
-                                 dict(base=0.0), dict(base=-1.0), dict(base=math.nan), dict(base=math.inf), dict(sign=0), dict(sign=2)], ids=str)
+                                 dict(base=0.0), dict(base=-1.0), dict(base=math.nan), dict(base=math.inf), dict(sign=0), dict(sign=2), dict(T=(1 << 26) + 1)], ids=str)
 def test_refusals(bad):
     assert code(**bad) == zs.STAGE_ERR_ARG
 
 
 def test_no_tokens():
+    assert code(T=0, q=None, k=None, qo=None, ko=None, positions=None) == zs.STAGE_OK and code(T=0, sections=[3]) == zs.STAGE_ERR_ARG
     assert code(T=0) == zs.STAGE_OK and code(T=0, nk=0, k=None, ko=None) == zs.STAGE_OK
