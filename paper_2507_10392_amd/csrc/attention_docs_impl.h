@@ -315,7 +315,7 @@ __device__ __forceinline__ void dq_block(char* smem_raw, const DocAttn& a, int w
           s = M::rows(at.frag(0, 32 * j, c), qf[c], s);
           dp = M::rows(at.frag(TILE, 32 * j, c), dof[c], dp);
         }
-        doc_weights<E, MODE>(s, dp, sc, (float)(kb + 4 * (lane >> 5) - my_q), unit, [&](int) { return f32x4{lse2, lse2, lse2, lse2}; },
+        doc_weights<E, MODE>(s, dp, sc, (float)(kb + 4 * (lane >> 5) - my_q), DOC_UNIT<E, MODE> * unit, [&](int) { return f32x4{lse2, lse2, lse2, lse2}; },
                              [&](int) { return f32x4{delta, delta, delta, delta}; });
         if (part) {
           const int from = kb + 4 * (lane >> 5) - lo;
@@ -530,7 +530,7 @@ __device__ __forceinline__ void dkv_block(char* smem_raw, const DocAttn& a, int 
         // Two waves per SIMD have 256 registers each, of which 192 hold K, dK, dV and the scores: the phases are kept apart, or the compiler
         // spills accumulators to read ahead.
         if constexpr (sizeof(E) == 2) __builtin_amdgcn_sched_barrier(0);
-        doc_weights<E, MODE>(s, dp, sc, (float)(rb + 4 * (lane >> 5) - my_k), HALF<E> ? unit / 16384.f : 1.f,
+        doc_weights<E, MODE>(s, dp, sc, (float)(rb + 4 * (lane >> 5) - my_k), HALF<E> ? DOC_UNIT<E, MODE> / 16384.f * unit : 1.f,
                              [&](int c) { return lds_read<f32x4>(stat_at + 4 * (32 * j + 8 * c)); },
                              [&](int c) { return lds_read<f32x4>(stat_at + 4 * (ROWS + 32 * j + 8 * c)); });
         if (part) {

@@ -257,10 +257,12 @@ template <bool ROWS> __device__ __forceinline__ int heavy_block(const int32_t* r
 //   of themselves.  fp32 keeps tanh_f.
 //   biased: with the bias in.
 // The vector units bound a capped kernel, so its additions are folded: g goes with the reference or the log-sum-exp that is subtracted anyway, and the
-// cap's slope 1 - tanh^2 = 4 (r - r^2) leaves its 4 to the gradients' last factor.
+// cap's slope 1 - tanh^2 = 4 (r - r^2) leaves its 4 (DOC_UNIT) to a factor that is there anyway: the gradients' last one (DOC_SLOPE), or in half, where a
+// quarter of a score gradient may lie below the normal numbers, the one that it is multiplied by before its rounding.
 enum DocMode { DOC_PLAIN = 0, DOC_CAP = 1, DOC_BIAS = 2 };   // or-ed
 template <typename E, int MODE> constexpr bool DOC_FALLS = MODE == DOC_CAP && sizeof(E) == 2;   // f < 0
-template <typename E, int MODE> constexpr float DOC_SLOPE = (MODE & DOC_CAP) && sizeof(E) == 2 ? 4.f : 1.f;
+template <typename E, int MODE> constexpr float DOC_UNIT = (MODE & DOC_CAP) && sizeof(E) == 2 ? 4.f : 1.f;
+template <typename E, int MODE> constexpr float DOC_SLOPE = __is_same(E, f16) ? 1.f : DOC_UNIT<E, MODE>;
 struct DocScale {
   float log2, cap, into_tanh, slope, g;   // scale log2 e; of tanh or r; 2 scale log2 e / softcap, or (fp32) scale / softcap; slope log2 e; see above
   template <int MODE> __device__ __forceinline__ float f() const { return MODE == DOC_PLAIN ? log2 : MODE == DOC_CAP ? cap : 1.f; }
@@ -298,7 +300,7 @@ template <typename E, int MODE> __device__ __forceinline__ void doc_scores(f32x1
     if constexpr (MODE & DOC_BIAS) s[r] = fmaf(s[r], MODE & DOC_CAP ? c.cap : c.log2, bias_score(c, apart, r));
   }
 }
-// Weights p = exp2(score - lse2) into s, and p * (dp - delta) * (the cap's slope / DOC_SLOPE) * factor into dp.  lse2(c), less g, and delta(c): of the rows
+// Weights p = exp2(score - lse2) into s, and p * (dp - delta) * (the cap's slope / DOC_UNIT) * (half: factor) into dp.  lse2(c), less g, and delta(c): of the rows
 // (dK/dV) that the registers 4 c .. 4 c + 3 stand for, or of the lane's own (dQ).
 template <typename E, int MODE, typename F, typename G>
 __device__ __forceinline__ void doc_weights(f32x16& s, f32x16& dp, const DocScale& c, float apart, float factor, F&& lse2, G&& delta) {

@@ -272,6 +272,18 @@ def test_large_scores(gpu_device, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+def test_capped_gradients_of_small_weights(gpu_device, dtype):
+    """Scores of a few times their usual size: most weights, and their score gradients, lie far below the largest, in half among its subnormal numbers,
+    whose step a factor left out of the rounded value would coarsen."""
+    c = Case(1138, 6, 3, 80, [339, 0, 0, 0, 167, 615, 0, 1, 16], softcap=50.0)
+    say(c, dtype)
+    r = Run(c, dtype, seed=66, std=2.0)
+    r.all()
+    r.check()
+
+
+@gpu
 @pytest.mark.parametrize("dtype,softcap", [(0, 1e6), (0, 1024.0), (1, 1024.0), (2, 1024.0)])
 def test_caps_far_above_the_scores(gpu_device, dtype, softcap):
     """Such a cap changes nothing that the type shows.  Scores of up to about 5 differ from uncapped ones by s^3 / (3 softcap^2) < 2^-14, and are off by
