@@ -1,4 +1,4 @@
-// Flash-style attention inside packed documents on the matrix cores, forward and backward, of one element type (bf16, half and float each
+// Attention inside packed documents on the matrix cores, in one pass over the keys, forward and backward, of one element type (bf16, half and float each
 // build it: attention_docs_*.hip).
 //
 // The T x T scores are never stored.  A block of rows reads only the keys that its documents' ranges span, from the first of them on:
