@@ -94,7 +94,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || KS == 1 ? 2 : 1) void doc_fwd_k
   f32x16 oacc[TL::BLOCKS];
 #pragma unroll
   for (int i = 0; i < TL::BLOCKS; ++i) oacc[i] = f32x16{};
-  float m = -INFINITY, l = 0.f;   // the reference of the weights, less g, and their sum
+  float m = -INFINITY, l = 0.f;   // the reference of the weights, less g, and the sum of the lane's own
   if (tiles > 0) {
     fetch(smem, all.lo);
     if constexpr (LINES) load_frags_by_lines<E, D>(qf, smem + 2 * TILE + wave * TL::bytes(32), qh, a.ldq, w0, a.T, lane, dd);
@@ -131,11 +131,10 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || KS == 1 ? 2 : 1) void doc_fwd_k
 #pragma unroll
         for (int r = 0; r < 16; ++r) mx = DOC_FALLS<E, MODE> ? fminf(mx, s[j][r]) : fmaxf(mx, s[j][r]);
       mx *= f;
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
       // The reference moves only when some row's maximum has outgrown it by 2^8: weights are at most 2^(8 + LAG), the sums and the result refer to the
-      // same reference whenever it moves.
+      // same reference whenever it moves.  The two lanes of a row share the reference, but meet only here, and their sums at the end.
       if (__any(seen > 0 && mx > m + (8.f + LAG))) {
-        const float mn = fmaxf(m, mx - LAG), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+        const float mn = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32, 64)) - LAG), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
         l *= alpha;
         m = mn;
 #pragma unroll
@@ -153,8 +152,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || KS == 1 ? 2 : 1) void doc_fwd_k
           s[j][r] = p;
           part[r & 1] += p;
         }
-      const float sum = part[0] + part[1];
-      l += sum + __shfl_xor(sum, 32, 64);
+      l += part[0] + part[1];
 #pragma unroll
       for (int j = 0; j < SUB; ++j)
 #pragma unroll
@@ -168,6 +166,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 || KS == 1 ? 2 : 1) void doc_fwd_k
     at.move(t & 1 ? -2 * TILE : 2 * TILE);
     __syncthreads();
   }
+  l += __shfl_xor(l, 32, 64);
   if constexpr (KS > 1) {
     float* stat = reinterpret_cast<float*>(smem_raw) + grp * KS * 64;   // [GROUPS][KS][m | l][32]
     if (lane < 32) {
