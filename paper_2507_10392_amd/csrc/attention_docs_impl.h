@@ -55,10 +55,11 @@ __device__ __attribute__((noinline)) void redo_fwd(DocRedo<NW>* redo, int groups
 // NW waves in groups that have 32 rows of their own.  KS = 1: a wave to a group, which walks all keys of a tile; two workgroups of four waves to a CU.
 // KS = 2, 4: that many waves share a group's rows, each takes its part of a tile's keys, and their sums meet at the end: for few rows.
 // What bounds it: a long document's 32 x 32 blocks cost 16 matrix instructions of 32 cycles (heads of 128) and about as many vector cycles (exponentials,
-// maximum, sums, conversion; with a cap twice that), which two waves per SIMD overlap little: of 8192 tokens after a prefix, 32 heads, 49 % of the
-// SIMDs' cycles are matrix and 43 % vector instructions at 1.04 PFLOP/s (a library product of 8192^3: 1.11).  Two waves held half a step apart by
+// maximum, sums, conversion; with a cap twice that), which two waves per SIMD overlap little: of 8192 tokens after a prefix, 32 heads, 52 % of the
+// SIMDs' cycles are matrix and 45 % vector instructions at 1.05 PFLOP/s (a library product of 8192^3: 1.11).  Two waves held half a step apart by
 // barriers, one at its products while the other forms weights, were slower (529 -> 639 us), and so were the next tile's scores issued between this one's
-// exponentials (531 -> 564).  Raised wave priority around the products: no difference.
+// exponentials (531 -> 564), and tiles without the maximum, which is formed again only where the sums show that it has moved (574 -> 595: the sums' test
+// keeps the exponentials apart from the products behind it).  Raised wave priority around the products: no difference.
 template <typename E, int D, int MODE, int NW, int KS, int ROWS>
 __global__ __launch_bounds__(64 * NW, NW == 8 || KS == 1 ? 2 : 1) void doc_fwd_kernel(DocAttn a, int heads) {
   typedef Tile<E, D> TL;

@@ -55,7 +55,7 @@ template <typename T> __device__ __forceinline__ T lds_read(unsigned at) { retur
 // the lanes arrange by what they load; squares of 8 rows are followed by a gap of 128 bytes.  Then the 16 rows that one cycle of a fragment
 // read touches lie in 16 different groups of 4 banks, and so do the 4 rows x 64 bytes of half a transposing read.  Of a fragment's
 // address only the place inside a square depends on the lane: four values for row fragments and two (fp32: four) for columns.  Measured on the forward
-// of 8192 tokens: 0.8 M of 74.5 M LDS cycles are conflicts; tiles that came through registers (two dozen of them) into padded rows, 619 us, now 555.
+// of 8192 tokens: 0.8 M of 70.6 M LDS cycles are conflicts; tiles that came through registers (two dozen of them) into padded rows 619 us, these 555.
 template <typename E, int D> struct Tile {
   static constexpr int SZ = (int)sizeof(E), VN = 16 / SZ, FRAGS = D / (2 * VN), BLOCKS = D / 32, SQUARES = (D * SZ + 127) / 128;
   static constexpr int OCTET = SQUARES * 1024 + 128;   // bytes of 8 rows
