@@ -11,7 +11,7 @@
 //
 // 16-bit types round the weights P and the score gradients dS to their type for the second product: half a step of each term, about what the
 // result's own rounding costs.  Half's range is helped by powers of two, taken out at the end: P goes in times 2^7 or 2^14, dS relative to the
-// largest dO of its row (dQ) or of the rows so far (dK).
+// largest dO of its row (dQ), or of the rows so far that see its key (dK): a key's own, or another document's dO would coarsen it.
 #pragma once
 #include "attention_docs_tiles.h"
 
@@ -461,7 +461,7 @@ __device__ __forceinline__ void dkv_block(char* smem_raw, const DocAttn& a, int 
   f32x16 dk[TL::BLOCKS], dv[TL::BLOCKS];
 #pragma unroll
   for (int i = 0; i < TL::BLOCKS; ++i) dk[i] = dv[i] = f32x16{};
-  float unit = 0.f;   // half: of the score gradients, none yet
+  float unit = 0.f;   // half: of the lane's score gradients, none yet
   int h = h0, t = 0;
   if (NBUF == 2 && total > 0) {
     fetch(0, h, all.lo);
@@ -487,20 +487,21 @@ __device__ __forceinline__ void dkv_block(char* smem_raw, const DocAttn& a, int 
       tile_wait();
       __syncthreads();
     }
-    float own_largest = 0.f;
     if constexpr (OWN) {   // lane and lane ^ 32 hold a row
-      float x = 0.f;
+      float x = 0.f, largest = 0.f;
 #pragma unroll
       for (int c = 0; c < TL::FRAGS; ++c) {
         const typename M::vec d = at.frag(TILE, 0, c);
 #pragma unroll
         for (int e = 0; e < TL::VN; ++e) {
           x = fmaf((float)d[e], (float)of[c][e], x);
-          if constexpr (HALF<E>) own_largest = fmaxf(own_largest, fabsf((float)d[e]));
+          if constexpr (HALF<E>) largest = fmaxf(largest, fabsf((float)d[e]));
         }
       }
       x += __shfl_xor(x, 32, 64);
-      *(__attribute__((address_space(3))) float*)(uintptr_t)(stat_at - 16 * (lane >> 5) + 4 * (ROWS + (lane & 31))) = x;
+      const unsigned to = stat_at - 16 * (lane >> 5) + 4 * (lane & 31);
+      *(__attribute__((address_space(3))) float*)(uintptr_t)(to + 4 * ROWS) = x;
+      if constexpr (HALF<E>) *(__attribute__((address_space(3))) float*)(uintptr_t)(to + 8 * ROWS) = fmaxf(largest, __shfl_xor(largest, 32, 64));
       wave_lds_order();
     }
     if (NBUF == 2 && it + 1 < total) fetch(buf ^ 1, hn, rown);
@@ -510,22 +511,37 @@ __device__ __forceinline__ void dkv_block(char* smem_raw, const DocAttn& a, int 
 #pragma unroll
       for (int j = 0; j < SUB; ++j) {
         const int rb = rb0 + 32 * j;
-        f32x16 s = f32x16{}, dp = f32x16{};
+        if constexpr (HALF<E>) {   // the unit of a key, and lane, follows the largest |dO| of the rows so far that see it
+          float top = 0.f;
 #pragma unroll
-        for (int c = 0; c < TL::FRAGS; ++c) {
-          s = M::rows(at.frag(0, 32 * j, c), kf[c], s);
-          dp = M::rows(at.frag(TILE, 32 * j, c), at_v.frag(0, 0, c), dp);
-        }
-        if constexpr (HALF<E>) {   // the unit follows the largest |dO| so far
-          const float top = wave_max(OWN ? own_largest : lds_read<float>(stat_at - 16 * (lane >> 5) + 4 * (2 * ROWS + 32 * j + (lane & 31)))), now = unit_of(top);
-          if (top > 0.f && (unit == 0.f || now < unit)) {
-            const float f = unit == 0.f ? 1.f : now / unit;
-            unit = now;
+          for (int c = 0; c < 4; ++c) {
+            f32x4 x = lds_read<f32x4>(stat_at + 4 * (2 * ROWS + 32 * j + 8 * c));
+            if (part) {
+              const int from = rb + 4 * (lane >> 5) - lo;
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if ((unsigned)(from + 8 * c + e) >= (unsigned)seen) x[e] = 0.f;
+            }
+            top = fmaxf(top, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])));
+          }
+          top = fmaxf(top, __shfl_xor(top, 32, 64));
+          const float now = unit_of(top);
+          const bool moves = top > 0.f && (unit == 0.f || now < unit);
+          if (__any(moves)) {
+            const float f = moves && unit != 0.f ? now / unit : 1.f;
+            if (moves) unit = now;
 #pragma unroll
             for (int b = 0; b < TL::BLOCKS; ++b)
 #pragma unroll
               for (int r = 0; r < 16; ++r) dk[b][r] *= f;
           }
+          __builtin_amdgcn_sched_barrier(0);   // before the products: behind them heads of 128 spill 100 registers (backward of 4096 tokens 214 -> 445 us)
+        }
+        f32x16 s = f32x16{}, dp = f32x16{};
+#pragma unroll
+        for (int c = 0; c < TL::FRAGS; ++c) {
+          s = M::rows(at.frag(0, 32 * j, c), kf[c], s);
+          dp = M::rows(at.frag(TILE, 32 * j, c), at_v.frag(0, 0, c), dp);
         }
         // Two waves per SIMD have 256 registers each, of which 192 hold K, dK, dV and the scores: the phases are kept apart, or the compiler
         // spills accumulators to read ahead.
