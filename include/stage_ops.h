@@ -158,7 +158,8 @@ int stage_op_doc_ranges(void* stream, int32_t T, int32_t ndocs, const int32_t* o
  * T * nh <= 2^30.  0 < scale <= 2^100; softcap is 0 or between 2^-100 and 2^100 (bf16 and half: 2^10, their
  * capped scores are off by up to 2^-22 softcap) with scale / softcap <= 2^100; slopes are finite.
  * No output overlaps an input or another output.  T = 0 does nothing (the pointers may be NULL).  The GPU that owns `stream` must be the current device.
- * inf or NaN in a token's q, k, v or dout reaches only the rows that see the token, here and in the gradients below. */
+ * inf or NaN in a token's k or v reaches only the rows that see the token, in its q or dout only its own row; and in the gradients below the keys and
+ * values that those rows see. */
 int stage_op_attention_docs_fwd(void* stream, int32_t dtype, int32_t T, int32_t nh, int32_t nkv, int32_t d, const void* q, int64_t ldq,
                                 const void* k, const void* v, int64_t ldkv, const int32_t* ranges, float scale, float softcap,
                                 const float* slopes, void* o, int64_t ldo, float* lse);
