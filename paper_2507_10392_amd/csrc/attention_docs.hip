@@ -1,6 +1,8 @@
 // Attention inside packed documents: the choice of the element type's kernels (attention_docs_impl.h).
 #include "kernels.h"
 
+#include <algorithm>
+
 namespace zs {
 
 hipError_t attn_docs_bf16(hipStream_t st, const DocAttn& a, bool backward);
@@ -30,8 +32,22 @@ namespace {
 int64_t delta_bytes(DType dt, int T, int nh) { return cdiv((int64_t)T * nh * 4 * (dt == F16 ? 2 : 1), 256) * 256; }
 }  // namespace
 int64_t attn_docs_bwd_scratch(DType dt, int T, int nh, int nkv, int d) {
-  const int parts = doc_dkv_parts(dt, T, nh, nkv);
-  return delta_bytes(dt, T, nh) + (parts > 1 ? cdiv(2ll * parts * T * nkv * d * 4, 256) * 256 : 0);
+  const int group = nh / nkv;
+  auto need = [&](int t) {
+    const int parts = doc_dkv_parts(dt, t, nh, nkv);
+    return delta_bytes(dt, t, nh) + (parts > 1 ? cdiv(2ll * parts * t * nkv * d * 4, 256) * 256 : 0);
+  };
+  // Fewer tokens may share the query heads out over more parts and need more, so this is the most that any length up to T needs: in a range of
+  // lengths with the same blocks and parts the need grows, and these ranges end where p parts just do not suffice, or the blocks change.
+  int64_t most = need(T);
+  auto end = [&](int64_t t) {
+    if (t > 0 && t < T) most = std::max(most, need((int)t));
+  };
+  end((dt == F32 ? 128 : 64) * (255 / nh));
+  for (int p = 1; p <= group && p * nkv <= 255; ++p)
+    if (group % p == 0)
+      for (int keys = 32; keys <= 128; keys *= 2) end(keys * (255 / (nkv * p)));
+  return most;
 }
 hipError_t attn_docs_fwd(hipStream_t st, DType dt, const DocAttn& a) { return run(st, dt, a, false); }
 hipError_t attn_docs_bwd(hipStream_t st, DType dt, const DocAttn& in, void* scratch) {

@@ -236,7 +236,7 @@ struct DocAttn {
 int doc_dkv_keys(DType dt, int T, int nh, int nkv);
 int doc_dkv_parts(DType dt, int T, int nh, int nkv);
 hipError_t attn_docs_fwd(hipStream_t st, DType dt, const DocAttn& a);
-int64_t attn_docs_bwd_scratch(DType dt, int T, int nh, int nkv, int d);   // bytes
+int64_t attn_docs_bwd_scratch(DType dt, int T, int nh, int nkv, int d);   // bytes, of the largest need of any length up to T
 hipError_t attn_docs_bwd(hipStream_t st, DType dt, const DocAttn& a, void* scratch);
 
 // Rotary positions with several axes: n heads, d wide, of rows in and out (which may be the same).  Pair i of a head turns with the position
