@@ -224,19 +224,21 @@ template <bool ROWS, int N> __device__ __forceinline__ Span block_span(const int
   for (int i = 1; i < N; ++i) all = span_join(all, span_of(lo[i], hi[i]));
   return all;
 }
-// The rank-th longest of `blocks` (at most 256) blocks of `rows` tokens, by the keys that they see or the rows that see them, in steps of 128 and, where
-// equal, the earlier one first.  Which tokens begin a document is known on the device only, so each workgroup finds its block by itself: the blocks'
+// The rank-th longest of `blocks` (at most 256) blocks of `rows` (at most 128) tokens, by the keys that they see or the rows that see them, in 128
+// steps of 128 (above 127 * 128 tokens 256) and, where equal, the earlier one first.  Which tokens begin a document is known on the device only, so each workgroup finds its block by itself: the blocks'
 // numbers (length, then place) lie four to a lane, and the one with `rank` larger ones is found bit by bit, by counting.
 template <bool ROWS> __device__ __forceinline__ int heavy_block(const int32_t* ranges, int T, int rows, int blocks, int rank, int lane) {
   int number[4];
+  const int step = T <= 127 * 128 ? 7 : 8;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int b = lane + 64 * i;
     number[i] = -1;
     if (b < blocks) {
       const int4 first = doc_range((const int4*)ranges, b * rows, T), last = doc_range((const int4*)ranges, min(b * rows + rows, T) - 1, T);
-      const int span = ROWS ? last.w - first.z : last.y - first.x;
-      number[i] = min(max((span + 127) >> 7, 0), 127) << 8 | (255 - b);
+      const int4 &a = first.x < first.y ? first : last, &z = last.x < last.y ? last : first;   // of a document, where the block has padding before or behind it
+      const int span = ROWS ? z.w - a.z : z.y - a.x;
+      number[i] = min(max((span + (1 << step) - 1) >> step, 0), 127) << 8 | (255 - b);
     }
   }
   int found = 0;
