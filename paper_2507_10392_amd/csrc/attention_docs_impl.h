@@ -685,10 +685,16 @@ template <typename E, int D, int MODE, int NW, int KS, int ROWS, bool BWD> hipEr
   return hipGetLastError();
 }
 // The forward's and dQ's workgroups by the groups of 32 rows that there are, for 1024 SIMDs: with few of them the waves of a workgroup share rows and
-// each walks a part of the keys.  us, bf16, heads of 128, forward: 500 tokens, 8 heads (125 groups) four waves on 32 rows 11.3, on
-// 128 rows 14.5, eight waves on 64 rows 12.5; 1024 tokens, 16 heads (512) 25.2, 24.1, 18.3; 2048 tokens, 16 heads over 4 (1024) 44, 26.6, 28.1
-// and eight waves on 128 rows 23.4; 4096 tokens, 32 heads over 8 (4096), six documents four waves on 128 rows 75, eight on 256 rows 84 (one
-// document 155 and 144: the only kind that gains, by 7 % and less the longer).  dQ likewise.
+// each walks a part of the keys.  us, bf16, heads of 128, one document (in brackets three of 48, 34 and 15 %), heads of 64 alike:
+//   256 groups   four waves on 32 rows : eight on 64   2048 tokens 24.9 : 23.9 (16.0 : 16.1); 1024 tokens 192 groups 16.2 : 15.9, 384 groups 22.1 : 16.1
+//   768 groups   eight waves on 64 rows : on 128        512 groups, 1024 tokens 17.5 : 20.7 (12.3 : 13.6), 2048 tokens 24.6 : 32.0 (16.8 : 19.8); 640 groups 22.0 : 20.8
+//                (19.4 : 14.5) and 30.6 : 35.1 (22.2 : 21.8); 768 groups 23.6 : 20.3 (20.4 : 13.9) and 30.8 : 33.9 (23.3 : 21.2); longer documents alone
+//                would have the cut later, packed ones earlier
+//   2048 groups  eight waves on 128 rows : four          two eight-wave workgroups for every CU, more begin a third round.  2048 tokens, 1792 groups 45.8 : 47.5
+//                (31.6 : 32.2), 2048 groups 48.6 : 49.9 (33.3 : 31.5), 2560 groups 66.9 : 55.1 (45.1 : 34.4); 4096 tokens, 1536 groups 68.3 : 82.0 (37.5 : 51.9), 2048 groups
+//                79.9 : 90.6 (46.7 : 49.8), 3072 groups 126 : 116 (66.6 : 55.5)
+// dQ likewise.  Eight waves on 256 rows: 4096 tokens, 32 heads over 8, six documents 84, four on 128 rows 75, one document 144 and 155: the only kind that
+// gains, by 7 % and less the longer.
 template <typename E, int D, int MODE, bool BWD> hipError_t doc_by_rows(hipStream_t st, const DocAttn& a) {
   constexpr int S = SHARE<E, D>;
   const int64_t groups = cdiv(a.T, 32) * a.nh;
@@ -696,7 +702,7 @@ template <typename E, int D, int MODE, bool BWD> hipError_t doc_by_rows(hipStrea
     if (groups < (sizeof(E) == 2 ? 256 : 1024)) return doc_rows<E, D, MODE, 4, S, 32 * S, BWD>(st, a);
   if constexpr (sizeof(E) == 2) {
     if (groups < 768) return doc_rows<E, D, MODE, 8, 4, 128, BWD>(st, a);
-    if (groups < 2000) return doc_rows<E, D, MODE, 8, 2, 128, BWD>(st, a);
+    if (groups <= 2048) return doc_rows<E, D, MODE, 8, 2, 128, BWD>(st, a);
     return doc_rows<E, D, MODE, 4, 1, 64, BWD>(st, a);
   } else return doc_rows<E, D, MODE, 4, 1, 32, BWD>(st, a);
 }
