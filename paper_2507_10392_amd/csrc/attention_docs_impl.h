@@ -378,7 +378,7 @@ __device__ __attribute__((noinline)) void redo_dkv(DocRedo<NW>* redo, int groups
     row_to_lds(redo->rows[wave] + 128, v + j * ldkv, d, lane);
     wave_lds_order();
     float xk[2] = {0.f, 0.f}, xv[2] = {0.f, 0.f};
-    for (int h = 0; h < group; ++h)
+    for (int h = 0; h < group && !(all_nan(xk, d, lane) && all_nan(xv, d, lane)); ++h)
       doc_dkv_head<E>(redo->rows[wave], j, range.z, range.w, d, DocRows<E>{q + h * d, ldq}, DocRows<E>{dout + h * d, ldo}, DocRows<E>{o + h * d, ldo},
                       lse + (int64_t)h * T, delta ? delta + (int64_t)h * T : nullptr, scale, DocScore{softcap, slopes ? slopes[h] : 0.f}, lane, xk, xv);
 #pragma unroll

@@ -108,3 +108,34 @@ def test_padding_on_every_launch(gpu_device, c, dtype):
             g[t] = value
         for a, b in zip(clean, r.all()):
             assert torch.equal(a, b), value
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [1, 2])
+def test_nan_throughout_does_not_take_long(gpu_device, dtype):
+    """A step that has overflowed: every row is NaN, and no row's walk goes on once it is.  Walks to their ends take 200 times a finite call's time, as they are 5 to 9."""
+    c = Case(4096, 32, 8, 128, [4096])
+    r = Run(c, dtype)
+
+    def took(f):
+        ms = []
+        for _ in range(3):
+            a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            a.record()
+            f()
+            b.record()
+            torch.cuda.synchronize()
+            ms.append(a.elapsed_time(b))
+        return min(ms)
+
+    r.all()
+    fwd, bwd = took(r.fwd), took(r.bwd)
+    r.gdout.fill_(math.nan)
+    say(c, dtype, "dout")
+    assert took(r.bwd) < 40 * bwd
+    assert all(x.isnan().all() for x in (r.dq, r.dk, r.dv))
+    r.gq.fill_(math.nan)
+    say(c, dtype, "q")
+    assert took(r.fwd) < 40 * fwd
+    assert r.go.isnan().all() and r.lse.isnan().all()
+    assert took(r.bwd) < 40 * bwd
