@@ -168,7 +168,8 @@ int stage_op_attention_docs_fwd(void* stream, int32_t dtype, int32_t T, int32_t 
  * Half: score gradients enter the second products as halves in units that follow dout.  In dq they are off by at most 2^-25 of the largest |dout| of their
  * row, in dk of the largest of the rows that see their key, over the query heads that share it, or by half a step of their own if that is more.
  * scratch: device, 256-byte aligned, at least stage_op_attention_docs_bwd_scratch_bytes (host only; never less for more tokens, so one
- * for the longest microbatch serves all; negative STAGE_ERR_ARG for invalid sizes), the caller's, free again when the call's work on the stream has finished; calls that may overlap need scratch
+ * for the longest microbatch serves all; negative STAGE_ERR_ARG for invalid sizes), the caller's, free again when the call's work on
+ * the stream has finished; calls that may overlap need scratch
  * of their own.  STAGE_ERR_WORKSPACE when it is missing, misaligned or too small. */
 int64_t stage_op_attention_docs_bwd_scratch_bytes(int32_t dtype, int32_t T, int32_t nh, int32_t nkv, int32_t d);
 int stage_op_attention_docs_bwd(void* stream, int32_t dtype, int32_t T, int32_t nh, int32_t nkv, int32_t d, const void* q, int64_t ldq,

@@ -37,9 +37,9 @@ __device__ __forceinline__ DocBlock row_block(const DocAttn& a, int workgroup, i
   return DocBlock{a.sorted ? heavy_block<false>(a.ranges, a.T, rows, blocks, rank, lane) : blocks - 1 - rank, kv, kv * group + set / a.nkv * heads};
 }
 
-// Calls of their own, not inlined, so that the registers of the kernels' loops are not planned around them.  A kernel is given as many as the calls need all
-// the same: heads of 64 forward 150 (without the call 102 to 126, four waves per SIMD instead of three), dQ 179 and 168 (bf16, half; 122 to 145), dK/dV 209 and 198
-// (160 to 179, 182 to 189); heads of 96 and 128 need more themselves.
+// Calls of their own, not inlined, so that the registers of the kernels' loops are not planned around them. A kernel is given as many as the calls
+// need all the same: heads of 64 forward 150 (without the call 102 to 126, four waves per SIMD instead of three), dQ 179 and 168 (bf16, half; 122 to
+// 145), dK/dV 209 and 198 (160 to 179, 182 to 189); heads of 96 and 128 need more themselves.
 template <typename E, int NW>
 __device__ __attribute__((noinline)) void redo_fwd(DocRedo<NW>* redo, int groups, int row_groups, int t0, const int32_t* ranges, int T, int d, const E* q,
                                                    int64_t ldq, const E* k, const E* v, int64_t ldkv, float scale, float softcap, const float* slopes,
@@ -363,10 +363,10 @@ __global__ __launch_bounds__(64 * NW, sizeof(E) == 2 && (NW == 8 || KS == 1) ? 2
 }
 
 // ------------------------------------------------------------------------------------------ dK, dV
-// dV^T += dO^T P, dK^T += Q^T dS with S = Q K^T: lanes are keys, registers rows.  KG groups of 32 keys, each with QS waves, which share out the rows of a
-// tile; a wave's V rows sit in LDS, which leaves registers for two waves per SIMD: all of them in heads of 128, where half spills up to 12, and bf16 with cap and bias 4
-// (in one launch with dQ up to 20 and 17).  Bound like the forward, with 32 matrix instructions per block: 4096
-// tokens, 32 heads, one document 275 us (1000 TFLOP/s of the 4 products), capped 308; dQ, with 24, 204 (1010 of 3) and 238.
+// dV^T += dO^T P, dK^T += Q^T dS with S = Q K^T: lanes are keys, registers rows. KG groups of 32 keys, each with QS waves, which share out the rows
+// of a tile; a wave's V rows sit in LDS, which leaves registers for two waves per SIMD: all of them in heads of 128, where half spills up to 12, and
+// bf16 with cap and bias 4 (in one launch with dQ up to 20 and 17). Bound like the forward, with 32 matrix instructions per block: 4096 tokens, 32
+// heads, one document 275 us (1000 TFLOP/s of the 4 products), capped 308; dQ, with 24, 204 (1010 of 3) and 238.
 template <typename E, int NW>
 __device__ __attribute__((noinline)) void redo_dkv(DocRedo<NW>* redo, int groups, int t0, const int32_t* ranges, int T, int d, int group, const E* q,
                                                    int64_t ldq, const E* k, const E* v, int64_t ldkv, const E* dout, const E* o, int64_t ldo,
@@ -688,16 +688,16 @@ template <typename E, int D, int MODE, int NW, int KS, int ROWS, bool BWD> hipEr
   return hipGetLastError();
 }
 // The forward's and dQ's workgroups by the groups of 32 rows that there are, for 1024 SIMDs: with few of them the waves of a workgroup share rows and
-// each walks a part of the keys.  us, bf16, heads of 128, one document (in brackets three of 48, 34 and 15 %), heads of 64 alike:
-//   256 groups   four waves on 32 rows : eight on 64   2048 tokens 24.9 : 23.9 (16.0 : 16.1); 1024 tokens 192 groups 16.2 : 15.9, 384 groups 22.1 : 16.1
-//   768 groups   eight waves on 64 rows : on 128        512 groups, 1024 tokens 17.5 : 20.7 (12.3 : 13.6), 2048 tokens 24.6 : 32.0 (16.8 : 19.8); 640 groups 22.0 : 20.8
-//                (19.4 : 14.5) and 30.6 : 35.1 (22.2 : 21.8); 768 groups 23.6 : 20.3 (20.4 : 13.9) and 30.8 : 33.9 (23.3 : 21.2); longer documents alone
-//                would have the cut later, packed ones earlier
-//   2048 groups  eight waves on 128 rows : four          two eight-wave workgroups for every CU, one after the other; more begin a third turn.  2048 tokens, 1792 groups 45.8 : 47.5
-//                (31.6 : 32.2), 2048 groups 48.6 : 49.9 (33.3 : 31.5), 2560 groups 66.9 : 55.1 (45.1 : 34.4); 4096 tokens, 1536 groups 68.3 : 82.0 (37.5 : 51.9), 2048 groups
-//                79.9 : 90.6 (46.7 : 49.8), 3072 groups 126 : 116 (66.6 : 55.5)
-// dQ likewise.  Eight waves on 256 rows: 4096 tokens, 32 heads over 8, six documents 84, four on 128 rows 75, one document 144 and 155: the only kind that
-// gains, by 7 % and less the longer.
+// each walks a part of the keys. us, bf16, heads of 128, one document (in brackets three of 48, 34 and 15 %), heads of 64 alike:
+//   256 groups, four waves on 32 rows : eight on 64.  2048 tokens 24.9 : 23.9 (16.0 : 16.1); 1024 tokens 192 groups 16.2 : 15.9, 384 groups 22.1 : 16.1
+//   768 groups, eight waves on 64 rows : on 128.  512 groups, 1024 tokens 17.5 : 20.7 (12.3 : 13.6), 2048 tokens 24.6 : 32.0 (16.8 : 19.8); 640 groups
+//     22.0 : 20.8 (19.4 : 14.5) and 30.6 : 35.1 (22.2 : 21.8); 768 groups 23.6 : 20.3 (20.4 : 13.9) and 30.8 : 33.9 (23.3 : 21.2); longer documents
+//     alone would have the cut later, packed ones earlier
+//   2048 groups, eight waves on 128 rows : four.  Two eight-wave workgroups for every CU, one after the other; more begin a third turn. 2048 tokens,
+//     1792 groups 45.8 : 47.5 (31.6 : 32.2), 2048 groups 48.6 : 49.9 (33.3 : 31.5), 2560 groups 66.9 : 55.1 (45.1 : 34.4); 4096 tokens, 1536 groups
+//     68.3 : 82.0 (37.5 : 51.9), 2048 groups 79.9 : 90.6 (46.7 : 49.8), 3072 groups 126 : 116 (66.6 : 55.5)
+// dQ likewise. Eight waves on 256 rows: 4096 tokens, 32 heads over 8, six documents 84, four on 128 rows 75, one document 144 and 155: the only kind
+// that gains, by 7 % and less the longer.
 template <typename E, int D, int MODE, bool BWD> hipError_t doc_by_rows(hipStream_t st, const DocAttn& a) {
   constexpr int S = SHARE<E, D>;
   const int64_t groups = cdiv(a.T, 32) * a.nh;
@@ -719,17 +719,18 @@ template <typename E, int D, int MODE, int KG, int QS, int ROWS, int NBUF> hipEr
   hipLaunchKernelGGL((doc_dkv_kernel<E, D, MODE, KG, QS, ROWS, NBUF>), dim3((unsigned)wgs), dim3(64 * KG * QS), 0, st, a);
   return hipGetLastError();
 }
-// dK/dV's workgroups: with many key blocks, four waves on 128 keys, two workgroups to a CU, which hide one another's beginnings and ends; with fewer four
-// waves on 64 keys; below that eight waves on 64 keys, and then the query heads of a key head in parts (doc_dkv_parts); with few rows one launch with dQ.  us of the whole
-// backward, bf16, heads of 128, one document (in brackets three of 48, 34 and 15 %), heads of 64 alike but for the first cut, which they would have at twice the rows:
-//   256 blocks of 64 keys and query head   one launch : eight waves    2048 tokens, 8 heads (256) 68 : 66 (44.8 : 45.7); 1024 tokens, 12 heads (192) 40.4 : 41.8 (30.0 : 32.5), 16 heads
-//                                          (256) 46.6 : 42.9 (35.7 : 32.8), 20 heads 58.3 : 54.7 (42.9 : 48.5)
-//   384 blocks of 128 keys                 eight waves : four, 64 keys   2048 tokens, 320 blocks 120 : 116 (79 : 73), 384 130 : 117 (87 : 74); 4096 tokens, 320 blocks 205 : 216 (112 : 117), 384 223 : 225
-//                                          (119 : 121), 448 252 : 247 (141 : 132)
-//   1024 blocks of 128 keys                four, 64 keys : 128 keys      2048 tokens, 768 blocks 216 : 204 (125 : 118), 1024 283 : 263 (162 : 145); 4096 tokens, 768 385 : 376 (182 : 187), 1024 504 : 483
-//                                          (234 : 219), 1280 620 : 593 (298 : 281)
-// 8 key heads, 4096 tokens, capped, in two parts 236 and 216, whole 207.  Eight waves on 128 keys, which bring in half the rows, are never the fastest: 190, 178, 275
-// where four on 128, four on 64 and eight on 64 take 175, 168 and 207.
+// dK/dV's workgroups: with many key blocks, four waves on 128 keys, two workgroups to a CU, which hide one another's beginnings and ends; with fewer
+// four waves on 64 keys; below that eight waves on 64 keys, and then the query heads of a key head in parts (doc_dkv_parts); with few rows one launch
+// with dQ. us of the whole backward, bf16, heads of 128, one document (in brackets three of 48, 34 and 15 %), heads of 64 alike but for the first
+// cut, which they would have at twice the rows:
+//   256 blocks of 64 keys and query head, one launch : eight waves.  2048 tokens, 8 heads (256) 68 : 66 (44.8 : 45.7); 1024 tokens, 12 heads (192) 40.4
+//     : 41.8 (30.0 : 32.5), 16 heads (256) 46.6 : 42.9 (35.7 : 32.8), 20 heads 58.3 : 54.7 (42.9 : 48.5)
+//   384 blocks of 128 keys, eight waves : four, 64 keys.  2048 tokens, 320 blocks 120 : 116 (79 : 73), 384 130 : 117 (87 : 74); 4096 tokens, 320 blocks
+//     205 : 216 (112 : 117), 384 223 : 225 (119 : 121), 448 252 : 247 (141 : 132)
+//   1024 blocks of 128 keys, four, 64 keys : 128 keys.  2048 tokens, 768 blocks 216 : 204 (125 : 118), 1024 283 : 263 (162 : 145); 4096 tokens, 768 385
+//     : 376 (182 : 187), 1024 504 : 483 (234 : 219), 1280 620 : 593 (298 : 281)
+// 8 key heads, 4096 tokens, capped, in two parts 236 and 216, whole 207. Eight waves on 128 keys, which bring in half the rows, are never the
+// fastest: 190, 178, 275 where four on 128, four on 64 and eight on 64 take 175, 168 and 207.
 template <typename E, int D, int MODE> hipError_t doc_bwd(hipStream_t st, const DocAttn& a) {
   const int keys = doc_dkv_keys((DType)(sizeof(E) == 4 ? F32 : BF16), a.T, a.nh, a.nkv);
   if (keys == 32) {

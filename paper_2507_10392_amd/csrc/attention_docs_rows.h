@@ -27,9 +27,10 @@ template <typename T> __device__ __forceinline__ void row_to_lds(float* to, cons
   for (int c = lane; c < d; c += 64) to[c] = to_f(row[c]);
 }
 
-// NaN in all of a row's columns, which lie lane + 64 c over the wave: no further term changes that, so the walks below end there.  Where a training step has
-// overflowed, most rows are of this kind: one document of 4096 tokens, 32 heads of 128 over 8, forward of q all NaN 39 ms without the ends, 1.4 with them, gradient of dout all NaN
-// 101 and 2.4 (0.16 and 0.5 where all is finite).  A row that is not NaN throughout walks on: a single inf in dout, whose 32 keys are then formed here, 29 ms.
+// NaN in all of a row's columns, which lie lane + 64 c over the wave: no further term changes that, so the walks below end there. Where a training
+// step has overflowed, most rows are of this kind: one document of 4096 tokens, 32 heads of 128 over 8, forward of q all NaN 39 ms without the ends,
+// 1.4 with them, gradient of dout all NaN 101 and 2.4 (0.16 and 0.5 where all is finite). A row that is not NaN throughout walks on: a single inf in
+// dout, whose 32 keys are then formed here, 29 ms.
 __device__ __forceinline__ bool all_nan(const float (&x)[2], int d, int lane) {
   return __all((lane >= d || x[0] != x[0]) && (64 + lane >= d || x[1] != x[1]));
 }

@@ -225,8 +225,9 @@ template <bool ROWS, int N> __device__ __forceinline__ Span block_span(const int
   return all;
 }
 // The rank-th longest of `blocks` (at most 256) blocks of `rows` (at most 128) tokens, by the keys that they see or the rows that see them, in 128
-// steps of 128 (above 127 * 128 tokens 256) and, where equal, the earlier one first.  Which tokens begin a document is known on the device only, so each workgroup finds its block by itself: the blocks'
-// numbers (length, then place) lie four to a lane, and the one with `rank` larger ones is found bit by bit, by counting.
+// steps of 128 (above 127 * 128 tokens 256) and, where equal, the earlier one first. Which tokens begin a document is known on the device only, so
+// each workgroup finds its block by itself: the blocks' numbers (length, then place) lie four to a lane, and the one with `rank` larger ones is found
+// bit by bit, by counting.
 template <bool ROWS> __device__ __forceinline__ int heavy_block(const int32_t* ranges, int T, int rows, int blocks, int rank, int lane) {
   int number[4];
   const int step = T <= 127 * 128 ? 7 : 8;
@@ -275,9 +276,9 @@ template <typename E, int MODE> __device__ __forceinline__ DocScale doc_scale(co
   return DocScale{a.scale * DOC_LOG2E, HALF_SIZE ? -2.f * cap : cap, CAP ? (HALF_SIZE ? 2.f * DOC_LOG2E * a.scale : a.scale) / a.softcap : 0.f,
                   MODE & DOC_BIAS ? a.slopes[h] * DOC_LOG2E : 0.f, CAP && HALF_SIZE ? cap : 0.f};
 }
-// tanh within 1.9e-7 of itself (the largest of all floats from 2^-20 on, in 0.6 .. 1; below 0.5 6.3e-8), without branches: below 0.6 an odd polynomial (fitted by least
-// squares in the relative error, which is 4e-9 with these coefficients), above from the exponential, whose cancellation is harmless there.  12 vector and 2
-// transcendental instructions.
+// tanh within 1.9e-7 of itself (the largest of all floats from 2^-20 on, in 0.6 .. 1; below 0.5 6.3e-8), without branches: below 0.6 an odd
+// polynomial (fitted by least squares in the relative error, which is 4e-9 with these coefficients), above from the exponential, whose cancellation
+// is harmless there. 12 vector and 2 transcendental instructions.
 __device__ __forceinline__ float tanh_f(float u) {
   const float z = u * u;
   float p = 0.0022269718f;
