@@ -695,7 +695,7 @@ template <typename E, int D, int MODE, int NW, int KS, int ROWS, bool BWD> hipEr
 //     alone would have the cut later, packed ones earlier
 //   2048 groups, eight waves on 128 rows : four.  Two eight-wave workgroups for every CU, one after the other; more begin a third turn. 2048 tokens,
 //     1792 groups 45.8 : 47.5 (31.6 : 32.2), 2048 groups 48.6 : 49.9 (33.3 : 31.5), 2560 groups 66.9 : 55.1 (45.1 : 34.4); 4096 tokens, 1536 groups
-//     68.3 : 82.0 (37.5 : 51.9), 2048 groups 79.9 : 90.6 (46.7 : 49.8), 3072 groups 126 : 116 (66.6 : 55.5)
+//     68.3 : 82.0 (37.5 : 51.9), 2048 groups 79.9 : 90.6 (46.7 : 49.8), 4096 groups 156 : 152 (86.9 : 68.5)
 // dQ likewise. Eight waves on 256 rows: 4096 tokens, 32 heads over 8, six documents 84, four on 128 rows 75, one document 144 and 155: the only kind
 // that gains, by 7 % and less the longer.
 template <typename E, int D, int MODE, bool BWD> hipError_t doc_by_rows(hipStream_t st, const DocAttn& a) {
