@@ -215,6 +215,12 @@ int stage_set_overflow_flag(stage_t* s, int32_t* device_flag);
 int stage_loss_scale_update(float* scale, int32_t* good_steps, int32_t found_inf, float backoff, float growth,
                             int32_t growth_interval);
 
+/* Clipping by the gradients' norm.  Once a device factor is set (NULL = off again), every stage_optimizer_step multiplies its grad_scale by
+ * *device_factor (float, caller-owned), which it reads when it runs: stage_op_grad_norm and stage_op_grad_factor of stage_ops.h write it,
+ * the gradients themselves are not rewritten.  The norm is that of all the model's gradients, so the caller adds the sums of squares of the
+ * stages and of the data-parallel shards before the factor is formed; scale there is grad_scale here. */
+int stage_set_grad_factor(stage_t* s, const float* device_factor);
+
 /* Per-kernel-class timing with HIP events on the stage's stream.  stage_profile(s, 1) starts
  * bracketing every launch with events, stage_profile(s, 0) stops.  stage_profile_read
  * synchronises the recorded events and returns, for up to n classes, the class name, number of

@@ -231,6 +231,32 @@ int stage_op_adamw(void* stream, int32_t dtype, int64_t n, int64_t begin, void* 
                    float* m, float* v, float lr, float beta1, float beta2, float eps, float wd, int64_t t,
                    float grad_scale);
 
+/* The norm of many gradient tensors taken together, and clipping by it.  tensors: HOST array of ntensors >= 0 (the pointers and sizes are read during the
+ * call): in: device, n >= 0 elements of dtype, at a multiple of the element's size; out: for stage_op_grad_scale alone (else NULL is fine), the
+ * same place as in, or n elements that overlap none of the list's; n = 0: both may be NULL.  In total less than 2^52 bytes.
+ * Squares and sums are formed in 64 bits and in a fixed order: no overflow, the same bits on every call with the same sizes.
+ *
+ * stage_op_grad_norm: *sumsq = the sum of all squares; *norm = scale sqrt(sumsq), scale > 0 finite (1 / loss scale);
+ * *factor = max_norm / norm where norm > max_norm >= 0, else 1.  Where the norm is inf or NaN (some gradient is), the factor is 1 and 1 is ORed into
+ * *overflow (int32, cleared by the caller; what stage_set_overflow_flag takes).  sumsq (double), norm, factor (float), overflow:
+ * device, any of them may be NULL.  scratch: device, 256-byte aligned, stage_op_grad_norm_scratch_bytes (host only, of the same list; negative
+ * STAGE_ERR_ARG for an invalid one), free again when the call's work on the stream has finished; calls that may overlap need scratch of their
+ * own.  STAGE_ERR_WORKSPACE when it is missing, misaligned or too small.
+ * stage_op_grad_factor: the same from nsums >= 1 sums of squares (device double[nsums], added in their order: of stages, or of shards after a gather).
+ * stage_op_grad_scale: out = in * *factor, rounded once; where the factor is 1 and out is in, nothing is touched. */
+typedef struct {
+  const void* in;
+  void* out;
+  int64_t n;
+  int32_t dtype, reserved;
+} stage_op_tensor;
+int64_t stage_op_grad_norm_scratch_bytes(int32_t ntensors, const stage_op_tensor* tensors);
+int stage_op_grad_norm(void* stream, int32_t ntensors, const stage_op_tensor* tensors, float scale, float max_norm, double* sumsq, float* norm,
+                       float* factor, int32_t* overflow, void* scratch, int64_t scratch_bytes);
+int stage_op_grad_factor(void* stream, int32_t nsums, const double* sums, float scale, float max_norm, double* sumsq, float* norm, float* factor,
+                         int32_t* overflow);
+int stage_op_grad_scale(void* stream, int32_t ntensors, const stage_op_tensor* tensors, const float* factor);
+
 #ifdef __cplusplus
 }
 #endif

@@ -56,6 +56,10 @@ class StageSegmentC(C.Structure):
     _fields_ = [("name", C.c_char * 32), ("offset", C.c_int64), ("rows", C.c_int64), ("cols", C.c_int64)]
 
 
+class TensorC(C.Structure):
+    _fields_ = [("input", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
 class StageKernelStatC(C.Structure):
     _fields_ = [("name", C.c_char * 32), ("launches", C.c_int64), ("ms", C.c_double), ("flops", C.c_double),
                 ("bytes", C.c_double)]
@@ -139,6 +143,12 @@ def lib():
         L.stage_op_embed.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, i32]
         L.stage_op_cross_entropy.argtypes = [vp, i32, i32, i32, vp, i64, vp, vp, vp, vp, f32, i32]
         L.stage_op_adamw.argtypes = [vp, i32, i64, i64, vp, vp, vp, vp, vp, f32, f32, f32, f32, f32, i64, f32]
+        L.stage_set_grad_factor.argtypes = [vp, vp]
+        L.stage_op_grad_norm_scratch_bytes.argtypes = [i32, C.POINTER(TensorC)]
+        L.stage_op_grad_norm_scratch_bytes.restype = i64
+        L.stage_op_grad_norm.argtypes = [vp, i32, C.POINTER(TensorC), f32, f32, vp, vp, vp, vp, vp, i64]
+        L.stage_op_grad_factor.argtypes = [vp, i32, vp, f32, f32, vp, vp, vp, vp]
+        L.stage_op_grad_scale.argtypes = [vp, i32, C.POINTER(TensorC), vp]
         L.stage_op_mfma_rate.argtypes = [vp, i32, i32, vp, vp]
         L.stage_op_lds_probe.argtypes = [vp, i32, C.POINTER(i32), vp, i32, vp]
         _lib = L
@@ -227,6 +237,11 @@ class Stage:
 
     def optimizer_step(self, t, grad_scale=1.0):
         _check(lib().stage_optimizer_step(self.h, t, grad_scale), self.h)
+
+    def set_grad_factor(self, factor):
+        """factor: a float32 tensor of one element on the stage's GPU, or None."""
+        self._factor = factor
+        _check(lib().stage_set_grad_factor(self.h, _ptr(factor)), self.h)
 
     def profile(self, enable):
         _check(lib().stage_profile(self.h, 1 if enable else 0), self.h)
@@ -387,3 +402,44 @@ def attention_docs_bwd_scratch_bytes(dtype, T, nh, nkv, d):
     if n < 0:
         raise StageError(-n, "stage_op_attention_docs_bwd_scratch_bytes")
     return n
+
+
+class TensorList:
+    """Tensors as stage_op_grad_norm and stage_op_grad_scale take them; it keeps them alive, and holds their places and sizes of when it was made."""
+
+    def __init__(self, tensors, outs):
+        import torch
+        types = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+        if len(tensors) != len(outs):
+            raise ValueError("tensor_list: as many outputs as tensors")
+        for x, y in zip(tensors, outs):
+            if x.dtype not in types or x.dtype != y.dtype or x.numel() != y.numel() or not (x.is_contiguous() and y.is_contiguous()):
+                raise ValueError("tensor_list: contiguous float32, bfloat16 or float16 tensors, outputs of the same type and size")
+            if not (x.is_cuda and y.device == x.device == tensors[0].device):
+                raise ValueError("tensor_list: all tensors lie on one GPU")
+        self._keep = (list(tensors), list(outs))
+        self.n = len(tensors)
+        self.c = (TensorC * max(1, self.n))(*[TensorC(x.data_ptr(), y.data_ptr(), x.numel(), types[x.dtype], 0) for x, y in zip(tensors, outs)])
+
+
+def tensor_list(tensors, outs=None):
+    """outs: where grad_scale writes; None: in the tensors' own place."""
+    return TensorList(tensors, tensors if outs is None else outs)
+
+
+def grad_norm_scratch_bytes(tensors):
+    """stage_op_grad_norm_scratch_bytes of a tensor_list (host only)."""
+    n = lib().stage_op_grad_norm_scratch_bytes(tensors.n, tensors.c)
+    if n < 0:
+        raise StageError(-n, "stage_op_grad_norm_scratch_bytes")
+    return n
+
+
+def grad_norm(stream, tensors, scale, max_norm, sumsq, norm, factor, overflow, scratch):
+    """stage_op_grad_norm of a tensor_list; sumsq, norm, factor, overflow: device tensors or None."""
+    ops.grad_norm(stream, tensors.n, tensors.c, scale, max_norm, sumsq, norm, factor, overflow, scratch, scratch.numel() * scratch.element_size())
+
+
+def grad_scale(stream, tensors, factor):
+    """stage_op_grad_scale of a tensor_list."""
+    ops.grad_scale(stream, tensors.n, tensors.c, factor)

@@ -924,6 +924,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(int64_t n, int64_t begin, vo
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * (VEC ? 4 : 1);
   if (i >= n) return;
   const bool skip = h.skip != nullptr && *h.skip != 0;
+  if (h.factor) h.grad_scale *= *h.factor;
   float* pm = LOW ? master + i : (float*)params + begin + i;
   if (VEC) {
     const f32x4 zero = {0.f, 0.f, 0.f, 0.f};

@@ -259,7 +259,8 @@ hipError_t ce_fwd(hipStream_t st, DType dt, int T, int V, const void* z, int64_t
 hipError_t ce_bwd(hipStream_t st, DType dt, int T, int V, void* z, int64_t ldz, const int32_t* targets,
                   const float* lse, float scale);
 
-struct AdamW { float lr, beta1, beta2, eps, wd, inv_bc1, inv_bc2, grad_scale; const int* skip = nullptr; bool zero_grad = true; };
+// factor (or NULL): a device float that multiplies grad_scale.
+struct AdamW { float lr, beta1, beta2, eps, wd, inv_bc1, inv_bc2, grad_scale; const int* skip = nullptr; bool zero_grad = true; const float* factor = nullptr; };
 // Elements i in [0,n): flat parameter index begin+i.  dtype BF16: master/m/v indexed by i, grad and
 // params_bf16 by begin+i.  dtype F32: params (float) indexed by begin+i is the master.  grad[begin, begin+n) is
 // zeroed when h.zero_grad is set; a caller that clears the whole accumulator anyway leaves that to its fill, which
@@ -278,6 +279,15 @@ hipError_t adamw(hipStream_t st, DType dt, int64_t n, int64_t begin, void* param
 hipError_t fill_zero(hipStream_t st, float* p, int64_t n);
 // *flag |= 1 when any of g[0..n) is inf or nan.
 hipError_t nonfinite_check(hipStream_t st, const float* g, int64_t n, int* flag);
+// Gradient tensors of any types (DType) and sizes; in and out may be the same.
+struct GradTensor { const void* in; void* out; int64_t n; int32_t dtype, reserved; };
+// norm = scale sqrt(sum of squares); factor = max_norm / norm where the norm is above that, else 1; *overflow |= 1 where it is inf or NaN (the factor is 1
+// then).  Any of the results may be NULL.
+struct GradClip { float scale, max_norm; double* sumsq; float *norm, *factor; int* overflow; };
+int64_t grad_norm_pieces(const GradTensor* t, int count);   // of the pieces, a double each, that grad_norm leaves in sums
+hipError_t grad_norm(hipStream_t st, const GradTensor* t, int count, const GradClip& c, double* sums);
+hipError_t grad_factor(hipStream_t st, int64_t n, const double* sums, const GradClip& c);
+hipError_t grad_scale(hipStream_t st, const GradTensor* t, int count, const float* factor);
 hipError_t copy_bytes(hipStream_t st, void* dst, const void* src, int64_t bytes);
 
 }  // namespace zs

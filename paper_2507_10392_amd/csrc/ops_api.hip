@@ -365,6 +365,52 @@ int stage_op_adamw(void* stream, int32_t dtype, int64_t n, int64_t begin, void* 
   return rc(adamw((hipStream_t)stream, (DType)dtype, n, begin, params, master, grad, m, v, h));
 }
 
+}  // extern "C"
+namespace {
+static_assert(sizeof(stage_op_tensor) == sizeof(GradTensor), "");
+const GradTensor* grad_tensors(const stage_op_tensor* t) { return reinterpret_cast<const GradTensor*>(t); }
+bool tensors_ok(int32_t n, const stage_op_tensor* t, bool out) {
+  if (n < 0 || (n > 0 && !t)) return false;
+  int64_t total = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const int size = t[i].dtype == 0 ? 4 : 2;
+    if (!dt_ok(t[i].dtype) || t[i].n < 0 || t[i].n > (1ll << 50)) return false;
+    if (t[i].n == 0) continue;
+    if (!t[i].in || (uintptr_t)t[i].in % size || (out && (!t[i].out || (uintptr_t)t[i].out % size))) return false;
+    total += t[i].n * size;
+    if (total >= 1ll << 52) return false;
+  }
+  return true;
+}
+bool clip_ok(float scale, float max_norm, const double* sumsq, const float* norm, const float* factor, const int32_t* overflow) {
+  return scale > 0.f && !std::isinf(scale) && max_norm >= 0.f && !((uintptr_t)sumsq & 7) && words_ok(norm) && words_ok(factor) && words_ok(overflow);
+}
+}  // namespace
+extern "C" {
+
+int64_t stage_op_grad_norm_scratch_bytes(int32_t ntensors, const stage_op_tensor* tensors) {
+  if (!tensors_ok(ntensors, tensors, false)) return -STAGE_ERR_ARG;
+  return cdiv(8 * grad_norm_pieces(grad_tensors(tensors), ntensors) + 8, 256) * 256;
+}
+
+int stage_op_grad_norm(void* stream, int32_t ntensors, const stage_op_tensor* tensors, float scale, float max_norm, double* sumsq, float* norm,
+                       float* factor, int32_t* overflow, void* scratch, int64_t scratch_bytes) {
+  if (!tensors_ok(ntensors, tensors, false) || !clip_ok(scale, max_norm, sumsq, norm, factor, overflow)) return STAGE_ERR_ARG;
+  if (!scratch || ((uintptr_t)scratch & 255) || scratch_bytes < stage_op_grad_norm_scratch_bytes(ntensors, tensors)) return STAGE_ERR_WORKSPACE;
+  return rc(grad_norm((hipStream_t)stream, grad_tensors(tensors), ntensors, GradClip{scale, max_norm, sumsq, norm, factor, overflow}, (double*)scratch));
+}
+
+int stage_op_grad_factor(void* stream, int32_t nsums, const double* sums, float scale, float max_norm, double* sumsq, float* norm, float* factor,
+                         int32_t* overflow) {
+  if (nsums < 1 || !sums || ((uintptr_t)sums & 7) || !clip_ok(scale, max_norm, sumsq, norm, factor, overflow)) return STAGE_ERR_ARG;
+  return rc(grad_factor((hipStream_t)stream, nsums, sums, GradClip{scale, max_norm, sumsq, norm, factor, overflow}));
+}
+
+int stage_op_grad_scale(void* stream, int32_t ntensors, const stage_op_tensor* tensors, const float* factor) {
+  if (!tensors_ok(ntensors, tensors, true) || !factor || !words_ok(factor)) return STAGE_ERR_ARG;
+  return rc(grad_scale((hipStream_t)stream, grad_tensors(tensors), ntensors, factor));
+}
+
 int stage_op_mfma_rate(void* stream, int32_t shape, int32_t iters, const void* operands, float* sink) {
   if ((shape != 16 && shape != 32) || iters < 1 || !operands || !sink) return STAGE_ERR_ARG;
   return rc(mfma_rate((hipStream_t)stream, shape, iters, operands, sink));

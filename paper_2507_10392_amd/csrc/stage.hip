@@ -289,6 +289,7 @@ struct stage {
   int outstanding = 0, accumulated = 0;
   std::vector<int> deferred; // pair_wgrad: slots whose weight-gradient products wait for a later backward (set i = deferred[i])
   int* overflow = nullptr;   // device flag of loss-scaled training (stage_set_overflow_flag), or NULL
+  const float* factor = nullptr;   // device factor of the gradients (stage_set_grad_factor), or NULL
   std::vector<ReduceJob> jobs_host;
   int njobs = 0, max_job_width = 0;
   std::string err;
@@ -1025,6 +1026,7 @@ int stage_optimizer_step(stage_t* s, int64_t t, float grad_scale) {
   h.inv_bc2 = (float)(1.0 / (1.0 - std::pow((double)c.beta2, (double)t)));
   h.grad_scale = grad_scale;
   h.skip = s->overflow;
+  h.factor = s->factor;
   h.zero_grad = false;   // the whole accumulator is cleared by the fill below
   const int64_t P = count_params(c), b = c.shard_begin, e = c.shard_end, n = e - b;
   // loss-scaled training: a non-finite gradient anywhere in the shard raises the flag, and the update that reads
@@ -1046,6 +1048,13 @@ int stage_set_overflow_flag(stage_t* s, int32_t* device_flag) {
   if (!s) return STAGE_ERR_ARG;
   if ((uintptr_t)device_flag & 3) return fail(s, STAGE_ERR_ARG, "device_flag must be 4-byte aligned");
   s->overflow = (int*)device_flag;
+  return STAGE_OK;
+}
+
+int stage_set_grad_factor(stage_t* s, const float* device_factor) {
+  if (!s) return STAGE_ERR_ARG;
+  if ((uintptr_t)device_factor & 3) return fail(s, STAGE_ERR_ARG, "device_factor must be 4-byte aligned");
+  s->factor = device_factor;
   return STAGE_OK;
 }
 
