@@ -177,6 +177,54 @@ int stage_op_attention_docs_bwd(void* stream, int32_t dtype, int32_t T, int32_t 
                                 const float* slopes, const void* o, const void* dout, int64_t ldo, const float* lse, void* dq,
                                 int64_t lddq, void* dk, void* dv, int64_t lddkv, void* scratch, int64_t scratch_bytes);
 
+/* The gated delta rule inside packed documents: a recurrent mixer of tokens.  Every value head of a document has a state S of dk x dv, zero or given at its
+ * begin; a token, with its key k, value v, log decay g, rate beta and query q, makes of it
+ *   S <- exp(g) S;  u = beta (v - S^T k);  S <- S + k u^T;  o = scale S^T q.
+ * T tokens in ndocs documents, document n owning the tokens offsets[n] .. offsets[n+1]-1 (as above; rows of no document get o = 0, theirs of q, k, v, g and
+ * beta may hold anything).  Shared key heads: q and k have nk heads, dk wide, v and o nv heads, dv wide, nv a multiple of nk; value head h reads key
+ * head h / (nv / nk).  g, beta: float[T, nv].  States: float[ndocs, nv, dk, dv].
+ *
+ * stage_op_delta_chunks writes the table of the documents' chunks of 64 tokens that the two calls below read: one call per microbatch serves all
+ * layers, forward and backward.  chunks: device int32[stage_op_delta_chunks_ints(T, ndocs)] (host only; negative STAGE_ERR_ARG), 16-byte aligned.  The
+ * offsets live on the device and are not checked: ones that fall, or leave [0, T], make documents of unspecified tokens, but nothing outside of [0, T] is
+ * read or written for them.
+ * stage_op_delta_fwd: o (stride ldo); h0: the documents' first states, or NULL for zeros; ht: receives their last ones (of an empty document its
+ * first one), or NULL.
+ * stage_op_delta_bwd: from dout (stride ldo) and dht, the gradient of ht (NULL: zeros), the gradients of all inputs: dq, dk_out, dv_out (strides lddq,
+ * lddk, lddv), dg and dbeta (float[T, nv]) and dh0 (or NULL); the forward's results are not needed.
+ * No atomics: a repeat gives the same bits.
+ *
+ * The rule is stable where beta |k|^2 lies between 0 and 2 and g <= 0, so keys have length one (stage_op_norm_fwd, RMSNorm over heads with gains 1/sqrt(dk)).
+ * g below -138, -inf too, forgets everything and counts as that; its own dg is a difference of sums that cancel.  Half: |k_i.k_j| beta and |q_i.k_j| stay below
+ * 65504.  inf or NaN in a token's q, k, v, g, beta or dout may reach every result of its document for the value heads that read
+ * it, and no other document's.
+ * dk and dv: multiples of 8, dk up to 128, dv up to 256.  Rows start at multiples of 16 bytes, strides are multiples of 16 bytes and at most
+ * 2^22 elements; states are 16-byte aligned; T <= 2^26, nv <= 4096, T * nv <= 2^30, ndocs <= 2^20 and ndocs * nv <= 2^20.  scale is finite.
+ * No output overlaps an input or another output.  T = 0 and ndocs = 0 together do nothing.  The GPU that owns `stream` must be the
+ * current device.  scratch: device, 256-byte aligned, at least the bytes of the function beside each call (host only; never less for more
+ * tokens or documents; negative STAGE_ERR_ARG for invalid sizes), the caller's, free again when the call's work on the stream has finished; calls that may
+ * overlap need scratch of their own.  STAGE_ERR_WORKSPACE when it is missing, misaligned or too small. */
+int64_t stage_op_delta_chunks_ints(int32_t T, int32_t ndocs);
+int stage_op_delta_chunks(void* stream, int32_t T, int32_t ndocs, const int32_t* offsets, int32_t* chunks);
+int64_t stage_op_delta_fwd_scratch_bytes(int32_t dtype, int32_t T, int32_t ndocs, int32_t nk, int32_t nv, int32_t dk, int32_t dv);
+int stage_op_delta_fwd(void* stream, int32_t dtype, int32_t T, int32_t nk, int32_t nv, int32_t dk, int32_t dv, const void* q, int64_t ldq,
+                       const void* k, int64_t ldk, const void* v, int64_t ldv, const float* g, const float* beta, int32_t ndocs,
+                       const int32_t* chunks, float scale, const float* h0, void* o, int64_t ldo, float* ht, void* scratch,
+                       int64_t scratch_bytes);
+int64_t stage_op_delta_bwd_scratch_bytes(int32_t dtype, int32_t T, int32_t ndocs, int32_t nk, int32_t nv, int32_t dk, int32_t dv);
+int stage_op_delta_bwd(void* stream, int32_t dtype, int32_t T, int32_t nk, int32_t nv, int32_t dk, int32_t dv, const void* q, int64_t ldq,
+                       const void* k, int64_t ldk, const void* v, int64_t ldv, const float* g, const float* beta, int32_t ndocs,
+                       const int32_t* chunks, float scale, const float* h0, const void* dout, int64_t ldo, const float* dht, void* dq, int64_t lddq,
+                       void* dk_out, int64_t lddk, void* dv_out, int64_t lddv, float* dg, float* dbeta, float* dh0, void* scratch,
+                       int64_t scratch_bytes);
+/* The rule for single tokens (decoding): n tokens, token i of the state slots[i] of state[nstates, nv, dk, dv], which is updated in place; in fp32
+ * arithmetic.  slots: device int32[n], or NULL: token i has state i, n <= nstates.  Tokens with the same state take it one after the other, in their order (as drafts
+ * of several tokens do).  A slot outside [0, nstates) gives o = 0 and touches no state.  Rows, widths and limits as above; n <= 65535.  n = 0 does
+ * nothing. */
+int stage_op_delta_step(void* stream, int32_t dtype, int32_t n, int32_t nk, int32_t nv, int32_t dk, int32_t dv, const void* q, int64_t ldq,
+                        const void* k, int64_t ldk, const void* v, int64_t ldv, const float* g, const float* beta, const int32_t* slots,
+                        float scale, int32_t nstates, float* state, void* o, int64_t ldo);
+
 /* Rotary positions with several axes (time, height and width of video, height and width of images; one axis: text with positions of
  * its own, as packed documents have), of nq query heads and nk key heads (0: k is not read) in one pass.  Axis a turns sections[a] of the
  * d/2 adjacent pairs (2i, 2i+1) of every head, the first sections[0] of them with axis 0 and so on; sections: HOST int32[naxes], not

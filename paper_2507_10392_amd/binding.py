@@ -140,6 +140,16 @@ def lib():
         L.stage_op_attention_docs_bwd_scratch_bytes.restype = i64
         L.stage_op_attention_docs_bwd.argtypes = [vp, i32, i32, i32, i32, i32, vp, i64, vp, vp, i64, vp, f32, f32, vp, vp, vp, i64, vp, vp, i64,
                                                   vp, vp, i64, vp, i64]
+        L.stage_op_delta_chunks_ints.argtypes = [i32, i32]
+        L.stage_op_delta_chunks_ints.restype = i64
+        L.stage_op_delta_chunks.argtypes = [vp, i32, i32, vp, vp]
+        for name in ("fwd", "bwd"):
+            f = getattr(L, f"stage_op_delta_{name}_scratch_bytes")
+            f.argtypes, f.restype = [i32] * 7, i64
+        heads = [vp, i32, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp]
+        L.stage_op_delta_fwd.argtypes = heads + [i32, vp, f32, vp, vp, i64, vp, vp, i64]
+        L.stage_op_delta_bwd.argtypes = heads + [i32, vp, f32, vp, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64]
+        L.stage_op_delta_step.argtypes = heads + [vp, f32, i32, vp, vp, i64]
         L.stage_op_embed.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, i32]
         L.stage_op_cross_entropy.argtypes = [vp, i32, i32, i32, vp, i64, vp, vp, vp, vp, f32, i32]
         L.stage_op_adamw.argtypes = [vp, i32, i64, i64, vp, vp, vp, vp, vp, f32, f32, f32, f32, f32, i64, f32]
@@ -402,6 +412,28 @@ def attention_docs_bwd_scratch_bytes(dtype, T, nh, nkv, d):
     if n < 0:
         raise StageError(-n, "stage_op_attention_docs_bwd_scratch_bytes")
     return n
+
+
+def _bytes(name, *sizes):
+    n = getattr(lib(), name)(*sizes)
+    if n < 0:
+        raise StageError(-n, name)
+    return n
+
+
+def delta_chunks_ints(T, ndocs):
+    """stage_op_delta_chunks_ints (host only)."""
+    return _bytes("stage_op_delta_chunks_ints", T, ndocs)
+
+
+def delta_fwd_scratch_bytes(dtype, T, ndocs, nk, nv, dk, dv):
+    """stage_op_delta_fwd_scratch_bytes (host only)."""
+    return _bytes("stage_op_delta_fwd_scratch_bytes", dtype, T, ndocs, nk, nv, dk, dv)
+
+
+def delta_bwd_scratch_bytes(dtype, T, ndocs, nk, nv, dk, dv):
+    """stage_op_delta_bwd_scratch_bytes (host only)."""
+    return _bytes("stage_op_delta_bwd_scratch_bytes", dtype, T, ndocs, nk, nv, dk, dv)
 
 
 class TensorList:

@@ -1,0 +1,1005 @@
+// The gated delta rule inside packed documents on the matrix cores, forward and backward, of one element type (bf16, half and float each build it:
+// delta_rule_*.hip).
+//
+// With a = exp(g), a token's state is S_t = a_t S_(t-1) + k_t u_t^T, u_t = beta_t (v_t - a_t S_(t-1)^T k_t), and its result scale S_t^T q_t.  A document is
+// cut into chunks of 64 tokens.  With G the running sum of a chunk's g, D_ij = exp(G_i - G_j) for j <= i, and S the state before the chunk, the u of
+// its tokens solve (1 + A) U = beta (V - exp(G) K S), A_ij = beta_i D_ij k_i.k_j for j < i, so that with T = (1 + A)^-1
+//   U = T beta (V - exp(G) K S),  O = scale (exp(G) Q S + P U), P = D o Q K^T,  S' = exp(G_last) S + K^T (exp(G_last - G) U).
+// Backward, from dO and dS' (o: element by element):
+//   dU = scale P^T dO + exp(G_last - G) K dS',  Y = T^T dU,  dV = beta Y,
+//   dS = exp(G_last) dS' + scale Q^T (exp(G) dO) - K^T (beta exp(G) Y),
+//   dQ = scale (exp(G) dO S^T + M K),  M = D o dO U^T,  H = -beta D o Y U^T (below the diagonal),
+//   dK = -beta exp(G) Y S^T + exp(G_last - G) U dS'^T + scale M^T Q + (H + H^T) K,
+// and dbeta and dg from the same products' sums over rows and columns; dg is the sum of dG from a token to its chunk's end.
+//
+// Three steps: what a chunk has of its own (delta_prep_kernel: T and P, all chunks side by side), the walk from chunk to chunk (delta_walk: the state
+// and, backward, its gradient, which needs nothing of the forward walk, so that both share a launch), and the gradients of all chunks side by side
+// (delta_grad_kernel).  No atomics: a repeat gives the same bits.
+//
+// Precision.  q, k, v and dO are operands as they stand.  What is computed stays fp32 in registers; where it is an operand it is taken as two values of
+// the type, the rounded one and what that leaves (16 bits of a bf16 pair, 22 of a half pair), in two or three products: the states, the final one
+// and dg and dbeta among them, are sums over the whole document, and the matrix cores have time, since the walk waits for its own last product.
+// Half pairs have a power of two per column in them (the walk), or are bf16 pairs (delta_grad_kernel), so that no size of state or gradient
+// leaves their range.  fp32: v_mfma_f32_16x16x4, no pairs.
+#pragma once
+#include "attention_docs_tiles.h"
+
+namespace zs {
+namespace {
+
+constexpr int DELTA_C = DELTA_CHUNK;
+constexpr float DELTA_FORGETS = -200.f;   // log2 of a decay that fp32 does not tell from 0; lower ones, -inf among them, count as this
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+
+// Operands of products of 16 x 16 results over 32 terms: a lane holds 8 values of row (or column) lane % 16, the terms 4 (lane/16) + {0 .. 3, 16 .. 19}:
+// the order in which two results above one another, whose rows are 4 (lane/16) + {0 .. 3}, lie in a lane's registers.
+template <typename E> struct Op8 { typedef E type __attribute__((ext_vector_type(8))); };
+template <typename E> using op8 = typename Op8<E>::type;
+__device__ __forceinline__ f32x4 mma1(op8<bf16> a, op8<bf16> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma1(op8<f16> a, op8<f16> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mma1(op8<float> a, op8<float> b, f32x4 c) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+  return c;
+}
+// A value as one operand, or as the sum of two.
+template <typename E, int TERMS> struct Opnd { op8<E> t[TERMS]; };
+template <typename E, int A, int B> __device__ __forceinline__ f32x4 mma(const Opnd<E, A>& a, const Opnd<E, B>& b, f32x4 c) {
+  if constexpr (A == 2) c = mma1(a.t[1], b.t[0], c);
+  if constexpr (B == 2) c = mma1(a.t[0], b.t[1], c);
+  return mma1(a.t[0], b.t[0], c);
+}
+template <typename M> constexpr int PAIR = sizeof(M) == 2 ? 2 : 1;
+template <typename M> using Pair = Opnd<M, PAIR<M>>;
+template <typename M> __device__ __forceinline__ Pair<M> pair_of(const f32x4& a, const f32x4& b) {
+  Pair<M> o;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float x = e < 4 ? a[e & 3] : b[e & 3];
+    o.t[0][e] = from_f<M>(x);
+    if constexpr (PAIR<M> == 2) o.t[1][e] = from_f<M>(fp32_value(x - (float)o.t[0][e]));
+  }
+  return o;
+}
+
+// Half: the power of two that brings the largest of a column's values, which lie in the four lanes that share lane % 16, to 2^13 .. 2^14; else 1.
+template <typename M, int N> __device__ __forceinline__ float column_unit(const f32x4 (&x)[N]) {
+  if constexpr (!__is_same(M, f16)) return 1.f;
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(x[i][r]));
+  m = fmaxf(m, __shfl_xor(m, 16, 64));
+  m = fmaxf(m, __shfl_xor(m, 32, 64));
+  const int e = (int)(__float_as_uint(m) >> 23) & 255;
+  return m > 0.f && e < 255 ? __uint_as_float((unsigned)min(max(127 + 13 + 127 - e, 1), 253) << 23) : 1.f;
+}
+template <typename M> __device__ __forceinline__ float inverse_unit(float unit) {   // of a power of two: exact
+  if constexpr (!__is_same(M, f16)) return 1.f;
+  return __uint_as_float((254u << 23) - __float_as_uint(unit));
+}
+template <typename M, int N> __device__ __forceinline__ void pairs_of(Pair<M> (&o)[N / 2], const f32x4 (&x)[N], float unit) {
+#pragma unroll
+  for (int i = 0; i < N / 2; ++i) {
+    if constexpr (__is_same(M, f16)) o[i] = pair_of<M>(x[2 * i] * unit, x[2 * i + 1] * unit);
+    else o[i] = pair_of<M>(x[2 * i], x[2 * i + 1]);
+  }
+}
+
+// Places of operands in a tile of rows (Tile: rows come straight from memory, pieces of 16 bytes changed about).
+template <typename E, int D> struct TileOps {
+  typedef Tile<E, D> TL;
+  static constexpr int SZ = TL::SZ, OCTET = TL::OCTET;
+  unsigned row_[SZ == 4 ? 2 : 4], col_[SZ == 4 ? 8 : 4];
+  __device__ __forceinline__ TileOps(unsigned base, int lane) {
+    const int g = lane >> 4, i = lane & 15;
+#pragma unroll
+    for (int p = 0; p < (SZ == 4 ? 2 : 4); ++p)
+      row_[p] = base + (i >> 3) * OCTET + (SZ == 4 ? TL::place(i & 7, 4 * p + g) : TL::place(i & 7, 2 * p + (g >> 1)) + 8 * (g & 1));
+    if constexpr (SZ == 4) {
+#pragma unroll
+      for (int p = 0; p < 8; ++p) col_[p] = base + (g >> 1) * OCTET + TL::place(4 * (g & 1) + (p & 3), 4 * (p >> 2) + (i >> 2)) + 4 * (i & 3);
+    } else {
+#pragma unroll
+      for (int p = 0; p < 4; ++p) col_[p] = base + (g >> 1) * OCTET + TL::place(4 * (g & 1) + (i >> 2), 2 * p + ((i & 3) >> 1)) + 8 * (i & 1);
+    }
+  }
+  // row 16 m + lane % 16, columns 32 s + ..
+  __device__ __forceinline__ Opnd<E, 1> row(unsigned tile, int m, int s) const {
+    Opnd<E, 1> o;
+    if constexpr (SZ == 4) {
+      const unsigned at = tile + m * 2 * OCTET + s * 1024;
+      union { f32x4 h[2]; op8<E> v; } u;
+      u.h[0] = lds_read<f32x4>(row_[0] + at);
+      u.h[1] = lds_read<f32x4>(row_[1] + at);
+      o.t[0] = u.v;
+    } else {
+      const unsigned at = tile + m * 2 * OCTET + (s >> 1) * 1024;
+      union { u32x2 h[2]; op8<E> v; } u;
+      u.h[0] = lds_read<u32x2>(row_[2 * (s & 1)] + at);
+      u.h[1] = lds_read<u32x2>(row_[2 * (s & 1) + 1] + at);
+      o.t[0] = u.v;
+    }
+    return o;
+  }
+  // column 16 b + lane % 16, rows 32 s + ..
+  __device__ __forceinline__ Opnd<E, 1> column(unsigned tile, int b, int s) const {
+    Opnd<E, 1> o;
+    if constexpr (SZ == 4) {
+      const unsigned at = tile + s * 4 * OCTET + (b >> 1) * 1024;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o.t[0][e] = lds_read<float>(col_[(b & 1) * 4 + (e & 3)] + at + (e >> 2) * 2 * OCTET);
+    } else {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+      const unsigned at = col_[b & 3] + tile + s * 4 * OCTET + (b >> 2) * 1024;
+      union { s16x4 h[2]; op8<E> v; } u;
+      u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)at);
+      u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(at + 2 * OCTET));
+      o.t[0] = u.v;
+    }
+    return o;
+  }
+  // row 16 m + lane % 16, columns 16 b + 4 (lane/16) ..
+  __device__ __forceinline__ f32x4 quad(unsigned tile, int m, int b) const {
+    f32x4 o;
+    if constexpr (SZ == 4) o = lds_read<f32x4>(row_[b & 1] + tile + m * 2 * OCTET + (b >> 1) * 1024);
+    else {
+      typedef E quad_t __attribute__((ext_vector_type(4)));
+      const quad_t q = lds_read<quad_t>(row_[b & 3] + tile + m * 2 * OCTET + (b >> 2) * 1024);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = (float)q[e];
+    }
+    return o;
+  }
+};
+
+// What delta_prep_kernel leaves of a chunk and value head: per token exp(G), exp(G_last - G), beta, and exp(G_last) in the fourth row's first place;
+// then matrices as operands, pair by pair: of T and P, lower triangles, rows by m and terms by s <= m/2; of T^T and P^T, upper ones, s >= m/2.
+constexpr int REC_GATES = 1024, REC_OP = 2048, REC_TRIANGLE = 6 * REC_OP;
+constexpr int REC_T = REC_GATES, REC_P = REC_T + REC_TRIANGLE, REC_FWD = REC_P + REC_TRIANGLE;
+constexpr int REC_TT = REC_P + REC_TRIANGLE, REC_BWD = REC_TT + REC_TRIANGLE;   // backward: P^T in the place of P
+static_assert(REC_FWD == DELTA_RECORD_FWD && REC_BWD == DELTA_RECORD_BWD, "");
+__device__ __forceinline__ constexpr int lower_op(int m, int s) { return m < 2 ? m : 2 + (m - 2) * 2 + s; }
+__device__ __forceinline__ constexpr int upper_op(int m, int s) { return m < 2 ? 2 * m + s : 4 + (m - 2); }
+template <typename M> __device__ __forceinline__ void store_op(char* to, const Pair<M>& o, int lane) {
+  if constexpr (sizeof(M) == 4) {
+    union { op8<M> v; f32x4 h[2]; } u;
+    u.v = o.t[0];
+    reinterpret_cast<f32x4*>(to)[lane] = u.h[0];
+    reinterpret_cast<f32x4*>(to)[64 + lane] = u.h[1];
+  } else {
+    reinterpret_cast<op8<M>*>(to)[lane] = o.t[0];
+    reinterpret_cast<op8<M>*>(to)[64 + lane] = o.t[1];
+  }
+}
+template <typename M> __device__ __forceinline__ Pair<M> load_op(unsigned from, int lane) {   // LDS
+  Pair<M> o;
+  if constexpr (sizeof(M) == 4) {
+    union { op8<M> v; f32x4 h[2]; } u;
+    u.h[0] = lds_read<f32x4>(from + 16 * lane);
+    u.h[1] = lds_read<f32x4>(from + 1024 + 16 * lane);
+    o.t[0] = u.v;
+  } else {
+    o.t[0] = lds_read<op8<M>>(from + 16 * lane);
+    o.t[1] = lds_read<op8<M>>(from + 1024 + 16 * lane);
+  }
+  return o;
+}
+// `bytes` (a multiple of 1024) that lie together, into LDS as they are, by NW waves.
+template <int NW> __device__ __forceinline__ void fetch_bytes(unsigned lds, const char* from, int bytes, int wave, int lane) {
+  const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, bytes, 0x00020000);
+  for (int at = wave * 1024; at < bytes; at += NW * 1024)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(uintptr_t)(lds + at), 16, (unsigned)(at + 16 * lane), 0, 0, 0);
+}
+
+// ------------------------------------------------------------------------------------------ a chunk's own matrices
+constexpr int TRI_LD = 68;   // floats of a row of a 64 x 64 matrix in LDS: rows 16 bytes aligned, four banks apart
+// T = (1 + A)^-1 of a strictly lower A, both in LDS, by four waves.  Blocks of 16 on the diagonal by substitution, a lane per column; then block by
+// block away from it, T_ij = -T_ii (sum over k of A_ik T_kj), in fp32 products.  Every step solves for values of T itself, which are bounded where the
+// rule is stable; powers of A, which are not, do not occur.
+__device__ __forceinline__ void invert_lower(const float* A, float* T, int wave, int lane) {
+  const int g = lane >> 4, c = lane & 15;
+  if (lane < 16) {
+    float x[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      float s[2] = {r == c ? 1.f : 0.f, 0.f};
+#pragma unroll
+      for (int q = 0; q < (r + 3) / 4; ++q) {
+        const f32x4 a = *reinterpret_cast<const f32x4*>(A + (16 * wave + r) * TRI_LD + 16 * wave + 4 * q);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (4 * q + e < r) s[e & 1] = fmaf(-a[e], x[4 * q + e], s[e & 1]);
+      }
+      x[r] = s[0] + s[1];
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) T[(16 * wave + r) * TRI_LD + 16 * wave + c] = x[r];
+  }
+  for (int d = 1; d < 4; ++d) {
+    __syncthreads();
+    const int i = wave, j = wave - d;
+    if (j >= 0) {
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+      for (int k = j; k < i; ++k) {
+        const f32x4 a = *reinterpret_cast<const f32x4*>(A + (16 * i + c) * TRI_LD + 16 * k + 4 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], T[(16 * k + 4 * g + e) * TRI_LD + 16 * j + c], x, 0, 0, 0);
+      }
+      const f32x4 a = *reinterpret_cast<const f32x4*>(T + (16 * i + c) * TRI_LD + 16 * i + 4 * g);
+      f32x4 y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], x[e], y, 0, 0, 0);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) T[(16 * i + 4 * g + r) * TRI_LD + 16 * j + c] = -y[r];
+    }
+  }
+  __syncthreads();
+}
+
+// The running sum of a chunk's log2 decays in 64 bits: sums of many small and a few large ones, of which small differences are wanted.
+__device__ __forceinline__ double running_sum(double x, int lane) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+__device__ __forceinline__ float decay(double to, double from) { return __builtin_amdgcn_exp2f((float)(to - from)); }
+
+struct ChunkRow { int first, count, doc, index; };
+__device__ __forceinline__ ChunkRow chunk_row(const DeltaRule& a, int c) {
+  const int4 r = reinterpret_cast<const int4*>(a.chunks)[1 + a.ndocs + c];
+  return ChunkRow{r.x, r.y, r.z, r.w};
+}
+
+// Rows of no document become zeros: the last DELTA_FILL blocks of a grid of chunks share them.
+template <typename E> __device__ __forceinline__ void fill_rows(E* p, int64_t ld, int width, int T, int begin, int end, int block) {
+  const int rows = begin + (T - end), vecs = width / Vec<E>::N;
+  for (int64_t i = (int64_t)block * 256 + threadIdx.x; i < (int64_t)rows * vecs; i += DELTA_FILL * 256) {
+    const int r = (int)(i / vecs), t = r < begin ? r : end + (r - begin);
+    *reinterpret_cast<typename Vec<E>::type*>(p + t * ld + (i % vecs) * Vec<E>::N) = typename Vec<E>::type{};
+  }
+}
+
+// A workgroup per chunk and key head; the value heads of the key head one after the other.
+template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaRule a) {
+  typedef Tile<E, DK> TL;
+  constexpr int TILE = TL::bytes(DELTA_C), KS = DK / 32;
+  __shared__ __align__(16) char tiles[2 * TILE];
+  __shared__ __align__(16) float A[64 * TRI_LD], Tm[64 * TRI_LD];
+  __shared__ double G[64];
+  __shared__ float B[64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i16 = lane & 15;
+  const int kv = blockIdx.y, group = a.nv / a.nk;
+  if ((int)blockIdx.x >= a.nchunks) {
+    const int4 head = *reinterpret_cast<const int4*>(a.chunks);
+    const int begin = min(max(head.y, 0), a.T), end = min(max(head.z, begin), a.T), block = (int)blockIdx.x - a.nchunks;
+    if constexpr (BWD) {
+      fill_rows((E*)a.dq + kv * a.dk, a.lddq, a.dk, a.T, begin, end, block);
+      fill_rows((E*)a.dkey + kv * a.dk, a.lddk, a.dk, a.T, begin, end, block);
+      fill_rows((E*)a.dval + kv * group * a.dv, a.lddv, group * a.dv, a.T, begin, end, block);
+      for (int i = block * 256 + threadIdx.x; i < begin + (a.T - end); i += DELTA_FILL * 256) {
+        const int t = i < begin ? i : end + (i - begin);
+        for (int h = 0; h < group; ++h) a.dg[(int64_t)t * a.nv + kv * group + h] = a.dbeta[(int64_t)t * a.nv + kv * group + h] = 0.f;
+      }
+    } else fill_rows((E*)a.o + kv * group * a.dv, a.ldo, group * a.dv, a.T, begin, end, block);
+    return;
+  }
+  const ChunkRow c = chunk_row(a, blockIdx.x);
+  if (c.count <= 0) return;
+  const unsigned smem = lds_address(tiles);
+  {
+    const TileLoad<E, DK, DELTA_C, 4> load_k(a.ldk, lane, a.dk), load_q(a.ldq, lane, a.dk);
+    load_k.fetch(smem, (const E*)a.k + kv * a.dk, c.first, c.first + c.count, wave);
+    load_q.fetch(smem + TILE, (const E*)a.q + kv * a.dk, c.first, c.first + c.count, wave);
+  }
+  tile_wait();
+  __syncthreads();
+  const TileOps<E, DK> at(smem, lane);
+  // This wave's rows (kk, and qk of P^T backward: rows j) or columns (qk of P: rows of P^T are keys) against all tiles of the other side.
+  f32x4 kk[4], qk[4];
+#pragma unroll
+  for (int n = 0; n < 4; ++n) kk[n] = qk[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    const Opnd<E, 1> mine = at.row(0, wave, s), q_mine = at.row(TILE, wave, s);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const Opnd<E, 1> k_n = at.row(0, n, s);
+      if (n <= wave) kk[n] = mma(mine, k_n, kk[n]);                                     // rows i of this wave, columns j of tile n
+      if constexpr (BWD) {
+        if (n >= wave) qk[n] = mma(at.row(TILE, n, s), mine, qk[n]);                    // rows i of tile n, columns j of this wave
+      } else if (n <= wave) qk[n] = mma(k_n, q_mine, qk[n]);                            // rows j of tile n, columns i of this wave
+    }
+  }
+  for (int hg = 0; hg < group; ++hg) {
+    const int h = kv * group + hg;
+    char* rec = a.records + ((int64_t)blockIdx.x * a.nv + h) * (BWD ? REC_BWD : REC_FWD);
+    __syncthreads();   // the head before is done with the LDS
+    if (wave == 0) {
+      const bool in = lane < c.count;
+      const int64_t t = (int64_t)(c.first + (in ? lane : 0)) * a.nv + h;
+      const float gl = in ? a.g[t] * 1.4426950408889634f : 0.f;
+      const double sum = running_sum((double)(gl < DELTA_FORGETS ? DELTA_FORGETS : gl), lane), last = __shfl(sum, 63, 64);
+      const float beta = in ? a.beta[t] : 0.f;
+      G[lane] = sum;
+      B[lane] = beta;
+      float* gates = reinterpret_cast<float*>(rec);
+      gates[lane] = in ? decay(sum, 0.0) : 0.f;
+      gates[64 + lane] = in ? decay(last, sum) : 0.f;
+      gates[128 + lane] = beta;
+      gates[192 + lane] = lane == 0 ? decay(last, 0.0) : 0.f;
+    }
+    __syncthreads();
+    {   // A
+      double gi[4];
+      float bi[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        gi[r] = G[16 * wave + 4 * g + r];
+        bi[r] = B[16 * wave + 4 * g + r];
+      }
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const double gj = G[16 * n + i16];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int i = 16 * wave + 4 * g + r, j = 16 * n + i16;
+          if (n <= wave) A[i * TRI_LD + j] = j < i ? bi[r] * decay(gi[r], gj) * kk[n][r] : 0.f;
+          if (n > wave) Tm[i * TRI_LD + j] = 0.f;
+        }
+      }
+    }
+    // P: tiles as they lie, two of them an operand
+    f32x4 p[4];
+    const double gc = G[16 * wave + i16];
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = 16 * n + 4 * g + r, col = 16 * wave + i16;
+        const double gr = G[row];
+        if constexpr (BWD) p[n][r] = row >= col ? qk[n][r] * decay(gr, gc) : 0.f;   // P_row,col
+        else p[n][r] = row <= col ? qk[n][r] * decay(gc, gr) : 0.f;                 // P_col,row
+      }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if constexpr (BWD) {
+        if (2 * s + 1 >= wave) store_op<E>(rec + REC_P + upper_op(wave, s) * REC_OP, pair_of<E>(p[2 * s], p[2 * s + 1]), lane);
+      } else if (2 * s <= wave) store_op<E>(rec + REC_P + lower_op(wave, s) * REC_OP, pair_of<E>(p[2 * s], p[2 * s + 1]), lane);
+    }
+    __syncthreads();
+    invert_lower(A, Tm, wave, lane);
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      if (2 * s <= wave) {
+        const float* row = Tm + (16 * wave + i16) * TRI_LD + 32 * s + 4 * g;
+        store_op<E>(rec + REC_T + lower_op(wave, s) * REC_OP, pair_of<E>(*reinterpret_cast<const f32x4*>(row), *reinterpret_cast<const f32x4*>(row + 16)), lane);
+      }
+      if constexpr (BWD)
+        if (2 * s + 1 >= wave) {
+          f32x4 x, y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[e] = Tm[(32 * s + 4 * g + e) * TRI_LD + 16 * wave + i16];
+            y[e] = Tm[(32 * s + 16 + 4 * g + e) * TRI_LD + 16 * wave + i16];
+          }
+          store_op<E>(rec + REC_TT + upper_op(wave, s) * REC_OP, pair_of<E>(x, y), lane);
+        }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------ from chunk to chunk
+// A workgroup of NW waves walks a document's chunks for one value head and 16 NW columns of its state; a wave has 16 columns of all rows in its registers,
+// and they never leave it: a result's registers, two above one another, are the next product's operand.  Keys, queries and the chunk's
+// matrices come straight into LDS, a chunk ahead.
+enum DeltaWalk { WALK_RESULTS = 0, WALK_STATES = 1, WALK_GRADIENTS = 2 };   // o and the last state; the states and u for the gradients; the states' gradients and y
+
+template <typename E, int DK, int NW, int KIND> struct WalkLds {
+  typedef Tile<E, DK> TL;
+  typedef Tile<E, 64> VL;
+  static constexpr int K = 0, V = TL::bytes(DELTA_C), Q = V + VL::bytes(DELTA_C), R = Q + (KIND == WALK_STATES ? 0 : TL::bytes(DELTA_C));
+  static constexpr int REC = KIND == WALK_RESULTS ? REC_FWD : KIND == WALK_STATES ? REC_P : REC_GATES + 2 * REC_TRIANGLE;
+  static constexpr int BUF = R + REC;
+  static constexpr int NBUF = 2 * BUF <= 160 * 1024 ? 2 : 1;
+};
+
+template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void delta_walk(char* smem_raw, const DeltaRule& a, int doc_rank, int h, int c0) {
+  typedef WalkLds<E, DK, NW, KIND> L;
+  constexpr int RT = DK / 16, KS = DK / 32;
+  constexpr bool HALF_E = __is_same(E, f16), BACK = KIND == WALK_GRADIENTS;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i16 = lane & 15;
+  const int4 row = reinterpret_cast<const int4*>(a.chunks)[1 + doc_rank];   // first token, tokens, first chunk, document
+  const int first = row.x, count = row.y, chunk0 = row.z, doc = row.w, chunks = (count + DELTA_C - 1) / DELTA_C;
+  const int kv = h / (a.nv / a.nk), col = c0 + 16 * wave + i16;   // column of the lane
+  const bool live = col < a.dv;
+  const E *kh = (const E*)a.k + kv * a.dk, *qh = (const E*)a.q + kv * a.dk;
+  const E* vh = BACK ? (const E*)a.dout + h * a.dv + c0 : (const E*)a.v + h * a.dv + c0;
+  const unsigned smem = lds_address(smem_raw);
+  const TileLoad<E, DK, DELTA_C, NW> load_k(a.ldk, lane, a.dk), load_q(a.ldq, lane, a.dk);
+  const TileLoad<E, 64, DELTA_C, NW> load_v(BACK ? a.ldo : a.ldv, lane, min(a.dv - c0, 16 * NW));
+  const TileOps<E, DK> at(smem, lane);
+  const TileOps<E, 64> at_v(smem, lane);
+  const int64_t states = (int64_t)a.dk * a.dv;
+  auto fetch = [&](int c, unsigned to) {
+    const int t0 = first + DELTA_C * c, end = min(first + count, t0 + DELTA_C);
+    load_k.fetch(to + L::K, kh, t0, end, wave);
+    load_v.fetch(to + L::V, vh, t0, end, wave);
+    if constexpr (KIND != WALK_STATES) load_q.fetch(to + L::Q, qh, t0, end, wave);
+    const char* rec = a.records + ((int64_t)(chunk0 + c) * a.nv + h) * (KIND == WALK_RESULTS ? REC_FWD : REC_BWD);
+    if constexpr (BACK) {   // P^T and T^T lie side by side
+      fetch_bytes<NW>(to + L::R, rec, REC_GATES, wave, lane);
+      fetch_bytes<NW>(to + L::R + REC_GATES, rec + REC_P, 2 * REC_TRIANGLE, wave, lane);
+    } else fetch_bytes<NW>(to + L::R, rec, L::REC, wave, lane);
+  };
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  f32x4 S[RT];
+  const float* from = BACK ? a.dht : a.h0;
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    S[i] = zero;
+    if (from)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (live && 16 * i + 4 * g + r < a.dk) S[i][r] = from[((int64_t)doc * a.nv + h) * states + (int64_t)(16 * i + 4 * g + r) * a.dv + col];
+  }
+  const int step = BACK ? -1 : 1;
+  int c = BACK ? chunks - 1 : 0;
+  if (chunks > 0 && L::NBUF == 2) {
+    fetch(c, smem);
+    tile_wait();
+    __syncthreads();
+  }
+  for (int n = 0; n < chunks; ++n, c += step) {
+    const unsigned buf = L::NBUF == 2 ? (unsigned)(n & 1) * L::BUF : 0u;
+    if constexpr (L::NBUF == 2) {
+      if (n + 1 < chunks) fetch(c + step, smem + (L::BUF - buf));   // last read before the barrier that ended the step before
+    } else {
+      fetch(c, smem);
+      tile_wait();
+      __syncthreads();
+    }
+    const unsigned gates = smem + buf + L::R;
+    const int64_t rec = (int64_t)(chunk0 + c) * a.nv + h;
+    if constexpr (KIND != WALK_RESULTS) {   // the state before the chunk, or the gradient of the one behind it
+      float* to = (BACK ? a.dstates : a.states) + rec * DK * a.dvp + col;
+      if (col < a.dvp)
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) to[(16 * i + 4 * g + r) * a.dvp] = S[i][r];
+    }
+    Pair<E> sp[KS];
+    const float s_unit = column_unit<E>(S), s_inv = inverse_unit<E>(s_unit);
+    pairs_of<E>(sp, S, s_unit);
+    f32x4 x[4];   // K S
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      x[m] = zero;
+#pragma unroll
+      for (int s = 0; s < KS; ++s) x[m] = mma(at.row(buf + L::K, m, s), sp[s], x[m]);
+    }
+    f32x4 o[4];   // (Q S)^T: rows are columns of the state, a lane has the token lane % 16
+    if constexpr (KIND == WALK_RESULTS) {
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        o[m] = zero;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) o[m] = mma(sp[s], at.row(buf + L::Q, m, s), o[m]);
+      }
+    }
+    Opnd<E, 1> vf[2];   // columns of v, or dO
+    vf[0] = at_v.column(buf + L::V, wave, 0);
+    vf[1] = at_v.column(buf + L::V, wave, 1);
+    f32x4 u[4], next[4];
+    Pair<E> up[2];
+    if constexpr (!BACK) {
+      f32x4 z[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const f32x4 since = lds_read<f32x4>(gates + 4 * (16 * m + 4 * g)), beta = lds_read<f32x4>(gates + 512 + 4 * (16 * m + 4 * g));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z[m][r] = beta[r] * ((float)vf[m >> 1].t[0][4 * (m & 1) + r] - since[r] * (x[m][r] * s_inv));
+      }
+      Pair<E> zp[2];
+      const float unit = column_unit<E>(z), inv = inverse_unit<E>(unit);
+      pairs_of<E>(zp, z, unit);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        u[m] = zero;
+#pragma unroll
+        for (int s = 0; s <= m / 2; ++s) u[m] = mma(load_op<E>(gates + REC_T + lower_op(m, s) * REC_OP, lane), zp[s], u[m]);
+        if constexpr (HALF_E) u[m] *= inv;
+      }
+      if constexpr (KIND == WALK_RESULTS) {
+        const float u_unit = column_unit<E>(u), u_inv = inverse_unit<E>(u_unit);
+        pairs_of<E>(up, u, u_unit);
+        E* oh = (E*)a.o + h * a.dv + c0 + 16 * wave;
+        f32x4 back_s = {s_inv, s_inv, s_inv, s_inv}, back_u = {u_inv, u_inv, u_inv, u_inv};   // of the rows' columns
+        if constexpr (HALF_E) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            back_s[r] = __shfl(s_inv, 4 * g + r, 64);
+            back_u[r] = __shfl(u_inv, 4 * g + r, 64);
+          }
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const float since = lds_read<float>(gates + 4 * (16 * m + i16));
+          f32x4 pu = zero;
+          if constexpr (HALF_E) o[m] *= back_s * since;
+          else pu = o[m] * since;
+#pragma unroll
+          for (int s = 0; s <= m / 2; ++s) pu = mma(up[s], load_op<E>(gates + REC_P + lower_op(m, s) * REC_OP, lane), pu);
+          if constexpr (HALF_E) pu = pu * back_u + o[m];
+          const int t = DELTA_C * c + 16 * m + i16;
+          if (t < count && c0 + 16 * wave + 4 * g < a.dv) {
+            typedef E quad_t __attribute__((ext_vector_type(4)));
+            quad_t w;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) w[r] = from_f<E>(fp32_value(pu[r] * a.scale));
+            *reinterpret_cast<quad_t*>(oh + (first + t) * a.ldo + 4 * g) = w;
+          }
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < 4; ++m) next[m] = u[m] * lds_read<f32x4>(gates + 256 + 4 * (16 * m + 4 * g));
+    } else {
+      f32x4 du[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        f32x4 pd = zero;
+#pragma unroll
+        for (int s = m / 2; s < 2; ++s) pd = mma(load_op<E>(gates + REC_GATES + upper_op(m, s) * REC_OP, lane), vf[s], pd);
+        const f32x4 until = lds_read<f32x4>(gates + 256 + 4 * (16 * m + 4 * g));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) du[m][r] = a.scale * pd[r] + until[r] * (x[m][r] * s_inv);
+      }
+      Pair<E> dp[2];
+      const float unit = column_unit<E>(du), inv = inverse_unit<E>(unit);
+      pairs_of<E>(dp, du, unit);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        u[m] = zero;   // y
+#pragma unroll
+        for (int s = m / 2; s < 2; ++s) u[m] = mma(load_op<E>(gates + REC_GATES + REC_TRIANGLE + upper_op(m, s) * REC_OP, lane), dp[s], u[m]);
+        if constexpr (HALF_E) u[m] *= inv;
+        const f32x4 since = lds_read<f32x4>(gates + 4 * (16 * m + 4 * g)), beta = lds_read<f32x4>(gates + 512 + 4 * (16 * m + 4 * g));
+        next[m] = u[m] * since * beta * -1.f;
+      }
+    }
+    if constexpr (KIND != WALK_RESULTS) {
+      float* to = (BACK ? a.y : a.u) + rec * DELTA_C * a.dvp + col;
+      if (col < a.dvp)
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) to[(16 * m + 4 * g + r) * a.dvp] = u[m][r];
+    }
+    const float whole = lds_read<float>(gates + 768);
+    Pair<E> np[2], qp[2];
+    const float n_unit = column_unit<E>(next), n_inv = inverse_unit<E>(n_unit);
+    pairs_of<E>(np, next, n_unit);
+    float q_inv = 1.f;
+    if constexpr (BACK) {   // scale exp(G) dO
+      f32x4 d[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const f32x4 since = lds_read<f32x4>(gates + 4 * (16 * m + 4 * g));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) d[m][r] = a.scale * since[r] * (float)vf[m >> 1].t[0][4 * (m & 1) + r];
+      }
+      const float q_unit = column_unit<E>(d);
+      q_inv = inverse_unit<E>(q_unit);
+      pairs_of<E>(qp, d, q_unit);
+    }
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      f32x4 acc = S[i] * whole;
+      if constexpr (HALF_E) {
+        f32x4 p = zero;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) p = mma(at.column(buf + L::K, i, s), np[s], p);
+        acc += p * n_inv;
+        if constexpr (BACK) {
+          p = zero;
+#pragma unroll
+          for (int s = 0; s < 2; ++s) p = mma(at.column(buf + L::Q, i, s), qp[s], p);
+          acc += p * q_inv;
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) acc = mma(at.column(buf + L::K, i, s), np[s], acc);
+        if constexpr (BACK)
+#pragma unroll
+          for (int s = 0; s < 2; ++s) acc = mma(at.column(buf + L::Q, i, s), qp[s], acc);
+      }
+      S[i] = acc;
+    }
+    tile_wait();
+    __syncthreads();
+  }
+  float* last = KIND == WALK_RESULTS ? a.ht : BACK ? a.dh0 : nullptr;
+  if (last && live)
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (16 * i + 4 * g + r < a.dk) last[((int64_t)doc * a.nv + h) * states + (int64_t)(16 * i + 4 * g + r) * a.dv + col] = S[i][r];
+}
+
+// Block of the grid -> document and head, and columns: the blocks that share keys and matrices lie eight apart, on one XCD.
+struct WalkBlock { int doc, h, c0; bool in; };
+__device__ __forceinline__ WalkBlock walk_block(const DeltaRule& a, int block, int slices, int width) {
+  const int j = block / 8, pair = j / slices * 8 + block % 8;
+  return WalkBlock{pair / a.nv, pair % a.nv, j % slices * width, pair < a.ndocs * a.nv};
+}
+template <typename E, int DK, int NW> __global__ __launch_bounds__(64 * NW, 1) void delta_walk_kernel(DeltaRule a, int slices) {
+  typedef WalkLds<E, DK, NW, WALK_RESULTS> L;
+  __shared__ __align__(16) char smem[L::NBUF * L::BUF];
+  const WalkBlock b = walk_block(a, blockIdx.x, slices, 16 * NW);
+  if (b.in) delta_walk<E, DK, NW, WALK_RESULTS>(smem, a, b.doc, b.h, b.c0);
+}
+// Both walks of the backward: they need nothing of one another.
+template <typename E, int DK, int NW> __global__ __launch_bounds__(64 * NW, 1) void delta_walks_kernel(DeltaRule a, int slices, int blocks) {
+  typedef WalkLds<E, DK, NW, WALK_STATES> L;
+  typedef WalkLds<E, DK, NW, WALK_GRADIENTS> LG;
+  __shared__ __align__(16) char smem[L::NBUF * L::BUF > LG::NBUF * LG::BUF ? L::NBUF * L::BUF : LG::NBUF * LG::BUF];
+  const bool back = (int)blockIdx.x < blocks;
+  const WalkBlock b = walk_block(a, back ? (int)blockIdx.x : (int)blockIdx.x - blocks, slices, 16 * NW);
+  if (!b.in) return;
+  if (back) delta_walk<E, DK, NW, WALK_GRADIENTS>(smem, a, b.doc, b.h, b.c0);
+  else delta_walk<E, DK, NW, WALK_STATES>(smem, a, b.doc, b.h, b.c0);
+}
+
+// ------------------------------------------------------------------------------------------ gradients of a chunk
+// What the products take their operands in: half as bf16 pairs, whose exponent holds whatever a gradient may be (a half is exactly such a pair).
+template <typename E> struct GradOf { typedef bf16 type; };
+template <> struct GradOf<float> { typedef float type; };
+template <typename E> constexpr int GRAD_IN = __is_same(E, f16) ? 2 : 1;
+template <typename E> __device__ __forceinline__ Opnd<typename GradOf<E>::type, GRAD_IN<E>> grad_in(const Opnd<E, 1>& x) {
+  if constexpr (__is_same(E, f16)) {
+    Opnd<bf16, 2> o;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float v = (float)x.t[0][e];
+      o.t[0][e] = (bf16)v;
+      o.t[1][e] = (bf16)(v - (float)o.t[0][e]);
+    }
+    return o;
+  } else return x;
+}
+
+// A workgroup of four waves per chunk and key head; the value heads of the key head one after the other, their dq and dk in the same registers.  A wave has a
+// quarter of the head's columns of dq and dk, for all tokens: results are transposed (rows are columns of the head, a lane has a token), so that a
+// state's rows are read by one wave only and a token's factors are a lane's own.  Columns of the value head come in blocks of 64.
+template <typename E, int DK> __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaRule a) {
+  typedef typename GradOf<E>::type M;
+  typedef Opnd<M, GRAD_IN<E>> In;
+  typedef Tile<E, DK> TL;
+  typedef Tile<E, 64> VL;
+  constexpr int TILE = TL::bytes(DELTA_C), KS = DK / 32, CT = DK / 64, OPS = 8 * REC_OP;   // OPS: 64 tokens by 64 columns as operands
+  constexpr int STAGE = VL::bytes(DELTA_C) + 2 * OPS, MATS = 2 * 64 * TRI_LD * 4;
+  __shared__ __align__(16) char smem_raw[2 * TILE + (STAGE > MATS ? STAGE : MATS)];
+  __shared__ double G[64];
+  __shared__ float gate[4][64], dots[4][3][64], cols[4][64], rows[3][64], whole_dots[4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i16 = lane & 15;
+  const ChunkRow c = chunk_row(a, blockIdx.x);
+  if (c.count <= 0) return;
+  const int kv = blockIdx.y, group = a.nv / a.nk, end = c.first + c.count;
+  const unsigned smem = lds_address(smem_raw), stage = 2 * TILE;
+  {
+    const TileLoad<E, DK, DELTA_C, 4> load_k(a.ldk, lane, a.dk), load_q(a.ldq, lane, a.dk);
+    load_k.fetch(smem, (const E*)a.k + kv * a.dk, c.first, end, wave);
+    load_q.fetch(smem + TILE, (const E*)a.q + kv * a.dk, c.first, end, wave);
+  }
+  const TileOps<E, DK> at(smem, lane);
+  const TileOps<E, 64> at_do(smem + stage, lane);
+  const unsigned n_ops = smem + stage + VL::bytes(DELTA_C), y_ops = n_ops + OPS;
+  float *Mm = reinterpret_cast<float*>(smem_raw + stage), *H = Mm + 64 * TRI_LD;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  f32x4 kk[4], qk[4], dq[CT][4], dk[CT][4];
+#pragma unroll
+  for (int n = 0; n < 4; ++n) {
+    kk[n] = qk[n] = zero;
+#pragma unroll
+    for (int t = 0; t < CT; ++t) dq[t][n] = dk[t][n] = zero;
+  }
+  tile_wait();
+  __syncthreads();
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    const Opnd<E, 1> k_i = at.row(0, wave, s), q_i = at.row(TILE, wave, s);
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+      if (n <= wave) {
+        const Opnd<E, 1> k_j = at.row(0, n, s);
+        kk[n] = mma(k_i, k_j, kk[n]);
+        qk[n] = mma(q_i, k_j, qk[n]);
+      }
+  }
+  for (int hg = 0; hg < group; ++hg) {
+    const int h = kv * group + hg;
+    const int64_t rec = (int64_t)blockIdx.x * a.nv + h;
+    const float *S = a.states + rec * DK * a.dvp, *dS = a.dstates + rec * DK * a.dvp, *U = a.u + rec * DELTA_C * a.dvp, *Y = a.y + rec * DELTA_C * a.dvp;
+    __syncthreads();   // the head before is done with the LDS
+    if (wave == 0) {
+      const bool in = lane < c.count;
+      const int64_t t = (int64_t)(c.first + (in ? lane : 0)) * a.nv + h;
+      const float gl = in ? a.g[t] * 1.4426950408889634f : 0.f;
+      const double sum = running_sum((double)(gl < DELTA_FORGETS ? DELTA_FORGETS : gl), lane), last = __shfl(sum, 63, 64);
+      G[lane] = sum;
+      gate[0][lane] = in ? decay(sum, 0.0) : 0.f;
+      gate[1][lane] = in ? decay(last, sum) : 0.f;
+      gate[2][lane] = in ? a.beta[t] : 0.f;
+      gate[3][lane] = decay(last, 0.0);
+    }
+    f32x4 qi[CT][4], ks[CT][4], kn[CT][4], dp[4], da[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      dp[n] = da[n] = zero;
+#pragma unroll
+      for (int t = 0; t < CT; ++t) qi[t][n] = ks[t][n] = kn[t][n] = zero;
+    }
+    float sds = 0.f, yv = 0.f;
+    const int my_t = 16 * wave + i16;   // the token whose rows of U and Y this lane brings
+    const bool my_in = my_t < c.count;
+    for (int b0 = 0; b0 < a.dv; b0 += 64) {
+      __syncthreads();   // the block before has been read; the gates are there
+      {
+        const TileLoad<E, 64, DELTA_C, 4> load(a.ldo, lane, min(a.dv - b0, 64));
+        load.fetch(smem + stage, (const E*)a.dout + h * a.dv + b0, c.first, end, wave);
+      }
+      const float beta = gate[2][my_t];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        f32x4 u[2], y[2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const int col = b0 + 32 * s + 16 * p + 4 * g;
+          u[p] = y[p] = zero;
+          if (col < a.dvp) {
+            u[p] = *reinterpret_cast<const f32x4*>(U + my_t * a.dvp + col);
+            y[p] = *reinterpret_cast<const f32x4*>(Y + my_t * a.dvp + col);
+          }
+          if (my_in && col < a.dv) {
+            typedef E quad_t __attribute__((ext_vector_type(4)));
+            const int64_t t = c.first + my_t;
+            const quad_t v = *reinterpret_cast<const quad_t*>((const E*)a.v + t * a.ldv + h * a.dv + col);
+            quad_t w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              yv = fmaf(y[p][e], (float)v[e], yv);
+              w[e] = from_f<E>(fp32_value(beta * y[p][e]));
+            }
+            *reinterpret_cast<quad_t*>((E*)a.dval + t * a.lddv + h * a.dv + col) = w;
+          }
+        }
+        store_op<M>(smem_raw + (n_ops - smem) + (2 * wave + s) * REC_OP, pair_of<M>(u[0], u[1]), lane);
+        store_op<M>(smem_raw + (y_ops - smem) + (2 * wave + s) * REC_OP, pair_of<M>(y[0], y[1]), lane);
+      }
+      tile_wait();
+      __syncthreads();
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        Pair<M> sp[CT], dsp[CT];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          f32x4 x[2], y[2];
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            const int col = b0 + 32 * s + 16 * p + 4 * g, at_row = (16 * (CT * wave + t) + i16) * a.dvp + col;
+            x[p] = y[p] = zero;
+            if (col < a.dvp) {
+              x[p] = *reinterpret_cast<const f32x4*>(S + at_row);
+              y[p] = *reinterpret_cast<const f32x4*>(dS + at_row);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sds = fmaf(x[p][e], y[p][e], sds);
+          }
+          sp[t] = pair_of<M>(x[0], x[1]);
+          dsp[t] = pair_of<M>(y[0], y[1]);
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const In d = grad_in<E>(at_do.row(0, m, s));
+          const Pair<M> u = load_op<M>(n_ops + (2 * m + s) * REC_OP, lane), y = load_op<M>(y_ops + (2 * m + s) * REC_OP, lane);
+#pragma unroll
+          for (int t = 0; t < CT; ++t) {
+            qi[t][m] = mma(sp[t], d, qi[t][m]);
+            ks[t][m] = mma(sp[t], y, ks[t][m]);
+            kn[t][m] = mma(dsp[t], u, kn[t][m]);
+          }
+        }
+        const In d_i = grad_in<E>(at_do.row(0, wave, s));
+        const Pair<M> y_i = load_op<M>(y_ops + (2 * wave + s) * REC_OP, lane);
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+          if (n <= wave) {
+            const Pair<M> u_j = load_op<M>(n_ops + (2 * n + s) * REC_OP, lane);
+            dp[n] = mma(d_i, u_j, dp[n]);
+            da[n] = mma(y_i, u_j, da[n]);
+          }
+      }
+    }
+    __syncthreads();   // Mm and H lie over the blocks
+    // the states' shares, and their products with q and k
+    {
+      float dot[4][3];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const float since = gate[0][16 * m + i16], until = gate[1][16 * m + i16], beta = gate[2][16 * m + i16];
+        dot[m][0] = dot[m][1] = dot[m][2] = 0.f;
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          const f32x4 k4 = at.quad(0, m, CT * wave + t), q4 = at.quad(TILE, m, CT * wave + t);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float q_state = a.scale * since * qi[t][m][r], k_state = -since * ks[t][m][r], k_next = until * kn[t][m][r];
+            dot[m][0] = fmaf(q4[r], q_state, dot[m][0]);
+            dot[m][1] = fmaf(k4[r], k_state, dot[m][1]);
+            dot[m][2] = fmaf(k4[r], k_next, dot[m][2]);
+            dq[t][m][r] += q_state;
+            dk[t][m][r] += fmaf(beta, k_state, k_next);
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < 3; ++x) {
+          dot[m][x] += __shfl_xor(dot[m][x], 16, 64);
+          dot[m][x] += __shfl_xor(dot[m][x], 32, 64);
+          if (lane < 16) dots[wave][x][16 * m + lane] = dot[m][x];
+        }
+      }
+      sds = wave_sum(sds);
+      yv += __shfl_xor(yv, 16, 64);
+      yv += __shfl_xor(yv, 32, 64);
+      if (lane == 0) whole_dots[wave] = sds;
+      if (lane < 16) rows[2][16 * wave + lane] = yv;
+    }
+    // M and H, and the sums by rows and by columns that the decays and beta get
+    {
+      float by_row[4] = {0.f, 0.f, 0.f, 0.f}, by_beta[4] = {0.f, 0.f, 0.f, 0.f};
+      double gi[4];
+      float bi[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        gi[r] = G[16 * wave + 4 * g + r];
+        bi[r] = gate[2][16 * wave + 4 * g + r];
+      }
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const int j = 16 * n + i16;
+        const double gj = G[j];
+        float by_col = 0.f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int i = 16 * wave + 4 * g + r;
+          const float dec = j <= i && n <= wave ? decay(gi[r], gj) : 0.f;
+          const float m = a.scale * dec * dp[n][r], hb = j < i ? -dec * da[n][r] : 0.f;
+          Mm[i * TRI_LD + j] = m;
+          H[i * TRI_LD + j] = bi[r] * hb;
+          const float e = fmaf(m, qk[n][r], bi[r] * hb * kk[n][r]);
+          by_row[r] += e;
+          by_beta[r] = fmaf(hb, kk[n][r], by_beta[r]);
+          by_col += e;
+        }
+        by_col += __shfl_xor(by_col, 16, 64);
+        by_col += __shfl_xor(by_col, 32, 64);
+        if (lane < 16) cols[wave][j] = by_col;
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+#pragma unroll
+        for (int o = 1; o < 16; o <<= 1) {
+          by_row[r] += __shfl_xor(by_row[r], o, 64);
+          by_beta[r] += __shfl_xor(by_beta[r], o, 64);
+        }
+        if (i16 == 0) {
+          rows[0][16 * wave + 4 * g + r] = by_row[r];
+          rows[1][16 * wave + 4 * g + r] = by_beta[r];
+        }
+      }
+    }
+    __syncthreads();
+    if (wave == 0) {
+      double d = rows[0][lane], kn_sum = 0.0, sds_sum = 0.0;
+      float kst = 0.f, knx = 0.f, qst = 0.f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        d -= cols[w][lane];
+        qst += dots[w][0][lane];
+        kst += dots[w][1][lane];
+        knx += dots[w][2][lane];
+        sds_sum += whole_dots[w];
+      }
+      kn_sum = knx;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) kn_sum += __shfl_xor(kn_sum, o, 64);
+      d += (double)qst + (double)gate[2][lane] * kst - knx;
+      if (lane == 63) d += kn_sum + (double)gate[3][lane] * sds_sum;
+      // from each token to the end
+      const double upto = running_sum(d, lane), all = __shfl(upto, 63, 64);
+      if (lane < c.count) {
+        const int64_t t = (int64_t)(c.first + lane) * a.nv + h;
+        a.dg[t] = (float)(all - upto + d);
+        a.dbeta[t] = rows[2][lane] + kst + rows[1][lane];
+      }
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int from = 32 * s + 4 * g, mine = 16 * m + i16;
+        f32x4 across[2], down[2], h_across[2], h_down[2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          across[p] = *reinterpret_cast<const f32x4*>(Mm + mine * TRI_LD + from + 16 * p);
+          h_across[p] = *reinterpret_cast<const f32x4*>(H + mine * TRI_LD + from + 16 * p);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            down[p][e] = Mm[(from + 16 * p + e) * TRI_LD + mine];
+            h_down[p][e] = H[(from + 16 * p + e) * TRI_LD + mine];
+          }
+        }
+        const Pair<M> both = pair_of<M>(h_across[0] + h_down[0], h_across[1] + h_down[1]), m_across = pair_of<M>(across[0], across[1]),
+                      m_down = pair_of<M>(down[0], down[1]);
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+          const In k_col = grad_in<E>(at.column(0, CT * wave + t, s));
+          dk[t][m] = mma(k_col, both, dk[t][m]);
+          if (2 * s <= m) dq[t][m] = mma(k_col, m_across, dq[t][m]);
+          if (2 * s + 1 >= m) dk[t][m] = mma(grad_in<E>(at.column(TILE, CT * wave + t, s)), m_down, dk[t][m]);
+        }
+      }
+  }
+  typedef E quad_t __attribute__((ext_vector_type(4)));
+#pragma unroll
+  for (int t = 0; t < CT; ++t)
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const int col = 16 * (CT * wave + t) + 4 * g, tok = 16 * m + i16;
+      if (tok < c.count && col < a.dk) {
+        quad_t x, y;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          x[r] = from_f<E>(fp32_value(dq[t][m][r]));
+          y[r] = from_f<E>(fp32_value(dk[t][m][r]));
+        }
+        *reinterpret_cast<quad_t*>((E*)a.dq + (int64_t)(c.first + tok) * a.lddq + kv * a.dk + col) = x;
+        *reinterpret_cast<quad_t*>((E*)a.dkey + (int64_t)(c.first + tok) * a.lddk + kv * a.dk + col) = y;
+      }
+    }
+}
+
+// ------------------------------------------------------------------------------------------ launches
+template <typename E, int DK, int NW> hipError_t delta_walks(hipStream_t st, const DeltaRule& a, bool backward) {
+  const int slices = (int)cdiv(a.dv, 16 * NW);
+  const int blocks = (int)(cdiv((int64_t)a.ndocs * a.nv, 8) * 8 * slices);
+  if (backward) hipLaunchKernelGGL((delta_walks_kernel<E, DK, NW>), dim3((unsigned)(2 * blocks)), dim3(64 * NW), 0, st, a, slices, blocks);
+  else hipLaunchKernelGGL((delta_walk_kernel<E, DK, NW>), dim3((unsigned)blocks), dim3(64 * NW), 0, st, a, slices);
+  return hipGetLastError();
+}
+template <typename E, int DK> hipError_t delta_run(hipStream_t st, const DeltaRule& a, bool backward) {
+  const dim3 prep((unsigned)(a.nchunks + DELTA_FILL), (unsigned)a.nk);
+  if (backward) hipLaunchKernelGGL((delta_prep_kernel<E, DK, true>), prep, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((delta_prep_kernel<E, DK, false>), prep, dim3(256), 0, st, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.ndocs == 0) return e;
+  // Workgroups of four waves share what they bring into LDS; fewer waves where that would leave CUs without one.
+  const int64_t waves = (int64_t)a.ndocs * a.nv * cdiv(a.dv, 16) * (backward ? 2 : 1);
+  e = waves >= 1024 ? delta_walks<E, DK, 4>(st, a, backward) : waves >= 512 ? delta_walks<E, DK, 2>(st, a, backward) : delta_walks<E, DK, 1>(st, a, backward);
+  if (e != hipSuccess || !backward || a.nchunks == 0) return e;
+  hipLaunchKernelGGL((delta_grad_kernel<E, DK>), dim3((unsigned)a.nchunks, (unsigned)a.nk), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+template <typename E> hipError_t delta_rule_of(hipStream_t st, const DeltaRule& a, bool backward) {
+  return a.dk <= 64 ? delta_run<E, 64>(st, a, backward) : delta_run<E, 128>(st, a, backward);
+}
+
+}  // namespace
+}  // namespace zs

@@ -247,6 +247,35 @@ struct RopeHeads { const void* in; void* out; int64_t ld_in, ld_out; int n; };
 hipError_t rope_axes(hipStream_t st, DType dt, int T, int d, const RopeHeads& q, const RopeHeads& k, const int32_t* positions, int naxes,
                      const int32_t* sections, int own_spectrum, double base, int sign);
 
+// The gated delta rule inside packed documents (delta_rule_impl.h has the formulas): rows of nk heads of q and k, dk wide, and of nv heads of v and o,
+// dv wide; value head h reads key head h / (nv / nk).  g, beta: float[T, nv].  chunks: the table that delta_chunks writes.  States are
+// float[ndocs, nv, dk, dv].
+constexpr int DELTA_CHUNK = 64;   // tokens of a document that are worked on together
+constexpr int DELTA_FILL = 16;    // blocks that clear the rows of no document
+constexpr int DELTA_RECORD_FWD = 25600, DELTA_RECORD_BWD = 37888;   // bytes of a chunk's own matrices
+struct DeltaRule {
+  int T, nk, nv, dk, dv, ndocs;
+  const void *q, *k, *v; int64_t ldq, ldk, ldv;
+  const float *g, *beta; const int32_t* chunks;
+  float scale;
+  const float* h0; void* o; int64_t ldo; float* ht;                  // h0, ht may be NULL
+  const void* dout; const float* dht;                                // backward: dout with the stride ldo
+  void *dq, *dkey, *dval; int64_t lddq, lddk, lddv; float *dg, *dbeta, *dh0;
+  char* records; float *states, *dstates, *u, *y; int nchunks, dvp;  // set by delta_rule, in scratch
+};
+int64_t delta_chunk_rows(int T, int ndocs);   // chunks that the table has room for
+hipError_t delta_chunks(hipStream_t st, int T, int ndocs, const int32_t* offsets, int32_t* table);
+int64_t delta_scratch(bool backward, int T, int ndocs, int nv, int dk, int dv);
+hipError_t delta_rule(hipStream_t st, DType dt, const DeltaRule& a, bool backward, void* scratch);
+// One token each of n states of nstates, float[nstates, nv, dk, dv], which are updated in place.  slots: int32[n] or NULL, token i has state i.
+struct DeltaStep {
+  int n, nk, nv, dk, dv, nstates;
+  const void *q, *k, *v; int64_t ldq, ldk, ldv;
+  const float *g, *beta; const int32_t* slots;
+  float scale; float* state; void* o; int64_t ldo;
+};
+hipError_t delta_step(hipStream_t st, DType dt, const DeltaStep& a);
+
 // x[t,:] = E[ids[t],:] (rows of ids outside [0,V) give zeros).  keep (or NULL) receives the ids.
 hipError_t embed_fwd(hipStream_t st, DType dt, int T, int H, int V, const int32_t* ids, const void* E, void* x, int32_t* keep = nullptr);
 // dE[id,:] += sum over the tokens with that id, added in increasing token order.

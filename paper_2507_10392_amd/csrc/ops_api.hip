@@ -332,6 +332,89 @@ int stage_op_attention_docs_bwd(void* stream, int32_t dtype, int32_t T, int32_t 
   return rc(attn_docs_bwd((hipStream_t)stream, (DType)dtype, a, scratch));
 }
 
+}  // extern "C"
+namespace {
+constexpr int DELTA_MAX_TOKENS = 1 << 26, DELTA_MAX_HEADS = 4096, DELTA_MAX_DOCS = 1 << 20;   // documents, and documents times value heads: threads of a launch
+bool aligned16(const void* p) { return !((uintptr_t)p & 15); }   // or nothing
+bool delta_heads_ok(int dtype, int nk, int nv, int dk, int dv) {
+  return dt_ok(dtype) && nk >= 1 && nv >= nk && nv % nk == 0 && nv <= DELTA_MAX_HEADS && dk >= 8 && dk % 8 == 0 && dk <= 128 && dv >= 8 && dv % 8 == 0 && dv <= 256;
+}
+bool delta_docs_ok(int T, int ndocs) { return T >= 0 && T <= DELTA_MAX_TOKENS && ndocs >= 0 && ndocs <= DELTA_MAX_DOCS; }
+bool delta_shape_ok(int dtype, int T, int ndocs, int nk, int nv, int dk, int dv) {
+  return delta_heads_ok(dtype, nk, nv, dk, dv) && delta_docs_ok(T, ndocs) && (int64_t)T * nv <= 1 << 30 && (int64_t)ndocs * nv <= DELTA_MAX_DOCS;
+}
+bool delta_rows_ok(int dtype, int nk, int nv, int dk, int dv, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                   const float* g, const float* beta, float scale, const void* o, int64_t ldo) {
+  return rows_ok(dtype, q, ldq, nk, dk) && rows_ok(dtype, k, ldk, nk, dk) && rows_ok(dtype, v, ldv, nv, dv) && rows_ok(dtype, o, ldo, nv, dv) && g && beta &&
+         words_ok(g) && words_ok(beta) && std::isfinite(scale);
+}
+int64_t delta_scratch_bytes(bool backward, int32_t dtype, int32_t T, int32_t ndocs, int32_t nk, int32_t nv, int32_t dk, int32_t dv) {
+  return delta_shape_ok(dtype, T, ndocs, nk, nv, dk, dv) ? delta_scratch(backward, T, ndocs, nv, dk, dv) : -STAGE_ERR_ARG;
+}
+}  // namespace
+extern "C" {
+
+int64_t stage_op_delta_chunks_ints(int32_t T, int32_t ndocs) {
+  return delta_docs_ok(T, ndocs) ? 4 * (1 + ndocs + delta_chunk_rows(T, ndocs)) : -STAGE_ERR_ARG;
+}
+
+int stage_op_delta_chunks(void* stream, int32_t T, int32_t ndocs, const int32_t* offsets, int32_t* chunks) {
+  if (!delta_docs_ok(T, ndocs) || !offsets || !words_ok(offsets) || !chunks || !aligned16(chunks)) return STAGE_ERR_ARG;
+  return rc(delta_chunks((hipStream_t)stream, T, ndocs, offsets, chunks));
+}
+
+int64_t stage_op_delta_fwd_scratch_bytes(int32_t dtype, int32_t T, int32_t ndocs, int32_t nk, int32_t nv, int32_t dk, int32_t dv) {
+  return delta_scratch_bytes(false, dtype, T, ndocs, nk, nv, dk, dv);
+}
+
+int64_t stage_op_delta_bwd_scratch_bytes(int32_t dtype, int32_t T, int32_t ndocs, int32_t nk, int32_t nv, int32_t dk, int32_t dv) {
+  return delta_scratch_bytes(true, dtype, T, ndocs, nk, nv, dk, dv);
+}
+
+int stage_op_delta_fwd(void* stream, int32_t dtype, int32_t T, int32_t nk, int32_t nv, int32_t dk, int32_t dv, const void* q, int64_t ldq,
+                       const void* k, int64_t ldk, const void* v, int64_t ldv, const float* g, const float* beta, int32_t ndocs, const int32_t* chunks,
+                       float scale, const float* h0, void* o, int64_t ldo, float* ht, void* scratch, int64_t scratch_bytes) {
+  if (!delta_shape_ok(dtype, T, ndocs, nk, nv, dk, dv)) return STAGE_ERR_ARG;
+  if (T == 0 && ndocs == 0) return STAGE_OK;
+  if (!delta_rows_ok(dtype, nk, nv, dk, dv, q, ldq, k, ldk, v, ldv, g, beta, scale, o, ldo) || !chunks || !aligned16(chunks) || !aligned16(h0) ||
+      !aligned16(ht))
+    return STAGE_ERR_ARG;
+  if (!scratch || ((uintptr_t)scratch & 255) || scratch_bytes < delta_scratch(false, T, ndocs, nv, dk, dv)) return STAGE_ERR_WORKSPACE;
+  DeltaRule a = {};
+  a.T = T; a.nk = nk; a.nv = nv; a.dk = dk; a.dv = dv; a.ndocs = ndocs; a.q = q; a.k = k; a.v = v; a.ldq = ldq; a.ldk = ldk; a.ldv = ldv;
+  a.g = g; a.beta = beta; a.chunks = chunks; a.scale = scale; a.h0 = h0; a.o = o; a.ldo = ldo; a.ht = ht;
+  return rc(delta_rule((hipStream_t)stream, (DType)dtype, a, false, scratch));
+}
+
+int stage_op_delta_bwd(void* stream, int32_t dtype, int32_t T, int32_t nk, int32_t nv, int32_t dk, int32_t dv, const void* q, int64_t ldq,
+                       const void* k, int64_t ldk, const void* v, int64_t ldv, const float* g, const float* beta, int32_t ndocs, const int32_t* chunks,
+                       float scale, const float* h0, const void* dout, int64_t ldo, const float* dht, void* dq, int64_t lddq, void* dk_out,
+                       int64_t lddk, void* dv_out, int64_t lddv, float* dg, float* dbeta, float* dh0, void* scratch, int64_t scratch_bytes) {
+  if (!delta_shape_ok(dtype, T, ndocs, nk, nv, dk, dv)) return STAGE_ERR_ARG;
+  if (T == 0 && ndocs == 0) return STAGE_OK;
+  if (!delta_rows_ok(dtype, nk, nv, dk, dv, q, ldq, k, ldk, v, ldv, g, beta, scale, dout, ldo) || !rows_ok(dtype, dq, lddq, nk, dk) ||
+      !rows_ok(dtype, dk_out, lddk, nk, dk) || !rows_ok(dtype, dv_out, lddv, nv, dv) || !dg || !words_ok(dg) || !dbeta || !words_ok(dbeta) || !chunks ||
+      !aligned16(chunks) || !aligned16(h0) || !aligned16(dht) || !aligned16(dh0))
+    return STAGE_ERR_ARG;
+  if (!scratch || ((uintptr_t)scratch & 255) || scratch_bytes < delta_scratch(true, T, ndocs, nv, dk, dv)) return STAGE_ERR_WORKSPACE;
+  DeltaRule a = {};
+  a.T = T; a.nk = nk; a.nv = nv; a.dk = dk; a.dv = dv; a.ndocs = ndocs; a.q = q; a.k = k; a.v = v; a.ldq = ldq; a.ldk = ldk; a.ldv = ldv;
+  a.g = g; a.beta = beta; a.chunks = chunks; a.scale = scale; a.h0 = h0; a.dout = dout; a.ldo = ldo; a.dht = dht;
+  a.dq = dq; a.lddq = lddq; a.dkey = dk_out; a.lddk = lddk; a.dval = dv_out; a.lddv = lddv; a.dg = dg; a.dbeta = dbeta; a.dh0 = dh0;
+  return rc(delta_rule((hipStream_t)stream, (DType)dtype, a, true, scratch));
+}
+
+int stage_op_delta_step(void* stream, int32_t dtype, int32_t n, int32_t nk, int32_t nv, int32_t dk, int32_t dv, const void* q, int64_t ldq,
+                        const void* k, int64_t ldk, const void* v, int64_t ldv, const float* g, const float* beta, const int32_t* slots, float scale,
+                        int32_t nstates, float* state, void* o, int64_t ldo) {
+  if (!delta_heads_ok(dtype, nk, nv, dk, dv) || n < 0 || n > 65535 || nstates < 0 || (!slots && n > nstates)) return STAGE_ERR_ARG;
+  if (n == 0) return STAGE_OK;
+  if (!delta_rows_ok(dtype, nk, nv, dk, dv, q, ldq, k, ldk, v, ldv, g, beta, scale, o, ldo) || !words_ok(slots) || !state || !aligned16(state))
+    return STAGE_ERR_ARG;
+  return rc(delta_step((hipStream_t)stream, (DType)dtype,
+                       DeltaStep{n, nk, nv, dk, dv, nstates, q, k, v, ldq, ldk, ldv, g, beta, slots, scale, state, o, ldo}));
+}
+
 int stage_op_embed(void* stream, int32_t dtype, int32_t T, int32_t H, int32_t V, const int32_t* ids, const void* E,
                    void* x, const void* dx, float* dE, int32_t backward) {
   if (!dt_ok(dtype) || T < 0 || H < 1 || H % vec_of(dtype) || V < 1 || !ids) return STAGE_ERR_ARG;
