@@ -51,13 +51,36 @@ template <typename E, int A, int B> __device__ __forceinline__ f32x4 mma(const O
 }
 template <typename M> constexpr int PAIR = sizeof(M) == 2 ? 2 : 1;
 template <typename M> using Pair = Opnd<M, PAIR<M>>;
+// bf16: both of two values at once, six instructions.
+__device__ __forceinline__ void split_two(float x, float y, unsigned& hi, unsigned& lo) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  union { bf16x2 v; unsigned w; } h, l;
+  h.v = __builtin_convertvector(f32x2{x, y}, bf16x2);
+  l.v = __builtin_convertvector(f32x2{x - __uint_as_float(h.w << 16), y - __uint_as_float(h.w & 0xffff0000u)}, bf16x2);
+  hi = h.w;
+  lo = l.w;
+}
 template <typename M> __device__ __forceinline__ Pair<M> pair_of(const f32x4& a, const f32x4& b) {
   Pair<M> o;
+  if constexpr (__is_same(M, bf16)) {
+    union { u32x4 w; op8<bf16> v; } h, l;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float x = e < 4 ? a[e & 3] : b[e & 3];
-    o.t[0][e] = from_f<M>(x);
-    if constexpr (PAIR<M> == 2) o.t[1][e] = from_f<M>(fp32_value(x - (float)o.t[0][e]));
+    for (int e = 0; e < 4; ++e) {
+      const f32x4& x = e < 2 ? a : b;
+      unsigned hi, lo;
+      split_two(x[2 * (e & 1)], x[2 * (e & 1) + 1], hi, lo);
+      h.w[e] = hi;
+      l.w[e] = lo;
+    }
+    o.t[0] = h.v;
+    o.t[1] = l.v;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float x = e < 4 ? a[e & 3] : b[e & 3];
+      o.t[0][e] = from_f<M>(x);
+      if constexpr (PAIR<M> == 2) o.t[1][e] = from_f<M>(fp32_value(x - (float)o.t[0][e]));
+    }
   }
   return o;
 }
@@ -187,11 +210,33 @@ template <typename M> __device__ __forceinline__ Pair<M> load_op(unsigned from, 
   }
   return o;
 }
-// `bytes` (a multiple of 1024) that lie together, into LDS as they are, by NW waves.
-template <int NW> __device__ __forceinline__ void fetch_bytes(unsigned lds, const char* from, int bytes, int wave, int lane) {
-  const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), 0, bytes, 0x00020000);
-  for (int at = wave * 1024; at < bytes; at += NW * 1024)
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(uintptr_t)(lds + at), 16, (unsigned)(at + 16 * lane), 0, 0, 0);
+// Loads into LDS that run ahead.  The compiler waits for all of those that it knows of before the next transposing read, whatever that reads; these it
+// does not know, and the waits are the callers' (tile_wait before the barrier that publishes them).  64 times 16 bytes, from the
+// lanes' offsets behind `base`, of which `bytes` may be read (zeros behind them), to `lds` on.
+__device__ __forceinline__ void load_ahead(unsigned lds, const void* base, int bytes, unsigned offset) {
+  const uint64_t at = (uint64_t)(uintptr_t)base;
+  u32x4 rs;
+  rs[0] = __builtin_amdgcn_readfirstlane((unsigned)at);
+  rs[1] = __builtin_amdgcn_readfirstlane((unsigned)(at >> 32) & 0xffffu);
+  rs[2] = __builtin_amdgcn_readfirstlane((unsigned)bytes);
+  rs[3] = 0x00020000u;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(rs) : "memory", "m0");
+}
+template <typename E, int D, int ROWS, int NW> __device__ __forceinline__ void tile_ahead(const TileLoad<E, D, ROWS, NW>& t, unsigned lds, const E* head, int row0, int end, int wave) {
+  typedef Tile<E, D> TL;
+  const int rows = min(end - row0, ROWS), bytes = rows > 0 ? (rows - 1) * t.ld * TL::SZ + t.width : 0;
+#pragma unroll
+  for (int i = 0; i < TileLoad<E, D, ROWS, NW>::N; ++i) {
+    const int sq = wave + NW * i, oct = sq / TL::SQUARES, q = sq % TL::SQUARES;
+    unsigned from = t.at[0];
+#pragma unroll
+    for (int k = 1; k < TL::SQUARES; ++k) from = q == k ? t.at[k] : from;
+    load_ahead(lds + oct * TL::OCTET + q * 1024, head + (int64_t)row0 * t.ld, bytes, from + (unsigned)(8 * oct * t.ld * TL::SZ));
+  }
+}
+// `bytes` (a multiple of 1024) that lie together, as they are, by NW waves.
+template <int NW> __device__ __forceinline__ void bytes_ahead(unsigned lds, const char* from, int bytes, int wave, int lane) {
+  for (int at = wave * 1024; at < bytes; at += NW * 1024) load_ahead(lds + at, from, bytes, (unsigned)(at + 16 * lane));
 }
 
 // ------------------------------------------------------------------------------------------ a chunk's own matrices
@@ -395,237 +440,341 @@ template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256) void d
 }
 
 // ------------------------------------------------------------------------------------------ from chunk to chunk
-// A workgroup of NW waves walks a document's chunks for one value head and 16 NW columns of its state; a wave has 16 columns of all rows in its registers,
-// and they never leave it: a result's registers, two above one another, are the next product's operand.  Keys, queries and the chunk's
-// matrices come straight into LDS, a chunk ahead.
+// A workgroup walks a document's chunks for one value head and 16 NW columns of its state.  NW of its waves carry the state, 16 columns of all rows each, in
+// their registers, and it never leaves them: a result's registers, two above one another, are the next product's operand.  What a chunk waits for
+// is the chain of these waves: state as pairs, K S, T times what that leaves, K^T times that, so all else is done by as many others beside them, a
+// chain's wave and its helper sharing 12 KB of LDS: the results, what the gradients' walk adds to its state, and the stores of states.
+// Two barriers a chunk: the first publishes the state and the chunk's tiles, the second u.  Keys, queries, values and the chunk's matrices come
+// straight into LDS, a chunk ahead where two of them fit.
 enum DeltaWalk { WALK_RESULTS = 0, WALK_STATES = 1, WALK_GRADIENTS = 2 };   // o and the last state; the states and u for the gradients; the states' gradients and y
 
 template <typename E, int DK, int NW, int KIND> struct WalkLds {
   typedef Tile<E, DK> TL;
   typedef Tile<E, 64> VL;
-  static constexpr int K = 0, V = TL::bytes(DELTA_C), Q = V + VL::bytes(DELTA_C), R = Q + (KIND == WALK_STATES ? 0 : TL::bytes(DELTA_C));
-  static constexpr int REC = KIND == WALK_RESULTS ? REC_FWD : KIND == WALK_STATES ? REC_P : REC_GATES + 2 * REC_TRIANGLE;
-  static constexpr int BUF = R + REC;
-  static constexpr int NBUF = 2 * BUF <= 160 * 1024 ? 2 : 1;
+  static constexpr int REC = KIND == WALK_STATES ? REC_P : REC_FWD;   // gates and T; and P; or gates, P^T and T^T
+  static constexpr int K = 0, R = TL::bytes(DELTA_C), BUF = R + REC;  // of these two, in turn, where they fit
+  static constexpr int VSIZE = VL::bytes(DELTA_C), QSIZE = KIND == WALK_STATES ? 0 : TL::bytes(DELTA_C);
+  static constexpr int HAND = DK * 64 + 4096, UNITS = 128;            // of a wave: its state, fp32 or pairs; u; half's units
+  static constexpr int NBUF = 2 * BUF + VSIZE + QSIZE + NW * (HAND + UNITS) <= 160 * 1024 ? 2 : 1;
+  static constexpr int V = NBUF * BUF, Q = V + VSIZE, H = Q + QSIZE, U = H + NW * HAND, BYTES = U + NW * UNITS;
+  static_assert(BYTES <= 160 * 1024, "");
 };
+
+// A lane's part of a wave's results, which lie as registers in LDS, as rows of 16 columns: row 16 i + lane / 4, columns 4 (lane % 4) ..
+__device__ __forceinline__ f32x4 by_rows(unsigned from, int i, int lane) {
+  const int q = lane >> 2;
+  f32x4 o;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) o[e] = lds_read<float>(from + 4 * ((i * 64 + (q >> 2) * 16 + 4 * (lane & 3) + e) * 4 + (q & 3)));
+  return o;
+}
+template <typename T> __device__ __forceinline__ void lds_write(unsigned at, const T& v) { *(__attribute__((address_space(3))) T*)(uintptr_t)at = v; }
 
 template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void delta_walk(char* smem_raw, const DeltaRule& a, int doc_rank, int h, int c0) {
   typedef WalkLds<E, DK, NW, KIND> L;
-  constexpr int RT = DK / 16, KS = DK / 32;
-  constexpr bool HALF_E = __is_same(E, f16), BACK = KIND == WALK_GRADIENTS;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i16 = lane & 15;
+  constexpr int RT = DK / 16, KS = DK / 32, WAVES = 2 * NW;
+  constexpr bool HALF_E = __is_same(E, f16), BACK = KIND == WALK_GRADIENTS, RESULTS = KIND == WALK_RESULTS;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = wave % NW, g = lane >> 4, i16 = lane & 15;
+  const bool helps = wave >= NW;
   const int4 row = reinterpret_cast<const int4*>(a.chunks)[1 + doc_rank];   // first token, tokens, first chunk, document
   const int first = row.x, count = row.y, chunk0 = row.z, doc = row.w, chunks = (count + DELTA_C - 1) / DELTA_C;
-  const int kv = h / (a.nv / a.nk), col = c0 + 16 * wave + i16;   // column of the lane
+  const int kv = h / (a.nv / a.nk), w0 = c0 + 16 * mine, col = w0 + i16;    // the wave's first column and the lane's
   const bool live = col < a.dv;
   const E *kh = (const E*)a.k + kv * a.dk, *qh = (const E*)a.q + kv * a.dk;
-  const E* vh = BACK ? (const E*)a.dout + h * a.dv + c0 : (const E*)a.v + h * a.dv + c0;
-  const unsigned smem = lds_address(smem_raw);
-  const TileLoad<E, DK, DELTA_C, NW> load_k(a.ldk, lane, a.dk), load_q(a.ldq, lane, a.dk);
-  const TileLoad<E, 64, DELTA_C, NW> load_v(BACK ? a.ldo : a.ldv, lane, min(a.dv - c0, 16 * NW));
+  const E* vh = (BACK ? (const E*)a.dout : (const E*)a.v) + h * a.dv + c0;
+  const unsigned smem = lds_address(smem_raw), hand = smem + L::H + mine * L::HAND, hand_u = hand + DK * 64, units = smem + L::U + mine * L::UNITS;
+  const TileLoad<E, DK, DELTA_C, WAVES> load_k(a.ldk, lane, a.dk), load_q(a.ldq, lane, a.dk);
+  const TileLoad<E, 64, DELTA_C, WAVES> load_v(BACK ? a.ldo : a.ldv, lane, min(a.dv - c0, 16 * NW));
   const TileOps<E, DK> at(smem, lane);
-  const TileOps<E, 64> at_v(smem, lane);
+  const TileOps<E, 64> at_v(smem + L::V, lane);
   const int64_t states = (int64_t)a.dk * a.dv;
-  auto fetch = [&](int c, unsigned to) {
+  const int step = BACK ? -1 : 1;
+  auto fetch_first = [&](int c, unsigned to) {
     const int t0 = first + DELTA_C * c, end = min(first + count, t0 + DELTA_C);
-    load_k.fetch(to + L::K, kh, t0, end, wave);
-    load_v.fetch(to + L::V, vh, t0, end, wave);
-    if constexpr (KIND != WALK_STATES) load_q.fetch(to + L::Q, qh, t0, end, wave);
-    const char* rec = a.records + ((int64_t)(chunk0 + c) * a.nv + h) * (KIND == WALK_RESULTS ? REC_FWD : REC_BWD);
+    tile_ahead(load_k, to + L::K, kh, t0, end, wave);
+    const char* rec = a.records + ((int64_t)(chunk0 + c) * a.nv + h) * (RESULTS ? REC_FWD : REC_BWD);
     if constexpr (BACK) {   // P^T and T^T lie side by side
-      fetch_bytes<NW>(to + L::R, rec, REC_GATES, wave, lane);
-      fetch_bytes<NW>(to + L::R + REC_GATES, rec + REC_P, 2 * REC_TRIANGLE, wave, lane);
-    } else fetch_bytes<NW>(to + L::R, rec, L::REC, wave, lane);
+      bytes_ahead<WAVES>(to + L::R, rec, REC_GATES, wave, lane);
+      bytes_ahead<WAVES>(to + L::R + REC_GATES, rec + REC_P, 2 * REC_TRIANGLE, wave, lane);
+    } else bytes_ahead<WAVES>(to + L::R, rec, L::REC, wave, lane);
+  };
+  auto fetch_second = [&](int c) {
+    const int t0 = first + DELTA_C * c, end = min(first + count, t0 + DELTA_C);
+    tile_ahead(load_v, smem + L::V, vh, t0, end, wave);
+    if constexpr (KIND != WALK_STATES) tile_ahead(load_q, smem + L::Q, qh, t0, end, wave);
   };
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   f32x4 S[RT];
-  const float* from = BACK ? a.dht : a.h0;
+  Pair<E> sp[KS];
+  float s_inv = 1.f;
+  auto publish_state = [&]() {   // after a change of S
+    const float unit = column_unit<E>(S);
+    s_inv = inverse_unit<E>(unit);
+    pairs_of<E>(sp, S, unit);
+    if constexpr (RESULTS) {
 #pragma unroll
-  for (int i = 0; i < RT; ++i) {
-    S[i] = zero;
-    if (from)
+      for (int s = 0; s < KS; ++s) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (live && 16 * i + 4 * g + r < a.dk) S[i][r] = from[((int64_t)doc * a.nv + h) * states + (int64_t)(16 * i + 4 * g + r) * a.dv + col];
+        for (int p = 0; p < 2; ++p) {
+          union { op8<E> v; f32x4 h[sizeof(op8<E>) / 16]; } u;
+          u.v = sp[s].t[PAIR<E> == 2 ? p : 0];
+          lds_write(hand + (2 * s + p) * 1024 + 16 * lane, u.h[PAIR<E> == 2 ? 0 : p]);
+        }
+      }
+      if (HALF_E && lane < 16) lds_write(units + 4 * lane, s_inv);
+    } else {
+#pragma unroll
+      for (int i = 0; i < RT; ++i) lds_write(hand + i * 1024 + 16 * lane, S[i]);
+    }
+  };
+  if (!helps) {
+    const float* from = BACK ? a.dht : a.h0;
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      S[i] = zero;
+      if (from)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (live && 16 * i + 4 * g + r < a.dk) S[i][r] = from[((int64_t)doc * a.nv + h) * states + (int64_t)(16 * i + 4 * g + r) * a.dv + col];
+    }
   }
-  const int step = BACK ? -1 : 1;
   int c = BACK ? chunks - 1 : 0;
-  if (chunks > 0 && L::NBUF == 2) {
-    fetch(c, smem);
+  if (chunks > 0) {
+    fetch_first(c, smem);
+    fetch_second(c);
+    if (!helps) publish_state();
     tile_wait();
-    __syncthreads();
   }
+  __syncthreads();
   for (int n = 0; n < chunks; ++n, c += step) {
     const unsigned buf = L::NBUF == 2 ? (unsigned)(n & 1) * L::BUF : 0u;
-    if constexpr (L::NBUF == 2) {
-      if (n + 1 < chunks) fetch(c + step, smem + (L::BUF - buf));   // last read before the barrier that ended the step before
-    } else {
-      fetch(c, smem);
-      tile_wait();
-      __syncthreads();
-    }
+    const bool more = n + 1 < chunks;
+    if (L::NBUF == 2 && more) fetch_first(c + step, smem + (L::BUF - buf));   // last read before the barrier that ended the chunk before
     const unsigned gates = smem + buf + L::R;
     const int64_t rec = (int64_t)(chunk0 + c) * a.nv + h;
-    if constexpr (KIND != WALK_RESULTS) {   // the state before the chunk, or the gradient of the one behind it
-      float* to = (BACK ? a.dstates : a.states) + rec * DK * a.dvp + col;
-      if (col < a.dvp)
+    if (!helps) {
+      Opnd<E, 1> kf[KS][4], vf[2];
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
+      for (int s = 0; s < KS; ++s)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) to[(16 * i + 4 * g + r) * a.dvp] = S[i][r];
-    }
-    Pair<E> sp[KS];
-    const float s_unit = column_unit<E>(S), s_inv = inverse_unit<E>(s_unit);
-    pairs_of<E>(sp, S, s_unit);
-    f32x4 x[4];   // K S
+        for (int m = 0; m < 4; ++m) kf[s][m] = at.row(buf + L::K, m, s);
+      vf[0] = at_v.column(0, mine, 0);
+      vf[1] = at_v.column(0, mine, 1);
+      Pair<E> tf[6];   // T, or P^T
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      x[m] = zero;
+      for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(gates + REC_GATES + i * REC_OP, lane);
+      __builtin_amdgcn_sched_barrier(0);
+      f32x4 x[4], y[4], u[4], next[4];   // K S; P^T dO
 #pragma unroll
-      for (int s = 0; s < KS; ++s) x[m] = mma(at.row(buf + L::K, m, s), sp[s], x[m]);
-    }
-    f32x4 o[4];   // (Q S)^T: rows are columns of the state, a lane has the token lane % 16
-    if constexpr (KIND == WALK_RESULTS) {
+      for (int m = 0; m < 4; ++m) x[m] = y[m] = zero;
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) x[m] = mma(kf[s][m], sp[s], x[m]);
+      f32x4 since[4], other[4];
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
-        o[m] = zero;
-#pragma unroll
-        for (int s = 0; s < KS; ++s) o[m] = mma(sp[s], at.row(buf + L::Q, m, s), o[m]);
+        since[m] = lds_read<f32x4>(gates + 4 * (16 * m + 4 * g));
+        other[m] = lds_read<f32x4>(gates + (BACK ? 256 : 512) + 4 * (16 * m + 4 * g));
       }
-    }
-    Opnd<E, 1> vf[2];   // columns of v, or dO
-    vf[0] = at_v.column(buf + L::V, wave, 0);
-    vf[1] = at_v.column(buf + L::V, wave, 1);
-    f32x4 u[4], next[4];
-    Pair<E> up[2];
-    if constexpr (!BACK) {
       f32x4 z[4];
+      if constexpr (BACK) {
 #pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const f32x4 since = lds_read<f32x4>(gates + 4 * (16 * m + 4 * g)), beta = lds_read<f32x4>(gates + 512 + 4 * (16 * m + 4 * g));
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) z[m][r] = beta[r] * ((float)vf[m >> 1].t[0][4 * (m & 1) + r] - since[r] * (x[m][r] * s_inv));
+          for (int m = 0; m < 4; ++m)
+            if (s >= m / 2) y[m] = mma(tf[upper_op(m, s)], vf[s], y[m]);
+#pragma unroll
+        for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(gates + REC_GATES + REC_TRIANGLE + i * REC_OP, lane);   // T^T
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) z[m][r] = a.scale * y[m][r] + other[m][r] * (x[m][r] * s_inv);
+      } else {
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) z[m][r] = other[m][r] * ((float)vf[m >> 1].t[0][4 * (m & 1) + r] - since[m][r] * (x[m][r] * s_inv));
       }
       Pair<E> zp[2];
       const float unit = column_unit<E>(z), inv = inverse_unit<E>(unit);
       pairs_of<E>(zp, z, unit);
+      __builtin_amdgcn_sched_barrier(0);
+      Opnd<E, 1> kc[2][RT];
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int i = 0; i < RT; ++i) kc[s][i] = at.column(buf + L::K, i, s);
+      f32x4 more_gates[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) more_gates[m] = lds_read<f32x4>(gates + (BACK ? 512 : 256) + 4 * (16 * m + 4 * g));
+      const float whole = lds_read<float>(gates + 768);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) u[m] = zero;
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+          if (BACK ? s >= m / 2 : s <= m / 2) u[m] = mma(tf[BACK ? upper_op(m, s) : lower_op(m, s)], zp[s], u[m]);
+      if constexpr (HALF_E)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) u[m] *= inv;
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
-        u[m] = zero;
-#pragma unroll
-        for (int s = 0; s <= m / 2; ++s) u[m] = mma(load_op<E>(gates + REC_T + lower_op(m, s) * REC_OP, lane), zp[s], u[m]);
-        if constexpr (HALF_E) u[m] *= inv;
+        if constexpr (BACK) next[m] = u[m] * since[m] * more_gates[m] * -1.f;
+        else next[m] = u[m] * more_gates[m];
       }
-      if constexpr (KIND == WALK_RESULTS) {
-        const float u_unit = column_unit<E>(u), u_inv = inverse_unit<E>(u_unit);
+      if constexpr (RESULTS) {
+        Pair<E> up[2];
+        const float u_unit = column_unit<E>(u);
         pairs_of<E>(up, u, u_unit);
-        E* oh = (E*)a.o + h * a.dv + c0 + 16 * wave;
-        f32x4 back_s = {s_inv, s_inv, s_inv, s_inv}, back_u = {u_inv, u_inv, u_inv, u_inv};   // of the rows' columns
-        if constexpr (HALF_E) {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            back_s[r] = __shfl(s_inv, 4 * g + r, 64);
-            back_u[r] = __shfl(u_inv, 4 * g + r, 64);
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            union { op8<E> v; f32x4 h[sizeof(op8<E>) / 16]; } w;
+            w.v = up[s].t[PAIR<E> == 2 ? p : 0];
+            lds_write(hand_u + (2 * s + p) * 1024 + 16 * lane, w.h[PAIR<E> == 2 ? 0 : p]);
           }
-        }
+        if (HALF_E && lane < 16) lds_write(units + 64 + 4 * lane, inverse_unit<E>(u_unit));
+      } else {
+#pragma unroll
+        for (int m = 0; m < 4; ++m) lds_write(hand_u + m * 1024 + 16 * lane, u[m]);
+      }
+      Pair<E> np[2];
+      const float n_unit = column_unit<E>(next), n_inv = inverse_unit<E>(n_unit);
+      pairs_of<E>(np, next, n_unit);
+      __syncthreads();
+      if (more && L::NBUF == 2) fetch_second(c + step);
+      f32x4 add[RT];
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        add[i] = zero;
+        if constexpr (BACK) add[i] = lds_read<f32x4>(hand + i * 1024 + 16 * lane);
+        if constexpr (HALF_E) {
+          add[i] += S[i] * whole;
+          S[i] = zero;
+        } else S[i] = add[i] + S[i] * whole;
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int i = 0; i < RT; ++i) S[i] = mma(kc[s][i], np[s], S[i]);
+      if constexpr (HALF_E)
+#pragma unroll
+        for (int i = 0; i < RT; ++i) S[i] = add[i] + S[i] * n_inv;
+      if (more) publish_state();
+    } else if constexpr (RESULTS) {
+      Pair<E> sf[KS];
+      f32x4 o[4];   // transposed: rows are columns of the state, a lane has the token lane % 16
+#pragma unroll
+      for (int s = 0; s < KS; ++s) sf[s] = load_op<E>(hand + s * 2048, lane);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) o[m] = zero;
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) o[m] = mma(sf[s], at.row(L::Q, m, s), o[m]);
+      f32x4 back_s, back_u;   // half: of the rows' columns
+      if constexpr (HALF_E) back_s = lds_read<f32x4>(units + 16 * g);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const float since = lds_read<float>(gates + 4 * (16 * m + i16));
+        if constexpr (HALF_E) o[m] *= back_s * since;
+        else o[m] *= since;
+      }
+      Pair<E> pf[6];
+#pragma unroll
+      for (int i = 0; i < 6; ++i) pf[i] = load_op<E>(gates + REC_P + i * REC_OP, lane);
+      __syncthreads();
+      if (more && L::NBUF == 2) fetch_second(c + step);
+      Pair<E> uf[2];
+      uf[0] = load_op<E>(hand_u, lane);
+      uf[1] = load_op<E>(hand_u + 2048, lane);
+      if constexpr (HALF_E) back_u = lds_read<f32x4>(units + 64 + 16 * g);
+      f32x4 p[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) p[m] = HALF_E ? zero : o[m];
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+          if (s <= m / 2) p[m] = mma(uf[s], pf[lower_op(m, s)], p[m]);
+      if (L::NBUF == 2) tile_wait();   // for the loads, before the stores, which need not have ended at the barrier
+      E* oh = (E*)a.o + h * a.dv + w0 + 4 * g;
+      if (w0 + 4 * g < a.dv)
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-          const float since = lds_read<float>(gates + 4 * (16 * m + i16));
-          f32x4 pu = zero;
-          if constexpr (HALF_E) o[m] *= back_s * since;
-          else pu = o[m] * since;
-#pragma unroll
-          for (int s = 0; s <= m / 2; ++s) pu = mma(up[s], load_op<E>(gates + REC_P + lower_op(m, s) * REC_OP, lane), pu);
-          if constexpr (HALF_E) pu = pu * back_u + o[m];
           const int t = DELTA_C * c + 16 * m + i16;
-          if (t < count && c0 + 16 * wave + 4 * g < a.dv) {
+          if constexpr (HALF_E) p[m] = p[m] * back_u + o[m];
+          if (t < count) {
             typedef E quad_t __attribute__((ext_vector_type(4)));
             quad_t w;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) w[r] = from_f<E>(fp32_value(pu[r] * a.scale));
-            *reinterpret_cast<quad_t*>(oh + (first + t) * a.ldo + 4 * g) = w;
+            for (int r = 0; r < 4; ++r) w[r] = from_f<E>(fp32_value(p[m][r] * a.scale));
+            *reinterpret_cast<quad_t*>(oh + (first + t) * a.ldo) = w;
           }
         }
-      }
-#pragma unroll
-      for (int m = 0; m < 4; ++m) next[m] = u[m] * lds_read<f32x4>(gates + 256 + 4 * (16 * m + 4 * g));
     } else {
-      f32x4 du[4];
+      const int out = w0 + 4 * (lane & 3);   // columns of the lane's part of a row
+      float* to = (BACK ? a.dstates : a.states) + rec * DK * a.dvp + (lane >> 2) * a.dvp + out;
+      f32x4 part[RT];
 #pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        f32x4 pd = zero;
+      for (int i = 0; i < RT; ++i) part[i] = by_rows(hand, i, lane);
+      if (out < a.dvp)
 #pragma unroll
-        for (int s = m / 2; s < 2; ++s) pd = mma(load_op<E>(gates + REC_GATES + upper_op(m, s) * REC_OP, lane), vf[s], pd);
-        const f32x4 until = lds_read<f32x4>(gates + 256 + 4 * (16 * m + 4 * g));
+        for (int i = 0; i < RT; ++i) *reinterpret_cast<f32x4*>(to + 16 * i * a.dvp) = part[i];
+      if constexpr (BACK) {   // scale Q^T (exp(G) dO)
+        Opnd<E, 1> vf[2];
+        vf[0] = at_v.column(0, mine, 0);
+        vf[1] = at_v.column(0, mine, 1);
+        f32x4 d[4], add[RT];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) du[m][r] = a.scale * pd[r] + until[r] * (x[m][r] * s_inv);
-      }
-      Pair<E> dp[2];
-      const float unit = column_unit<E>(du), inv = inverse_unit<E>(unit);
-      pairs_of<E>(dp, du, unit);
+        for (int m = 0; m < 4; ++m) {
+          const f32x4 since = lds_read<f32x4>(gates + 4 * (16 * m + 4 * g));
 #pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        u[m] = zero;   // y
-#pragma unroll
-        for (int s = m / 2; s < 2; ++s) u[m] = mma(load_op<E>(gates + REC_GATES + REC_TRIANGLE + upper_op(m, s) * REC_OP, lane), dp[s], u[m]);
-        if constexpr (HALF_E) u[m] *= inv;
-        const f32x4 since = lds_read<f32x4>(gates + 4 * (16 * m + 4 * g)), beta = lds_read<f32x4>(gates + 512 + 4 * (16 * m + 4 * g));
-        next[m] = u[m] * since * beta * -1.f;
-      }
-    }
-    if constexpr (KIND != WALK_RESULTS) {
-      float* to = (BACK ? a.y : a.u) + rec * DELTA_C * a.dvp + col;
-      if (col < a.dvp)
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) to[(16 * m + 4 * g + r) * a.dvp] = u[m][r];
-    }
-    const float whole = lds_read<float>(gates + 768);
-    Pair<E> np[2], qp[2];
-    const float n_unit = column_unit<E>(next), n_inv = inverse_unit<E>(n_unit);
-    pairs_of<E>(np, next, n_unit);
-    float q_inv = 1.f;
-    if constexpr (BACK) {   // scale exp(G) dO
-      f32x4 d[4];
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const f32x4 since = lds_read<f32x4>(gates + 4 * (16 * m + 4 * g));
-#pragma unroll
-        for (int r = 0; r < 4; ++r) d[m][r] = a.scale * since[r] * (float)vf[m >> 1].t[0][4 * (m & 1) + r];
-      }
-      const float q_unit = column_unit<E>(d);
-      q_inv = inverse_unit<E>(q_unit);
-      pairs_of<E>(qp, d, q_unit);
-    }
-#pragma unroll
-    for (int i = 0; i < RT; ++i) {
-      f32x4 acc = S[i] * whole;
-      if constexpr (HALF_E) {
-        f32x4 p = zero;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) p = mma(at.column(buf + L::K, i, s), np[s], p);
-        acc += p * n_inv;
-        if constexpr (BACK) {
-          p = zero;
-#pragma unroll
-          for (int s = 0; s < 2; ++s) p = mma(at.column(buf + L::Q, i, s), qp[s], p);
-          acc += p * q_inv;
+          for (int r = 0; r < 4; ++r) d[m][r] = a.scale * since[r] * (float)vf[m >> 1].t[0][4 * (m & 1) + r];
         }
-      } else {
+        Pair<E> dp[2];
+        const float unit = column_unit<E>(d), inv = inverse_unit<E>(unit);
+        pairs_of<E>(dp, d, unit);
 #pragma unroll
-        for (int s = 0; s < 2; ++s) acc = mma(at.column(buf + L::K, i, s), np[s], acc);
-        if constexpr (BACK)
+        for (int i = 0; i < RT; ++i) add[i] = zero;
 #pragma unroll
-          for (int s = 0; s < 2; ++s) acc = mma(at.column(buf + L::Q, i, s), qp[s], acc);
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int i = 0; i < RT; ++i) add[i] = mma(at.column(L::Q, i, s), dp[s], add[i]);
+        wave_lds_order();   // the state has been read
+#pragma unroll
+        for (int i = 0; i < RT; ++i) lds_write(hand + i * 1024 + 16 * lane, HALF_E ? add[i] * inv : add[i]);
       }
-      S[i] = acc;
+      __syncthreads();
+      if (more && L::NBUF == 2) fetch_second(c + step);
+      f32x4 pu[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) pu[m] = by_rows(hand_u, m, lane);
+      if (L::NBUF == 2) tile_wait();
+      float* to_u = (BACK ? a.y : a.u) + rec * DELTA_C * a.dvp + (lane >> 2) * a.dvp + out;
+      if (out < a.dvp)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) *reinterpret_cast<f32x4*>(to_u + 16 * m * a.dvp) = pu[m];
     }
-    tile_wait();
-    __syncthreads();
+    if constexpr (L::NBUF == 2) {
+      if (!helps) tile_wait();
+      __syncthreads();
+    } else {
+      __syncthreads();
+      if (more) {
+        fetch_first(c + step, smem);
+        fetch_second(c + step);
+      }
+      tile_wait();
+      __syncthreads();
+    }
   }
-  float* last = KIND == WALK_RESULTS ? a.ht : BACK ? a.dh0 : nullptr;
-  if (last && live)
+  float* last = RESULTS ? a.ht : BACK ? a.dh0 : nullptr;
+  if (last && live && !helps)
 #pragma unroll
     for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -639,17 +788,15 @@ __device__ __forceinline__ WalkBlock walk_block(const DeltaRule& a, int block, i
   const int j = block / 8, pair = j / slices * 8 + block % 8;
   return WalkBlock{pair / a.nv, pair % a.nv, j % slices * width, pair < a.ndocs * a.nv};
 }
-template <typename E, int DK, int NW> __global__ __launch_bounds__(64 * NW, 1) void delta_walk_kernel(DeltaRule a, int slices) {
-  typedef WalkLds<E, DK, NW, WALK_RESULTS> L;
-  __shared__ __align__(16) char smem[L::NBUF * L::BUF];
+template <typename E, int DK, int NW> __global__ __launch_bounds__(128 * NW, 1) void delta_walk_kernel(DeltaRule a, int slices) {
+  __shared__ __align__(16) char smem[WalkLds<E, DK, NW, WALK_RESULTS>::BYTES];
   const WalkBlock b = walk_block(a, blockIdx.x, slices, 16 * NW);
   if (b.in) delta_walk<E, DK, NW, WALK_RESULTS>(smem, a, b.doc, b.h, b.c0);
 }
 // Both walks of the backward: they need nothing of one another.
-template <typename E, int DK, int NW> __global__ __launch_bounds__(64 * NW, 1) void delta_walks_kernel(DeltaRule a, int slices, int blocks) {
-  typedef WalkLds<E, DK, NW, WALK_STATES> L;
-  typedef WalkLds<E, DK, NW, WALK_GRADIENTS> LG;
-  __shared__ __align__(16) char smem[L::NBUF * L::BUF > LG::NBUF * LG::BUF ? L::NBUF * L::BUF : LG::NBUF * LG::BUF];
+template <typename E, int DK, int NW> __global__ __launch_bounds__(128 * NW, 1) void delta_walks_kernel(DeltaRule a, int slices, int blocks) {
+  constexpr int LS = WalkLds<E, DK, NW, WALK_STATES>::BYTES, LG = WalkLds<E, DK, NW, WALK_GRADIENTS>::BYTES;
+  __shared__ __align__(16) char smem[LS > LG ? LS : LG];
   const bool back = (int)blockIdx.x < blocks;
   const WalkBlock b = walk_block(a, back ? (int)blockIdx.x : (int)blockIdx.x - blocks, slices, 16 * NW);
   if (!b.in) return;
@@ -980,8 +1127,8 @@ template <typename E, int DK> __global__ __launch_bounds__(256, 1) void delta_gr
 template <typename E, int DK, int NW> hipError_t delta_walks(hipStream_t st, const DeltaRule& a, bool backward) {
   const int slices = (int)cdiv(a.dv, 16 * NW);
   const int blocks = (int)(cdiv((int64_t)a.ndocs * a.nv, 8) * 8 * slices);
-  if (backward) hipLaunchKernelGGL((delta_walks_kernel<E, DK, NW>), dim3((unsigned)(2 * blocks)), dim3(64 * NW), 0, st, a, slices, blocks);
-  else hipLaunchKernelGGL((delta_walk_kernel<E, DK, NW>), dim3((unsigned)blocks), dim3(64 * NW), 0, st, a, slices);
+  if (backward) hipLaunchKernelGGL((delta_walks_kernel<E, DK, NW>), dim3((unsigned)(2 * blocks)), dim3(128 * NW), 0, st, a, slices, blocks);
+  else hipLaunchKernelGGL((delta_walk_kernel<E, DK, NW>), dim3((unsigned)blocks), dim3(128 * NW), 0, st, a, slices);
   return hipGetLastError();
 }
 template <typename E, int DK> hipError_t delta_run(hipStream_t st, const DeltaRule& a, bool backward) {
