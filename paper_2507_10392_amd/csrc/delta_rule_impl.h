@@ -113,6 +113,7 @@ template <typename M, int N> __device__ __forceinline__ void pairs_of(Pair<M> (&
 // Places of operands in a tile of rows (Tile: rows come straight from memory, pieces of 16 bytes changed about).
 template <typename E, int D> struct TileOps {
   typedef Tile<E, D> TL;
+  __device__ __forceinline__ TileOps() {}
   static constexpr int SZ = TL::SZ, OCTET = TL::OCTET;
   unsigned row_[SZ == 4 ? 2 : 4], col_[SZ == 4 ? 8 : 4];
   __device__ __forceinline__ TileOps(unsigned base, int lane) {
@@ -164,6 +165,54 @@ template <typename E, int D> struct TileOps {
     }
     return o;
   }
+  // The same with the 32 columns of a block in another order, in which a row operand's lie together: lane group g has 8 g .. 8 g + 7, so that row
+  // 4 g + r of the even (odd) one of two results above one another is the block's 8 g + r (8 g + 4 + r): state_row.
+  unsigned srow_[2], scol_[SZ == 4 ? 8 : 2];
+  __device__ __forceinline__ void state_places(unsigned base, int lane) {
+    const int g = lane >> 4, i = lane & 15;
+#pragma unroll
+    for (int p = 0; p < 2; ++p) srow_[p] = base + (i >> 3) * OCTET + (SZ == 4 ? TL::place(i & 7, 2 * g + p) : TL::place(i & 7, 4 * p + g));
+#pragma unroll
+    for (int p = 0; p < (SZ == 4 ? 8 : 2); ++p)
+      scol_[p] = base + (g >> 1) * OCTET + (SZ == 4 ? TL::place(4 * (g & 1) + (p & 3), 2 * (i >> 2) + (p >> 2)) + 4 * (i & 3)
+                                                    : TL::place(4 * (g & 1) + (i >> 2), 4 * p + (i & 3)));
+  }
+  // row 16 m + lane % 16, columns of block s
+  __device__ __forceinline__ Opnd<E, 1> state_row(unsigned tile, int m, int s) const {
+    Opnd<E, 1> o;
+    if constexpr (SZ == 4) {
+      const unsigned at = tile + m * 2 * OCTET + s * 1024;
+      union { f32x4 h[2]; op8<E> v; } u;
+      u.h[0] = lds_read<f32x4>(srow_[0] + at);
+      u.h[1] = lds_read<f32x4>(srow_[1] + at);
+      o.t[0] = u.v;
+    } else o.t[0] = lds_read<op8<E>>(srow_[s & 1] + tile + m * 2 * OCTET + (s >> 1) * 1024);
+    return o;
+  }
+  // result b's row lane % 16 of the columns, rows 32 s + ..
+  __device__ __forceinline__ Opnd<E, 1> state_column(unsigned tile, int b, int s) const {
+    Opnd<E, 1> o;
+    if constexpr (SZ == 4) {
+      const unsigned at = tile + s * 4 * OCTET + (b >> 1) * 1024;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o.t[0][e] = lds_read<float>(scol_[(b & 1) * 4 + (e & 3)] + at + (e >> 2) * 2 * OCTET);
+    } else {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+      const unsigned at = scol_[(b >> 1) & 1] + tile + s * 4 * OCTET + (b >> 2) * 1024 + 8 * (b & 1);
+      union { s16x4 h[2]; op8<E> v; } u;
+      u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)at);
+      u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(at + 2 * OCTET));
+      o.t[0] = u.v;
+    }
+    return o;
+  }
+  __device__ __forceinline__ void move_state_places(unsigned by) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) srow_[p] += by;
+#pragma unroll
+    for (int p = 0; p < (SZ == 4 ? 8 : 2); ++p) scol_[p] += by;
+  }
   // row 16 m + lane % 16, columns 16 b + 4 (lane/16) ..
   __device__ __forceinline__ f32x4 quad(unsigned tile, int m, int b) const {
     f32x4 o;
@@ -197,16 +246,16 @@ template <typename M> __device__ __forceinline__ void store_op(char* to, const P
     reinterpret_cast<op8<M>*>(to)[64 + lane] = o.t[1];
   }
 }
-template <typename M> __device__ __forceinline__ Pair<M> load_op(unsigned from, int lane) {   // LDS
+template <typename M> __device__ __forceinline__ Pair<M> load_op(unsigned lds_of_lane) {   // 16 lane bytes behind the operand's begin
   Pair<M> o;
   if constexpr (sizeof(M) == 4) {
     union { op8<M> v; f32x4 h[2]; } u;
-    u.h[0] = lds_read<f32x4>(from + 16 * lane);
-    u.h[1] = lds_read<f32x4>(from + 1024 + 16 * lane);
+    u.h[0] = lds_read<f32x4>(lds_of_lane);
+    u.h[1] = lds_read<f32x4>(lds_of_lane + 1024);
     o.t[0] = u.v;
   } else {
-    o.t[0] = lds_read<op8<M>>(from + 16 * lane);
-    o.t[1] = lds_read<op8<M>>(from + 1024 + 16 * lane);
+    o.t[0] = lds_read<op8<M>>(lds_of_lane);
+    o.t[1] = lds_read<op8<M>>(lds_of_lane + 1024);
   }
   return o;
 }
@@ -442,11 +491,13 @@ template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256) void d
 // ------------------------------------------------------------------------------------------ from chunk to chunk
 // A workgroup walks a document's chunks for one value head and 16 NW columns of its state.  NW of its waves carry the state, 16 columns of all rows each, in
 // their registers, and it never leaves them: a result's registers, two above one another, are the next product's operand.  What a chunk waits for
-// is the chain of these waves: state as pairs, K S, T times what that leaves, K^T times that, so all else is done by as many others beside them, a
-// chain's wave and its helper sharing 12 KB of LDS: the results, what the gradients' walk adds to its state, and the stores of states.
-// Two barriers a chunk: the first publishes the state and the chunk's tiles, the second u.  Keys, queries, values and the chunk's matrices come
-// straight into LDS, a chunk ahead where two of them fit.
+// is the chain of these waves: K S, T times what that leaves, K^T times that, the new state as pairs.  All else is done by others: each has a
+// helper (the results, what the gradients' walk adds to its state, the stores of states), with which it shares 12 KB of LDS, and the loads are a wave's of
+// its own, or the helpers' where eight waves fill the registers.  Two barriers a chunk: the first publishes the state, and values and queries of the
+// chunk, the second u, and the next chunk's keys and matrices.  All of these come straight into LDS, a chunk ahead where two of them fit.
 enum DeltaWalk { WALK_RESULTS = 0, WALK_STATES = 1, WALK_GRADIENTS = 2 };   // o and the last state; the states and u for the gradients; the states' gradients and y
+constexpr int walk_loaders(int NW) { return NW < 4 ? 1 : 0; }
+constexpr int walk_threads(int NW) { return 64 * (2 * NW + walk_loaders(NW)); }
 
 template <typename E, int DK, int NW, int KIND> struct WalkLds {
   typedef Tile<E, DK> TL;
@@ -460,7 +511,7 @@ template <typename E, int DK, int NW, int KIND> struct WalkLds {
   static_assert(BYTES <= 160 * 1024, "");
 };
 
-// A lane's part of a wave's results, which lie as registers in LDS, as rows of 16 columns: row 16 i + lane / 4, columns 4 (lane % 4) ..
+// Results i of a wave, which lie in LDS as a lane's registers: of row lane / 4 the columns 4 (lane % 4) ..
 __device__ __forceinline__ f32x4 by_rows(unsigned from, int i, int lane) {
   const int q = lane >> 2;
   f32x4 o;
@@ -468,66 +519,101 @@ __device__ __forceinline__ f32x4 by_rows(unsigned from, int i, int lane) {
   for (int e = 0; e < 4; ++e) o[e] = lds_read<float>(from + 4 * ((i * 64 + (q >> 2) * 16 + 4 * (lane & 3) + e) * 4 + (q & 3)));
   return o;
 }
+// Row of the state that a lane's register r of result i has (lane group g), see TileOps.
+__device__ __forceinline__ int state_row(int i, int g, int r) { return 32 * (i >> 1) + 8 * g + 4 * (i & 1) + r; }
 template <typename T> __device__ __forceinline__ void lds_write(unsigned at, const T& v) { *(__attribute__((address_space(3))) T*)(uintptr_t)at = v; }
+template <typename M> __device__ __forceinline__ void write_op(unsigned lds_of_lane, const Pair<M>& x) {   // as load_op reads it
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    union { op8<M> v; f32x4 h[sizeof(op8<M>) / 16]; } u;
+    u.v = x.t[PAIR<M> == 2 ? p : 0];
+    lds_write(lds_of_lane + p * 1024, u.h[PAIR<M> == 2 ? 0 : p]);
+  }
+}
 
 template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void delta_walk(char* smem_raw, const DeltaRule& a, int doc_rank, int h, int c0) {
   typedef WalkLds<E, DK, NW, KIND> L;
-  constexpr int RT = DK / 16, KS = DK / 32, WAVES = 2 * NW;
-  constexpr bool HALF_E = __is_same(E, f16), BACK = KIND == WALK_GRADIENTS, RESULTS = KIND == WALK_RESULTS;
+  constexpr int RT = DK / 16, KS = DK / 32, LOADERS = walk_loaders(NW), FW = LOADERS ? LOADERS : NW;
+  constexpr bool HALF_E = __is_same(E, f16), BACK = KIND == WALK_GRADIENTS, RESULTS = KIND == WALK_RESULTS, AHEAD = L::NBUF == 2;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = wave % NW, g = lane >> 4, i16 = lane & 15;
-  const bool helps = wave >= NW;
+  const bool chain = wave < NW, helps = !chain && wave < 2 * NW, loads = LOADERS ? wave >= 2 * NW : helps;
+  const int fw = LOADERS ? wave - 2 * NW : mine;
   const int4 row = reinterpret_cast<const int4*>(a.chunks)[1 + doc_rank];   // first token, tokens, first chunk, document
   const int first = row.x, count = row.y, chunk0 = row.z, doc = row.w, chunks = (count + DELTA_C - 1) / DELTA_C;
   const int kv = h / (a.nv / a.nk), w0 = c0 + 16 * mine, col = w0 + i16;    // the wave's first column and the lane's
-  const bool live = col < a.dv;
-  const E *kh = (const E*)a.k + kv * a.dk, *qh = (const E*)a.q + kv * a.dk;
-  const E* vh = (BACK ? (const E*)a.dout : (const E*)a.v) + h * a.dv + c0;
-  const unsigned smem = lds_address(smem_raw), hand = smem + L::H + mine * L::HAND, hand_u = hand + DK * 64, units = smem + L::U + mine * L::UNITS;
-  const TileLoad<E, DK, DELTA_C, WAVES> load_k(a.ldk, lane, a.dk), load_q(a.ldq, lane, a.dk);
-  const TileLoad<E, 64, DELTA_C, WAVES> load_v(BACK ? a.ldo : a.ldv, lane, min(a.dv - c0, 16 * NW));
-  const TileOps<E, DK> at(smem, lane);
-  const TileOps<E, 64> at_v(smem + L::V, lane);
-  const int64_t states = (int64_t)a.dk * a.dv;
+  const unsigned smem = lds_address(smem_raw), hand = smem + L::H + mine * L::HAND + 16 * lane, units = smem + L::U + mine * L::UNITS;
+  const unsigned hand_u = hand + DK * 64;
   const int step = BACK ? -1 : 1;
+  const int64_t states = (int64_t)a.dk * a.dv;
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+
+  // ---- loads
+  const TileLoad<E, DK, DELTA_C, FW> load_k(a.ldk, lane, a.dk), load_q(a.ldq, lane, a.dk);
+  const TileLoad<E, 64, DELTA_C, FW> load_v(BACK ? a.ldo : a.ldv, lane, min(a.dv - c0, 16 * NW));
   auto fetch_first = [&](int c, unsigned to) {
     const int t0 = first + DELTA_C * c, end = min(first + count, t0 + DELTA_C);
-    tile_ahead(load_k, to + L::K, kh, t0, end, wave);
+    tile_ahead(load_k, to + L::K, (const E*)a.k + kv * a.dk, t0, end, fw);
     const char* rec = a.records + ((int64_t)(chunk0 + c) * a.nv + h) * (RESULTS ? REC_FWD : REC_BWD);
     if constexpr (BACK) {   // P^T and T^T lie side by side
-      bytes_ahead<WAVES>(to + L::R, rec, REC_GATES, wave, lane);
-      bytes_ahead<WAVES>(to + L::R + REC_GATES, rec + REC_P, 2 * REC_TRIANGLE, wave, lane);
-    } else bytes_ahead<WAVES>(to + L::R, rec, L::REC, wave, lane);
+      bytes_ahead<FW>(to + L::R, rec, REC_GATES, fw, lane);
+      bytes_ahead<FW>(to + L::R + REC_GATES, rec + REC_P, 2 * REC_TRIANGLE, fw, lane);
+    } else bytes_ahead<FW>(to + L::R, rec, L::REC, fw, lane);
   };
   auto fetch_second = [&](int c) {
     const int t0 = first + DELTA_C * c, end = min(first + count, t0 + DELTA_C);
-    tile_ahead(load_v, smem + L::V, vh, t0, end, wave);
-    if constexpr (KIND != WALK_STATES) tile_ahead(load_q, smem + L::Q, qh, t0, end, wave);
+    tile_ahead(load_v, smem + L::V, (BACK ? (const E*)a.dout : (const E*)a.v) + h * a.dv + c0, t0, end, fw);
+    if constexpr (KIND != WALK_STATES) tile_ahead(load_q, smem + L::Q, (const E*)a.q + kv * a.dk, t0, end, fw);
   };
-  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  f32x4 S[RT];
-  Pair<E> sp[KS];
-  float s_inv = 1.f;
-  auto publish_state = [&]() {   // after a change of S
-    const float unit = column_unit<E>(S);
-    s_inv = inverse_unit<E>(unit);
-    pairs_of<E>(sp, S, unit);
-    if constexpr (RESULTS) {
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          union { op8<E> v; f32x4 h[sizeof(op8<E>) / 16]; } u;
-          u.v = sp[s].t[PAIR<E> == 2 ? p : 0];
-          lds_write(hand + (2 * s + p) * 1024 + 16 * lane, u.h[PAIR<E> == 2 ? 0 : p]);
-        }
+  int c = BACK ? chunks - 1 : 0;
+  if (loads && chunks > 0) {
+    fetch_first(c, smem);
+    fetch_second(c);
+    tile_wait();
+  }
+  // The barriers that end a chunk, with what the loading waves have to see arrived.
+  auto end_chunk = [&](bool more) {
+    if (AHEAD && loads && more) tile_wait();
+    __syncthreads();
+    if constexpr (!AHEAD) {
+      if (loads && more) {
+        fetch_first(c + step, smem);
+        fetch_second(c + step);
+        tile_wait();
       }
-      if (HALF_E && lane < 16) lds_write(units + 4 * lane, s_inv);
-    } else {
-#pragma unroll
-      for (int i = 0; i < RT; ++i) lds_write(hand + i * 1024 + 16 * lane, S[i]);
+      __syncthreads();
     }
   };
-  if (!helps) {
+  // The loading waves' part around the second barrier.
+  auto load_next = [&](int n, bool more) {
+    if (AHEAD && loads && more) fetch_first(c + step, smem + ((n & 1) ? 0 : L::BUF));   // last read before the barrier that ended the chunk before
+  };
+  auto middle = [&](bool more) {
+    if (AHEAD && loads && more) tile_wait();
+    __syncthreads();
+    if (AHEAD && loads && more) fetch_second(c + step);
+  };
+
+  if (chain) {
+    const TileOps<E, 64> at_v(smem + L::V, lane);
+    TileOps<E, DK> at;
+    at.state_places(smem + L::K, lane);
+    const bool live = col < a.dv;
+    f32x4 S[RT];
+    Pair<E> sp[KS];
+    float s_inv = 1.f;
+    auto publish_state = [&]() {   // the whole state, after a change
+      const float unit = column_unit<E>(S);
+      s_inv = inverse_unit<E>(unit);
+      pairs_of<E>(sp, S, unit);
+      if constexpr (RESULTS) {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) write_op<E>(hand + s * 2048, sp[s]);
+        if (HALF_E && lane < 16) lds_write(units + 4 * lane, s_inv);
+      } else {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) lds_write(hand + i * 1024, S[i]);
+      }
+    };
     const float* from = BACK ? a.dht : a.h0;
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
@@ -535,34 +621,33 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
       if (from)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          if (live && 16 * i + 4 * g + r < a.dk) S[i][r] = from[((int64_t)doc * a.nv + h) * states + (int64_t)(16 * i + 4 * g + r) * a.dv + col];
+          if (live && state_row(i, g, r) < a.dk) S[i][r] = from[((int64_t)doc * a.nv + h) * states + (int64_t)state_row(i, g, r) * a.dv + col];
     }
-  }
-  int c = BACK ? chunks - 1 : 0;
-  if (chunks > 0) {
-    fetch_first(c, smem);
-    fetch_second(c);
-    if (!helps) publish_state();
-    tile_wait();
-  }
-  __syncthreads();
-  for (int n = 0; n < chunks; ++n, c += step) {
-    const unsigned buf = L::NBUF == 2 ? (unsigned)(n & 1) * L::BUF : 0u;
-    const bool more = n + 1 < chunks;
-    if (L::NBUF == 2 && more) fetch_first(c + step, smem + (L::BUF - buf));   // last read before the barrier that ended the chunk before
-    const unsigned gates = smem + buf + L::R;
-    const int64_t rec = (int64_t)(chunk0 + c) * a.nv + h;
-    if (!helps) {
-      Opnd<E, 1> kf[KS][4], vf[2];
+    if (chunks > 0) publish_state();
+    __syncthreads();
+    Opnd<E, 1> kf[KS][4];   // rows of the chunk's keys
+    auto load_keys = [&]() {
 #pragma unroll
       for (int s = 0; s < KS; ++s)
 #pragma unroll
-        for (int m = 0; m < 4; ++m) kf[s][m] = at.row(buf + L::K, m, s);
-      vf[0] = at_v.column(0, mine, 0);
-      vf[1] = at_v.column(0, mine, 1);
+        for (int m = 0; m < 4; ++m) kf[s][m] = at.state_row(0, m, s);
+    };
+    if (chunks > 0) load_keys();
+    for (int n = 0; n < chunks; ++n, c += step) {
+      const unsigned buf = AHEAD ? (unsigned)(n & 1) * L::BUF : 0u, gates = smem + buf + L::R, ops = gates + REC_GATES + 16 * lane, gates4 = gates + 16 * g;
+      const bool more = n + 1 < chunks;
+      f32x4 since[4], other[4];
+      Opnd<E, 1> vf[2];
       Pair<E> tf[6];   // T, or P^T
 #pragma unroll
-      for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(gates + REC_GATES + i * REC_OP, lane);
+      for (int m = 0; m < 4; ++m) {
+        since[m] = lds_read<f32x4>(gates4 + 64 * m);
+        other[m] = lds_read<f32x4>(gates4 + (BACK ? 256 : 512) + 64 * m);
+      }
+      vf[0] = at_v.column(0, mine, 0);
+      vf[1] = at_v.column(0, mine, 1);
+#pragma unroll
+      for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(ops + i * REC_OP);
       __builtin_amdgcn_sched_barrier(0);
       f32x4 x[4], y[4], u[4], next[4];   // K S; P^T dO
 #pragma unroll
@@ -571,12 +656,6 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
       for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int m = 0; m < 4; ++m) x[m] = mma(kf[s][m], sp[s], x[m]);
-      f32x4 since[4], other[4];
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        since[m] = lds_read<f32x4>(gates + 4 * (16 * m + 4 * g));
-        other[m] = lds_read<f32x4>(gates + (BACK ? 256 : 512) + 4 * (16 * m + 4 * g));
-      }
       f32x4 z[4];
       if constexpr (BACK) {
 #pragma unroll
@@ -585,7 +664,7 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
           for (int m = 0; m < 4; ++m)
             if (s >= m / 2) y[m] = mma(tf[upper_op(m, s)], vf[s], y[m]);
 #pragma unroll
-        for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(gates + REC_GATES + REC_TRIANGLE + i * REC_OP, lane);   // T^T
+        for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(ops + REC_TRIANGLE + i * REC_OP);   // T^T
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -600,14 +679,14 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
       const float unit = column_unit<E>(z), inv = inverse_unit<E>(unit);
       pairs_of<E>(zp, z, unit);
       __builtin_amdgcn_sched_barrier(0);
-      Opnd<E, 1> kc[2][RT];
+      Opnd<E, 1> kc[2][RT];   // columns of the keys
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+      for (int i = 0; i < RT; ++i)
 #pragma unroll
-        for (int i = 0; i < RT; ++i) kc[s][i] = at.column(buf + L::K, i, s);
-      f32x4 more_gates[4];
+        for (int s = 0; s < 2; ++s) kc[s][i] = at.state_column(0, i, s);
+      f32x4 factor[4];
 #pragma unroll
-      for (int m = 0; m < 4; ++m) more_gates[m] = lds_read<f32x4>(gates + (BACK ? 512 : 256) + 4 * (16 * m + 4 * g));
+      for (int m = 0; m < 4; ++m) factor[m] = lds_read<f32x4>(gates4 + (BACK ? 512 : 256) + 64 * m);
       const float whole = lds_read<float>(gates + 768);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -617,91 +696,106 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
 #pragma unroll
         for (int m = 0; m < 4; ++m)
           if (BACK ? s >= m / 2 : s <= m / 2) u[m] = mma(tf[BACK ? upper_op(m, s) : lower_op(m, s)], zp[s], u[m]);
-      if constexpr (HALF_E)
-#pragma unroll
-        for (int m = 0; m < 4; ++m) u[m] *= inv;
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
-        if constexpr (BACK) next[m] = u[m] * since[m] * more_gates[m] * -1.f;
-        else next[m] = u[m] * more_gates[m];
-      }
-      if constexpr (RESULTS) {
-        Pair<E> up[2];
-        const float u_unit = column_unit<E>(u);
-        pairs_of<E>(up, u, u_unit);
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            union { op8<E> v; f32x4 h[sizeof(op8<E>) / 16]; } w;
-            w.v = up[s].t[PAIR<E> == 2 ? p : 0];
-            lds_write(hand_u + (2 * s + p) * 1024 + 16 * lane, w.h[PAIR<E> == 2 ? 0 : p]);
-          }
-        if (HALF_E && lane < 16) lds_write(units + 64 + 4 * lane, inverse_unit<E>(u_unit));
-      } else {
-#pragma unroll
-        for (int m = 0; m < 4; ++m) lds_write(hand_u + m * 1024 + 16 * lane, u[m]);
+        if constexpr (HALF_E) u[m] *= inv;
+        lds_write(hand_u + m * 1024, u[m]);
+        if constexpr (BACK) next[m] = u[m] * since[m] * factor[m] * -1.f;
+        else next[m] = u[m] * factor[m];
       }
       Pair<E> np[2];
       const float n_unit = column_unit<E>(next), n_inv = inverse_unit<E>(n_unit);
       pairs_of<E>(np, next, n_unit);
-      __syncthreads();
-      if (more && L::NBUF == 2) fetch_second(c + step);
+      middle(more);
+      const unsigned turn = AHEAD ? ((n & 1) ? (unsigned)-L::BUF : (unsigned)L::BUF) : 0u;
+      at.move_state_places(turn);
       f32x4 add[RT];
 #pragma unroll
       for (int i = 0; i < RT; ++i) {
         add[i] = zero;
-        if constexpr (BACK) add[i] = lds_read<f32x4>(hand + i * 1024 + 16 * lane);
-        if constexpr (HALF_E) {
+        if constexpr (BACK) add[i] = lds_read<f32x4>(hand + i * 1024);
+      }
+      if (AHEAD && more) load_keys();
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (HALF_E) {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
           add[i] += S[i] * whole;
           S[i] = zero;
-        } else S[i] = add[i] + S[i] * whole;
-      }
+        }
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int i = 0; i < RT; ++i) S[i] = mma(kc[s][i], np[s], S[i]);
-      if constexpr (HALF_E)
+          for (int i = 0; i < RT; ++i) S[i] = mma(kc[s][i], np[s], S[i]);
 #pragma unroll
         for (int i = 0; i < RT; ++i) S[i] = add[i] + S[i] * n_inv;
-      if (more) publish_state();
-    } else if constexpr (RESULTS) {
-      Pair<E> sf[KS];
-      f32x4 o[4];   // transposed: rows are columns of the state, a lane has the token lane % 16
+        if (more) publish_state();
+      } else {   // two results at a time, published while the next two are made
+        auto publish = [&](int t) {
+          sp[t] = pair_of<E>(S[2 * t], S[2 * t + 1]);
+          if constexpr (RESULTS) write_op<E>(hand + t * 2048, sp[t]);
+          else {
+            lds_write(hand + 2 * t * 1024, S[2 * t]);
+            lds_write(hand + (2 * t + 1) * 1024, S[2 * t + 1]);
+          }
+        };
 #pragma unroll
-      for (int s = 0; s < KS; ++s) sf[s] = load_op<E>(hand + s * 2048, lane);
+        for (int t = 0; t < KS; ++t) {
 #pragma unroll
-      for (int m = 0; m < 4; ++m) o[m] = zero;
+          for (int i = 2 * t; i < 2 * t + 2; ++i) S[i] = add[i] + S[i] * whole;
 #pragma unroll
-      for (int s = 0; s < KS; ++s)
+          for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int m = 0; m < 4; ++m) o[m] = mma(sf[s], at.row(L::Q, m, s), o[m]);
-      f32x4 back_s, back_u;   // half: of the rows' columns
-      if constexpr (HALF_E) back_s = lds_read<f32x4>(units + 16 * g);
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const float since = lds_read<float>(gates + 4 * (16 * m + i16));
-        if constexpr (HALF_E) o[m] *= back_s * since;
-        else o[m] *= since;
+            for (int i = 2 * t; i < 2 * t + 2; ++i) S[i] = mma(kc[s][i], np[s], S[i]);
+          if (t > 0) publish(t - 1);
+        }
+        publish(KS - 1);
       }
-      Pair<E> pf[6];
+      end_chunk(more);
+      if (!AHEAD && more) load_keys();
+    }
+    float* last = RESULTS ? a.ht : BACK ? a.dh0 : nullptr;
+    if (last && live)
 #pragma unroll
-      for (int i = 0; i < 6; ++i) pf[i] = load_op<E>(gates + REC_P + i * REC_OP, lane);
-      __syncthreads();
-      if (more && L::NBUF == 2) fetch_second(c + step);
-      Pair<E> uf[2];
-      uf[0] = load_op<E>(hand_u, lane);
-      uf[1] = load_op<E>(hand_u + 2048, lane);
-      if constexpr (HALF_E) back_u = lds_read<f32x4>(units + 64 + 16 * g);
+      for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (state_row(i, g, r) < a.dk) last[((int64_t)doc * a.nv + h) * states + (int64_t)state_row(i, g, r) * a.dv + col] = S[i][r];
+    return;
+  }
+
+  __syncthreads();
+  if (!helps) {
+    for (int n = 0; n < chunks; ++n, c += step) {
+      const bool more = n + 1 < chunks;
+      load_next(n, more);
+      middle(more);
+      end_chunk(more);
+    }
+    return;
+  }
+  if constexpr (RESULTS) {
+    // A chunk's results are finished while the next one's u is still being made.
+    TileOps<E, DK> at;
+    at.state_places(smem + L::Q, lane);
+    f32x4 o[4], u[4], back_s, back_u;   // o transposed: rows are columns of the state, a lane has the token lane % 16
+    Pair<E> pf[6];
+    auto finish = [&](int c) {
       f32x4 p[4];
+      Pair<E> up[2];
+      const float unit = column_unit<E>(u), inv = inverse_unit<E>(unit);
+      pairs_of<E>(up, u, unit);
+      if constexpr (HALF_E) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) back_u[r] = __shfl(inv, 4 * g + r, 64);
+      }
 #pragma unroll
       for (int m = 0; m < 4; ++m) p[m] = HALF_E ? zero : o[m];
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int m = 0; m < 4; ++m)
-          if (s <= m / 2) p[m] = mma(uf[s], pf[lower_op(m, s)], p[m]);
-      if (L::NBUF == 2) tile_wait();   // for the loads, before the stores, which need not have ended at the barrier
+          if (s <= m / 2) p[m] = mma(up[s], pf[lower_op(m, s)], p[m]);
       E* oh = (E*)a.o + h * a.dv + w0 + 4 * g;
       if (w0 + 4 * g < a.dv)
 #pragma unroll
@@ -716,15 +810,54 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
             *reinterpret_cast<quad_t*>(oh + (first + t) * a.ldo) = w;
           }
         }
-    } else {
-      const int out = w0 + 4 * (lane & 3);   // columns of the lane's part of a row
-      float* to = (BACK ? a.dstates : a.states) + rec * DK * a.dvp + (lane >> 2) * a.dvp + out;
+    };
+    for (int n = 0; n < chunks; ++n, c += step) {
+      const unsigned gates = smem + (AHEAD ? (unsigned)(n & 1) * L::BUF : 0u) + L::R, ops = gates + REC_GATES + 16 * lane;
+      const bool more = n + 1 < chunks;
+      load_next(n, more);
+      Pair<E> sf[KS];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) sf[s] = load_op<E>(hand + s * 2048);
+      if (n > 0) finish(c - step);
+      if constexpr (HALF_E) back_s = lds_read<f32x4>(units + 16 * g);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) o[m] = zero;
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) o[m] = mma(sf[s], at.state_row(0, m, s), o[m]);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const float since = lds_read<float>(gates + 4 * (16 * m + i16));
+        if constexpr (HALF_E) o[m] *= back_s * since;
+        else o[m] *= since;
+      }
+#pragma unroll
+      for (int i = 0; i < 6; ++i) pf[i] = load_op<E>(ops + REC_TRIANGLE + i * REC_OP);
+      middle(more);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) u[m] = lds_read<f32x4>(hand_u + m * 1024);
+      end_chunk(more);
+    }
+    if (chunks > 0) finish(chunks - 1);
+  } else {
+    const int out = w0 + 4 * (lane & 3), q = lane >> 2;   // columns of the lane's part of a row
+    const unsigned hand0 = hand - 16 * lane, hand0_u = hand_u - 16 * lane;
+    TileOps<E, DK> at;
+    at.state_places(smem + L::Q, lane);
+    const TileOps<E, 64> at_v(smem + L::V, lane);
+    for (int n = 0; n < chunks; ++n, c += step) {
+      const unsigned gates = smem + (AHEAD ? (unsigned)(n & 1) * L::BUF : 0u) + L::R, gates4 = gates + 16 * g;
+      const bool more = n + 1 < chunks;
+      const int64_t rec = (int64_t)(chunk0 + c) * a.nv + h;
+      load_next(n, more);
+      float* to = (BACK ? a.dstates : a.states) + rec * DK * a.dvp + out;
       f32x4 part[RT];
 #pragma unroll
-      for (int i = 0; i < RT; ++i) part[i] = by_rows(hand, i, lane);
+      for (int i = 0; i < RT; ++i) part[i] = by_rows(hand0, i, lane);
       if (out < a.dvp)
 #pragma unroll
-        for (int i = 0; i < RT; ++i) *reinterpret_cast<f32x4*>(to + 16 * i * a.dvp) = part[i];
+        for (int i = 0; i < RT; ++i) *reinterpret_cast<f32x4*>(to + state_row(i, q >> 2, q & 3) * a.dvp) = part[i];
       if constexpr (BACK) {   // scale Q^T (exp(G) dO)
         Opnd<E, 1> vf[2];
         vf[0] = at_v.column(0, mine, 0);
@@ -732,7 +865,7 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
         f32x4 d[4], add[RT];
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-          const f32x4 since = lds_read<f32x4>(gates + 4 * (16 * m + 4 * g));
+          const f32x4 since = lds_read<f32x4>(gates4 + 64 * m);
 #pragma unroll
           for (int r = 0; r < 4; ++r) d[m][r] = a.scale * since[r] * (float)vf[m >> 1].t[0][4 * (m & 1) + r];
         }
@@ -744,42 +877,22 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int i = 0; i < RT; ++i) add[i] = mma(at.column(L::Q, i, s), dp[s], add[i]);
+          for (int i = 0; i < RT; ++i) add[i] = mma(at.state_column(0, i, s), dp[s], add[i]);
         wave_lds_order();   // the state has been read
 #pragma unroll
-        for (int i = 0; i < RT; ++i) lds_write(hand + i * 1024 + 16 * lane, HALF_E ? add[i] * inv : add[i]);
+        for (int i = 0; i < RT; ++i) lds_write(hand + i * 1024, HALF_E ? add[i] * inv : add[i]);
       }
-      __syncthreads();
-      if (more && L::NBUF == 2) fetch_second(c + step);
+      middle(more);
       f32x4 pu[4];
 #pragma unroll
-      for (int m = 0; m < 4; ++m) pu[m] = by_rows(hand_u, m, lane);
-      if (L::NBUF == 2) tile_wait();
-      float* to_u = (BACK ? a.y : a.u) + rec * DELTA_C * a.dvp + (lane >> 2) * a.dvp + out;
+      for (int m = 0; m < 4; ++m) pu[m] = by_rows(hand0_u, m, lane);
+      float* to_u = (BACK ? a.y : a.u) + rec * DELTA_C * a.dvp + q * a.dvp + out;
       if (out < a.dvp)
 #pragma unroll
         for (int m = 0; m < 4; ++m) *reinterpret_cast<f32x4*>(to_u + 16 * m * a.dvp) = pu[m];
-    }
-    if constexpr (L::NBUF == 2) {
-      if (!helps) tile_wait();
-      __syncthreads();
-    } else {
-      __syncthreads();
-      if (more) {
-        fetch_first(c + step, smem);
-        fetch_second(c + step);
-      }
-      tile_wait();
-      __syncthreads();
+      end_chunk(more);
     }
   }
-  float* last = RESULTS ? a.ht : BACK ? a.dh0 : nullptr;
-  if (last && live && !helps)
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (16 * i + 4 * g + r < a.dk) last[((int64_t)doc * a.nv + h) * states + (int64_t)(16 * i + 4 * g + r) * a.dv + col] = S[i][r];
 }
 
 // Block of the grid -> document and head, and columns: the blocks that share keys and matrices lie eight apart, on one XCD.
@@ -788,13 +901,13 @@ __device__ __forceinline__ WalkBlock walk_block(const DeltaRule& a, int block, i
   const int j = block / 8, pair = j / slices * 8 + block % 8;
   return WalkBlock{pair / a.nv, pair % a.nv, j % slices * width, pair < a.ndocs * a.nv};
 }
-template <typename E, int DK, int NW> __global__ __launch_bounds__(128 * NW, 1) void delta_walk_kernel(DeltaRule a, int slices) {
+template <typename E, int DK, int NW> __global__ __launch_bounds__(walk_threads(NW), 1) void delta_walk_kernel(DeltaRule a, int slices) {
   __shared__ __align__(16) char smem[WalkLds<E, DK, NW, WALK_RESULTS>::BYTES];
   const WalkBlock b = walk_block(a, blockIdx.x, slices, 16 * NW);
   if (b.in) delta_walk<E, DK, NW, WALK_RESULTS>(smem, a, b.doc, b.h, b.c0);
 }
 // Both walks of the backward: they need nothing of one another.
-template <typename E, int DK, int NW> __global__ __launch_bounds__(128 * NW, 1) void delta_walks_kernel(DeltaRule a, int slices, int blocks) {
+template <typename E, int DK, int NW> __global__ __launch_bounds__(walk_threads(NW), 1) void delta_walks_kernel(DeltaRule a, int slices, int blocks) {
   constexpr int LS = WalkLds<E, DK, NW, WALK_STATES>::BYTES, LG = WalkLds<E, DK, NW, WALK_GRADIENTS>::BYTES;
   __shared__ __align__(16) char smem[LS > LG ? LS : LG];
   const bool back = (int)blockIdx.x < blocks;
@@ -955,7 +1068,7 @@ template <typename E, int DK> __global__ __launch_bounds__(256, 1) void delta_gr
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
           const In d = grad_in<E>(at_do.row(0, m, s));
-          const Pair<M> u = load_op<M>(n_ops + (2 * m + s) * REC_OP, lane), y = load_op<M>(y_ops + (2 * m + s) * REC_OP, lane);
+          const Pair<M> u = load_op<M>(n_ops + 16 * lane + (2 * m + s) * REC_OP), y = load_op<M>(y_ops + 16 * lane + (2 * m + s) * REC_OP);
 #pragma unroll
           for (int t = 0; t < CT; ++t) {
             qi[t][m] = mma(sp[t], d, qi[t][m]);
@@ -964,11 +1077,11 @@ template <typename E, int DK> __global__ __launch_bounds__(256, 1) void delta_gr
           }
         }
         const In d_i = grad_in<E>(at_do.row(0, wave, s));
-        const Pair<M> y_i = load_op<M>(y_ops + (2 * wave + s) * REC_OP, lane);
+        const Pair<M> y_i = load_op<M>(y_ops + 16 * lane + (2 * wave + s) * REC_OP);
 #pragma unroll
         for (int n = 0; n < 4; ++n)
           if (n <= wave) {
-            const Pair<M> u_j = load_op<M>(n_ops + (2 * n + s) * REC_OP, lane);
+            const Pair<M> u_j = load_op<M>(n_ops + 16 * lane + (2 * n + s) * REC_OP);
             dp[n] = mma(d_i, u_j, dp[n]);
             da[n] = mma(y_i, u_j, da[n]);
           }
@@ -1127,8 +1240,8 @@ template <typename E, int DK> __global__ __launch_bounds__(256, 1) void delta_gr
 template <typename E, int DK, int NW> hipError_t delta_walks(hipStream_t st, const DeltaRule& a, bool backward) {
   const int slices = (int)cdiv(a.dv, 16 * NW);
   const int blocks = (int)(cdiv((int64_t)a.ndocs * a.nv, 8) * 8 * slices);
-  if (backward) hipLaunchKernelGGL((delta_walks_kernel<E, DK, NW>), dim3((unsigned)(2 * blocks)), dim3(128 * NW), 0, st, a, slices, blocks);
-  else hipLaunchKernelGGL((delta_walk_kernel<E, DK, NW>), dim3((unsigned)blocks), dim3(128 * NW), 0, st, a, slices);
+  if (backward) hipLaunchKernelGGL((delta_walks_kernel<E, DK, NW>), dim3((unsigned)(2 * blocks)), dim3(walk_threads(NW)), 0, st, a, slices, blocks);
+  else hipLaunchKernelGGL((delta_walk_kernel<E, DK, NW>), dim3((unsigned)blocks), dim3(walk_threads(NW)), 0, st, a, slices);
   return hipGetLastError();
 }
 template <typename E, int DK> hipError_t delta_run(hipStream_t st, const DeltaRule& a, bool backward) {
