@@ -14,6 +14,9 @@ SOURCES = ["stage.hip", "ministages.hip", "ops_api.hip", "elementwise.hip", "gem
            "attention_simple.hip", "attention_f32.hip", "attention_mfma.hip", "attention_mfma_f16.hip", "attention_split.hip", "attention_split_f16.hip", "docs.hip", "attention_docs.hip", "attention_docs_bf16.hip", "attention_docs_f16.hip", "attention_docs_f32.hip", "delta_rule.hip", "delta_rule_bf16.hip", "delta_rule_f16.hip", "delta_rule_f32.hip", "grad_norm.hip", "mfma_rate.hip", "lds_probe.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]
+# Matrix instructions on ordinary registers: kernels with one wave to a SIMD, which have 512, otherwise keep their accumulators in the other half and move them
+# to and fro for every use by vector instructions.
+FLAGS_OF = {s: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for s in ("delta_rule_bf16.hip", "delta_rule_f16.hip")}
 
 
 def _hipcc() -> str:
@@ -31,7 +34,7 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
 
     def compile_one(src):
         obj = os.path.join(objdir, src.replace(".hip", ".o"))
-        cmd = [hipcc, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [hipcc, *FLAGS, *FLAGS_OF.get(src, []), "-c", os.path.join(CSRC, src), "-o", obj]
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"hipcc failed for {src}:\n{r.stderr[-6000:]}")

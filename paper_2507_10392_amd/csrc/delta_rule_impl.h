@@ -269,7 +269,9 @@ __device__ __forceinline__ void load_ahead(unsigned lds, const void* base, int b
   rs[1] = __builtin_amdgcn_readfirstlane((unsigned)(at >> 32) & 0xffffu);
   rs[2] = __builtin_amdgcn_readfirstlane((unsigned)bytes);
   rs[3] = 0x00020000u;
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(rs) : "memory", "m0");
+  unsigned m0;   // as it was: the compiler may have a use for it
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(rs) : "memory");
 }
 template <typename E, int D, int ROWS, int NW> __device__ __forceinline__ void tile_ahead(const TileLoad<E, D, ROWS, NW>& t, unsigned lds, const E* head, int row0, int end, int wave) {
   typedef Tile<E, D> TL;
@@ -282,6 +284,13 @@ template <typename E, int D, int ROWS, int NW> __device__ __forceinline__ void t
     for (int k = 1; k < TL::SQUARES; ++k) from = q == k ? t.at[k] : from;
     load_ahead(lds + oct * TL::OCTET + q * 1024, head + (int64_t)row0 * t.ld, bytes, from + (unsigned)(8 * oct * t.ld * TL::SZ));
   }
+}
+// Waits until at most N of a wave's loads and stores are under way: all but its last N.
+template <int N> __device__ __forceinline__ void loads_but() {
+  static_assert(N < 64, "");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
+  __builtin_amdgcn_sched_barrier(0);
 }
 // `bytes` (a multiple of 1024) that lie together, as they are, by NW waves.
 template <int NW> __device__ __forceinline__ void bytes_ahead(unsigned lds, const char* from, int bytes, int wave, int lane) {
@@ -496,18 +505,20 @@ template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256) void d
 // its own, or the helpers' where eight waves fill the registers.  Two barriers a chunk: the first publishes the state, and values and queries of the
 // chunk, the second u, and the next chunk's keys and matrices.  All of these come straight into LDS, a chunk ahead where two of them fit.
 enum DeltaWalk { WALK_RESULTS = 0, WALK_STATES = 1, WALK_GRADIENTS = 2 };   // o and the last state; the states and u for the gradients; the states' gradients and y
-constexpr int walk_loaders(int NW) { return NW < 4 ? 1 : 0; }
+constexpr int walk_loaders(int NW) { return NW == 1 ? 2 : 0; }   // the waves fill the SIMDs, or leave them half of the registers
 constexpr int walk_threads(int NW) { return 64 * (2 * NW + walk_loaders(NW)); }
 
 template <typename E, int DK, int NW, int KIND> struct WalkLds {
   typedef Tile<E, DK> TL;
   typedef Tile<E, 64> VL;
   static constexpr int REC = KIND == WALK_STATES ? REC_P : REC_FWD;   // gates and T; and P; or gates, P^T and T^T
-  static constexpr int K = 0, R = TL::bytes(DELTA_C), BUF = R + REC;  // of these two, in turn, where they fit
   static constexpr int VSIZE = VL::bytes(DELTA_C), QSIZE = KIND == WALK_STATES ? 0 : TL::bytes(DELTA_C);
-  static constexpr int HAND = DK * 64 + 4096, UNITS = 128;            // of a wave: its state, fp32 or pairs; u; half's units
-  static constexpr int NBUF = 2 * BUF + VSIZE + QSIZE + NW * (HAND + UNITS) <= 160 * 1024 ? 2 : 1;
-  static constexpr int V = NBUF * BUF, Q = V + VSIZE, H = Q + QSIZE, U = H + NW * HAND, BYTES = U + NW * UNITS;
+  static constexpr int HAND = DK * 64 + 4096;   // of a wave: its state, fp32 or pairs; u
+  static constexpr int FIRST = TL::bytes(DELTA_C) + REC, SECOND = VSIZE + QSIZE, ROOM = 160 * 1024 - NW * HAND;
+  // Two buffers of all a chunk brings, or of its keys and matrices, or one.
+  static constexpr int NBUF = 2 * FIRST + SECOND <= ROOM ? 2 : 1, VBUF = 2 * (FIRST + SECOND) <= ROOM ? 2 : 1;
+  static constexpr int K = 0, R = TL::bytes(DELTA_C), V = NBUF * FIRST, Q = V + VSIZE, H = V + VBUF * SECOND, BYTES = H + NW * HAND;
+  static constexpr int UNITS = TL::OCTET - 128;   // half's units of wave w: the gap behind octet w of the first keys
   static_assert(BYTES <= 160 * 1024, "");
 };
 
@@ -534,14 +545,14 @@ template <typename M> __device__ __forceinline__ void write_op(unsigned lds_of_l
 template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void delta_walk(char* smem_raw, const DeltaRule& a, int doc_rank, int h, int c0) {
   typedef WalkLds<E, DK, NW, KIND> L;
   constexpr int RT = DK / 16, KS = DK / 32, LOADERS = walk_loaders(NW), FW = LOADERS ? LOADERS : NW;
-  constexpr bool HALF_E = __is_same(E, f16), BACK = KIND == WALK_GRADIENTS, RESULTS = KIND == WALK_RESULTS, AHEAD = L::NBUF == 2;
+  constexpr bool HALF_E = __is_same(E, f16), BACK = KIND == WALK_GRADIENTS, RESULTS = KIND == WALK_RESULTS, AHEAD = L::NBUF == 2, ALL_AHEAD = L::VBUF == 2, EARLY = !LOADERS || !ALL_AHEAD;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = wave % NW, g = lane >> 4, i16 = lane & 15;
   const bool chain = wave < NW, helps = !chain && wave < 2 * NW, loads = LOADERS ? wave >= 2 * NW : helps;
   const int fw = LOADERS ? wave - 2 * NW : mine;
   const int4 row = reinterpret_cast<const int4*>(a.chunks)[1 + doc_rank];   // first token, tokens, first chunk, document
   const int first = row.x, count = row.y, chunk0 = row.z, doc = row.w, chunks = (count + DELTA_C - 1) / DELTA_C;
   const int kv = h / (a.nv / a.nk), w0 = c0 + 16 * mine, col = w0 + i16;    // the wave's first column and the lane's
-  const unsigned smem = lds_address(smem_raw), hand = smem + L::H + mine * L::HAND + 16 * lane, units = smem + L::U + mine * L::UNITS;
+  const unsigned smem = lds_address(smem_raw), hand = smem + L::H + mine * L::HAND + 16 * lane, units = smem + L::UNITS + mine * Tile<E, DK>::OCTET;
   const unsigned hand_u = hand + DK * 64;
   const int step = BACK ? -1 : 1;
   const int64_t states = (int64_t)a.dk * a.dv;
@@ -550,47 +561,75 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
   // ---- loads
   const TileLoad<E, DK, DELTA_C, FW> load_k(a.ldk, lane, a.dk), load_q(a.ldq, lane, a.dk);
   const TileLoad<E, 64, DELTA_C, FW> load_v(BACK ? a.ldo : a.ldv, lane, min(a.dv - c0, 16 * NW));
-  auto fetch_first = [&](int c, unsigned to) {
+  // Loads of a wave, at least: of the keys, of the chunk's matrices, of values and queries.
+  constexpr int KEYS = TileLoad<E, DK, DELTA_C, FW>::N, MATS = BACK ? REC_GATES / 1024 / FW + 2 * REC_TRIANGLE / 1024 / FW : L::REC / 1024 / FW;
+  constexpr int SECOND = TileLoad<E, 64, DELTA_C, FW>::N + (KIND == WALK_STATES ? 0 : TileLoad<E, DK, DELTA_C, FW>::N);
+  auto fetch_keys = [&](int c, unsigned to) {
     const int t0 = first + DELTA_C * c, end = min(first + count, t0 + DELTA_C);
     tile_ahead(load_k, to + L::K, (const E*)a.k + kv * a.dk, t0, end, fw);
+  };
+  auto fetch_mats = [&](int c, unsigned to) {
     const char* rec = a.records + ((int64_t)(chunk0 + c) * a.nv + h) * (RESULTS ? REC_FWD : REC_BWD);
     if constexpr (BACK) {   // P^T and T^T lie side by side
       bytes_ahead<FW>(to + L::R, rec, REC_GATES, fw, lane);
       bytes_ahead<FW>(to + L::R + REC_GATES, rec + REC_P, 2 * REC_TRIANGLE, fw, lane);
     } else bytes_ahead<FW>(to + L::R, rec, L::REC, fw, lane);
   };
-  auto fetch_second = [&](int c) {
+  auto fetch_second = [&](int c, unsigned by) {
     const int t0 = first + DELTA_C * c, end = min(first + count, t0 + DELTA_C);
-    tile_ahead(load_v, smem + L::V, (BACK ? (const E*)a.dout : (const E*)a.v) + h * a.dv + c0, t0, end, fw);
-    if constexpr (KIND != WALK_STATES) tile_ahead(load_q, smem + L::Q, (const E*)a.q + kv * a.dk, t0, end, fw);
+    tile_ahead(load_v, smem + L::V + by, (BACK ? (const E*)a.dout : (const E*)a.v) + h * a.dv + c0, t0, end, fw);
+    if constexpr (KIND != WALK_STATES) tile_ahead(load_q, smem + L::Q + by, (const E*)a.q + kv * a.dk, t0, end, fw);
+  };
+  auto fetch_all = [&](int c) {
+    fetch_keys(c, smem);
+    fetch_mats(c, smem);
+    fetch_second(c, 0);
   };
   int c = BACK ? chunks - 1 : 0;
   if (loads && chunks > 0) {
-    fetch_first(c, smem);
-    fetch_second(c);
-    tile_wait();
+    fetch_all(c);
+    if (AHEAD && chunks > 1) {
+      fetch_keys(c + step, smem + L::FIRST);
+      if constexpr (EARLY) fetch_mats(c + step, smem + L::FIRST);
+      loads_but<KEYS + (EARLY ? MATS : 0)>();
+    } else tile_wait();
   }
-  // The barriers that end a chunk, with what the loading waves have to see arrived.
-  auto end_chunk = [&](bool more) {
-    if (AHEAD && loads && more) tile_wait();
+  // The two barriers of chunk n, and the loading waves' part of them: what they have to see arrived before, what they ask for behind.  After the second one
+  // nothing of the chunk's keys, matrices, values and queries is read from LDS any more, and the chunk after the next takes their place: the keys, which
+  // the chain reads a phase ahead, at once, the others of a loader of its own in the next phase, so that it comes to the barriers in time.
+  auto begin_chunk = [&](int n) {
+    if (ALL_AHEAD && loads && n + 1 < chunks) {
+      if constexpr (!EARLY) fetch_mats(c + step, smem + ((n + 1) & 1) * L::FIRST);
+      fetch_second(c + step, ((n + 1) & 1) * L::SECOND);
+    }
+  };
+  auto middle = [&](int n) {
+    if (AHEAD && loads && n + 1 < chunks) {   // the next keys
+      if constexpr (ALL_AHEAD) loads_but<(EARLY ? 0 : MATS) + SECOND>();
+      else tile_wait();
+    }
+    __syncthreads();
+    if (AHEAD && loads && n + 1 < chunks) {
+      if constexpr (!ALL_AHEAD) fetch_second(c + step, 0);
+      if (n + 2 < chunks) {
+        fetch_keys(c + 2 * step, smem + (n & 1) * L::FIRST);
+        if constexpr (EARLY) fetch_mats(c + 2 * step, smem + (n & 1) * L::FIRST);
+      }
+    }
+  };
+  auto end_chunk = [&](int n) {
+    if (AHEAD && loads) {   // the next matrices, values and queries
+      if (n + 2 < chunks) loads_but<KEYS + (EARLY ? MATS : 0)>();
+      else tile_wait();
+    }
     __syncthreads();
     if constexpr (!AHEAD) {
-      if (loads && more) {
-        fetch_first(c + step, smem);
-        fetch_second(c + step);
+      if (loads && n + 1 < chunks) {
+        fetch_all(c + step);
         tile_wait();
       }
       __syncthreads();
     }
-  };
-  // The loading waves' part around the second barrier.
-  auto load_next = [&](int n, bool more) {
-    if (AHEAD && loads && more) fetch_first(c + step, smem + ((n & 1) ? 0 : L::BUF));   // last read before the barrier that ended the chunk before
-  };
-  auto middle = [&](bool more) {
-    if (AHEAD && loads && more) tile_wait();
-    __syncthreads();
-    if (AHEAD && loads && more) fetch_second(c + step);
   };
 
   if (chain) {
@@ -634,28 +673,35 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
     };
     if (chunks > 0) load_keys();
     for (int n = 0; n < chunks; ++n, c += step) {
-      const unsigned buf = AHEAD ? (unsigned)(n & 1) * L::BUF : 0u, gates = smem + buf + L::R, ops = gates + REC_GATES + 16 * lane, gates4 = gates + 16 * g;
+      const unsigned buf = AHEAD ? (unsigned)(n & 1) * L::FIRST : 0u, gates = smem + buf + L::R, ops = gates + REC_GATES + 16 * lane, gates4 = gates + 16 * g;
       const bool more = n + 1 < chunks;
+      const unsigned second = ALL_AHEAD ? (unsigned)(n & 1) * L::SECOND : 0u;
+      // What comes from LDS is asked for a product ahead and not earlier: two waves of a SIMD have 256 registers each.
       f32x4 since[4], other[4];
       Opnd<E, 1> vf[2];
-      Pair<E> tf[6];   // T, or P^T
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        since[m] = lds_read<f32x4>(gates4 + 64 * m);
-        other[m] = lds_read<f32x4>(gates4 + (BACK ? 256 : 512) + 64 * m);
-      }
-      vf[0] = at_v.column(0, mine, 0);
-      vf[1] = at_v.column(0, mine, 1);
-#pragma unroll
-      for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(ops + i * REC_OP);
-      __builtin_amdgcn_sched_barrier(0);
+      Pair<E> tf[6];           // T, or P^T
       f32x4 x[4], y[4], u[4], next[4];   // K S; P^T dO
 #pragma unroll
       for (int m = 0; m < 4; ++m) x[m] = y[m] = zero;
 #pragma unroll
-      for (int s = 0; s < KS; ++s)
+      for (int s = 0; s < KS; ++s) {
 #pragma unroll
         for (int m = 0; m < 4; ++m) x[m] = mma(kf[s][m], sp[s], x[m]);
+        if (s == KS / 2 - 1) {
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            since[m] = lds_read<f32x4>(gates4 + 64 * m);
+            other[m] = lds_read<f32x4>(gates4 + (BACK ? 256 : 512) + 64 * m);
+          }
+          vf[0] = at_v.column(second, mine, 0);
+          vf[1] = at_v.column(second, mine, 1);
+          if constexpr (BACK)
+#pragma unroll
+            for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(ops + i * REC_OP);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
       f32x4 z[4];
       if constexpr (BACK) {
 #pragma unroll
@@ -663,13 +709,19 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
 #pragma unroll
           for (int m = 0; m < 4; ++m)
             if (s >= m / 2) y[m] = mma(tf[upper_op(m, s)], vf[s], y[m]);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(ops + REC_TRIANGLE + i * REC_OP);   // T^T
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
           for (int r = 0; r < 4; ++r) z[m][r] = a.scale * y[m][r] + other[m][r] * (x[m][r] * s_inv);
       } else {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(ops + i * REC_OP);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -706,8 +758,8 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
       Pair<E> np[2];
       const float n_unit = column_unit<E>(next), n_inv = inverse_unit<E>(n_unit);
       pairs_of<E>(np, next, n_unit);
-      middle(more);
-      const unsigned turn = AHEAD ? ((n & 1) ? (unsigned)-L::BUF : (unsigned)L::BUF) : 0u;
+      middle(n);
+      const unsigned turn = AHEAD ? ((n & 1) ? (unsigned)-L::FIRST : (unsigned)L::FIRST) : 0u;
       at.move_state_places(turn);
       f32x4 add[RT];
 #pragma unroll
@@ -715,7 +767,7 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
         add[i] = zero;
         if constexpr (BACK) add[i] = lds_read<f32x4>(hand + i * 1024);
       }
-      if (AHEAD && more) load_keys();
+      if (AHEAD) load_keys();   // (behind the last chunk nothing is there, and nothing takes them)
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (HALF_E) {
 #pragma unroll
@@ -748,10 +800,18 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
 #pragma unroll
             for (int i = 2 * t; i < 2 * t + 2; ++i) S[i] = mma(kc[s][i], np[s], S[i]);
           if (t > 0) publish(t - 1);
+          if constexpr (sizeof(E) == 2) {   // a matrix instruction leaves time for three others
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+              __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
         publish(KS - 1);
       }
-      end_chunk(more);
+      end_chunk(n);
       if (!AHEAD && more) load_keys();
     }
     float* last = RESULTS ? a.ht : BACK ? a.dh0 : nullptr;
@@ -767,10 +827,9 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
   __syncthreads();
   if (!helps) {
     for (int n = 0; n < chunks; ++n, c += step) {
-      const bool more = n + 1 < chunks;
-      load_next(n, more);
-      middle(more);
-      end_chunk(more);
+      begin_chunk(n);
+      middle(n);
+      end_chunk(n);
     }
     return;
   }
@@ -812,9 +871,9 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
         }
     };
     for (int n = 0; n < chunks; ++n, c += step) {
-      const unsigned gates = smem + (AHEAD ? (unsigned)(n & 1) * L::BUF : 0u) + L::R, ops = gates + REC_GATES + 16 * lane;
+      const unsigned gates = smem + (AHEAD ? (unsigned)(n & 1) * L::FIRST : 0u) + L::R, ops = gates + REC_GATES + 16 * lane;
       const bool more = n + 1 < chunks;
-      load_next(n, more);
+      begin_chunk(n);
       Pair<E> sf[KS];
 #pragma unroll
       for (int s = 0; s < KS; ++s) sf[s] = load_op<E>(hand + s * 2048);
@@ -826,6 +885,7 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
       for (int s = 0; s < KS; ++s)
 #pragma unroll
         for (int m = 0; m < 4; ++m) o[m] = mma(sf[s], at.state_row(0, m, s), o[m]);
+      if constexpr (ALL_AHEAD) at.move_state_places((n & 1) ? (unsigned)-L::SECOND : (unsigned)L::SECOND);
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
         const float since = lds_read<float>(gates + 4 * (16 * m + i16));
@@ -834,10 +894,10 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
       }
 #pragma unroll
       for (int i = 0; i < 6; ++i) pf[i] = load_op<E>(ops + REC_TRIANGLE + i * REC_OP);
-      middle(more);
+      middle(n);
 #pragma unroll
       for (int m = 0; m < 4; ++m) u[m] = lds_read<f32x4>(hand_u + m * 1024);
-      end_chunk(more);
+      end_chunk(n);
     }
     if (chunks > 0) finish(chunks - 1);
   } else {
@@ -847,10 +907,10 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
     at.state_places(smem + L::Q, lane);
     const TileOps<E, 64> at_v(smem + L::V, lane);
     for (int n = 0; n < chunks; ++n, c += step) {
-      const unsigned gates = smem + (AHEAD ? (unsigned)(n & 1) * L::BUF : 0u) + L::R, gates4 = gates + 16 * g;
+      const unsigned gates = smem + (AHEAD ? (unsigned)(n & 1) * L::FIRST : 0u) + L::R, gates4 = gates + 16 * g;
       const bool more = n + 1 < chunks;
       const int64_t rec = (int64_t)(chunk0 + c) * a.nv + h;
-      load_next(n, more);
+      begin_chunk(n);
       float* to = (BACK ? a.dstates : a.states) + rec * DK * a.dvp + out;
       f32x4 part[RT];
 #pragma unroll
@@ -860,8 +920,9 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
         for (int i = 0; i < RT; ++i) *reinterpret_cast<f32x4*>(to + state_row(i, q >> 2, q & 3) * a.dvp) = part[i];
       if constexpr (BACK) {   // scale Q^T (exp(G) dO)
         Opnd<E, 1> vf[2];
-        vf[0] = at_v.column(0, mine, 0);
-        vf[1] = at_v.column(0, mine, 1);
+        const unsigned second = ALL_AHEAD ? (unsigned)(n & 1) * L::SECOND : 0u;
+        vf[0] = at_v.column(second, mine, 0);
+        vf[1] = at_v.column(second, mine, 1);
         f32x4 d[4], add[RT];
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
@@ -878,11 +939,12 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
         for (int s = 0; s < 2; ++s)
 #pragma unroll
           for (int i = 0; i < RT; ++i) add[i] = mma(at.state_column(0, i, s), dp[s], add[i]);
+        if constexpr (ALL_AHEAD) at.move_state_places((n & 1) ? (unsigned)-L::SECOND : (unsigned)L::SECOND);
         wave_lds_order();   // the state has been read
 #pragma unroll
         for (int i = 0; i < RT; ++i) lds_write(hand + i * 1024, HALF_E ? add[i] * inv : add[i]);
       }
-      middle(more);
+      middle(n);
       f32x4 pu[4];
 #pragma unroll
       for (int m = 0; m < 4; ++m) pu[m] = by_rows(hand0_u, m, lane);
@@ -890,7 +952,7 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
       if (out < a.dvp)
 #pragma unroll
         for (int m = 0; m < 4; ++m) *reinterpret_cast<f32x4*>(to_u + 16 * m * a.dvp) = pu[m];
-      end_chunk(more);
+      end_chunk(n);
     }
   }
 }
@@ -1252,7 +1314,8 @@ template <typename E, int DK> hipError_t delta_run(hipStream_t st, const DeltaRu
   if (e != hipSuccess || a.ndocs == 0) return e;
   // Workgroups of four waves share what they bring into LDS; fewer waves where that would leave CUs without one.
   const int64_t waves = (int64_t)a.ndocs * a.nv * cdiv(a.dv, 16) * (backward ? 2 : 1);
-  e = waves >= 1024 ? delta_walks<E, DK, 4>(st, a, backward) : waves >= 512 ? delta_walks<E, DK, 2>(st, a, backward) : delta_walks<E, DK, 1>(st, a, backward);
+  constexpr bool four = sizeof(E) == 2;   // fp32 has no registers for eight waves
+  e = waves >= 1024 && four && !backward ? delta_walks<E, DK, four ? 4 : 2>(st, a, backward) : waves >= 512 ? delta_walks<E, DK, 2>(st, a, backward) : delta_walks<E, DK, 1>(st, a, backward);
   if (e != hipSuccess || !backward || a.nchunks == 0) return e;
   hipLaunchKernelGGL((delta_grad_kernel<E, DK>), dim3((unsigned)a.nchunks, (unsigned)a.nk), dim3(256), 0, st, a);
   return hipGetLastError();
