@@ -85,6 +85,21 @@ template <typename M> __device__ __forceinline__ Pair<M> pair_of(const f32x4& a,
   return o;
 }
 
+// Sums over the lanes that share lane % 16, and over those that share lane / 16, without LDS.
+__device__ __forceinline__ float rows_sum(float x) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+template <int CTRL> __device__ __forceinline__ float dpp(float x) { return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true)); }
+__device__ __forceinline__ float columns_sum(float x) {
+  x += dpp<0xb1>(x);    // neighbours
+  x += dpp<0x4e>(x);    // pairs
+  x += dpp<0x141>(x);   // the two quads of eight lanes
+  return x + dpp<0x140>(x);
+}
+
 // Half: the power of two that brings the largest of a column's values, which lie in the four lanes that share lane % 16, to 2^13 .. 2^14; else 1.
 template <typename M, int N> __device__ __forceinline__ float column_unit(const f32x4 (&x)[N]) {
   if constexpr (!__is_same(M, f16)) return 1.f;
@@ -231,7 +246,7 @@ template <typename E, int D> struct TileOps {
 // then matrices as operands, pair by pair: of T and P, lower triangles, rows by m and terms by s <= m/2; of T^T and P^T, upper ones, s >= m/2.
 constexpr int REC_GATES = 1024, REC_OP = 2048, REC_TRIANGLE = 6 * REC_OP;
 constexpr int REC_T = REC_GATES, REC_P = REC_T + REC_TRIANGLE, REC_FWD = REC_P + REC_TRIANGLE;
-constexpr int REC_TT = REC_P + REC_TRIANGLE, REC_BWD = REC_TT + REC_TRIANGLE;   // backward: P^T in the place of P
+constexpr int REC_TT = REC_P + REC_TRIANGLE, REC_G = REC_TT + REC_TRIANGLE, REC_BWD = REC_G + 512;   // backward: P^T in the place of P; G, 64 bits
 static_assert(REC_FWD == DELTA_RECORD_FWD && REC_BWD == DELTA_RECORD_BWD, "");
 __device__ __forceinline__ constexpr int lower_op(int m, int s) { return m < 2 ? m : 2 + (m - 2) * 2 + s; }
 __device__ __forceinline__ constexpr int upper_op(int m, int s) { return m < 2 ? 2 * m + s : 4 + (m - 2); }
@@ -369,11 +384,12 @@ template <typename E> __device__ __forceinline__ void fill_rows(E* p, int64_t ld
 }
 
 // A workgroup per chunk and key head; the value heads of the key head one after the other.
-template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256) void delta_prep_kernel(DeltaRule a) {
+template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256, 4) void delta_prep_kernel(DeltaRule a) {
   typedef Tile<E, DK> TL;
   constexpr int TILE = TL::bytes(DELTA_C), KS = DK / 32;
-  __shared__ __align__(16) char tiles[2 * TILE];
-  __shared__ __align__(16) float A[64 * TRI_LD], Tm[64 * TRI_LD];
+  constexpr int MATS = 2 * 64 * TRI_LD * 4;
+  __shared__ __align__(16) char tiles[2 * TILE > MATS ? 2 * TILE : MATS];   // A and T take the place of keys and queries
+  float *A = reinterpret_cast<float*>(tiles), *Tm = A + 64 * TRI_LD;
   __shared__ double G[64];
   __shared__ float B[64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i16 = lane & 15;
@@ -436,6 +452,7 @@ template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256) void d
       gates[64 + lane] = in ? decay(last, sum) : 0.f;
       gates[128 + lane] = beta;
       gates[192 + lane] = lane == 0 ? decay(last, 0.0) : 0.f;
+      if constexpr (BWD) reinterpret_cast<double*>(rec + REC_G)[lane] = sum;
     }
     __syncthreads();
     {   // A
@@ -997,192 +1014,189 @@ template <typename E> __device__ __forceinline__ Opnd<typename GradOf<E>::type, 
   } else return x;
 }
 
-// A workgroup of four waves per chunk and key head; the value heads of the key head one after the other, their dq and dk in the same registers.  A wave has a
-// quarter of the head's columns of dq and dk, for all tokens: results are transposed (rows are columns of the head, a lane has a token), so that a
-// state's rows are read by one wave only and a token's factors are a lane's own.  Columns of the value head come in blocks of 64.
-template <typename E, int DK> __global__ __launch_bounds__(256, 1) void delta_grad_kernel(DeltaRule a) {
+// A workgroup per chunk and key head; the value heads of the key head one after the other, their dq and dk in the same registers.  A wave has 16 of the
+// head's columns of dq and dk, for all tokens: results are transposed (rows are columns of the head, a lane has a token), so that a
+// state's rows are read by one wave only and a token's factors are a lane's own.  The matrices of tokens by tokens are shared out by tiles: wave
+// w has the row tile w % 4, and of its column tiles those of its parity where there are eight waves.  Columns of the value head come in blocks of 64.
+constexpr int grad_waves(int DK) { return DK / 16; }
+template <typename E, int DK, bool SHARED> __global__ __launch_bounds__(64 * grad_waves(DK), 1) void delta_grad_kernel(DeltaRule a) {
   typedef typename GradOf<E>::type M;
   typedef Opnd<M, GRAD_IN<E>> In;
   typedef Tile<E, DK> TL;
   typedef Tile<E, 64> VL;
-  constexpr int TILE = TL::bytes(DELTA_C), KS = DK / 32, CT = DK / 64, OPS = 8 * REC_OP;   // OPS: 64 tokens by 64 columns as operands
-  constexpr int STAGE = VL::bytes(DELTA_C) + 2 * OPS, MATS = 2 * 64 * TRI_LD * 4;
-  __shared__ __align__(16) char smem_raw[2 * TILE + (STAGE > MATS ? STAGE : MATS)];
+  constexpr int W = grad_waves(DK), PARTS = W / 4, TILE = TL::bytes(DELTA_C), KS = DK / 32, OPS = 8 * REC_OP;   // OPS: 64 tokens by 64 columns as operands
+  struct Sums { float m[2][64][TRI_LD], dots[W][3][64], cols[4][64], rows[PARTS][2][64], whole[W]; };   // over the columns' blocks, when these are through
+  constexpr int BLOCKS = VL::bytes(DELTA_C) + 2 * OPS, STAGE = sizeof(Sums) > BLOCKS ? sizeof(Sums) : BLOCKS;
+  __shared__ __align__(16) char smem_raw[2 * TILE + STAGE + 20 * REC_OP];
   __shared__ double G[64];
-  __shared__ float gate[4][64], dots[4][3][64], cols[4][64], rows[3][64], whole_dots[4];
+  __shared__ float gate[4][64], yvs[2][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i16 = lane & 15;
   const ChunkRow c = chunk_row(a, blockIdx.x);
   if (c.count <= 0) return;
-  const int kv = blockIdx.y, group = a.nv / a.nk, end = c.first + c.count;
+  const int kv = blockIdx.y, group = SHARED ? a.nv / a.nk : 1, end = c.first + c.count, tile = wave & 3, part = wave >> 2;
   const unsigned smem = lds_address(smem_raw), stage = 2 * TILE;
   {
-    const TileLoad<E, DK, DELTA_C, 4> load_k(a.ldk, lane, a.dk), load_q(a.ldq, lane, a.dk);
-    load_k.fetch(smem, (const E*)a.k + kv * a.dk, c.first, end, wave);
-    load_q.fetch(smem + TILE, (const E*)a.q + kv * a.dk, c.first, end, wave);
+    const TileLoad<E, DK, DELTA_C, W> load_k(a.ldk, lane, a.dk), load_q(a.ldq, lane, a.dk);
+    tile_ahead(load_k, smem, (const E*)a.k + kv * a.dk, c.first, end, wave);
+    tile_ahead(load_q, smem + TILE, (const E*)a.q + kv * a.dk, c.first, end, wave);
   }
   const TileOps<E, DK> at(smem, lane);
   const TileOps<E, 64> at_do(smem + stage, lane);
-  const unsigned n_ops = smem + stage + VL::bytes(DELTA_C), y_ops = n_ops + OPS;
-  float *Mm = reinterpret_cast<float*>(smem_raw + stage), *H = Mm + 64 * TRI_LD;
+  const unsigned n_ops = smem + stage + VL::bytes(DELTA_C) + 16 * lane, y_ops = n_ops + OPS;
+  Sums& sums = *reinterpret_cast<Sums*>(smem_raw + stage);
+  float *Mm = sums.m[0][0], *H = sums.m[1][0];
+  const unsigned m_ops = smem + stage + STAGE + 16 * lane;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-  f32x4 kk[4], qk[4], dq[CT][4], dk[CT][4];
+  f32x4 dq[4], dk[4];
 #pragma unroll
-  for (int n = 0; n < 4; ++n) {
-    kk[n] = qk[n] = zero;
-#pragma unroll
-    for (int t = 0; t < CT; ++t) dq[t][n] = dk[t][n] = zero;
-  }
-  tile_wait();
-  __syncthreads();
-#pragma unroll
-  for (int s = 0; s < KS; ++s) {
-    const Opnd<E, 1> k_i = at.row(0, wave, s), q_i = at.row(TILE, wave, s);
-#pragma unroll
-    for (int n = 0; n < 4; ++n)
-      if (n <= wave) {
-        const Opnd<E, 1> k_j = at.row(0, n, s);
-        kk[n] = mma(k_i, k_j, kk[n]);
-        qk[n] = mma(q_i, k_j, qk[n]);
-      }
-  }
+  for (int n = 0; n < 4; ++n) dq[n] = dk[n] = zero;
   for (int hg = 0; hg < group; ++hg) {
     const int h = kv * group + hg;
     const int64_t rec = (int64_t)blockIdx.x * a.nv + h;
     const float *S = a.states + rec * DK * a.dvp, *dS = a.dstates + rec * DK * a.dvp, *U = a.u + rec * DELTA_C * a.dvp, *Y = a.y + rec * DELTA_C * a.dvp;
-    __syncthreads();   // the head before is done with the LDS
-    if (wave == 0) {
-      const bool in = lane < c.count;
-      const int64_t t = (int64_t)(c.first + (in ? lane : 0)) * a.nv + h;
-      const float gl = in ? a.g[t] * 1.4426950408889634f : 0.f;
-      const double sum = running_sum((double)(gl < DELTA_FORGETS ? DELTA_FORGETS : gl), lane), last = __shfl(sum, 63, 64);
-      G[lane] = sum;
-      gate[0][lane] = in ? decay(sum, 0.0) : 0.f;
-      gate[1][lane] = in ? decay(last, sum) : 0.f;
-      gate[2][lane] = in ? a.beta[t] : 0.f;
-      gate[3][lane] = decay(last, 0.0);
+    if (SHARED) __syncthreads();   // the head before is done with the LDS
+    if (wave < 4) {
+      const char* from = a.records + rec * REC_BWD;
+      gate[wave][lane] = reinterpret_cast<const float*>(from)[64 * wave + lane];
+      if (wave == 0) G[lane] = reinterpret_cast<const double*>(from + REC_G)[lane];
     }
-    f32x4 qi[CT][4], ks[CT][4], kn[CT][4], dp[4], da[4];
+    f32x4 qi[4], ks[4], kn[4], dp[4 / PARTS], da[4 / PARTS];
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      dp[n] = da[n] = zero;
+    for (int n = 0; n < 4; ++n) qi[n] = ks[n] = kn[n] = zero;
 #pragma unroll
-      for (int t = 0; t < CT; ++t) qi[t][n] = ks[t][n] = kn[t][n] = zero;
-    }
+    for (int n = 0; n < 4 / PARTS; ++n) dp[n] = da[n] = zero;
     float sds = 0.f, yv = 0.f;
-    const int my_t = 16 * wave + i16;   // the token whose rows of U and Y this lane brings
+    const int my_t = 16 * tile + i16;   // the token whose rows of U and Y this lane brings, of 64 columns or, as one of eight waves, of 32
     const bool my_in = my_t < c.count;
+    typedef E quad_t __attribute__((ext_vector_type(4)));
+    f32x4 sx[2], sy[2];                 // rows of S and dS, 32 columns ahead
+    auto load_states = [&](int col0) {
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const int col = col0 + 16 * p + 4 * g, at_row = (16 * wave + i16) * a.dvp + col;
+        sx[p] = sy[p] = zero;
+        if (col < a.dvp) {
+          sx[p] = *reinterpret_cast<const f32x4*>(S + at_row);
+          sy[p] = *reinterpret_cast<const f32x4*>(dS + at_row);
+        }
+      }
+    };
+    f32x4 u[2 / PARTS][2], y[2 / PARTS][2];   // rows of U, Y and v, 64 columns ahead
+    quad_t v[2 / PARTS][2];
+    auto load_rows = [&](int b0) {
+#pragma unroll
+      for (int s = 0; s < 2 / PARTS; ++s)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const int col = b0 + 32 * (s + part) + 16 * p + 4 * g;
+          u[s][p] = y[s][p] = zero;
+          v[s][p] = quad_t{};
+          if (col < a.dvp) {
+            u[s][p] = *reinterpret_cast<const f32x4*>(U + my_t * a.dvp + col);
+            y[s][p] = *reinterpret_cast<const f32x4*>(Y + my_t * a.dvp + col);
+          }
+          if (my_in && col < a.dv) v[s][p] = *reinterpret_cast<const quad_t*>((const E*)a.v + (int64_t)(c.first + my_t) * a.ldv + h * a.dv + col);
+        }
+    };
+    load_rows(0);
+    load_states(0);
     for (int b0 = 0; b0 < a.dv; b0 += 64) {
       __syncthreads();   // the block before has been read; the gates are there
       {
-        const TileLoad<E, 64, DELTA_C, 4> load(a.ldo, lane, min(a.dv - b0, 64));
-        load.fetch(smem + stage, (const E*)a.dout + h * a.dv + b0, c.first, end, wave);
+        const TileLoad<E, 64, DELTA_C, W> load(a.ldo, lane, min(a.dv - b0, 64));
+        tile_ahead(load, smem + stage, (const E*)a.dout + h * a.dv + b0, c.first, end, wave);
       }
       const float beta = gate[2][my_t];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        f32x4 u[2], y[2];
+      for (int s = 0; s < 2 / PARTS; ++s) {
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
-          const int col = b0 + 32 * s + 16 * p + 4 * g;
-          u[p] = y[p] = zero;
-          if (col < a.dvp) {
-            u[p] = *reinterpret_cast<const f32x4*>(U + my_t * a.dvp + col);
-            y[p] = *reinterpret_cast<const f32x4*>(Y + my_t * a.dvp + col);
-          }
-          if (my_in && col < a.dv) {
-            typedef E quad_t __attribute__((ext_vector_type(4)));
-            const int64_t t = c.first + my_t;
-            const quad_t v = *reinterpret_cast<const quad_t*>((const E*)a.v + t * a.ldv + h * a.dv + col);
-            quad_t w;
+          const int col = b0 + 32 * (s + part) + 16 * p + 4 * g;
+          quad_t w;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              yv = fmaf(y[p][e], (float)v[e], yv);
-              w[e] = from_f<E>(fp32_value(beta * y[p][e]));
-            }
-            *reinterpret_cast<quad_t*>((E*)a.dval + t * a.lddv + h * a.dv + col) = w;
+          for (int e = 0; e < 4; ++e) {
+            yv = fmaf(y[s][p][e], (float)v[s][p][e], yv);
+            w[e] = from_f<E>(fp32_value(beta * y[s][p][e]));
           }
+          if (my_in && col < a.dv) *reinterpret_cast<quad_t*>((E*)a.dval + (int64_t)(c.first + my_t) * a.lddv + h * a.dv + col) = w;
         }
-        store_op<M>(smem_raw + (n_ops - smem) + (2 * wave + s) * REC_OP, pair_of<M>(u[0], u[1]), lane);
-        store_op<M>(smem_raw + (y_ops - smem) + (2 * wave + s) * REC_OP, pair_of<M>(y[0], y[1]), lane);
+        write_op<M>(n_ops + (2 * tile + s + part) * REC_OP, pair_of<M>(u[s][0], u[s][1]));
+        write_op<M>(y_ops + (2 * tile + s + part) * REC_OP, pair_of<M>(y[s][0], y[s][1]));
       }
       tile_wait();
       __syncthreads();
+      __builtin_amdgcn_sched_barrier(0);
+      load_rows(b0 + 64);   // (zeros behind the last)
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        Pair<M> sp[CT], dsp[CT];
 #pragma unroll
-        for (int t = 0; t < CT; ++t) {
-          f32x4 x[2], y[2];
+        for (int p = 0; p < 2; ++p)
 #pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            const int col = b0 + 32 * s + 16 * p + 4 * g, at_row = (16 * (CT * wave + t) + i16) * a.dvp + col;
-            x[p] = y[p] = zero;
-            if (col < a.dvp) {
-              x[p] = *reinterpret_cast<const f32x4*>(S + at_row);
-              y[p] = *reinterpret_cast<const f32x4*>(dS + at_row);
-            }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sds = fmaf(x[p][e], y[p][e], sds);
-          }
-          sp[t] = pair_of<M>(x[0], x[1]);
-          dsp[t] = pair_of<M>(y[0], y[1]);
-        }
+          for (int e = 0; e < 4; ++e) sds = fmaf(sx[p][e], sy[p][e], sds);
+        const Pair<M> sp = pair_of<M>(sx[0], sx[1]), dsp = pair_of<M>(sy[0], sy[1]);
+        __builtin_amdgcn_sched_barrier(0);
+        load_states(b0 + 32 * (s + 1));
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
           const In d = grad_in<E>(at_do.row(0, m, s));
-          const Pair<M> u = load_op<M>(n_ops + 16 * lane + (2 * m + s) * REC_OP), y = load_op<M>(y_ops + 16 * lane + (2 * m + s) * REC_OP);
-#pragma unroll
-          for (int t = 0; t < CT; ++t) {
-            qi[t][m] = mma(sp[t], d, qi[t][m]);
-            ks[t][m] = mma(sp[t], y, ks[t][m]);
-            kn[t][m] = mma(dsp[t], u, kn[t][m]);
-          }
+          const Pair<M> un = load_op<M>(n_ops + (2 * m + s) * REC_OP), yn = load_op<M>(y_ops + (2 * m + s) * REC_OP);
+          qi[m] = mma(sp, d, qi[m]);
+          ks[m] = mma(sp, yn, ks[m]);
+          kn[m] = mma(dsp, un, kn[m]);
         }
-        const In d_i = grad_in<E>(at_do.row(0, wave, s));
-        const Pair<M> y_i = load_op<M>(y_ops + 16 * lane + (2 * wave + s) * REC_OP);
+        const In d_i = grad_in<E>(at_do.row(0, tile, s));
+        const Pair<M> y_i = load_op<M>(y_ops + (2 * tile + s) * REC_OP);
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
-          if (n <= wave) {
-            const Pair<M> u_j = load_op<M>(n_ops + 16 * lane + (2 * n + s) * REC_OP);
+        for (int n = 0; n < 4 / PARTS; ++n)
+          if (PARTS * n + part <= tile) {
+            const Pair<M> u_j = load_op<M>(n_ops + (2 * (PARTS * n + part) + s) * REC_OP);
             dp[n] = mma(d_i, u_j, dp[n]);
             da[n] = mma(y_i, u_j, da[n]);
           }
       }
     }
-    __syncthreads();   // Mm and H lie over the blocks
-    // the states' shares, and their products with q and k
-    {
-      float dot[4][3];
+    f32x4 kk[4 / PARTS], qk[4 / PARTS];
 #pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const float since = gate[0][16 * m + i16], until = gate[1][16 * m + i16], beta = gate[2][16 * m + i16];
-        dot[m][0] = dot[m][1] = dot[m][2] = 0.f;
+    for (int n = 0; n < 4 / PARTS; ++n) kk[n] = qk[n] = zero;
 #pragma unroll
-        for (int t = 0; t < CT; ++t) {
-          const f32x4 k4 = at.quad(0, m, CT * wave + t), q4 = at.quad(TILE, m, CT * wave + t);
+    for (int s = 0; s < KS; ++s) {
+      const Opnd<E, 1> k_i = at.row(0, tile, s), q_i = at.row(TILE, tile, s);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const float q_state = a.scale * since * qi[t][m][r], k_state = -since * ks[t][m][r], k_next = until * kn[t][m][r];
-            dot[m][0] = fmaf(q4[r], q_state, dot[m][0]);
-            dot[m][1] = fmaf(k4[r], k_state, dot[m][1]);
-            dot[m][2] = fmaf(k4[r], k_next, dot[m][2]);
-            dq[t][m][r] += q_state;
-            dk[t][m][r] += fmaf(beta, k_state, k_next);
-          }
+      for (int n = 0; n < 4 / PARTS; ++n)
+        if (PARTS * n + part <= tile) {
+          const Opnd<E, 1> k_j = at.row(0, PARTS * n + part, s);
+          kk[n] = mma(k_i, k_j, kk[n]);
+          qk[n] = mma(q_i, k_j, qk[n]);
         }
-#pragma unroll
-        for (int x = 0; x < 3; ++x) {
-          dot[m][x] += __shfl_xor(dot[m][x], 16, 64);
-          dot[m][x] += __shfl_xor(dot[m][x], 32, 64);
-          if (lane < 16) dots[wave][x][16 * m + lane] = dot[m][x];
-        }
-      }
-      sds = wave_sum(sds);
-      yv += __shfl_xor(yv, 16, 64);
-      yv += __shfl_xor(yv, 32, 64);
-      if (lane == 0) whole_dots[wave] = sds;
-      if (lane < 16) rows[2][16 * wave + lane] = yv;
     }
+    __syncthreads();   // the sums lie over the blocks
+    // the states' shares, and their products with q and k
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const float since = gate[0][16 * m + i16], until = gate[1][16 * m + i16], beta = gate[2][16 * m + i16];
+      float dot[3] = {0.f, 0.f, 0.f};
+      const f32x4 k4 = at.quad(0, m, wave), q4 = at.quad(TILE, m, wave);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float q_state = a.scale * since * qi[m][r], k_state = -since * ks[m][r], k_next = until * kn[m][r];
+        dot[0] = fmaf(q4[r], q_state, dot[0]);
+        dot[1] = fmaf(k4[r], k_state, dot[1]);
+        dot[2] = fmaf(k4[r], k_next, dot[2]);
+        dq[m][r] += q_state;
+        dk[m][r] += fmaf(beta, k_state, k_next);
+      }
+#pragma unroll
+      for (int x = 0; x < 3; ++x) {
+        dot[x] = rows_sum(dot[x]);
+        if (lane < 16) sums.dots[wave][x][16 * m + lane] = dot[x];
+      }
+    }
+    sds = wave_sum(sds);
+    yv = rows_sum(yv);
+    if (lane == 0) sums.whole[wave] = sds;
+    if (lane < 16) yvs[part][16 * tile + lane] = yv;
     // M and H, and the sums by rows and by columns that the decays and beta get
     {
       float by_row[4] = {0.f, 0.f, 0.f, 0.f}, by_beta[4] = {0.f, 0.f, 0.f, 0.f};
@@ -1190,18 +1204,18 @@ template <typename E, int DK> __global__ __launch_bounds__(256, 1) void delta_gr
       float bi[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        gi[r] = G[16 * wave + 4 * g + r];
-        bi[r] = gate[2][16 * wave + 4 * g + r];
+        gi[r] = G[16 * tile + 4 * g + r];
+        bi[r] = gate[2][16 * tile + 4 * g + r];
       }
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const int j = 16 * n + i16;
+      for (int n = 0; n < 4 / PARTS; ++n) {
+        const int nt = PARTS * n + part, j = 16 * nt + i16;
         const double gj = G[j];
         float by_col = 0.f;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int i = 16 * wave + 4 * g + r;
-          const float dec = j <= i && n <= wave ? decay(gi[r], gj) : 0.f;
+          const int i = 16 * tile + 4 * g + r;
+          const float dec = j <= i && nt <= tile ? decay(gi[r], gj) : 0.f;
           const float m = a.scale * dec * dp[n][r], hb = j < i ? -dec * da[n][r] : 0.f;
           Mm[i * TRI_LD + j] = m;
           H[i * TRI_LD + j] = bi[r] * hb;
@@ -1210,92 +1224,93 @@ template <typename E, int DK> __global__ __launch_bounds__(256, 1) void delta_gr
           by_beta[r] = fmaf(hb, kk[n][r], by_beta[r]);
           by_col += e;
         }
-        by_col += __shfl_xor(by_col, 16, 64);
-        by_col += __shfl_xor(by_col, 32, 64);
-        if (lane < 16) cols[wave][j] = by_col;
+        by_col = rows_sum(by_col);
+        if (lane < 16) sums.cols[tile][j] = by_col;
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-#pragma unroll
-        for (int o = 1; o < 16; o <<= 1) {
-          by_row[r] += __shfl_xor(by_row[r], o, 64);
-          by_beta[r] += __shfl_xor(by_beta[r], o, 64);
-        }
+        by_row[r] = columns_sum(by_row[r]);
+        by_beta[r] = columns_sum(by_beta[r]);
         if (i16 == 0) {
-          rows[0][16 * wave + 4 * g + r] = by_row[r];
-          rows[1][16 * wave + 4 * g + r] = by_beta[r];
+          sums.rows[part][0][16 * tile + 4 * g + r] = by_row[r];
+          sums.rows[part][1][16 * tile + 4 * g + r] = by_beta[r];
         }
       }
     }
     __syncthreads();
-    if (wave == 0) {
-      double d = rows[0][lane], kn_sum = 0.0, sds_sum = 0.0;
-      float kst = 0.f, knx = 0.f, qst = 0.f;
+    if (wave == W - 1) {
+      double d = 0.0, kn_sum = 0.0, sds_sum = 0.0;
+      float kst = 0.f, knx = 0.f, qst = 0.f, db = 0.f;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        d -= cols[w][lane];
-        qst += dots[w][0][lane];
-        kst += dots[w][1][lane];
-        knx += dots[w][2][lane];
-        sds_sum += whole_dots[w];
+      for (int w = 0; w < 4; ++w) d -= sums.cols[w][lane];
+#pragma unroll
+      for (int w = 0; w < PARTS; ++w) {
+        d += sums.rows[w][0][lane];
+        db += sums.rows[w][1][lane] + yvs[w][lane];
+      }
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        qst += sums.dots[w][0][lane];
+        kst += sums.dots[w][1][lane];
+        knx += sums.dots[w][2][lane];
+        sds_sum += sums.whole[w];
       }
       kn_sum = knx;
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) kn_sum += __shfl_xor(kn_sum, o, 64);
       d += (double)qst + (double)gate[2][lane] * kst - knx;
-      if (lane == 63) d += kn_sum + (double)gate[3][lane] * sds_sum;
+      if (lane == 63) d += kn_sum + (double)gate[3][0] * sds_sum;
       // from each token to the end
       const double upto = running_sum(d, lane), all = __shfl(upto, 63, 64);
       if (lane < c.count) {
         const int64_t t = (int64_t)(c.first + lane) * a.nv + h;
         a.dg[t] = (float)(all - upto + d);
-        a.dbeta[t] = rows[2][lane] + kst + rows[1][lane];
+        a.dbeta[t] = db + kst;
       }
     }
+    // M, M^T and H + H^T as operands, shared out over the waves: eight of the last, six of each of the others
+    for (int k = wave; k < 20; k += W) {
+      const int j = k < 8 ? k : k < 14 ? k - 8 : k - 14, m = k < 8 ? j >> 1 : k < 14 ? (j < 2 ? j : 1 + j / 2) : (j < 4 ? j >> 1 : j - 2),
+                s = k < 8 ? j & 1 : k < 14 ? (j < 2 ? 0 : j & 1) : (j < 4 ? j & 1 : 1);
+      const int from = 32 * s + 4 * g, mine = 16 * m + i16;
+      const float* mat = k < 8 ? H : Mm;
+      f32x4 x[2] = {zero, zero};
 #pragma unroll
-    for (int m = 0; m < 4; ++m)
+      for (int p = 0; p < 2; ++p) {
+        if (k < 14) x[p] = *reinterpret_cast<const f32x4*>(mat + mine * TRI_LD + from + 16 * p);
+        if (k < 8 || k >= 14)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const int from = 32 * s + 4 * g, mine = 16 * m + i16;
-        f32x4 across[2], down[2], h_across[2], h_down[2];
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          across[p] = *reinterpret_cast<const f32x4*>(Mm + mine * TRI_LD + from + 16 * p);
-          h_across[p] = *reinterpret_cast<const f32x4*>(H + mine * TRI_LD + from + 16 * p);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            down[p][e] = Mm[(from + 16 * p + e) * TRI_LD + mine];
-            h_down[p][e] = H[(from + 16 * p + e) * TRI_LD + mine];
-          }
-        }
-        const Pair<M> both = pair_of<M>(h_across[0] + h_down[0], h_across[1] + h_down[1]), m_across = pair_of<M>(across[0], across[1]),
-                      m_down = pair_of<M>(down[0], down[1]);
-#pragma unroll
-        for (int t = 0; t < CT; ++t) {
-          const In k_col = grad_in<E>(at.column(0, CT * wave + t, s));
-          dk[t][m] = mma(k_col, both, dk[t][m]);
-          if (2 * s <= m) dq[t][m] = mma(k_col, m_across, dq[t][m]);
-          if (2 * s + 1 >= m) dk[t][m] = mma(grad_in<E>(at.column(TILE, CT * wave + t, s)), m_down, dk[t][m]);
-        }
+          for (int e = 0; e < 4; ++e) x[p][e] += mat[(from + 16 * p + e) * TRI_LD + mine];
       }
+      write_op<M>(m_ops + k * REC_OP, pair_of<M>(x[0], x[1]));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const In k_col = grad_in<E>(at.column(0, wave, s)), q_col = grad_in<E>(at.column(TILE, wave, s));
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        dk[m] = mma(k_col, load_op<M>(m_ops + (2 * m + s) * REC_OP), dk[m]);
+        if (s <= m / 2) dq[m] = mma(k_col, load_op<M>(m_ops + (8 + lower_op(m, s)) * REC_OP), dq[m]);
+        if (s >= m / 2) dk[m] = mma(q_col, load_op<M>(m_ops + (14 + upper_op(m, s)) * REC_OP), dk[m]);
+      }
+    }
   }
   typedef E quad_t __attribute__((ext_vector_type(4)));
 #pragma unroll
-  for (int t = 0; t < CT; ++t)
+  for (int m = 0; m < 4; ++m) {
+    const int col = 16 * wave + 4 * g, tok = 16 * m + i16;
+    if (tok < c.count && col < a.dk) {
+      quad_t x, y;
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      const int col = 16 * (CT * wave + t) + 4 * g, tok = 16 * m + i16;
-      if (tok < c.count && col < a.dk) {
-        quad_t x, y;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          x[r] = from_f<E>(fp32_value(dq[t][m][r]));
-          y[r] = from_f<E>(fp32_value(dk[t][m][r]));
-        }
-        *reinterpret_cast<quad_t*>((E*)a.dq + (int64_t)(c.first + tok) * a.lddq + kv * a.dk + col) = x;
-        *reinterpret_cast<quad_t*>((E*)a.dkey + (int64_t)(c.first + tok) * a.lddk + kv * a.dk + col) = y;
+      for (int r = 0; r < 4; ++r) {
+        x[r] = from_f<E>(fp32_value(dq[m][r]));
+        y[r] = from_f<E>(fp32_value(dk[m][r]));
       }
+      *reinterpret_cast<quad_t*>((E*)a.dq + (int64_t)(c.first + tok) * a.lddq + kv * a.dk + col) = x;
+      *reinterpret_cast<quad_t*>((E*)a.dkey + (int64_t)(c.first + tok) * a.lddk + kv * a.dk + col) = y;
     }
+  }
 }
 
 // ------------------------------------------------------------------------------------------ launches
@@ -1317,7 +1332,9 @@ template <typename E, int DK> hipError_t delta_run(hipStream_t st, const DeltaRu
   constexpr bool four = sizeof(E) == 2;   // fp32 has no registers for eight waves
   e = waves >= 1024 && four && !backward ? delta_walks<E, DK, four ? 4 : 2>(st, a, backward) : waves >= 512 ? delta_walks<E, DK, 2>(st, a, backward) : delta_walks<E, DK, 1>(st, a, backward);
   if (e != hipSuccess || !backward || a.nchunks == 0) return e;
-  hipLaunchKernelGGL((delta_grad_kernel<E, DK>), dim3((unsigned)a.nchunks, (unsigned)a.nk), dim3(256), 0, st, a);
+  const dim3 grid((unsigned)a.nchunks, (unsigned)a.nk);
+  if (a.nv == a.nk) hipLaunchKernelGGL((delta_grad_kernel<E, DK, false>), grid, dim3(64 * grad_waves(DK)), 0, st, a);
+  else hipLaunchKernelGGL((delta_grad_kernel<E, DK, true>), grid, dim3(64 * grad_waves(DK)), 0, st, a);
   return hipGetLastError();
 }
 template <typename E> hipError_t delta_rule_of(hipStream_t st, const DeltaRule& a, bool backward) {

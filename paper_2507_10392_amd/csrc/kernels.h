@@ -252,7 +252,7 @@ hipError_t rope_axes(hipStream_t st, DType dt, int T, int d, const RopeHeads& q,
 // float[ndocs, nv, dk, dv].
 constexpr int DELTA_CHUNK = 64;   // tokens of a document that are worked on together
 constexpr int DELTA_FILL = 16;    // blocks that clear the rows of no document
-constexpr int DELTA_RECORD_FWD = 25600, DELTA_RECORD_BWD = 37888;   // bytes of a chunk's own matrices
+constexpr int DELTA_RECORD_FWD = 25600, DELTA_RECORD_BWD = 38400;   // bytes of a chunk's own matrices
 struct DeltaRule {
   int T, nk, nv, dk, dv, ndocs;
   const void *q, *k, *v; int64_t ldq, ldk, ldv;
