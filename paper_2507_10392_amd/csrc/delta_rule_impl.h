@@ -515,38 +515,31 @@ template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256, 4) voi
 }
 
 // ------------------------------------------------------------------------------------------ from chunk to chunk
-// A workgroup walks a document's chunks for one value head and 16 NW columns of its state.  NW of its waves carry the state, 16 columns of all rows each, in
-// their registers, and it never leaves them: a result's registers, two above one another, are the next product's operand.  What a chunk waits for
-// is the chain of these waves: K S, T times what that leaves, K^T times that, the new state as pairs.  All else is done by others: each has a
-// helper (the results, what the gradients' walk adds to its state, the stores of states), with which it shares 12 KB of LDS, and the loads are a wave's of
-// its own, or the helpers' where eight waves fill the registers.  Two barriers a chunk: the first publishes the state, and values and queries of the
-// chunk, the second u, and the next chunk's keys and matrices.  All of these come straight into LDS, a chunk ahead where two of them fit.
+// A workgroup walks a document's chunks for one value head and 16 NW columns of its state.  Two waves carry 16 columns of the state, a half of its rows
+// each, in their registers, and it never leaves them: a result's registers, two above one another, are the next product's operand.  What a chunk
+// waits for is the chain of these waves: K S, a half of the tokens each; what that leaves, Z, exchanged; T Z, by both; K^T of that into the
+// own rows; the new state as pairs, exchanged.  All else is done by others: each such pair of waves has a helper (T Z once more for the results, what the gradients'
+// walk adds to its state, the stores of states and u), with 12 KB of LDS between the three, and the loads are a wave's of its own, or the helpers'.
+// Two barriers a chunk: the first publishes the state, and matrices, values and queries of the chunk, the second Z, and the next chunk's
+// keys.  All of these come straight into LDS, a chunk ahead where two of them fit.
 enum DeltaWalk { WALK_RESULTS = 0, WALK_STATES = 1, WALK_GRADIENTS = 2 };   // o and the last state; the states and u for the gradients; the states' gradients and y
-constexpr int walk_loaders(int NW) { return NW == 1 ? 2 : 0; }   // the waves fill the SIMDs, or leave them half of the registers
-constexpr int walk_threads(int NW) { return 64 * (2 * NW + walk_loaders(NW)); }
+constexpr int walk_loaders(int NW) { return NW == 1 ? 4 : NW == 2 ? 2 : 0; }   // a wave issues a load of 1 KB in 50 to 70 cycles
+constexpr int walk_threads(int NW) { return 64 * (3 * NW + walk_loaders(NW)); }
 
 template <typename E, int DK, int NW, int KIND> struct WalkLds {
   typedef Tile<E, DK> TL;
   typedef Tile<E, 64> VL;
   static constexpr int REC = KIND == WALK_STATES ? REC_P : REC_FWD;   // gates and T; and P; or gates, P^T and T^T
   static constexpr int VSIZE = VL::bytes(DELTA_C), QSIZE = KIND == WALK_STATES ? 0 : TL::bytes(DELTA_C);
-  static constexpr int HAND = DK * 64 + 4096;   // of a wave: its state, fp32 or pairs; u
+  static constexpr int HAND = DK * 64 + 4096 + (KIND == WALK_GRADIENTS ? DK * 64 : 0);   // of 16 columns: the state as pairs (fp32: as it is); Z; what is added to it
   static constexpr int FIRST = TL::bytes(DELTA_C) + REC, SECOND = VSIZE + QSIZE, ROOM = 160 * 1024 - NW * HAND;
   // Two buffers of all a chunk brings, or of its keys and matrices, or one.
   static constexpr int NBUF = 2 * FIRST + SECOND <= ROOM ? 2 : 1, VBUF = 2 * (FIRST + SECOND) <= ROOM ? 2 : 1;
   static constexpr int K = 0, R = TL::bytes(DELTA_C), V = NBUF * FIRST, Q = V + VSIZE, H = V + VBUF * SECOND, BYTES = H + NW * HAND;
-  static constexpr int UNITS = TL::OCTET - 128;   // half's units of wave w: the gap behind octet w of the first keys
+  static constexpr int UNITS = TL::OCTET - 128;   // half's units of 16 columns: the gap behind an octet of the first keys
   static_assert(BYTES <= 160 * 1024, "");
 };
 
-// Results i of a wave, which lie in LDS as a lane's registers: of row lane / 4 the columns 4 (lane % 4) ..
-__device__ __forceinline__ f32x4 by_rows(unsigned from, int i, int lane) {
-  const int q = lane >> 2;
-  f32x4 o;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) o[e] = lds_read<float>(from + 4 * ((i * 64 + (q >> 2) * 16 + 4 * (lane & 3) + e) * 4 + (q & 3)));
-  return o;
-}
 // Row of the state that a lane's register r of result i has (lane group g), see TileOps.
 __device__ __forceinline__ int state_row(int i, int g, int r) { return 32 * (i >> 1) + 8 * g + 4 * (i & 1) + r; }
 template <typename T> __device__ __forceinline__ void lds_write(unsigned at, const T& v) { *(__attribute__((address_space(3))) T*)(uintptr_t)at = v; }
@@ -561,16 +554,17 @@ template <typename M> __device__ __forceinline__ void write_op(unsigned lds_of_l
 
 template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void delta_walk(char* smem_raw, const DeltaRule& a, int doc_rank, int h, int c0) {
   typedef WalkLds<E, DK, NW, KIND> L;
-  constexpr int RT = DK / 16, KS = DK / 32, LOADERS = walk_loaders(NW), FW = LOADERS ? LOADERS : NW;
-  constexpr bool HALF_E = __is_same(E, f16), BACK = KIND == WALK_GRADIENTS, RESULTS = KIND == WALK_RESULTS, AHEAD = L::NBUF == 2, ALL_AHEAD = L::VBUF == 2, EARLY = !LOADERS || !ALL_AHEAD;
+  constexpr int RT = DK / 16, KS = DK / 32, HT = RT / 2, HS = KS / 2, LOADERS = walk_loaders(NW), FW = LOADERS ? LOADERS : NW;
+  constexpr bool HALF_E = __is_same(E, f16), BACK = KIND == WALK_GRADIENTS, RESULTS = KIND == WALK_RESULTS, AHEAD = L::NBUF == 2, ALL_AHEAD = L::VBUF == 2,
+                 EARLY = !LOADERS || !ALL_AHEAD;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = wave % NW, g = lane >> 4, i16 = lane & 15;
-  const bool chain = wave < NW, helps = !chain && wave < 2 * NW, loads = LOADERS ? wave >= 2 * NW : helps;
-  const int fw = LOADERS ? wave - 2 * NW : mine;
+  const bool chain = wave < 2 * NW, helps = !chain && wave < 3 * NW, loads = LOADERS ? wave >= 3 * NW : helps;
+  const int fw = LOADERS ? wave - 3 * NW : mine;
   const int4 row = reinterpret_cast<const int4*>(a.chunks)[1 + doc_rank];   // first token, tokens, first chunk, document
   const int first = row.x, count = row.y, chunk0 = row.z, doc = row.w, chunks = (count + DELTA_C - 1) / DELTA_C;
   const int kv = h / (a.nv / a.nk), w0 = c0 + 16 * mine, col = w0 + i16;    // the wave's first column and the lane's
-  const unsigned smem = lds_address(smem_raw), hand = smem + L::H + mine * L::HAND + 16 * lane, units = smem + L::UNITS + mine * Tile<E, DK>::OCTET;
-  const unsigned hand_u = hand + DK * 64;
+  const unsigned smem = lds_address(smem_raw), hand = smem + L::H + mine * L::HAND + 16 * lane, hand_z = hand + DK * 64, hand_add = hand_z + 4096;
+  const unsigned units = smem + L::UNITS + mine * Tile<E, DK>::OCTET;       // of the state's columns, and 64 bytes on of Z's
   const int step = BACK ? -1 : 1;
   const int64_t states = (int64_t)a.dk * a.dv;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
@@ -650,194 +644,203 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
   };
 
   if (chain) {
+    const int half = wave / NW;   // of the state's rows, and of the tokens
     const TileOps<E, 64> at_v(smem + L::V, lane);
     TileOps<E, DK> at;
     at.state_places(smem + L::K, lane);
+    // Of keys' rows the columns that belong to this half of the state come first, of their columns only these: either 64 columns, whose places
+    // change places, or further ones.
+    constexpr bool SWAP = sizeof(E) == 2 && DK == 64;
+    if (SWAP && half) {
+      const unsigned r0 = at.srow_[0], c0_ = at.scol_[0];
+      at.srow_[0] = at.srow_[1];
+      at.srow_[1] = r0;
+      at.scol_[0] = at.scol_[1];
+      at.scol_[1] = c0_;
+    }
+    const unsigned own = SWAP ? 0u : (unsigned)(half * (sizeof(E) == 2 ? 1024 : HS * 1024)), not_own = SWAP ? 0u : (sizeof(E) == 2 ? 1024u : HS * 1024u) - own;
     const bool live = col < a.dv;
-    f32x4 S[RT];
-    Pair<E> sp[KS];
-    float s_inv = 1.f;
-    auto publish_state = [&]() {   // the whole state, after a change
-      const float unit = column_unit<E>(S);
-      s_inv = inverse_unit<E>(unit);
-      pairs_of<E>(sp, S, unit);
-      if constexpr (RESULTS) {
-#pragma unroll
-        for (int s = 0; s < KS; ++s) write_op<E>(hand + s * 2048, sp[s]);
-        if (HALF_E && lane < 16) lds_write(units + 4 * lane, s_inv);
-      } else {
-#pragma unroll
-        for (int i = 0; i < RT; ++i) lds_write(hand + i * 1024, S[i]);
+    f32x4 S[HT];
+    Pair<E> sp[HS];
+    float s_unit = 1.f;
+    auto publish_state = [&]() {
+      if constexpr (HALF_E) {   // of these rows; the other half's may be another
+        s_unit = column_unit<E>(S);
+        if (lane < 16) lds_write(units + 64 * half + 4 * lane, s_unit);
       }
+      pairs_of<E>(sp, S, s_unit);
+#pragma unroll
+      for (int s = 0; s < HS; ++s) write_op<E>(hand + (HS * half + s) * 2048, sp[s]);
     };
     const float* from = BACK ? a.dht : a.h0;
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
+    for (int i = 0; i < HT; ++i) {
       S[i] = zero;
       if (from)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (live && state_row(i, g, r) < a.dk) S[i][r] = from[((int64_t)doc * a.nv + h) * states + (int64_t)state_row(i, g, r) * a.dv + col];
+        for (int r = 0; r < 4; ++r) {
+          const int at_row = state_row(HT * half + i, g, r);
+          if (live && at_row < a.dk) S[i][r] = from[((int64_t)doc * a.nv + h) * states + (int64_t)at_row * a.dv + col];
+        }
     }
     if (chunks > 0) publish_state();
     __syncthreads();
-    Opnd<E, 1> kf[KS][4];   // rows of the chunk's keys
+    Opnd<E, 1> kf[HS][2], ko[HS][2];   // this half's rows of the chunk's keys: of this and of the other half's columns
     auto load_keys = [&]() {
+      const unsigned rows = half * 4 * Tile<E, DK>::OCTET;
 #pragma unroll
-      for (int s = 0; s < KS; ++s)
+      for (int s = 0; s < HS; ++s)
 #pragma unroll
-        for (int m = 0; m < 4; ++m) kf[s][m] = at.state_row(0, m, s);
+        for (int m = 0; m < 2; ++m) {
+          kf[s][m] = at.state_row(rows + own, m, s);
+          ko[s][m] = at.state_row(rows + not_own, m, SWAP ? 1 : s);
+        }
     };
     if (chunks > 0) load_keys();
     for (int n = 0; n < chunks; ++n, c += step) {
       const unsigned buf = AHEAD ? (unsigned)(n & 1) * L::FIRST : 0u, gates = smem + buf + L::R, ops = gates + REC_GATES + 16 * lane, gates4 = gates + 16 * g;
-      const bool more = n + 1 < chunks;
-      const unsigned second = ALL_AHEAD ? (unsigned)(n & 1) * L::SECOND : 0u;
-      // What comes from LDS is asked for a product ahead and not earlier: two waves of a SIMD have 256 registers each.
-      f32x4 since[4], other[4];
-      Opnd<E, 1> vf[2];
-      Pair<E> tf[6];           // T, or P^T
-      f32x4 x[4], y[4], u[4], next[4];   // K S; P^T dO
+      const unsigned second = ALL_AHEAD ? (unsigned)(n & 1) * L::SECOND : 0u, mine4 = gates4 + 128 * half;   // gates of this half's tokens
+      Pair<E> so[HS];   // the other half of the state
 #pragma unroll
-      for (int m = 0; m < 4; ++m) x[m] = y[m] = zero;
+      for (int s = 0; s < HS; ++s) so[s] = load_op<E>(hand + (HS * (1 - half) + s) * 2048);
+      float o_unit = 1.f;
+      if constexpr (HALF_E) o_unit = lds_read<float>(units + 4 * i16 + (half ? 0 : 64));
+      f32x4 x[2], xo[2], y[2], z[2];
 #pragma unroll
-      for (int s = 0; s < KS; ++s) {
+      for (int m = 0; m < 2; ++m) x[m] = xo[m] = y[m] = zero;
 #pragma unroll
-        for (int m = 0; m < 4; ++m) x[m] = mma(kf[s][m], sp[s], x[m]);
-        if (s == KS / 2 - 1) {
-          __builtin_amdgcn_sched_barrier(0);
+      for (int s = 0; s < HS; ++s)
 #pragma unroll
-          for (int m = 0; m < 4; ++m) {
-            since[m] = lds_read<f32x4>(gates4 + 64 * m);
-            other[m] = lds_read<f32x4>(gates4 + (BACK ? 256 : 512) + 64 * m);
-          }
-          vf[0] = at_v.column(second, mine, 0);
-          vf[1] = at_v.column(second, mine, 1);
-          if constexpr (BACK)
+        for (int m = 0; m < 2; ++m) x[m] = mma(kf[s][m], sp[s], x[m]);
+      f32x4 since[2], other[2];
 #pragma unroll
-            for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(ops + i * REC_OP);
-          __builtin_amdgcn_sched_barrier(0);
-        }
+      for (int m = 0; m < 2; ++m) {
+        since[m] = lds_read<f32x4>(mine4 + 64 * m);
+        other[m] = lds_read<f32x4>(mine4 + (BACK ? 256 : 512) + 64 * m);
       }
-      f32x4 z[4];
+      Opnd<E, 1> vf[2];   // columns of v of this half's tokens, or of dO of all
+      if constexpr (BACK) {
+        vf[0] = at_v.column(second, mine, 0);
+        vf[1] = at_v.column(second, mine, 1);
+      } else vf[0] = at_v.column(second + half * 4 * Tile<E, 64>::OCTET, mine, 0);
+      Pair<E> tf[6];
+      if constexpr (BACK) {   // P^T: its first four operands are the first half's rows, the others the second's
+#pragma unroll
+        for (int i = 0; i < 4; ++i) tf[i] = load_op<E>(ops + (half ? 4 + (i & 1) : i) * REC_OP);
+      }
+#pragma unroll
+      for (int s = 0; s < HS; ++s)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) xo[m] = mma(ko[s][m], so[s], xo[m]);
       if constexpr (BACK) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int m = 0; m < 4; ++m)
-            if (s >= m / 2) y[m] = mma(tf[upper_op(m, s)], vf[s], y[m]);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(ops + REC_TRIANGLE + i * REC_OP);   // T^T
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) z[m][r] = a.scale * y[m][r] + other[m][r] * (x[m][r] * s_inv);
-      } else {
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(ops + i * REC_OP);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) z[m][r] = other[m][r] * ((float)vf[m >> 1].t[0][4 * (m & 1) + r] - since[m][r] * (x[m][r] * s_inv));
+        for (int m = 0; m < 2; ++m) {
+          if (half) y[m] = mma(tf[m], vf[1], y[m]);
+          else y[m] = mma(tf[2 * m + 1], vf[1], mma(tf[2 * m], vf[0], y[m]));
+        }
       }
-      Pair<E> zp[2];
-      const float unit = column_unit<E>(z), inv = inverse_unit<E>(unit);
-      pairs_of<E>(zp, z, unit);
       __builtin_amdgcn_sched_barrier(0);
-      Opnd<E, 1> kc[2][RT];   // columns of the keys
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+      for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(ops + (BACK ? REC_TRIANGLE : 0) + i * REC_OP);   // T, or T^T
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int s = 0; s < 2; ++s) kc[s][i] = at.state_column(0, i, s);
+      for (int m = 0; m < 2; ++m) {
+        const f32x4 ks = HALF_E ? x[m] * inverse_unit<E>(s_unit) + xo[m] * inverse_unit<E>(o_unit) : x[m] + xo[m];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          if constexpr (BACK) z[m][r] = a.scale * y[m][r] + other[m][r] * ks[r];
+          else z[m][r] = other[m][r] * ((float)vf[0].t[0][4 * m + r] - since[m][r] * ks[r]);
+        }
+      }
+      {
+        const float unit = column_unit<E>(z);
+        Pair<E> zp[1];
+        pairs_of<E>(zp, z, unit);
+        write_op<E>(hand_z + half * 2048, zp[0]);
+        if (HALF_E && lane < 16) lds_write(units + Tile<E, DK>::OCTET * 4 + 64 * half + 4 * lane, unit);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      Opnd<E, 1> kc[HT][2];   // columns of the keys, this half's rows of the state
+#pragma unroll
+      for (int i = 0; i < HT; ++i)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) kc[i][s] = at.state_column(own, i, s);
       f32x4 factor[4];
 #pragma unroll
-      for (int m = 0; m < 4; ++m) factor[m] = lds_read<f32x4>(gates4 + (BACK ? 512 : 256) + 64 * m);
+      for (int m = 0; m < 4; ++m) {
+        factor[m] = lds_read<f32x4>(gates4 + (BACK ? 512 : 256) + 64 * m);
+        if constexpr (BACK) factor[m] *= -lds_read<f32x4>(gates4 + 64 * m);
+      }
       const float whole = lds_read<float>(gates + 768);
-      __builtin_amdgcn_sched_barrier(0);
+      middle(n);
+      Pair<E> zp[2];
+      float zi[2] = {1.f, 1.f};
 #pragma unroll
-      for (int m = 0; m < 4; ++m) u[m] = zero;
+      for (int s = 0; s < 2; ++s) {
+        zp[s] = load_op<E>(hand_z + s * 2048);
+        if constexpr (HALF_E) zi[s] = inverse_unit<E>(lds_read<float>(units + Tile<E, DK>::OCTET * 4 + 64 * s + 4 * i16));
+      }
+      f32x4 add[HT];
+      if constexpr (BACK)
+#pragma unroll
+        for (int i = 0; i < HT; ++i) add[i] = lds_read<f32x4>(hand_add + (HT * half + i) * 1024);
+      at.move_state_places(AHEAD ? ((n & 1) ? (unsigned)-L::FIRST : (unsigned)L::FIRST) : 0u);
+      f32x4 u[4], uo[4], next[4];   // uo: half's other tokens, which have a unit of their own
+#pragma unroll
+      for (int m = 0; m < 4; ++m) u[m] = uo[m] = zero;
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int m = 0; m < 4; ++m)
-          if (BACK ? s >= m / 2 : s <= m / 2) u[m] = mma(tf[BACK ? upper_op(m, s) : lower_op(m, s)], zp[s], u[m]);
+          if (BACK ? s >= m / 2 : s <= m / 2) {
+            const Pair<E>& t = tf[BACK ? upper_op(m, s) : lower_op(m, s)];
+            if (HALF_E && s == 1) uo[m] = mma(t, zp[s], uo[m]);
+            else u[m] = mma(t, zp[s], u[m]);
+          }
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
-        if constexpr (HALF_E) u[m] *= inv;
-        lds_write(hand_u + m * 1024, u[m]);
-        if constexpr (BACK) next[m] = u[m] * since[m] * factor[m] * -1.f;
-        else next[m] = u[m] * factor[m];
+        if constexpr (HALF_E) u[m] = u[m] * zi[0] + uo[m] * zi[1];
+        next[m] = u[m] * factor[m];
       }
       Pair<E> np[2];
       const float n_unit = column_unit<E>(next), n_inv = inverse_unit<E>(n_unit);
       pairs_of<E>(np, next, n_unit);
-      middle(n);
-      const unsigned turn = AHEAD ? ((n & 1) ? (unsigned)-L::FIRST : (unsigned)L::FIRST) : 0u;
-      at.move_state_places(turn);
-      f32x4 add[RT];
-#pragma unroll
-      for (int i = 0; i < RT; ++i) {
-        add[i] = zero;
-        if constexpr (BACK) add[i] = lds_read<f32x4>(hand + i * 1024);
-      }
       if (AHEAD) load_keys();   // (behind the last chunk nothing is there, and nothing takes them)
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (HALF_E) {
+        f32x4 p[HT];
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-          add[i] += S[i] * whole;
-          S[i] = zero;
-        }
+        for (int i = 0; i < HT; ++i) p[i] = zero;
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int i = 0; i < RT; ++i) S[i] = mma(kc[s][i], np[s], S[i]);
+          for (int i = 0; i < HT; ++i) p[i] = mma(kc[i][s], np[s], p[i]);
 #pragma unroll
-        for (int i = 0; i < RT; ++i) S[i] = add[i] + S[i] * n_inv;
-        if (more) publish_state();
-      } else {   // two results at a time, published while the next two are made
-        auto publish = [&](int t) {
-          sp[t] = pair_of<E>(S[2 * t], S[2 * t + 1]);
-          if constexpr (RESULTS) write_op<E>(hand + t * 2048, sp[t]);
-          else {
-            lds_write(hand + 2 * t * 1024, S[2 * t]);
-            lds_write(hand + (2 * t + 1) * 1024, S[2 * t + 1]);
-          }
-        };
-#pragma unroll
-        for (int t = 0; t < KS; ++t) {
-#pragma unroll
-          for (int i = 2 * t; i < 2 * t + 2; ++i) S[i] = add[i] + S[i] * whole;
-#pragma unroll
-          for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int i = 2 * t; i < 2 * t + 2; ++i) S[i] = mma(kc[s][i], np[s], S[i]);
-          if (t > 0) publish(t - 1);
-          if constexpr (sizeof(E) == 2) {   // a matrix instruction leaves time for three others
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-              __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
-            }
-          }
-          __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < HT; ++i) {
+          S[i] = S[i] * whole + p[i] * n_inv;
+          if constexpr (BACK) S[i] += add[i];
         }
-        publish(KS - 1);
+      } else {
+#pragma unroll
+        for (int i = 0; i < HT; ++i) S[i] = BACK ? S[i] * whole + add[i] : S[i] * whole;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int i = 0; i < HT; ++i) S[i] = mma(kc[i][s], np[s], S[i]);
       }
+      if (n + 1 < chunks) publish_state();
       end_chunk(n);
-      if (!AHEAD && more) load_keys();
+      if (!AHEAD && n + 1 < chunks) load_keys();
     }
     float* last = RESULTS ? a.ht : BACK ? a.dh0 : nullptr;
     if (last && live)
 #pragma unroll
-      for (int i = 0; i < RT; ++i)
+      for (int i = 0; i < HT; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (state_row(i, g, r) < a.dk) last[((int64_t)doc * a.nv + h) * states + (int64_t)state_row(i, g, r) * a.dv + col] = S[i][r];
+        for (int r = 0; r < 4; ++r) {
+          const int at_row = state_row(HT * half + i, g, r);
+          if (at_row < a.dk) last[((int64_t)doc * a.nv + h) * states + (int64_t)at_row * a.dv + col] = S[i][r];
+        }
     return;
   }
 
@@ -851,13 +854,68 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
     return;
   }
   if constexpr (RESULTS) {
-    // A chunk's results are finished while the next one's u is still being made.
     TileOps<E, DK> at;
     at.state_places(smem + L::Q, lane);
-    f32x4 o[4], u[4], back_s, back_u;   // o transposed: rows are columns of the state, a lane has the token lane % 16
-    Pair<E> pf[6];
-    auto finish = [&](int c) {
-      f32x4 p[4];
+    for (int n = 0; n < chunks; ++n, c += step) {
+      const unsigned gates = smem + (AHEAD ? (unsigned)(n & 1) * L::FIRST : 0u) + L::R, ops = gates + REC_GATES + 16 * lane;
+      begin_chunk(n);
+      Pair<E> sf[KS];
+#pragma unroll
+      for (int s = 0; s < KS; ++s) sf[s] = load_op<E>(hand + s * 2048);
+      f32x4 back_s[2];   // half: of the rows' columns, of either half of the state
+      if constexpr (HALF_E) {
+        back_s[0] = lds_read<f32x4>(units + 16 * g);
+        back_s[1] = lds_read<f32x4>(units + 64 + 16 * g);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          back_s[0][r] = inverse_unit<E>(back_s[0][r]);
+          back_s[1][r] = inverse_unit<E>(back_s[1][r]);
+        }
+      }
+      f32x4 o[4], oo[4];   // transposed: rows are columns of the state, a lane has the token lane % 16
+      float zi[2];         // half: the inverse units of Z
+      Pair<E> pf[6], tf[6], zp[2];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) o[m] = oo[m] = zero;
+#pragma unroll
+      for (int s = 0; s < KS; ++s)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          if (HALF_E && s >= HS) oo[m] = mma(sf[s], at.state_row(0, m, s), oo[m]);
+          else o[m] = mma(sf[s], at.state_row(0, m, s), o[m]);
+        }
+      if constexpr (ALL_AHEAD) at.move_state_places((n & 1) ? (unsigned)-L::SECOND : (unsigned)L::SECOND);
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const float since = lds_read<float>(gates + 4 * (16 * m + i16));
+        if constexpr (HALF_E) o[m] = (o[m] * back_s[0] + oo[m] * back_s[1]) * since;
+        else o[m] *= since;
+      }
+#pragma unroll
+      for (int i = 0; i < 6; ++i) {
+        tf[i] = load_op<E>(ops + i * REC_OP);
+        pf[i] = load_op<E>(ops + REC_TRIANGLE + i * REC_OP);
+      }
+      middle(n);
+      zp[0] = load_op<E>(hand_z);
+      zp[1] = load_op<E>(hand_z + 2048);
+      if constexpr (HALF_E)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) zi[s] = inverse_unit<E>(lds_read<float>(units + Tile<E, DK>::OCTET * 4 + 4 * i16 + 64 * s));
+      f32x4 u[4], uo[4], p[4], back_u = zero;
+#pragma unroll
+      for (int m = 0; m < 4; ++m) u[m] = uo[m] = zero;
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+          if (s <= m / 2) {
+            if (HALF_E && s == 1) uo[m] = mma(tf[lower_op(m, s)], zp[s], uo[m]);
+            else u[m] = mma(tf[lower_op(m, s)], zp[s], u[m]);
+          }
+      if constexpr (HALF_E)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) u[m] = u[m] * zi[0] + uo[m] * zi[1];
       Pair<E> up[2];
       const float unit = column_unit<E>(u), inv = inverse_unit<E>(unit);
       pairs_of<E>(up, u, unit);
@@ -886,58 +944,38 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
             *reinterpret_cast<quad_t*>(oh + (first + t) * a.ldo) = w;
           }
         }
-    };
-    for (int n = 0; n < chunks; ++n, c += step) {
-      const unsigned gates = smem + (AHEAD ? (unsigned)(n & 1) * L::FIRST : 0u) + L::R, ops = gates + REC_GATES + 16 * lane;
-      const bool more = n + 1 < chunks;
-      begin_chunk(n);
-      Pair<E> sf[KS];
-#pragma unroll
-      for (int s = 0; s < KS; ++s) sf[s] = load_op<E>(hand + s * 2048);
-      if (n > 0) finish(c - step);
-      if constexpr (HALF_E) back_s = lds_read<f32x4>(units + 16 * g);
-#pragma unroll
-      for (int m = 0; m < 4; ++m) o[m] = zero;
-#pragma unroll
-      for (int s = 0; s < KS; ++s)
-#pragma unroll
-        for (int m = 0; m < 4; ++m) o[m] = mma(sf[s], at.state_row(0, m, s), o[m]);
-      if constexpr (ALL_AHEAD) at.move_state_places((n & 1) ? (unsigned)-L::SECOND : (unsigned)L::SECOND);
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const float since = lds_read<float>(gates + 4 * (16 * m + i16));
-        if constexpr (HALF_E) o[m] *= back_s * since;
-        else o[m] *= since;
-      }
-#pragma unroll
-      for (int i = 0; i < 6; ++i) pf[i] = load_op<E>(ops + REC_TRIANGLE + i * REC_OP);
-      middle(n);
-#pragma unroll
-      for (int m = 0; m < 4; ++m) u[m] = lds_read<f32x4>(hand_u + m * 1024);
       end_chunk(n);
     }
-    if (chunks > 0) finish(chunks - 1);
   } else {
-    const int out = w0 + 4 * (lane & 3), q = lane >> 2;   // columns of the lane's part of a row
-    const unsigned hand0 = hand - 16 * lane, hand0_u = hand_u - 16 * lane;
     TileOps<E, DK> at;
     at.state_places(smem + L::Q, lane);
     const TileOps<E, 64> at_v(smem + L::V, lane);
     for (int n = 0; n < chunks; ++n, c += step) {
-      const unsigned gates = smem + (AHEAD ? (unsigned)(n & 1) * L::FIRST : 0u) + L::R, gates4 = gates + 16 * g;
-      const bool more = n + 1 < chunks;
+      const unsigned gates = smem + (AHEAD ? (unsigned)(n & 1) * L::FIRST : 0u) + L::R, gates4 = gates + 16 * g, ops = gates + REC_GATES + 16 * lane;
       const int64_t rec = (int64_t)(chunk0 + c) * a.nv + h;
       begin_chunk(n);
-      float* to = (BACK ? a.dstates : a.states) + rec * DK * a.dvp + out;
-      f32x4 part[RT];
+      // the state, as its pairs are: what the gradients' products take
+      float* to = (BACK ? a.dstates : a.states) + rec * DK * a.dvp + col;
+      Pair<E> sf[KS];
 #pragma unroll
-      for (int i = 0; i < RT; ++i) part[i] = by_rows(hand0, i, lane);
-      if (out < a.dvp)
+      for (int s = 0; s < KS; ++s) sf[s] = load_op<E>(hand + s * 2048);
+      float inv[2] = {1.f, 1.f};
+      if constexpr (HALF_E) {
+        inv[0] = inverse_unit<E>(lds_read<float>(units + 4 * i16));
+        inv[1] = inverse_unit<E>(lds_read<float>(units + 64 + 4 * i16));
+      }
+      if (col < a.dvp)
 #pragma unroll
-        for (int i = 0; i < RT; ++i) *reinterpret_cast<f32x4*>(to + state_row(i, q >> 2, q & 3) * a.dvp) = part[i];
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            float x = (float)sf[s].t[0][e];
+            if constexpr (PAIR<E> == 2) x += (float)sf[s].t[1][e];
+            to[(32 * s + 8 * g + e) * a.dvp] = HALF_E ? x * inv[s >= HS] : x;
+          }
       if constexpr (BACK) {   // scale Q^T (exp(G) dO)
-        Opnd<E, 1> vf[2];
         const unsigned second = ALL_AHEAD ? (unsigned)(n & 1) * L::SECOND : 0u;
+        Opnd<E, 1> vf[2];
         vf[0] = at_v.column(second, mine, 0);
         vf[1] = at_v.column(second, mine, 1);
         f32x4 d[4], add[RT];
@@ -948,7 +986,7 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
           for (int r = 0; r < 4; ++r) d[m][r] = a.scale * since[r] * (float)vf[m >> 1].t[0][4 * (m & 1) + r];
         }
         Pair<E> dp[2];
-        const float unit = column_unit<E>(d), inv = inverse_unit<E>(unit);
+        const float unit = column_unit<E>(d), back = inverse_unit<E>(unit);
         pairs_of<E>(dp, d, unit);
 #pragma unroll
         for (int i = 0; i < RT; ++i) add[i] = zero;
@@ -957,18 +995,38 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
 #pragma unroll
           for (int i = 0; i < RT; ++i) add[i] = mma(at.state_column(0, i, s), dp[s], add[i]);
         if constexpr (ALL_AHEAD) at.move_state_places((n & 1) ? (unsigned)-L::SECOND : (unsigned)L::SECOND);
-        wave_lds_order();   // the state has been read
 #pragma unroll
-        for (int i = 0; i < RT; ++i) lds_write(hand + i * 1024, HALF_E ? add[i] * inv : add[i]);
+        for (int i = 0; i < RT; ++i) lds_write(hand_add + i * 1024, HALF_E ? add[i] * back : add[i]);
       }
+      Pair<E> tf[6], zp[2];
+#pragma unroll
+      for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(ops + (BACK ? REC_TRIANGLE : 0) + i * REC_OP);
       middle(n);
-      f32x4 pu[4];
+      f32x4 u[4], uo[4], back_z[2];   // transposed: rows are columns of the state
 #pragma unroll
-      for (int m = 0; m < 4; ++m) pu[m] = by_rows(hand0_u, m, lane);
-      float* to_u = (BACK ? a.y : a.u) + rec * DELTA_C * a.dvp + q * a.dvp + out;
-      if (out < a.dvp)
+      for (int s = 0; s < 2; ++s) {
+        zp[s] = load_op<E>(hand_z + s * 2048);
+        if constexpr (HALF_E) {
+          back_z[s] = lds_read<f32x4>(units + Tile<E, DK>::OCTET * 4 + 64 * s + 16 * g);
 #pragma unroll
-        for (int m = 0; m < 4; ++m) *reinterpret_cast<f32x4*>(to_u + 16 * m * a.dvp) = pu[m];
+          for (int r = 0; r < 4; ++r) back_z[s][r] = inverse_unit<E>(back_z[s][r]);
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < 4; ++m) u[m] = uo[m] = zero;
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+          if (BACK ? s >= m / 2 : s <= m / 2) {
+            const Pair<E>& t = tf[BACK ? upper_op(m, s) : lower_op(m, s)];
+            if (HALF_E && s == 1) uo[m] = mma(zp[s], t, uo[m]);
+            else u[m] = mma(zp[s], t, u[m]);
+          }
+      float* to_u = (BACK ? a.y : a.u) + rec * DELTA_C * a.dvp + i16 * a.dvp + w0 + 4 * g;
+      if (w0 + 4 * g < a.dvp)
+#pragma unroll
+        for (int m = 0; m < 4; ++m) *reinterpret_cast<f32x4*>(to_u + 16 * m * a.dvp) = HALF_E ? u[m] * back_z[0] + uo[m] * back_z[1] : u[m];
       end_chunk(n);
     }
   }
@@ -1314,11 +1372,14 @@ template <typename E, int DK, bool SHARED> __global__ __launch_bounds__(64 * gra
 }
 
 // ------------------------------------------------------------------------------------------ launches
-template <typename E, int DK, int NW> hipError_t delta_walks(hipStream_t st, const DeltaRule& a, bool backward) {
-  const int slices = (int)cdiv(a.dv, 16 * NW);
-  const int blocks = (int)(cdiv((int64_t)a.ndocs * a.nv, 8) * 8 * slices);
-  if (backward) hipLaunchKernelGGL((delta_walks_kernel<E, DK, NW>), dim3((unsigned)(2 * blocks)), dim3(walk_threads(NW)), 0, st, a, slices, blocks);
-  else hipLaunchKernelGGL((delta_walk_kernel<E, DK, NW>), dim3((unsigned)blocks), dim3(walk_threads(NW)), 0, st, a, slices);
+template <typename E, int DK, int NW> hipError_t delta_walk_results(hipStream_t st, const DeltaRule& a) {
+  const int slices = (int)cdiv(a.dv, 16 * NW), blocks = (int)(cdiv((int64_t)a.ndocs * a.nv, 8) * 8 * slices);
+  hipLaunchKernelGGL((delta_walk_kernel<E, DK, NW>), dim3((unsigned)blocks), dim3(walk_threads(NW)), 0, st, a, slices);
+  return hipGetLastError();
+}
+template <typename E, int DK, int NW> hipError_t delta_walks(hipStream_t st, const DeltaRule& a) {
+  const int slices = (int)cdiv(a.dv, 16 * NW), blocks = (int)(cdiv((int64_t)a.ndocs * a.nv, 8) * 8 * slices);
+  hipLaunchKernelGGL((delta_walks_kernel<E, DK, NW>), dim3((unsigned)(2 * blocks)), dim3(walk_threads(NW)), 0, st, a, slices, blocks);
   return hipGetLastError();
 }
 template <typename E, int DK> hipError_t delta_run(hipStream_t st, const DeltaRule& a, bool backward) {
@@ -1327,10 +1388,11 @@ template <typename E, int DK> hipError_t delta_run(hipStream_t st, const DeltaRu
   else hipLaunchKernelGGL((delta_prep_kernel<E, DK, false>), prep, dim3(256), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.ndocs == 0) return e;
-  // Workgroups of four waves share what they bring into LDS; fewer waves where that would leave CUs without one.
-  const int64_t waves = (int64_t)a.ndocs * a.nv * cdiv(a.dv, 16) * (backward ? 2 : 1);
-  constexpr bool four = sizeof(E) == 2;   // fp32 has no registers for eight waves
-  e = waves >= 1024 && four && !backward ? delta_walks<E, DK, four ? 4 : 2>(st, a, backward) : waves >= 512 ? delta_walks<E, DK, 2>(st, a, backward) : delta_walks<E, DK, 1>(st, a, backward);
+  // Workgroups of several 16 columns share what they bring into LDS; of fewer where that would leave CUs without one.
+  const int64_t sets = (int64_t)a.ndocs * a.nv * cdiv(a.dv, 16) * (backward ? 2 : 1);
+  constexpr bool four = sizeof(E) == 2;   // fp32 has no registers for twelve waves
+  if (backward) e = sets >= 512 ? delta_walks<E, DK, 2>(st, a) : delta_walks<E, DK, 1>(st, a);
+  else e = sets >= 1024 && four ? delta_walk_results<E, DK, four ? 4 : 2>(st, a) : sets >= 512 ? delta_walk_results<E, DK, 2>(st, a) : delta_walk_results<E, DK, 1>(st, a);
   if (e != hipSuccess || !backward || a.nchunks == 0) return e;
   const dim3 grid((unsigned)a.nchunks, (unsigned)a.nk);
   if (a.nv == a.nk) hipLaunchKernelGGL((delta_grad_kernel<E, DK, false>), grid, dim3(64 * grad_waves(DK)), 0, st, a);
