@@ -523,7 +523,7 @@ template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256, 4) voi
 // Two barriers a chunk: the first publishes the state, and matrices, values and queries of the chunk, the second Z, and the next chunk's
 // keys.  All of these come straight into LDS, a chunk ahead where two of them fit.
 enum DeltaWalk { WALK_RESULTS = 0, WALK_STATES = 1, WALK_GRADIENTS = 2 };   // o and the last state; the states and u for the gradients; the states' gradients and y
-constexpr int walk_loaders(int NW) { return NW == 1 ? 4 : NW == 2 ? 2 : 0; }   // a wave issues a load of 1 KB in 50 to 70 cycles
+constexpr int walk_loaders(int NW) { return NW == 1 ? 4 : 2; }   // a wave issues a load of 1 KB in 50 to 70 cycles
 constexpr int walk_threads(int NW) { return 64 * (3 * NW + walk_loaders(NW)); }
 
 template <typename E, int DK, int NW, int KIND> struct WalkLds {
@@ -1090,9 +1090,80 @@ template <typename E, int DK, bool SHARED> __global__ __launch_bounds__(64 * gra
   __shared__ float gate[4][64], yvs[2][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, i16 = lane & 15;
   const ChunkRow c = chunk_row(a, blockIdx.x);
-  if (c.count <= 0) return;
-  const int kv = blockIdx.y, group = SHARED ? a.nv / a.nk : 1, end = c.first + c.count, tile = wave & 3, part = wave >> 2;
+  const int kv = blockIdx.y, group = SHARED ? a.nv / a.nk : 1, tile = wave & 3, part = wave >> 2;
   const unsigned smem = lds_address(smem_raw), stage = 2 * TILE;
+  typedef E quad_t __attribute__((ext_vector_type(4)));
+  const int my_t = 16 * tile + i16;         // the token whose rows of U and Y this lane brings, of 64 columns or, as one of eight waves, of 32
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  f32x4 sx[2], sy[2];                       // rows of S and dS, 32 columns ahead
+  f32x4 u[2 / PARTS][2], y[2 / PARTS][2];   // rows of U, Y and v, 64 columns ahead
+  quad_t v[2 / PARTS][2];
+  float my_gate = 0.f;
+  double my_G = 0.0;
+  // Through descriptors: an address is a register, and what lies behind a matrix, or in columns past its width, reads as zeros.
+  const unsigned my_state = (unsigned)((16 * wave + i16) * a.dvp + 4 * g) * 4, my_row = (unsigned)(my_t * a.dvp + 4 * g) * 4;
+  auto matrix = [&](const float* p, int rows) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p), 0, rows * a.dvp * 4, 0x00020000); };
+  auto quad_at = [&](const __amdgpu_buffer_rsrc_t& m, unsigned lane_at, int col) {
+    union { u32x4 w; f32x4 v; } x;
+    x.w = __builtin_amdgcn_raw_buffer_load_b128(m, lane_at + (col < a.dvp ? 4u * col : 0x80000000u), 0, 0);
+    return x.v;
+  };
+  auto load_states = [&](int64_t rec, int col0) {
+    const __amdgpu_buffer_rsrc_t S = matrix(a.states + rec * DK * a.dvp, DK), dS = matrix(a.dstates + rec * DK * a.dvp, DK);
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      sx[p] = quad_at(S, my_state, col0 + 16 * p);
+      sy[p] = quad_at(dS, my_state, col0 + 16 * p);
+    }
+  };
+  auto load_rows = [&](int64_t rec, int b0) {
+    const __amdgpu_buffer_rsrc_t U = matrix(a.u + rec * DELTA_C * a.dvp, DELTA_C), Y = matrix(a.y + rec * DELTA_C * a.dvp, DELTA_C);
+#pragma unroll
+    for (int s = 0; s < 2 / PARTS; ++s)
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        u[s][p] = quad_at(U, my_row, b0 + 32 * (s + part) + 16 * p);
+        y[s][p] = quad_at(Y, my_row, b0 + 32 * (s + part) + 16 * p);
+      }
+  };
+  auto load_v = [&](int h, int b0) {
+    const __amdgpu_buffer_rsrc_t vs = __builtin_amdgcn_make_buffer_rsrc(const_cast<E*>((const E*)a.v + (int64_t)c.first * a.ldv + h * a.dv), 0,
+                                                                        (int)(((c.count - 1) * a.ldv + a.dv) * sizeof(E)), 0x00020000);
+#pragma unroll
+    for (int s = 0; s < 2 / PARTS; ++s)
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        const int col = b0 + 32 * (s + part) + 16 * p + 4 * g;
+        const unsigned at_v = col < a.dv ? (unsigned)(my_t * (int)a.ldv + col) * (unsigned)sizeof(E) : 0x80000000u;
+        if constexpr (sizeof(E) == 4) {
+          union { u32x4 w; quad_t v; } x;
+          x.w = __builtin_amdgcn_raw_buffer_load_b128(vs, at_v, 0, 0);
+          v[s][p] = x.v;
+        } else {
+          union { u32x2 w; quad_t v; } x;
+          x.w = __builtin_amdgcn_raw_buffer_load_b64(vs, at_v, 0, 0);
+          v[s][p] = x.v;
+        }
+      }
+  };
+  auto load_head = [&](int64_t rec) {
+    const char* from = a.records + rec * REC_BWD;
+    if (wave < 4) my_gate = reinterpret_cast<const float*>(from)[64 * wave + lane];
+    if (wave == 0) my_G = reinterpret_cast<const double*>(from + REC_G)[lane];
+    load_rows(rec, 0);
+    load_states(rec, 0);
+  };
+  load_head((int64_t)blockIdx.x * a.nv + kv * group);   // while the chunk's row of the table is still under way
+  __builtin_amdgcn_sched_barrier(0);
+  if (c.count <= 0) return;
+  const int end = c.first + c.count;
+  const bool my_in = my_t < c.count;
+  auto fetch_do = [&](int h, int b0) {
+    const TileLoad<E, 64, DELTA_C, W> load(a.ldo, lane, min(a.dv - b0, 64));
+    tile_ahead(load, smem + stage, (const E*)a.dout + h * a.dv + b0, c.first, end, wave);
+  };
+  load_v(kv * group, 0);
+  fetch_do(kv * group, 0);
   {
     const TileLoad<E, DK, DELTA_C, W> load_k(a.ldk, lane, a.dk), load_q(a.ldq, lane, a.dk);
     tile_ahead(load_k, smem, (const E*)a.k + kv * a.dk, c.first, end, wave);
@@ -1104,66 +1175,29 @@ template <typename E, int DK, bool SHARED> __global__ __launch_bounds__(64 * gra
   Sums& sums = *reinterpret_cast<Sums*>(smem_raw + stage);
   float *Mm = sums.m[0][0], *H = sums.m[1][0];
   const unsigned m_ops = smem + stage + STAGE + 16 * lane;
-  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
   f32x4 dq[4], dk[4];
 #pragma unroll
   for (int n = 0; n < 4; ++n) dq[n] = dk[n] = zero;
   for (int hg = 0; hg < group; ++hg) {
     const int h = kv * group + hg;
     const int64_t rec = (int64_t)blockIdx.x * a.nv + h;
-    const float *S = a.states + rec * DK * a.dvp, *dS = a.dstates + rec * DK * a.dvp, *U = a.u + rec * DELTA_C * a.dvp, *Y = a.y + rec * DELTA_C * a.dvp;
-    if (SHARED) __syncthreads();   // the head before is done with the LDS
-    if (wave < 4) {
-      const char* from = a.records + rec * REC_BWD;
-      gate[wave][lane] = reinterpret_cast<const float*>(from)[64 * wave + lane];
-      if (wave == 0) G[lane] = reinterpret_cast<const double*>(from + REC_G)[lane];
+    if (SHARED && hg > 0) {
+      __syncthreads();   // the head before is done with the LDS
+      load_head(rec);
+      load_v(h, 0);
+      fetch_do(h, 0);
     }
+    if (wave < 4) gate[wave][lane] = my_gate;
+    if (wave == 0) G[lane] = my_G;
     f32x4 qi[4], ks[4], kn[4], dp[4 / PARTS], da[4 / PARTS];
 #pragma unroll
     for (int n = 0; n < 4; ++n) qi[n] = ks[n] = kn[n] = zero;
 #pragma unroll
     for (int n = 0; n < 4 / PARTS; ++n) dp[n] = da[n] = zero;
     float sds = 0.f, yv = 0.f;
-    const int my_t = 16 * tile + i16;   // the token whose rows of U and Y this lane brings, of 64 columns or, as one of eight waves, of 32
-    const bool my_in = my_t < c.count;
-    typedef E quad_t __attribute__((ext_vector_type(4)));
-    f32x4 sx[2], sy[2];                 // rows of S and dS, 32 columns ahead
-    auto load_states = [&](int col0) {
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const int col = col0 + 16 * p + 4 * g, at_row = (16 * wave + i16) * a.dvp + col;
-        sx[p] = sy[p] = zero;
-        if (col < a.dvp) {
-          sx[p] = *reinterpret_cast<const f32x4*>(S + at_row);
-          sy[p] = *reinterpret_cast<const f32x4*>(dS + at_row);
-        }
-      }
-    };
-    f32x4 u[2 / PARTS][2], y[2 / PARTS][2];   // rows of U, Y and v, 64 columns ahead
-    quad_t v[2 / PARTS][2];
-    auto load_rows = [&](int b0) {
-#pragma unroll
-      for (int s = 0; s < 2 / PARTS; ++s)
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          const int col = b0 + 32 * (s + part) + 16 * p + 4 * g;
-          u[s][p] = y[s][p] = zero;
-          v[s][p] = quad_t{};
-          if (col < a.dvp) {
-            u[s][p] = *reinterpret_cast<const f32x4*>(U + my_t * a.dvp + col);
-            y[s][p] = *reinterpret_cast<const f32x4*>(Y + my_t * a.dvp + col);
-          }
-          if (my_in && col < a.dv) v[s][p] = *reinterpret_cast<const quad_t*>((const E*)a.v + (int64_t)(c.first + my_t) * a.ldv + h * a.dv + col);
-        }
-    };
-    load_rows(0);
-    load_states(0);
     for (int b0 = 0; b0 < a.dv; b0 += 64) {
       __syncthreads();   // the block before has been read; the gates are there
-      {
-        const TileLoad<E, 64, DELTA_C, W> load(a.ldo, lane, min(a.dv - b0, 64));
-        tile_ahead(load, smem + stage, (const E*)a.dout + h * a.dv + b0, c.first, end, wave);
-      }
+      if (b0 > 0) fetch_do(h, b0);
       const float beta = gate[2][my_t];
 #pragma unroll
       for (int s = 0; s < 2 / PARTS; ++s) {
@@ -1184,7 +1218,8 @@ template <typename E, int DK, bool SHARED> __global__ __launch_bounds__(64 * gra
       tile_wait();
       __syncthreads();
       __builtin_amdgcn_sched_barrier(0);
-      load_rows(b0 + 64);   // (zeros behind the last)
+      load_rows(rec, b0 + 64);   // (zeros behind the last)
+      load_v(h, b0 + 64);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
@@ -1194,7 +1229,7 @@ template <typename E, int DK, bool SHARED> __global__ __launch_bounds__(64 * gra
           for (int e = 0; e < 4; ++e) sds = fmaf(sx[p][e], sy[p][e], sds);
         const Pair<M> sp = pair_of<M>(sx[0], sx[1]), dsp = pair_of<M>(sy[0], sy[1]);
         __builtin_amdgcn_sched_barrier(0);
-        load_states(b0 + 32 * (s + 1));
+        load_states(rec, b0 + 32 * (s + 1));
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
@@ -1354,7 +1389,6 @@ template <typename E, int DK, bool SHARED> __global__ __launch_bounds__(64 * gra
       }
     }
   }
-  typedef E quad_t __attribute__((ext_vector_type(4)));
 #pragma unroll
   for (int m = 0; m < 4; ++m) {
     const int col = 16 * wave + 4 * g, tok = 16 * m + i16;
@@ -1390,9 +1424,8 @@ template <typename E, int DK> hipError_t delta_run(hipStream_t st, const DeltaRu
   if (e != hipSuccess || a.ndocs == 0) return e;
   // Workgroups of several 16 columns share what they bring into LDS; of fewer where that would leave CUs without one.
   const int64_t sets = (int64_t)a.ndocs * a.nv * cdiv(a.dv, 16) * (backward ? 2 : 1);
-  constexpr bool four = sizeof(E) == 2;   // fp32 has no registers for twelve waves
   if (backward) e = sets >= 512 ? delta_walks<E, DK, 2>(st, a) : delta_walks<E, DK, 1>(st, a);
-  else e = sets >= 1024 && four ? delta_walk_results<E, DK, four ? 4 : 2>(st, a) : sets >= 512 ? delta_walk_results<E, DK, 2>(st, a) : delta_walk_results<E, DK, 1>(st, a);
+  else e = sets >= 512 ? delta_walk_results<E, DK, 2>(st, a) : delta_walk_results<E, DK, 1>(st, a);
   if (e != hipSuccess || !backward || a.nchunks == 0) return e;
   const dim3 grid((unsigned)a.nchunks, (unsigned)a.nk);
   if (a.nv == a.nk) hipLaunchKernelGGL((delta_grad_kernel<E, DK, false>), grid, dim3(64 * grad_waves(DK)), 0, st, a);
