@@ -186,9 +186,9 @@ template <typename E> __global__ __launch_bounds__(256) void delta_step_kernel(D
   }
 }
 
-struct DeltaScratch { int64_t records, states, dstates, u, y, total; };
-DeltaScratch delta_layout(bool backward, int T, int ndocs, int nv, int dk, int dv) {
-  const int64_t n = delta_chunk_rows(T, ndocs) * nv, rows = dk <= 64 ? 64 : 128, dvp = cdiv(dv, 16) * 16;
+struct DeltaScratch { int64_t records, halves, states, dstates, u, y, total; };
+DeltaScratch delta_layout(DType dt, bool backward, int T, int ndocs, int nk, int nv, int dk, int dv) {
+  const int64_t chunks = delta_chunk_rows(T, ndocs), n = chunks * nv, rows = dk <= 64 ? 64 : 128, dvp = cdiv(dv, 16) * 16;
   DeltaScratch s = {};
   int64_t at = 0;
   auto take = [&](int64_t bytes) {
@@ -197,6 +197,7 @@ DeltaScratch delta_layout(bool backward, int T, int ndocs, int nv, int dk, int d
     return p;
   };
   s.records = take(n * (backward ? DELTA_RECORD_BWD : DELTA_RECORD_FWD));
+  s.halves = take(backward && dt == BF16 ? chunks * nk * 2 * DELTA_CHUNK * rows * 2 : 0);   // bf16 keys and queries
   if (backward) {
     s.states = take(n * rows * dvp * 4);
     s.dstates = take(n * rows * dvp * 4);
@@ -213,14 +214,17 @@ hipError_t delta_chunks(hipStream_t st, int T, int ndocs, const int32_t* offsets
   hipLaunchKernelGGL(delta_chunks_kernel, dim3(1), dim3(TABLE_THREADS), 0, st, T, ndocs, (int)delta_chunk_rows(T, ndocs), offsets, (int4*)table);
   return hipGetLastError();
 }
-int64_t delta_scratch(bool backward, int T, int ndocs, int nv, int dk, int dv) { return delta_layout(backward, T, ndocs, nv, dk, dv).total; }
+int64_t delta_scratch(DType dt, bool backward, int T, int ndocs, int nk, int nv, int dk, int dv) {
+  return delta_layout(dt, backward, T, ndocs, nk, nv, dk, dv).total;
+}
 hipError_t delta_rule(hipStream_t st, DType dt, const DeltaRule& in, bool backward, void* scratch) {
   DeltaRule a = in;
-  const DeltaScratch s = delta_layout(backward, a.T, a.ndocs, a.nv, a.dk, a.dv);
+  const DeltaScratch s = delta_layout(dt, backward, a.T, a.ndocs, a.nk, a.nv, a.dk, a.dv);
   char* base = (char*)scratch;
   a.nchunks = (int)delta_chunk_rows(a.T, a.ndocs);
   a.dvp = (int)(cdiv(a.dv, 16) * 16);
   a.records = base + s.records;
+  a.halves = (f16*)(base + s.halves);
   a.states = (float*)(base + s.states);
   a.dstates = (float*)(base + s.dstates);
   a.u = (float*)(base + s.u);

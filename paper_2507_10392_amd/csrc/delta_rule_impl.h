@@ -16,11 +16,13 @@
 // and, backward, its gradient, which needs nothing of the forward walk, so that both share a launch), and the gradients of all chunks side by side
 // (delta_grad_kernel).  No atomics: a repeat gives the same bits.
 //
-// Precision.  q, k, v and dO are operands as they stand.  What is computed stays fp32 in registers; where it is an operand it is taken as two values of
-// the type, the rounded one and what that leaves (16 bits of a bf16 pair, 22 of a half pair), in two or three products: the states, the final one
-// and dg and dbeta among them, are sums over the whole document, and the matrix cores have time, since the walk waits for its own last product.
-// Half pairs have a power of two per column in them (the walk), or are bf16 pairs (delta_grad_kernel), so that no size of state or gradient
-// leaves their range.  fp32: v_mfma_f32_16x16x4, no pairs.
+// Precision.  q, k, v and dO are operands as they stand.  What is computed stays fp32 in registers; where it is an operand it is the sum of two or three
+// values of 16 bits, in two to six products.  Forward: two of the type (16 bits of a bf16 pair, 22 of a half pair), since the states, the final one
+// among them, are sums over the whole document and the walk waits for its own last product more than for the matrix cores.  Backward dg is what is left of
+// larger terms: with bf16 pairs throughout it was off by up to 1.5e-5 of its norm.  So the backward's walks take half pairs for bf16 too (keys and
+// queries as halves times a power of two that prep finds, computed values times one per column, so that no size of state or gradient leaves
+// a half's range), and a chunk's gradients three bf16, which are an fp32, of S, dS, U and Y: 1.2e-6, for 15 us in 104 and 5 in 112 (16 heads, 8192 tokens,
+// head widths of 128).  What only goes into dq and dk, which are rounded to 16 bits, stays pairs.  fp32: v_mfma_f32_16x16x4, no pairs.
 #pragma once
 #include "attention_docs_tiles.h"
 
@@ -42,12 +44,16 @@ __device__ __forceinline__ f32x4 mma1(op8<float> a, op8<float> b, f32x4 c) {
   for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
   return c;
 }
-// A value as one operand, or as the sum of two.
+// A value as one operand, or as the sum of two or three, each of what the ones before leave.  Products smaller than the last terms' are left out; small ones come first.
 template <typename E, int TERMS> struct Opnd { op8<E> t[TERMS]; };
 template <typename E, int A, int B> __device__ __forceinline__ f32x4 mma(const Opnd<E, A>& a, const Opnd<E, B>& b, f32x4 c) {
-  if constexpr (A == 2) c = mma1(a.t[1], b.t[0], c);
-  if constexpr (B == 2) c = mma1(a.t[0], b.t[1], c);
-  return mma1(a.t[0], b.t[0], c);
+  constexpr int MOST = A > B ? A : B;
+#pragma unroll
+  for (int order = MOST - 1; order >= 0; --order)
+#pragma unroll
+    for (int i = A - 1; i >= 0; --i)
+      if (i <= order && order - i < B) c = mma1(a.t[i], b.t[order - i], c);
+  return c;
 }
 template <typename M> constexpr int PAIR = sizeof(M) == 2 ? 2 : 1;
 template <typename M> using Pair = Opnd<M, PAIR<M>>;
@@ -59,6 +65,12 @@ __device__ __forceinline__ void split_two(float x, float y, unsigned& hi, unsign
   l.v = __builtin_convertvector(f32x2{x - __uint_as_float(h.w << 16), y - __uint_as_float(h.w & 0xffff0000u)}, bf16x2);
   hi = h.w;
   lo = l.w;
+}
+typedef f16 f16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void split_two(float x, float y, f16x2& hi, f16x2& lo) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  hi = __builtin_convertvector(f32x2{x, y}, f16x2);
+  lo = __builtin_convertvector(f32x2{x - (float)hi[0], y - (float)hi[1]}, f16x2);
 }
 template <typename M> __device__ __forceinline__ Pair<M> pair_of(const f32x4& a, const f32x4& b) {
   Pair<M> o;
@@ -74,6 +86,15 @@ template <typename M> __device__ __forceinline__ Pair<M> pair_of(const f32x4& a,
     }
     o.t[0] = h.v;
     o.t[1] = l.v;
+  } else if constexpr (__is_same(M, f16)) {
+    union { f16x2 w[4]; op8<f16> v; } h, l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const f32x4& x = e < 2 ? a : b;
+      split_two(x[2 * (e & 1)], x[2 * (e & 1) + 1], h.w[e], l.w[e]);
+    }
+    o.t[0] = h.v;
+    o.t[1] = l.v;
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -81,6 +102,18 @@ template <typename M> __device__ __forceinline__ Pair<M> pair_of(const f32x4& a,
       o.t[0][e] = from_f<M>(x);
       if constexpr (PAIR<M> == 2) o.t[1][e] = from_f<M>(fp32_value(x - (float)o.t[0][e]));
     }
+  }
+  return o;
+}
+template <typename M, int TERMS> __device__ __forceinline__ Opnd<M, TERMS> terms_of(f32x4 a, f32x4 b) {   // bf16: three terms are an fp32
+  Opnd<M, TERMS> o;
+  if constexpr (TERMS == 1) o.t[0] = pair_of<M>(a, b).t[0];
+  else {
+    const Pair<M> p = pair_of<M>(a, b);
+    o.t[0] = p.t[0];
+    o.t[1] = p.t[1];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o.t[2][e] = (M)((e < 4 ? a[e & 3] : b[e & 3]) - (float)p.t[0][e] - (float)p.t[1][e]);
   }
   return o;
 }
@@ -92,6 +125,12 @@ __device__ __forceinline__ float rows_sum(float x) {
   auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
+__device__ __forceinline__ float rows_max(float x) {
+  auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
 template <int CTRL> __device__ __forceinline__ float dpp(float x) { return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true)); }
 __device__ __forceinline__ float columns_sum(float x) {
   x += dpp<0xb1>(x);    // neighbours
@@ -99,6 +138,10 @@ __device__ __forceinline__ float columns_sum(float x) {
   x += dpp<0x141>(x);   // the two quads of eight lanes
   return x + dpp<0x140>(x);
 }
+
+// What a walk and a chunk's own matrices are computed in: backward bf16 as half.
+template <typename E, bool BWD> struct WalkOf { typedef E type; };
+template <> struct WalkOf<bf16, true> { typedef f16 type; };
 
 // Half: the power of two that brings the largest of a column's values, which lie in the four lanes that share lane % 16, to 2^13 .. 2^14; else 1.
 template <typename M, int N> __device__ __forceinline__ float column_unit(const f32x4 (&x)[N]) {
@@ -108,8 +151,7 @@ template <typename M, int N> __device__ __forceinline__ float column_unit(const 
   for (int i = 0; i < N; ++i)
 #pragma unroll
     for (int r = 0; r < 4; ++r) m = fmaxf(m, fabsf(x[i][r]));
-  m = fmaxf(m, __shfl_xor(m, 16, 64));
-  m = fmaxf(m, __shfl_xor(m, 32, 64));
+  m = rows_max(m);
   const int e = (int)(__float_as_uint(m) >> 23) & 255;
   return m > 0.f && e < 255 ? __uint_as_float((unsigned)min(max(127 + 13 + 127 - e, 1), 253) << 23) : 1.f;
 }
@@ -242,7 +284,8 @@ template <typename E, int D> struct TileOps {
   }
 };
 
-// What delta_prep_kernel leaves of a chunk and value head: per token exp(G), exp(G_last - G), beta, and exp(G_last) in the fourth row's first place;
+// What delta_prep_kernel leaves of a chunk and value head: per token exp(G), exp(G_last - G), beta, and exp(G_last) in the fourth row's first place,
+// behind it what undoes the units of keys and queries;
 // then matrices as operands, pair by pair: of T and P, lower triangles, rows by m and terms by s <= m/2; of T^T and P^T, upper ones, s >= m/2.
 constexpr int REC_GATES = 1024, REC_OP = 2048, REC_TRIANGLE = 6 * REC_OP;
 constexpr int REC_T = REC_GATES, REC_P = REC_T + REC_TRIANGLE, REC_FWD = REC_P + REC_TRIANGLE;
@@ -384,11 +427,14 @@ template <typename E> __device__ __forceinline__ void fill_rows(E* p, int64_t ld
 }
 
 // A workgroup per chunk and key head; the value heads of the key head one after the other.
-template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256, 4) void delta_prep_kernel(DeltaRule a) {
+constexpr int prep_lds(int tile) { return 2 * tile > 2 * 64 * TRI_LD * 4 ? 2 * tile : 2 * 64 * TRI_LD * 4; }   // A and T take the place of keys and queries
+template <typename E, int DK> constexpr int PREP_LDS = prep_lds(Tile<E, DK>::bytes(DELTA_C));
+template <typename E, int DK> constexpr int PREP_GROUPS = PREP_LDS<E, DK> <= 36 * 1024 ? 4 : 2;   // on a CU
+template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256, (PREP_GROUPS<E, DK>)) void delta_prep_kernel(DeltaRule a) {
   typedef Tile<E, DK> TL;
+  typedef typename WalkOf<E, BWD>::type A16;
   constexpr int TILE = TL::bytes(DELTA_C), KS = DK / 32;
-  constexpr int MATS = 2 * 64 * TRI_LD * 4;
-  __shared__ __align__(16) char tiles[2 * TILE > MATS ? 2 * TILE : MATS];   // A and T take the place of keys and queries
+  __shared__ __align__(16) char tiles[PREP_LDS<E, DK>];
   float *A = reinterpret_cast<float*>(tiles), *Tm = A + 64 * TRI_LD;
   __shared__ double G[64];
   __shared__ float B[64];
@@ -419,6 +465,47 @@ template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256, 4) voi
   tile_wait();
   __syncthreads();
   const TileOps<E, DK> at(smem, lane);
+  float k_unit = 1.f, q_unit = 1.f;
+  if constexpr (!__is_same(A16, E)) {   // keys and queries as halves, times powers of two that bring the largest of either to 2^3 .. 2^4
+    constexpr int PIECES = DK / 8, MINE = 64 * PIECES / 256;
+    bf16x8 x[2][MINE];
+    float most[2] = {0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < MINE; ++i) {
+        const int piece = (int)threadIdx.x + 256 * i, row = piece / PIECES, p = piece % PIECES;
+        x[t][i] = lds_read<bf16x8>(smem + t * TILE + row / 8 * TL::OCTET + (p >> 3) * 1024 + TL::place(row & 7, p & 7));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most[t] = fmaxf(most[t], fabsf((float)x[t][i][e]));
+      }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) most[t] = wave_max(most[t]);
+    __syncthreads();
+    if (lane == 0) {
+      B[wave] = most[0];
+      B[4 + wave] = most[1];
+    }
+    __syncthreads();
+    auto unit = [&](int at) {
+      const float m = fmaxf(fmaxf(B[at], B[at + 1]), fmaxf(B[at + 2], B[at + 3]));
+      const int e = (int)(__float_as_uint(m) >> 23);
+      return m > 0.f && e < 255 ? __uint_as_float((unsigned)min(max(257 - e, 77), 177) << 23) : 1.f;
+    };
+    k_unit = unit(0);
+    q_unit = unit(4);
+    f16* to = a.halves + ((int64_t)blockIdx.x * a.nk + kv) * (2 * 64 * DK);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int i = 0; i < MINE; ++i) {
+        f16x8 h;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] = (f16)((float)x[t][i][e] * (t ? q_unit : k_unit));
+        *reinterpret_cast<f16x8*>(to + t * 64 * DK + ((int)threadIdx.x + 256 * i) * 8) = h;
+      }
+  }
+  const float p_unit = k_unit * q_unit, k_inv = 1.f / k_unit, q_inv = 1.f / q_unit;   // powers of two
   // This wave's rows (kk, and qk of P^T backward: rows j) or columns (qk of P: rows of P^T are keys) against all tiles of the other side.
   f32x4 kk[4], qk[4];
 #pragma unroll
@@ -451,7 +538,7 @@ template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256, 4) voi
       gates[lane] = in ? decay(sum, 0.0) : 0.f;
       gates[64 + lane] = in ? decay(last, sum) : 0.f;
       gates[128 + lane] = beta;
-      gates[192 + lane] = lane == 0 ? decay(last, 0.0) : 0.f;
+      gates[192 + lane] = lane == 0 ? decay(last, 0.0) : lane == 1 ? k_inv : lane == 2 ? q_inv : 0.f;
       if constexpr (BWD) reinterpret_cast<double*>(rec + REC_G)[lane] = sum;
     }
     __syncthreads();
@@ -483,14 +570,14 @@ template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256, 4) voi
       for (int r = 0; r < 4; ++r) {
         const int row = 16 * n + 4 * g + r, col = 16 * wave + i16;
         const double gr = G[row];
-        if constexpr (BWD) p[n][r] = row >= col ? qk[n][r] * decay(gr, gc) : 0.f;   // P_row,col
-        else p[n][r] = row <= col ? qk[n][r] * decay(gc, gr) : 0.f;                 // P_col,row
+        if constexpr (BWD) p[n][r] = row >= col ? p_unit * qk[n][r] * decay(gr, gc) : 0.f;   // P_row,col
+        else p[n][r] = row <= col ? p_unit * qk[n][r] * decay(gc, gr) : 0.f;                 // P_col,row
       }
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       if constexpr (BWD) {
-        if (2 * s + 1 >= wave) store_op<E>(rec + REC_P + upper_op(wave, s) * REC_OP, pair_of<E>(p[2 * s], p[2 * s + 1]), lane);
-      } else if (2 * s <= wave) store_op<E>(rec + REC_P + lower_op(wave, s) * REC_OP, pair_of<E>(p[2 * s], p[2 * s + 1]), lane);
+        if (2 * s + 1 >= wave) store_op<A16>(rec + REC_P + upper_op(wave, s) * REC_OP, pair_of<A16>(p[2 * s], p[2 * s + 1]), lane);
+      } else if (2 * s <= wave) store_op<A16>(rec + REC_P + lower_op(wave, s) * REC_OP, pair_of<A16>(p[2 * s], p[2 * s + 1]), lane);
     }
     __syncthreads();
     invert_lower(A, Tm, wave, lane);
@@ -498,7 +585,7 @@ template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256, 4) voi
     for (int s = 0; s < 2; ++s) {
       if (2 * s <= wave) {
         const float* row = Tm + (16 * wave + i16) * TRI_LD + 32 * s + 4 * g;
-        store_op<E>(rec + REC_T + lower_op(wave, s) * REC_OP, pair_of<E>(*reinterpret_cast<const f32x4*>(row), *reinterpret_cast<const f32x4*>(row + 16)), lane);
+        store_op<A16>(rec + REC_T + lower_op(wave, s) * REC_OP, pair_of<A16>(*reinterpret_cast<const f32x4*>(row), *reinterpret_cast<const f32x4*>(row + 16)), lane);
       }
       if constexpr (BWD)
         if (2 * s + 1 >= wave) {
@@ -508,7 +595,7 @@ template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256, 4) voi
             x[e] = Tm[(32 * s + 4 * g + e) * TRI_LD + 16 * wave + i16];
             y[e] = Tm[(32 * s + 16 + 4 * g + e) * TRI_LD + 16 * wave + i16];
           }
-          store_op<E>(rec + REC_TT + upper_op(wave, s) * REC_OP, pair_of<E>(x, y), lane);
+          store_op<A16>(rec + REC_TT + upper_op(wave, s) * REC_OP, pair_of<A16>(x, y), lane);
         }
     }
   }
@@ -527,7 +614,7 @@ constexpr int walk_loaders(int NW) { return NW == 1 ? 4 : 2; }   // a wave issue
 constexpr int walk_threads(int NW) { return 64 * (3 * NW + walk_loaders(NW)); }
 
 template <typename E, int DK, int NW, int KIND> struct WalkLds {
-  typedef Tile<E, DK> TL;
+  typedef Tile<typename WalkOf<E, KIND != WALK_RESULTS>::type, DK> TL;
   typedef Tile<E, 64> VL;
   static constexpr int REC = KIND == WALK_STATES ? REC_P : REC_FWD;   // gates and T; and P; or gates, P^T and T^T
   static constexpr int VSIZE = VL::bytes(DELTA_C), QSIZE = KIND == WALK_STATES ? 0 : TL::bytes(DELTA_C);
@@ -554,30 +641,32 @@ template <typename M> __device__ __forceinline__ void write_op(unsigned lds_of_l
 
 template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void delta_walk(char* smem_raw, const DeltaRule& a, int doc_rank, int h, int c0) {
   typedef WalkLds<E, DK, NW, KIND> L;
-  constexpr int RT = DK / 16, KS = DK / 32, HT = RT / 2, HS = KS / 2, LOADERS = walk_loaders(NW), FW = LOADERS ? LOADERS : NW;
-  constexpr bool HALF_E = __is_same(E, f16), BACK = KIND == WALK_GRADIENTS, RESULTS = KIND == WALK_RESULTS, AHEAD = L::NBUF == 2, ALL_AHEAD = L::VBUF == 2,
-                 EARLY = !LOADERS || !ALL_AHEAD;
+  typedef typename WalkOf<E, KIND != WALK_RESULTS>::type M;   // of the products
+  constexpr int RT = DK / 16, KS = DK / 32, HT = RT / 2, HS = KS / 2, FW = walk_loaders(NW);
+  constexpr bool HALF_E = __is_same(M, f16), COPIES = !__is_same(M, E), BACK = KIND == WALK_GRADIENTS, RESULTS = KIND == WALK_RESULTS, AHEAD = L::NBUF == 2, ALL_AHEAD = L::VBUF == 2;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = wave % NW, g = lane >> 4, i16 = lane & 15;
-  const bool chain = wave < 2 * NW, helps = !chain && wave < 3 * NW, loads = LOADERS ? wave >= 3 * NW : helps;
-  const int fw = LOADERS ? wave - 3 * NW : mine;
+  const bool chain = wave < 2 * NW, helps = !chain && wave < 3 * NW, loads = wave >= 3 * NW;
+  const int fw = wave - 3 * NW;
   const int4 row = reinterpret_cast<const int4*>(a.chunks)[1 + doc_rank];   // first token, tokens, first chunk, document
   const int first = row.x, count = row.y, chunk0 = row.z, doc = row.w, chunks = (count + DELTA_C - 1) / DELTA_C;
   const int kv = h / (a.nv / a.nk), w0 = c0 + 16 * mine, col = w0 + i16;    // the wave's first column and the lane's
   const unsigned smem = lds_address(smem_raw), hand = smem + L::H + mine * L::HAND + 16 * lane, hand_z = hand + DK * 64, hand_add = hand_z + 4096;
-  const unsigned units = smem + L::UNITS + mine * Tile<E, DK>::OCTET;       // of the state's columns, and 64 bytes on of Z's
+  const unsigned units = smem + L::UNITS + mine * Tile<M, DK>::OCTET;       // of the state's columns, and 64 bytes on of Z's
   const int step = BACK ? -1 : 1;
   const int64_t states = (int64_t)a.dk * a.dv;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 
   // ---- loads
-  const TileLoad<E, DK, DELTA_C, FW> load_k(a.ldk, lane, a.dk), load_q(a.ldq, lane, a.dk);
+  const TileLoad<M, DK, DELTA_C, FW> load_k(COPIES ? DK : a.ldk, lane, COPIES ? DK : a.dk), load_q(COPIES ? DK : a.ldq, lane, COPIES ? DK : a.dk);
   const TileLoad<E, 64, DELTA_C, FW> load_v(BACK ? a.ldo : a.ldv, lane, min(a.dv - c0, 16 * NW));
   // Loads of a wave, at least: of the keys, of the chunk's matrices, of values and queries.
-  constexpr int KEYS = TileLoad<E, DK, DELTA_C, FW>::N, MATS = BACK ? REC_GATES / 1024 / FW + 2 * REC_TRIANGLE / 1024 / FW : L::REC / 1024 / FW;
-  constexpr int SECOND = TileLoad<E, 64, DELTA_C, FW>::N + (KIND == WALK_STATES ? 0 : TileLoad<E, DK, DELTA_C, FW>::N);
+  constexpr int KEYS = TileLoad<M, DK, DELTA_C, FW>::N, MATS = BACK ? REC_GATES / 1024 / FW + 2 * REC_TRIANGLE / 1024 / FW : L::REC / 1024 / FW;
+  constexpr int SECOND = TileLoad<E, 64, DELTA_C, FW>::N + (KIND == WALK_STATES ? 0 : TileLoad<M, DK, DELTA_C, FW>::N);
+  auto copies = [&](int c) { return a.halves + ((int64_t)(chunk0 + c) * a.nk + kv) * (2 * DELTA_C * DK); };
   auto fetch_keys = [&](int c, unsigned to) {
     const int t0 = first + DELTA_C * c, end = min(first + count, t0 + DELTA_C);
-    tile_ahead(load_k, to + L::K, (const E*)a.k + kv * a.dk, t0, end, fw);
+    if constexpr (COPIES) tile_ahead(load_k, to + L::K, copies(c), 0, DELTA_C, fw);
+    else tile_ahead(load_k, to + L::K, (const M*)a.k + kv * a.dk, t0, end, fw);
   };
   auto fetch_mats = [&](int c, unsigned to) {
     const char* rec = a.records + ((int64_t)(chunk0 + c) * a.nv + h) * (RESULTS ? REC_FWD : REC_BWD);
@@ -589,7 +678,10 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
   auto fetch_second = [&](int c, unsigned by) {
     const int t0 = first + DELTA_C * c, end = min(first + count, t0 + DELTA_C);
     tile_ahead(load_v, smem + L::V + by, (BACK ? (const E*)a.dout : (const E*)a.v) + h * a.dv + c0, t0, end, fw);
-    if constexpr (KIND != WALK_STATES) tile_ahead(load_q, smem + L::Q + by, (const E*)a.q + kv * a.dk, t0, end, fw);
+    if constexpr (KIND != WALK_STATES) {
+      if constexpr (COPIES) tile_ahead(load_q, smem + L::Q + by, copies(c) + DELTA_C * DK, 0, DELTA_C, fw);
+      else tile_ahead(load_q, smem + L::Q + by, (const M*)a.q + kv * a.dk, t0, end, fw);
+    }
   };
   auto fetch_all = [&](int c) {
     fetch_keys(c, smem);
@@ -601,8 +693,8 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
     fetch_all(c);
     if (AHEAD && chunks > 1) {
       fetch_keys(c + step, smem + L::FIRST);
-      if constexpr (EARLY) fetch_mats(c + step, smem + L::FIRST);
-      loads_but<KEYS + (EARLY ? MATS : 0)>();
+      if constexpr (!ALL_AHEAD) fetch_mats(c + step, smem + L::FIRST);
+      loads_but<KEYS + (ALL_AHEAD ? 0 : MATS)>();
     } else tile_wait();
   }
   // The two barriers of chunk n, and the loading waves' part of them: what they have to see arrived before, what they ask for behind.  After the second one
@@ -610,13 +702,13 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
   // the chain reads a phase ahead, at once, the others of a loader of its own in the next phase, so that it comes to the barriers in time.
   auto begin_chunk = [&](int n) {
     if (ALL_AHEAD && loads && n + 1 < chunks) {
-      if constexpr (!EARLY) fetch_mats(c + step, smem + ((n + 1) & 1) * L::FIRST);
+      fetch_mats(c + step, smem + ((n + 1) & 1) * L::FIRST);
       fetch_second(c + step, ((n + 1) & 1) * L::SECOND);
     }
   };
   auto middle = [&](int n) {
     if (AHEAD && loads && n + 1 < chunks) {   // the next keys
-      if constexpr (ALL_AHEAD) loads_but<(EARLY ? 0 : MATS) + SECOND>();
+      if constexpr (ALL_AHEAD) loads_but<MATS + SECOND>();
       else tile_wait();
     }
     __syncthreads();
@@ -624,13 +716,13 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
       if constexpr (!ALL_AHEAD) fetch_second(c + step, 0);
       if (n + 2 < chunks) {
         fetch_keys(c + 2 * step, smem + (n & 1) * L::FIRST);
-        if constexpr (EARLY) fetch_mats(c + 2 * step, smem + (n & 1) * L::FIRST);
+        if constexpr (!ALL_AHEAD) fetch_mats(c + 2 * step, smem + (n & 1) * L::FIRST);
       }
     }
   };
   auto end_chunk = [&](int n) {
     if (AHEAD && loads) {   // the next matrices, values and queries
-      if (n + 2 < chunks) loads_but<KEYS + (EARLY ? MATS : 0)>();
+      if (n + 2 < chunks) loads_but<KEYS + (ALL_AHEAD ? 0 : MATS)>();
       else tile_wait();
     }
     __syncthreads();
@@ -646,7 +738,7 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
   if (chain) {
     const int half = wave / NW;   // of the state's rows, and of the tokens
     const TileOps<E, 64> at_v(smem + L::V, lane);
-    TileOps<E, DK> at;
+    TileOps<M, DK> at;
     at.state_places(smem + L::K, lane);
     // Of keys' rows the columns that belong to this half of the state come first, of their columns only these: either 64 columns, whose places
     // change places, or further ones.
@@ -661,16 +753,16 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
     const unsigned own = SWAP ? 0u : (unsigned)(half * (sizeof(E) == 2 ? 1024 : HS * 1024)), not_own = SWAP ? 0u : (sizeof(E) == 2 ? 1024u : HS * 1024u) - own;
     const bool live = col < a.dv;
     f32x4 S[HT];
-    Pair<E> sp[HS];
+    Pair<M> sp[HS];
     float s_unit = 1.f;
     auto publish_state = [&]() {
       if constexpr (HALF_E) {   // of these rows; the other half's may be another
-        s_unit = column_unit<E>(S);
+        s_unit = column_unit<M>(S);
         if (lane < 16) lds_write(units + 64 * half + 4 * lane, s_unit);
       }
-      pairs_of<E>(sp, S, s_unit);
+      pairs_of<M>(sp, S, s_unit);
 #pragma unroll
-      for (int s = 0; s < HS; ++s) write_op<E>(hand + (HS * half + s) * 2048, sp[s]);
+      for (int s = 0; s < HS; ++s) write_op<M>(hand + (HS * half + s) * 2048, sp[s]);
     };
     const float* from = BACK ? a.dht : a.h0;
 #pragma unroll
@@ -685,9 +777,9 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
     }
     if (chunks > 0) publish_state();
     __syncthreads();
-    Opnd<E, 1> kf[HS][2], ko[HS][2];   // this half's rows of the chunk's keys: of this and of the other half's columns
+    Opnd<M, 1> kf[HS][2], ko[HS][2];   // this half's rows of the chunk's keys: of this and of the other half's columns
     auto load_keys = [&]() {
-      const unsigned rows = half * 4 * Tile<E, DK>::OCTET;
+      const unsigned rows = half * 4 * Tile<M, DK>::OCTET;
 #pragma unroll
       for (int s = 0; s < HS; ++s)
 #pragma unroll
@@ -700,10 +792,11 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
     for (int n = 0; n < chunks; ++n, c += step) {
       const unsigned buf = AHEAD ? (unsigned)(n & 1) * L::FIRST : 0u, gates = smem + buf + L::R, ops = gates + REC_GATES + 16 * lane, gates4 = gates + 16 * g;
       const unsigned second = ALL_AHEAD ? (unsigned)(n & 1) * L::SECOND : 0u, mine4 = gates4 + 128 * half;   // gates of this half's tokens
-      Pair<E> so[HS];   // the other half of the state
+      Pair<M> so[HS];   // the other half of the state
 #pragma unroll
-      for (int s = 0; s < HS; ++s) so[s] = load_op<E>(hand + (HS * (1 - half) + s) * 2048);
-      float o_unit = 1.f;
+      for (int s = 0; s < HS; ++s) so[s] = load_op<M>(hand + (HS * (1 - half) + s) * 2048);
+      float o_unit = 1.f, k_inv = 1.f, y_inv = 1.f;
+      if constexpr (HALF_E) k_inv = lds_read<float>(gates + 772);
       if constexpr (HALF_E) o_unit = lds_read<float>(units + 4 * i16 + (half ? 0 : 64));
       f32x4 x[2], xo[2], y[2], z[2];
 #pragma unroll
@@ -723,44 +816,62 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
         vf[0] = at_v.column(second, mine, 0);
         vf[1] = at_v.column(second, mine, 1);
       } else vf[0] = at_v.column(second + half * 4 * Tile<E, 64>::OCTET, mine, 0);
-      Pair<E> tf[6];
+      Pair<M> tf[6];
       if constexpr (BACK) {   // P^T: its first four operands are the first half's rows, the others the second's
 #pragma unroll
-        for (int i = 0; i < 4; ++i) tf[i] = load_op<E>(ops + (half ? 4 + (i & 1) : i) * REC_OP);
+        for (int i = 0; i < 4; ++i) tf[i] = load_op<M>(ops + (half ? 4 + (i & 1) : i) * REC_OP);
       }
 #pragma unroll
       for (int s = 0; s < HS; ++s)
 #pragma unroll
         for (int m = 0; m < 2; ++m) xo[m] = mma(ko[s][m], so[s], xo[m]);
       if constexpr (BACK) {
+        Opnd<M, 1> dof[2];
+        if constexpr (COPIES) {   // dO as halves: one operand, times a power of two
+          f32x4 d[4];
+#pragma unroll
+          for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) d[m][r] = (float)vf[m >> 1].t[0][4 * (m & 1) + r];
+          const float unit = column_unit<M>(d);
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dof[s].t[0][e] = (M)(d[2 * s + (e >> 2)][e & 3] * unit);
+          y_inv = inverse_unit<M>(unit);
+        } else {
+          dof[0].t[0] = vf[0].t[0];
+          dof[1].t[0] = vf[1].t[0];
+        }
+        if constexpr (HALF_E) y_inv *= k_inv * lds_read<float>(gates + 776);   // P^T has the units of keys and queries in it
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-          if (half) y[m] = mma(tf[m], vf[1], y[m]);
-          else y[m] = mma(tf[2 * m + 1], vf[1], mma(tf[2 * m], vf[0], y[m]));
+          if (half) y[m] = mma(tf[m], dof[1], y[m]);
+          else y[m] = mma(tf[2 * m + 1], dof[1], mma(tf[2 * m], dof[0], y[m]));
         }
       }
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(ops + (BACK ? REC_TRIANGLE : 0) + i * REC_OP);   // T, or T^T
+      for (int i = 0; i < 6; ++i) tf[i] = load_op<M>(ops + (BACK ? REC_TRIANGLE : 0) + i * REC_OP);   // T, or T^T
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
-        const f32x4 ks = HALF_E ? x[m] * inverse_unit<E>(s_unit) + xo[m] * inverse_unit<E>(o_unit) : x[m] + xo[m];
+        const f32x4 ks = HALF_E ? (x[m] * inverse_unit<M>(s_unit) + xo[m] * inverse_unit<M>(o_unit)) * k_inv : x[m] + xo[m];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          if constexpr (BACK) z[m][r] = a.scale * y[m][r] + other[m][r] * ks[r];
+          if constexpr (BACK) z[m][r] = a.scale * y_inv * y[m][r] + other[m][r] * ks[r];
           else z[m][r] = other[m][r] * ((float)vf[0].t[0][4 * m + r] - since[m][r] * ks[r]);
         }
       }
       {
-        const float unit = column_unit<E>(z);
-        Pair<E> zp[1];
-        pairs_of<E>(zp, z, unit);
-        write_op<E>(hand_z + half * 2048, zp[0]);
-        if (HALF_E && lane < 16) lds_write(units + Tile<E, DK>::OCTET * 4 + 64 * half + 4 * lane, unit);
+        const float unit = column_unit<M>(z);
+        Pair<M> zp[1];
+        pairs_of<M>(zp, z, unit);
+        write_op<M>(hand_z + half * 2048, zp[0]);
+        if (HALF_E && lane < 16) lds_write(units + Tile<M, DK>::OCTET * 4 + 64 * half + 4 * lane, unit);
       }
       __builtin_amdgcn_sched_barrier(0);
-      Opnd<E, 1> kc[HT][2];   // columns of the keys, this half's rows of the state
+      Opnd<M, 1> kc[HT][2];   // columns of the keys, this half's rows of the state
 #pragma unroll
       for (int i = 0; i < HT; ++i)
 #pragma unroll
@@ -773,12 +884,12 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
       }
       const float whole = lds_read<float>(gates + 768);
       middle(n);
-      Pair<E> zp[2];
+      Pair<M> zp[2];
       float zi[2] = {1.f, 1.f};
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        zp[s] = load_op<E>(hand_z + s * 2048);
-        if constexpr (HALF_E) zi[s] = inverse_unit<E>(lds_read<float>(units + Tile<E, DK>::OCTET * 4 + 64 * s + 4 * i16));
+        zp[s] = load_op<M>(hand_z + s * 2048);
+        if constexpr (HALF_E) zi[s] = inverse_unit<M>(lds_read<float>(units + Tile<M, DK>::OCTET * 4 + 64 * s + 4 * i16));
       }
       f32x4 add[HT];
       if constexpr (BACK)
@@ -793,7 +904,7 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
 #pragma unroll
         for (int m = 0; m < 4; ++m)
           if (BACK ? s >= m / 2 : s <= m / 2) {
-            const Pair<E>& t = tf[BACK ? upper_op(m, s) : lower_op(m, s)];
+            const Pair<M>& t = tf[BACK ? upper_op(m, s) : lower_op(m, s)];
             if (HALF_E && s == 1) uo[m] = mma(t, zp[s], uo[m]);
             else u[m] = mma(t, zp[s], u[m]);
           }
@@ -802,9 +913,9 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
         if constexpr (HALF_E) u[m] = u[m] * zi[0] + uo[m] * zi[1];
         next[m] = u[m] * factor[m];
       }
-      Pair<E> np[2];
-      const float n_unit = column_unit<E>(next), n_inv = inverse_unit<E>(n_unit);
-      pairs_of<E>(np, next, n_unit);
+      Pair<M> np[2];
+      const float n_unit = column_unit<M>(next), n_inv = inverse_unit<M>(n_unit);
+      pairs_of<M>(np, next, n_unit);
       if (AHEAD) load_keys();   // (behind the last chunk nothing is there, and nothing takes them)
       __builtin_amdgcn_sched_barrier(0);
       if constexpr (HALF_E) {
@@ -817,7 +928,7 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
           for (int i = 0; i < HT; ++i) p[i] = mma(kc[i][s], np[s], p[i]);
 #pragma unroll
         for (int i = 0; i < HT; ++i) {
-          S[i] = S[i] * whole + p[i] * n_inv;
+          S[i] = S[i] * whole + p[i] * (n_inv * k_inv);
           if constexpr (BACK) S[i] += add[i];
         }
       } else {
@@ -854,27 +965,32 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
     return;
   }
   if constexpr (RESULTS) {
-    TileOps<E, DK> at;
+    TileOps<M, DK> at;
     at.state_places(smem + L::Q, lane);
     for (int n = 0; n < chunks; ++n, c += step) {
       const unsigned gates = smem + (AHEAD ? (unsigned)(n & 1) * L::FIRST : 0u) + L::R, ops = gates + REC_GATES + 16 * lane;
       begin_chunk(n);
-      Pair<E> sf[KS];
+      Pair<M> sf[KS];
 #pragma unroll
-      for (int s = 0; s < KS; ++s) sf[s] = load_op<E>(hand + s * 2048);
+      for (int s = 0; s < KS; ++s) sf[s] = load_op<M>(hand + s * 2048);
       f32x4 back_s[2];   // half: of the rows' columns, of either half of the state
       if constexpr (HALF_E) {
         back_s[0] = lds_read<f32x4>(units + 16 * g);
         back_s[1] = lds_read<f32x4>(units + 64 + 16 * g);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          back_s[0][r] = inverse_unit<E>(back_s[0][r]);
-          back_s[1][r] = inverse_unit<E>(back_s[1][r]);
+          back_s[0][r] = inverse_unit<M>(back_s[0][r]);
+          back_s[1][r] = inverse_unit<M>(back_s[1][r]);
         }
+      }
+      float q_inv = 1.f, p_inv = 1.f;
+      if constexpr (HALF_E) {
+        q_inv = lds_read<float>(gates + 776);
+        p_inv = q_inv * lds_read<float>(gates + 772);
       }
       f32x4 o[4], oo[4];   // transposed: rows are columns of the state, a lane has the token lane % 16
       float zi[2];         // half: the inverse units of Z
-      Pair<E> pf[6], tf[6], zp[2];
+      Pair<M> pf[6], tf[6], zp[2];
 #pragma unroll
       for (int m = 0; m < 4; ++m) o[m] = oo[m] = zero;
 #pragma unroll
@@ -888,20 +1004,20 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
         const float since = lds_read<float>(gates + 4 * (16 * m + i16));
-        if constexpr (HALF_E) o[m] = (o[m] * back_s[0] + oo[m] * back_s[1]) * since;
+        if constexpr (HALF_E) o[m] = (o[m] * back_s[0] + oo[m] * back_s[1]) * (since * q_inv);
         else o[m] *= since;
       }
 #pragma unroll
       for (int i = 0; i < 6; ++i) {
-        tf[i] = load_op<E>(ops + i * REC_OP);
-        pf[i] = load_op<E>(ops + REC_TRIANGLE + i * REC_OP);
+        tf[i] = load_op<M>(ops + i * REC_OP);
+        pf[i] = load_op<M>(ops + REC_TRIANGLE + i * REC_OP);
       }
       middle(n);
-      zp[0] = load_op<E>(hand_z);
-      zp[1] = load_op<E>(hand_z + 2048);
+      zp[0] = load_op<M>(hand_z);
+      zp[1] = load_op<M>(hand_z + 2048);
       if constexpr (HALF_E)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) zi[s] = inverse_unit<E>(lds_read<float>(units + Tile<E, DK>::OCTET * 4 + 4 * i16 + 64 * s));
+        for (int s = 0; s < 2; ++s) zi[s] = inverse_unit<M>(lds_read<float>(units + Tile<M, DK>::OCTET * 4 + 4 * i16 + 64 * s));
       f32x4 u[4], uo[4], p[4], back_u = zero;
 #pragma unroll
       for (int m = 0; m < 4; ++m) u[m] = uo[m] = zero;
@@ -916,9 +1032,9 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
       if constexpr (HALF_E)
 #pragma unroll
         for (int m = 0; m < 4; ++m) u[m] = u[m] * zi[0] + uo[m] * zi[1];
-      Pair<E> up[2];
-      const float unit = column_unit<E>(u), inv = inverse_unit<E>(unit);
-      pairs_of<E>(up, u, unit);
+      Pair<M> up[2];
+      const float unit = column_unit<M>(u), inv = inverse_unit<M>(unit);
+      pairs_of<M>(up, u, unit);
       if constexpr (HALF_E) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) back_u[r] = __shfl(inv, 4 * g + r, 64);
@@ -935,7 +1051,7 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
           const int t = DELTA_C * c + 16 * m + i16;
-          if constexpr (HALF_E) p[m] = p[m] * back_u + o[m];
+          if constexpr (HALF_E) p[m] = p[m] * (back_u * p_inv) + o[m];
           if (t < count) {
             typedef E quad_t __attribute__((ext_vector_type(4)));
             quad_t w;
@@ -947,7 +1063,7 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
       end_chunk(n);
     }
   } else {
-    TileOps<E, DK> at;
+    TileOps<M, DK> at;
     at.state_places(smem + L::Q, lane);
     const TileOps<E, 64> at_v(smem + L::V, lane);
     for (int n = 0; n < chunks; ++n, c += step) {
@@ -956,13 +1072,13 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
       begin_chunk(n);
       // the state, as its pairs are: what the gradients' products take
       float* to = (BACK ? a.dstates : a.states) + rec * DK * a.dvp + col;
-      Pair<E> sf[KS];
+      Pair<M> sf[KS];
 #pragma unroll
-      for (int s = 0; s < KS; ++s) sf[s] = load_op<E>(hand + s * 2048);
+      for (int s = 0; s < KS; ++s) sf[s] = load_op<M>(hand + s * 2048);
       float inv[2] = {1.f, 1.f};
       if constexpr (HALF_E) {
-        inv[0] = inverse_unit<E>(lds_read<float>(units + 4 * i16));
-        inv[1] = inverse_unit<E>(lds_read<float>(units + 64 + 4 * i16));
+        inv[0] = inverse_unit<M>(lds_read<float>(units + 4 * i16));
+        inv[1] = inverse_unit<M>(lds_read<float>(units + 64 + 4 * i16));
       }
       if (col < a.dvp)
 #pragma unroll
@@ -970,7 +1086,7 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             float x = (float)sf[s].t[0][e];
-            if constexpr (PAIR<E> == 2) x += (float)sf[s].t[1][e];
+            if constexpr (PAIR<M> == 2) x += (float)sf[s].t[1][e];
             to[(32 * s + 8 * g + e) * a.dvp] = HALF_E ? x * inv[s >= HS] : x;
           }
       if constexpr (BACK) {   // scale Q^T (exp(G) dO)
@@ -985,9 +1101,9 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
 #pragma unroll
           for (int r = 0; r < 4; ++r) d[m][r] = a.scale * since[r] * (float)vf[m >> 1].t[0][4 * (m & 1) + r];
         }
-        Pair<E> dp[2];
-        const float unit = column_unit<E>(d), back = inverse_unit<E>(unit);
-        pairs_of<E>(dp, d, unit);
+        Pair<M> dp[2];
+        const float unit = column_unit<M>(d), back = inverse_unit<M>(unit);
+        pairs_of<M>(dp, d, unit);
 #pragma unroll
         for (int i = 0; i < RT; ++i) add[i] = zero;
 #pragma unroll
@@ -996,20 +1112,20 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
           for (int i = 0; i < RT; ++i) add[i] = mma(at.state_column(0, i, s), dp[s], add[i]);
         if constexpr (ALL_AHEAD) at.move_state_places((n & 1) ? (unsigned)-L::SECOND : (unsigned)L::SECOND);
 #pragma unroll
-        for (int i = 0; i < RT; ++i) lds_write(hand_add + i * 1024, HALF_E ? add[i] * back : add[i]);
+        for (int i = 0; i < RT; ++i) lds_write(hand_add + i * 1024, HALF_E ? add[i] * (back * lds_read<float>(gates + 776)) : add[i]);
       }
-      Pair<E> tf[6], zp[2];
+      Pair<M> tf[6], zp[2];
 #pragma unroll
-      for (int i = 0; i < 6; ++i) tf[i] = load_op<E>(ops + (BACK ? REC_TRIANGLE : 0) + i * REC_OP);
+      for (int i = 0; i < 6; ++i) tf[i] = load_op<M>(ops + (BACK ? REC_TRIANGLE : 0) + i * REC_OP);
       middle(n);
       f32x4 u[4], uo[4], back_z[2];   // transposed: rows are columns of the state
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        zp[s] = load_op<E>(hand_z + s * 2048);
+        zp[s] = load_op<M>(hand_z + s * 2048);
         if constexpr (HALF_E) {
-          back_z[s] = lds_read<f32x4>(units + Tile<E, DK>::OCTET * 4 + 64 * s + 16 * g);
+          back_z[s] = lds_read<f32x4>(units + Tile<M, DK>::OCTET * 4 + 64 * s + 16 * g);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) back_z[s][r] = inverse_unit<E>(back_z[s][r]);
+          for (int r = 0; r < 4; ++r) back_z[s][r] = inverse_unit<M>(back_z[s][r]);
         }
       }
 #pragma unroll
@@ -1019,7 +1135,7 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
 #pragma unroll
         for (int m = 0; m < 4; ++m)
           if (BACK ? s >= m / 2 : s <= m / 2) {
-            const Pair<E>& t = tf[BACK ? upper_op(m, s) : lower_op(m, s)];
+            const Pair<M>& t = tf[BACK ? upper_op(m, s) : lower_op(m, s)];
             if (HALF_E && s == 1) uo[m] = mma(zp[s], t, uo[m]);
             else u[m] = mma(zp[s], t, u[m]);
           }
@@ -1072,6 +1188,21 @@ template <typename E> __device__ __forceinline__ Opnd<typename GradOf<E>::type, 
   } else return x;
 }
 
+template <typename M> constexpr int GRAD_TERMS = sizeof(M) == 2 ? 3 : 1;
+template <typename M> using GradOpnd = Opnd<M, GRAD_TERMS<M>>;
+template <typename M> __device__ __forceinline__ void write_terms(unsigned lds_of_lane, const GradOpnd<M>& x) {
+  union { GradOpnd<M> v; f32x4 h[sizeof(x) / 16]; } u;
+  u.v = x;
+#pragma unroll
+  for (int p = 0; p < (int)sizeof(x) / 16; ++p) lds_write(lds_of_lane + p * 1024, u.h[p]);
+}
+template <typename M> __device__ __forceinline__ GradOpnd<M> load_terms(unsigned lds_of_lane) {
+  union { GradOpnd<M> v; f32x4 h[sizeof(GradOpnd<M>) / 16]; } u;
+#pragma unroll
+  for (int p = 0; p < (int)sizeof(u) / 16; ++p) u.h[p] = lds_read<f32x4>(lds_of_lane + p * 1024);
+  return u.v;
+}
+
 // A workgroup per chunk and key head; the value heads of the key head one after the other, their dq and dk in the same registers.  A wave has 16 of the
 // head's columns of dq and dk, for all tokens: results are transposed (rows are columns of the head, a lane has a token), so that a
 // state's rows are read by one wave only and a token's factors are a lane's own.  The matrices of tokens by tokens are shared out by tiles: wave
@@ -1082,7 +1213,7 @@ template <typename E, int DK, bool SHARED> __global__ __launch_bounds__(64 * gra
   typedef Opnd<M, GRAD_IN<E>> In;
   typedef Tile<E, DK> TL;
   typedef Tile<E, 64> VL;
-  constexpr int W = grad_waves(DK), PARTS = W / 4, TILE = TL::bytes(DELTA_C), KS = DK / 32, OPS = 8 * REC_OP;   // OPS: 64 tokens by 64 columns as operands
+  constexpr int W = grad_waves(DK), PARTS = W / 4, TILE = TL::bytes(DELTA_C), KS = DK / 32, OP = sizeof(GradOpnd<M>) * 64, OPS = 8 * OP;   // OPS: 64 tokens by 64 columns as operands
   struct Sums { float m[2][64][TRI_LD], dots[W][3][64], cols[4][64], rows[PARTS][2][64], whole[W]; };   // over the columns' blocks, when these are through
   constexpr int BLOCKS = VL::bytes(DELTA_C) + 2 * OPS, STAGE = sizeof(Sums) > BLOCKS ? sizeof(Sums) : BLOCKS;
   __shared__ __align__(16) char smem_raw[2 * TILE + STAGE + 20 * REC_OP];
@@ -1212,8 +1343,8 @@ template <typename E, int DK, bool SHARED> __global__ __launch_bounds__(64 * gra
           }
           if (my_in && col < a.dv) *reinterpret_cast<quad_t*>((E*)a.dval + (int64_t)(c.first + my_t) * a.lddv + h * a.dv + col) = w;
         }
-        write_op<M>(n_ops + (2 * tile + s + part) * REC_OP, pair_of<M>(u[s][0], u[s][1]));
-        write_op<M>(y_ops + (2 * tile + s + part) * REC_OP, pair_of<M>(y[s][0], y[s][1]));
+        write_terms<M>(n_ops + (2 * tile + s + part) * OP, terms_of<M, GRAD_TERMS<M>>(u[s][0], u[s][1]));
+        write_terms<M>(y_ops + (2 * tile + s + part) * OP, terms_of<M, GRAD_TERMS<M>>(y[s][0], y[s][1]));
       }
       tile_wait();
       __syncthreads();
@@ -1227,24 +1358,24 @@ template <typename E, int DK, bool SHARED> __global__ __launch_bounds__(64 * gra
         for (int p = 0; p < 2; ++p)
 #pragma unroll
           for (int e = 0; e < 4; ++e) sds = fmaf(sx[p][e], sy[p][e], sds);
-        const Pair<M> sp = pair_of<M>(sx[0], sx[1]), dsp = pair_of<M>(sy[0], sy[1]);
+        const GradOpnd<M> sp = terms_of<M, GRAD_TERMS<M>>(sx[0], sx[1]), dsp = terms_of<M, GRAD_TERMS<M>>(sy[0], sy[1]);
         __builtin_amdgcn_sched_barrier(0);
         load_states(rec, b0 + 32 * (s + 1));
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
           const In d = grad_in<E>(at_do.row(0, m, s));
-          const Pair<M> un = load_op<M>(n_ops + (2 * m + s) * REC_OP), yn = load_op<M>(y_ops + (2 * m + s) * REC_OP);
+          const GradOpnd<M> un = load_terms<M>(n_ops + (2 * m + s) * OP), yn = load_terms<M>(y_ops + (2 * m + s) * OP);
           qi[m] = mma(sp, d, qi[m]);
           ks[m] = mma(sp, yn, ks[m]);
           kn[m] = mma(dsp, un, kn[m]);
         }
         const In d_i = grad_in<E>(at_do.row(0, tile, s));
-        const Pair<M> y_i = load_op<M>(y_ops + (2 * tile + s) * REC_OP);
+        const GradOpnd<M> y_i = load_terms<M>(y_ops + (2 * tile + s) * OP);
 #pragma unroll
         for (int n = 0; n < 4 / PARTS; ++n)
           if (PARTS * n + part <= tile) {
-            const Pair<M> u_j = load_op<M>(n_ops + (2 * (PARTS * n + part) + s) * REC_OP);
+            const GradOpnd<M> u_j = load_terms<M>(n_ops + (2 * (PARTS * n + part) + s) * OP);
             dp[n] = mma(d_i, u_j, dp[n]);
             da[n] = mma(y_i, u_j, da[n]);
           }

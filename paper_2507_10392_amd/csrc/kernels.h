@@ -261,11 +261,11 @@ struct DeltaRule {
   const float* h0; void* o; int64_t ldo; float* ht;                  // h0, ht may be NULL
   const void* dout; const float* dht;                                // backward: dout with the stride ldo
   void *dq, *dkey, *dval; int64_t lddq, lddk, lddv; float *dg, *dbeta, *dh0;
-  char* records; float *states, *dstates, *u, *y; int nchunks, dvp;  // set by delta_rule, in scratch
+  char* records; f16* halves; float *states, *dstates, *u, *y; int nchunks, dvp;  // set by delta_rule, in scratch
 };
 int64_t delta_chunk_rows(int T, int ndocs);   // chunks that the table has room for
 hipError_t delta_chunks(hipStream_t st, int T, int ndocs, const int32_t* offsets, int32_t* table);
-int64_t delta_scratch(bool backward, int T, int ndocs, int nv, int dk, int dv);
+int64_t delta_scratch(DType dt, bool backward, int T, int ndocs, int nk, int nv, int dk, int dv);
 hipError_t delta_rule(hipStream_t st, DType dt, const DeltaRule& a, bool backward, void* scratch);
 // One token each of n states of nstates, float[nstates, nv, dk, dv], which are updated in place.  slots: int32[n] or NULL, token i has state i.
 struct DeltaStep {

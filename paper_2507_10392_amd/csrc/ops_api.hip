@@ -349,7 +349,7 @@ bool delta_rows_ok(int dtype, int nk, int nv, int dk, int dv, const void* q, int
          words_ok(g) && words_ok(beta) && std::isfinite(scale);
 }
 int64_t delta_scratch_bytes(bool backward, int32_t dtype, int32_t T, int32_t ndocs, int32_t nk, int32_t nv, int32_t dk, int32_t dv) {
-  return delta_shape_ok(dtype, T, ndocs, nk, nv, dk, dv) ? delta_scratch(backward, T, ndocs, nv, dk, dv) : -STAGE_ERR_ARG;
+  return delta_shape_ok(dtype, T, ndocs, nk, nv, dk, dv) ? delta_scratch((DType)dtype, backward, T, ndocs, nk, nv, dk, dv) : -STAGE_ERR_ARG;
 }
 }  // namespace
 extern "C" {
@@ -379,7 +379,7 @@ int stage_op_delta_fwd(void* stream, int32_t dtype, int32_t T, int32_t nk, int32
   if (!delta_rows_ok(dtype, nk, nv, dk, dv, q, ldq, k, ldk, v, ldv, g, beta, scale, o, ldo) || !chunks || !aligned16(chunks) || !aligned16(h0) ||
       !aligned16(ht))
     return STAGE_ERR_ARG;
-  if (!scratch || ((uintptr_t)scratch & 255) || scratch_bytes < delta_scratch(false, T, ndocs, nv, dk, dv)) return STAGE_ERR_WORKSPACE;
+  if (!scratch || ((uintptr_t)scratch & 255) || scratch_bytes < delta_scratch((DType)dtype, false, T, ndocs, nk, nv, dk, dv)) return STAGE_ERR_WORKSPACE;
   DeltaRule a = {};
   a.T = T; a.nk = nk; a.nv = nv; a.dk = dk; a.dv = dv; a.ndocs = ndocs; a.q = q; a.k = k; a.v = v; a.ldq = ldq; a.ldk = ldk; a.ldv = ldv;
   a.g = g; a.beta = beta; a.chunks = chunks; a.scale = scale; a.h0 = h0; a.o = o; a.ldo = ldo; a.ht = ht;
@@ -396,7 +396,7 @@ int stage_op_delta_bwd(void* stream, int32_t dtype, int32_t T, int32_t nk, int32
       !rows_ok(dtype, dk_out, lddk, nk, dk) || !rows_ok(dtype, dv_out, lddv, nv, dv) || !dg || !words_ok(dg) || !dbeta || !words_ok(dbeta) || !chunks ||
       !aligned16(chunks) || !aligned16(h0) || !aligned16(dht) || !aligned16(dh0))
     return STAGE_ERR_ARG;
-  if (!scratch || ((uintptr_t)scratch & 255) || scratch_bytes < delta_scratch(true, T, ndocs, nv, dk, dv)) return STAGE_ERR_WORKSPACE;
+  if (!scratch || ((uintptr_t)scratch & 255) || scratch_bytes < delta_scratch((DType)dtype, true, T, ndocs, nk, nv, dk, dv)) return STAGE_ERR_WORKSPACE;
   DeltaRule a = {};
   a.T = T; a.nk = nk; a.nv = nv; a.dk = dk; a.dv = dv; a.ndocs = ndocs; a.q = q; a.k = k; a.v = v; a.ldq = ldq; a.ldk = ldk; a.ldv = ldv;
   a.g = g; a.beta = beta; a.chunks = chunks; a.scale = scale; a.h0 = h0; a.dout = dout; a.ldo = ldo; a.dht = dht;
