@@ -174,6 +174,54 @@ def test_half_of_any_size(gpu_device, vstd, ostd):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+@pytest.mark.parametrize("sizes", [(4, 8, 128, 64), (8, 8, 72, 48), (4, 12, 64, 40)], ids=str)
+def test_many_documents(gpu_device, sizes, dtype):
+    """Enough of the states for workgroups of 32 columns, the last of them with 16 or 8."""
+    say("many", sizes, dtype)
+    c = Case(420, *sizes, [1, 64, 0, 7, 65] + [9] * 28 + [20], first=2, h0=True, ht=True)
+    x, want = reference(c, dtype)
+    r = Run(c, dtype, x)
+    r.all()
+    r.check(want)
+
+
+@gpu
+@pytest.mark.parametrize("kscale,qscale,vstd,ostd", [(1.0, 2.0 ** 40, 1e6, 1e-30), (2.0 ** -30, 1.0, 1e-20, 1e20), (2.0 ** -4, 2.0 ** -40, 1.0, 1e-25)])
+def test_bfloat16_of_any_size(gpu_device, kscale, qscale, vstd, ostd):
+    """What a half would not hold: keys, queries, values and gradients of other sizes, times powers of two so that they stay what the type holds."""
+    say("bf16", kscale, qscale, vstd, ostd)
+    c = Case(200, 2, 4, 96, 48, [70, 130], h0=True, ht=True, vstd=vstd, ostd=ostd)
+    x = c.inputs(1)
+    x["k"], x["q"] = x["k"] * kscale, x["q"] * qscale
+    r = Run(c, 1, x)
+    r.all()
+    r.check(reference_of(c, x))
+
+
+@gpu
+def test_rows_far_apart(gpu_device):
+    """Rows at the largest stride, their last ones behind 2^32 elements: the bits of rows that lie together."""
+    say("far")
+    c = Case(1200, 1, 2, 64, 32, [3, 70, 64], first=1000, h0=True, ht=True)
+    x = c.inputs(1)
+    near = Run(c, 1, x)
+    want, ld = near.all(), 1 << 22
+    far = Run(c, 1, x)
+    buf = torch.empty(c.T * ld, dtype=torch.bfloat16, device="cuda")
+    assert c.offsets[0] * ld < 1 << 32 < (c.offsets[0] + 30) * ld
+    at = 0
+    for n in ("q", "k", "v", "dout", "o", "dq", "dk", "dv"):
+        t = getattr(far, n)
+        w = torch.as_strided(buf, t.shape, (ld, 1), at)
+        w.copy_(t)
+        setattr(far, n, w)
+        at += t.shape[1]
+    for p, q in zip(want, far.all()):
+        assert torch.equal(p, q)
+
+
+@gpu
 def test_calls_repeat_their_bits_and_streams_do_not_meet(gpu_device):
     say("streams")
     c = Case(700, 2, 4, 128, 128, [300, 64, 336], h0=True, ht=True)
@@ -379,6 +427,21 @@ def test_single_tokens(gpu_device, sizes, dtype):
     mixed = step(r, order, [slots[t // 5] for t in order], state)
     assert torch.equal(mixed, out[order])
     check("ht", state[slots], want["ht"], 0, 1)
+
+
+@gpu
+def test_a_state_far_behind(gpu_device):
+    """States behind 2^32 bytes and 2^31 elements: the bits of the first ones."""
+    say("far state")
+    c = Case(3, 4, 16, 128, 128, [3], h0=True)
+    r = Run(c, 1, c.inputs(1))
+    states = 2 ** 31 // (16 * 128 * 128) + 2
+    state = torch.empty(states, 16, 128, 128, device="cuda")
+    slots = [states - 1, 0, states - 2]
+    state[slots] = r.h0[0]
+    near = r.h0.expand(3, -1, -1, -1).contiguous()
+    o, want = step(r, [0, 1, 2], slots, state), step(r, [0, 1, 2], None, near)
+    assert torch.equal(o, want) and torch.equal(state[slots], near)
 
 
 @gpu
