@@ -320,16 +320,28 @@ template <typename M> __device__ __forceinline__ Pair<M> load_op(unsigned lds_of
 // Loads into LDS that run ahead.  The compiler waits for all of those that it knows of before the next transposing read, whatever that reads; these it
 // does not know, and the waits are the callers' (tile_wait before the barrier that publishes them).  64 times 16 bytes, from the
 // lanes' offsets behind `base`, of which `bytes` may be read (zeros behind them), to `lds` on.
-__device__ __forceinline__ void load_ahead(unsigned lds, const void* base, int bytes, unsigned offset) {
+// RUN > 1: as many times, 1 KB on in both places, by offsets of the instructions.
+template <int RUN = 1> __device__ __forceinline__ void load_ahead(unsigned lds, const void* base, int bytes, unsigned offset) {
   const uint64_t at = (uint64_t)(uintptr_t)base;
   u32x4 rs;
   rs[0] = __builtin_amdgcn_readfirstlane((unsigned)at);
   rs[1] = __builtin_amdgcn_readfirstlane((unsigned)(at >> 32) & 0xffffu);
   rs[2] = __builtin_amdgcn_readfirstlane((unsigned)bytes);
   rs[3] = 0x00020000u;
+  static_assert(RUN == 1 || RUN == 2 || RUN == 4, "");
   unsigned m0;   // as it was: the compiler may have a use for it
-  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
-               : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(rs) : "memory");
+  if constexpr (RUN == 1)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(rs) : "memory");
+  else if constexpr (RUN == 2)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\t"
+                 "buffer_load_dwordx4 %2, %3, 0 offen offset:1024 lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(rs) : "memory");
+  else
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\t"
+                 "buffer_load_dwordx4 %2, %3, 0 offen offset:1024 lds\n\tbuffer_load_dwordx4 %2, %3, 0 offen offset:2048 lds\n\t"
+                 "buffer_load_dwordx4 %2, %3, 0 offen offset:3072 lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(rs) : "memory");
 }
 template <typename E, int D, int ROWS, int NW> __device__ __forceinline__ void tile_ahead(const TileLoad<E, D, ROWS, NW>& t, unsigned lds, const E* head, int row0, int end, int wave) {
   typedef Tile<E, D> TL;
@@ -350,9 +362,15 @@ template <int N> __device__ __forceinline__ void loads_but() {
   __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14);
   __builtin_amdgcn_sched_barrier(0);
 }
-// `bytes` (a multiple of 1024) that lie together, as they are, by NW waves.
-template <int NW> __device__ __forceinline__ void bytes_ahead(unsigned lds, const char* from, int bytes, int wave, int lane) {
-  for (int at = wave * 1024; at < bytes; at += NW * 1024) load_ahead(lds + at, from, bytes, (unsigned)(at + 16 * lane));
+// KB times 1024 bytes that lie together, as they are, by NW waves, KB / NW loads each.
+template <int KB, int NW> __device__ __forceinline__ void bytes_ahead(unsigned lds, const char* from, int wave, int lane) {
+  constexpr int RUN = KB % (4 * NW) == 0 ? 4 : KB % (2 * NW) == 0 ? 2 : 1;
+  static_assert(KB % (RUN * NW) == 0, "");
+#pragma unroll
+  for (int i = 0; i < KB / RUN / NW; ++i) {
+    const unsigned at = (unsigned)(wave + NW * i) * (RUN * 1024);
+    load_ahead<RUN>(lds + at, from, KB * 1024, at + 16 * lane);
+  }
 }
 
 // ------------------------------------------------------------------------------------------ a chunk's own matrices
@@ -605,13 +623,18 @@ template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256, (PREP_
 // A workgroup walks a document's chunks for one value head and 16 NW columns of its state.  Two waves carry 16 columns of the state, a half of its rows
 // each, in their registers, and it never leaves them: a result's registers, two above one another, are the next product's operand.  What a chunk
 // waits for is the chain of these waves: K S, a half of the tokens each; what that leaves, Z, exchanged; T Z, by both; K^T of that into the
-// own rows; the new state as pairs, exchanged.  All else is done by others: each such pair of waves has a helper (T Z once more for the results, what the gradients'
-// walk adds to its state, the stores of states and u), with 12 KB of LDS between the three, and the loads are a wave's of its own, or the helpers'.
-// Two barriers a chunk: the first publishes the state, and matrices, values and queries of the chunk, the second Z, and the next chunk's
-// keys.  All of these come straight into LDS, a chunk ahead where two of them fit.
+// own rows; the new state as pairs, exchanged.  All else is done by others: each such pair of waves has two helpers that share out what it does not wait for (T Z
+// once more for the results, what the gradients' walk adds to its state, the stores of states and u), with 12 KB of LDS between the four; the loads
+// are waves' of their own, or, with 32 columns, where these would be a third wave on a SIMD, the second helpers'.  Two barriers a chunk: the first publishes the
+// state, and matrices, values and queries of the chunk, the second Z, and the next chunk's keys.  All of these come straight into LDS, a chunk ahead where
+// two of them fit.  What bounds a walk: that chain, 3000 cycles a chunk (1.4 us) of a document alone, 4100 where two sets of columns and their
+// helpers share the SIMDs; with 16 heads and widths of 128, 8192 tokens in one document 177 us, in documents 47 (one helper, and loads out
+// of step with what it does: 188 and 53); the two of the backward together 114, in which they write 440 MB of states and u.
 enum DeltaWalk { WALK_RESULTS = 0, WALK_STATES = 1, WALK_GRADIENTS = 2 };   // o and the last state; the states and u for the gradients; the states' gradients and y
-constexpr int walk_loaders(int NW) { return NW == 1 ? 4 : 2; }   // a wave issues a load of 1 KB in 50 to 70 cycles
-constexpr int walk_threads(int NW) { return 64 * (3 * NW + walk_loaders(NW)); }
+constexpr int HELPERS = 2;                                       // of 16 columns
+constexpr int walk_loaders(int NW) { return NW == 1 ? 4 : 0; }   // waves that only load; to ask for 1 KB takes a wave 50 to 70 cycles
+constexpr int walk_threads(int NW) { return 64 * ((2 + HELPERS) * NW + walk_loaders(NW)); }
+template <int V> struct Int { static constexpr int value = V; };
 
 template <typename E, int DK, int NW, int KIND> struct WalkLds {
   typedef Tile<typename WalkOf<E, KIND != WALK_RESULTS>::type, DK> TL;
@@ -642,11 +665,11 @@ template <typename M> __device__ __forceinline__ void write_op(unsigned lds_of_l
 template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void delta_walk(char* smem_raw, const DeltaRule& a, int doc_rank, int h, int c0) {
   typedef WalkLds<E, DK, NW, KIND> L;
   typedef typename WalkOf<E, KIND != WALK_RESULTS>::type M;   // of the products
-  constexpr int RT = DK / 16, KS = DK / 32, HT = RT / 2, HS = KS / 2, FW = walk_loaders(NW);
+  constexpr int RT = DK / 16, KS = DK / 32, HT = RT / 2, HS = KS / 2, LOADERS = walk_loaders(NW), FW = LOADERS ? LOADERS : NW;
   constexpr bool HALF_E = __is_same(M, f16), COPIES = !__is_same(M, E), BACK = KIND == WALK_GRADIENTS, RESULTS = KIND == WALK_RESULTS, AHEAD = L::NBUF == 2, ALL_AHEAD = L::VBUF == 2;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = wave % NW, g = lane >> 4, i16 = lane & 15;
-  const bool chain = wave < 2 * NW, helps = !chain && wave < 3 * NW, loads = wave >= 3 * NW;
-  const int fw = wave - 3 * NW;
+  const bool chain = wave < 2 * NW, loads = wave >= (LOADERS ? 4 : 3) * NW;
+  const int fw = wave - (LOADERS ? 4 : 3) * NW;
   const int4 row = reinterpret_cast<const int4*>(a.chunks)[1 + doc_rank];   // first token, tokens, first chunk, document
   const int first = row.x, count = row.y, chunk0 = row.z, doc = row.w, chunks = (count + DELTA_C - 1) / DELTA_C;
   const int kv = h / (a.nv / a.nk), w0 = c0 + 16 * mine, col = w0 + i16;    // the wave's first column and the lane's
@@ -660,7 +683,7 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
   const TileLoad<M, DK, DELTA_C, FW> load_k(COPIES ? DK : a.ldk, lane, COPIES ? DK : a.dk), load_q(COPIES ? DK : a.ldq, lane, COPIES ? DK : a.dk);
   const TileLoad<E, 64, DELTA_C, FW> load_v(BACK ? a.ldo : a.ldv, lane, min(a.dv - c0, 16 * NW));
   // Loads of a wave, at least: of the keys, of the chunk's matrices, of values and queries.
-  constexpr int KEYS = TileLoad<M, DK, DELTA_C, FW>::N, MATS = BACK ? REC_GATES / 1024 / FW + 2 * REC_TRIANGLE / 1024 / FW : L::REC / 1024 / FW;
+  constexpr int KEYS = TileLoad<M, DK, DELTA_C, FW>::N, MATS = (L::REC - REC_GATES) / 1024 / FW;
   constexpr int SECOND = TileLoad<E, 64, DELTA_C, FW>::N + (KIND == WALK_STATES ? 0 : TileLoad<M, DK, DELTA_C, FW>::N);
   auto copies = [&](int c) { return a.halves + ((int64_t)(chunk0 + c) * a.nk + kv) * (2 * DELTA_C * DK); };
   auto fetch_keys = [&](int c, unsigned to) {
@@ -670,10 +693,8 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
   };
   auto fetch_mats = [&](int c, unsigned to) {
     const char* rec = a.records + ((int64_t)(chunk0 + c) * a.nv + h) * (RESULTS ? REC_FWD : REC_BWD);
-    if constexpr (BACK) {   // P^T and T^T lie side by side
-      bytes_ahead<FW>(to + L::R, rec, REC_GATES, fw, lane);
-      bytes_ahead<FW>(to + L::R + REC_GATES, rec + REC_P, 2 * REC_TRIANGLE, fw, lane);
-    } else bytes_ahead<FW>(to + L::R, rec, L::REC, fw, lane);
+    if (fw == 0) load_ahead(to + L::R, rec, REC_GATES, 16 * lane);
+    bytes_ahead<(L::REC - REC_GATES) / 1024, FW>(to + L::R + REC_GATES, rec + (BACK ? REC_P : REC_GATES), fw, lane);   // P^T and T^T lie side by side
   };
   auto fetch_second = [&](int c, unsigned by) {
     const int t0 = first + DELTA_C * c, end = min(first + count, t0 + DELTA_C);
@@ -693,18 +714,16 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
     fetch_all(c);
     if (AHEAD && chunks > 1) {
       fetch_keys(c + step, smem + L::FIRST);
-      if constexpr (!ALL_AHEAD) fetch_mats(c + step, smem + L::FIRST);
-      loads_but<KEYS + (ALL_AHEAD ? 0 : MATS)>();
+      if constexpr (ALL_AHEAD) fetch_second(c + step, L::SECOND);
+      else fetch_mats(c + step, smem + L::FIRST);
+      loads_but<KEYS + (ALL_AHEAD ? SECOND : MATS)>();
     } else tile_wait();
   }
   // The two barriers of chunk n, and the loading waves' part of them: what they have to see arrived before, what they ask for behind.  After the second one
-  // nothing of the chunk's keys, matrices, values and queries is read from LDS any more, and the chunk after the next takes their place: the keys, which
-  // the chain reads a phase ahead, at once, the others of a loader of its own in the next phase, so that it comes to the barriers in time.
+  // nothing of the chunk's keys, values and queries is read from LDS any more, and the chunk after the next takes their place; its matrices, where all
+  // is there twice, follow in the next phase, so that a wave has about as much to ask for in either.
   auto begin_chunk = [&](int n) {
-    if (ALL_AHEAD && loads && n + 1 < chunks) {
-      fetch_mats(c + step, smem + ((n + 1) & 1) * L::FIRST);
-      fetch_second(c + step, ((n + 1) & 1) * L::SECOND);
-    }
+    if (ALL_AHEAD && loads && n + 1 < chunks) fetch_mats(c + step, smem + ((n + 1) & 1) * L::FIRST);
   };
   auto middle = [&](int n) {
     if (AHEAD && loads && n + 1 < chunks) {   // the next keys
@@ -716,13 +735,14 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
       if constexpr (!ALL_AHEAD) fetch_second(c + step, 0);
       if (n + 2 < chunks) {
         fetch_keys(c + 2 * step, smem + (n & 1) * L::FIRST);
-        if constexpr (!ALL_AHEAD) fetch_mats(c + 2 * step, smem + (n & 1) * L::FIRST);
+        if constexpr (ALL_AHEAD) fetch_second(c + 2 * step, (n & 1) * L::SECOND);
+        else fetch_mats(c + 2 * step, smem + (n & 1) * L::FIRST);
       }
     }
   };
   auto end_chunk = [&](int n) {
     if (AHEAD && loads) {   // the next matrices, values and queries
-      if (n + 2 < chunks) loads_but<KEYS + (ALL_AHEAD ? 0 : MATS)>();
+      if (n + 2 < chunks) loads_but<KEYS + (ALL_AHEAD ? SECOND : MATS)>();
       else tile_wait();
     }
     __syncthreads();
@@ -956,7 +976,7 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
   }
 
   __syncthreads();
-  if (!helps) {
+  if (LOADERS && loads) {
     for (int n = 0; n < chunks; ++n, c += step) {
       begin_chunk(n);
       middle(n);
@@ -964,188 +984,215 @@ template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void 
     }
     return;
   }
-  if constexpr (RESULTS) {
-    TileOps<M, DK> at;
-    at.state_places(smem + L::Q, lane);
-    for (int n = 0; n < chunks; ++n, c += step) {
-      const unsigned gates = smem + (AHEAD ? (unsigned)(n & 1) * L::FIRST : 0u) + L::R, ops = gates + REC_GATES + 16 * lane;
-      begin_chunk(n);
-      Pair<M> sf[KS];
+  // Tokens, and rows of the state, in 16s: a helper has its part of HELPERS of them.
+  auto help = [&](auto part) {
+    constexpr int MT = 4 / HELPERS, M0 = part.value * MT;
+    if constexpr (RESULTS) {
+      constexpr int UT = M0 + MT;   // of u: what P's rows are not zero for
+      TileOps<M, DK> at;
+      at.state_places(smem + L::Q, lane);
+      for (int n = 0; n < chunks; ++n, c += step) {
+        const unsigned gates = smem + (AHEAD ? (unsigned)(n & 1) * L::FIRST : 0u) + L::R, ops = gates + REC_GATES + 16 * lane;
+        begin_chunk(n);
+        Pair<M> sf[KS];
 #pragma unroll
-      for (int s = 0; s < KS; ++s) sf[s] = load_op<M>(hand + s * 2048);
-      f32x4 back_s[2];   // half: of the rows' columns, of either half of the state
-      if constexpr (HALF_E) {
-        back_s[0] = lds_read<f32x4>(units + 16 * g);
-        back_s[1] = lds_read<f32x4>(units + 64 + 16 * g);
+        for (int s = 0; s < KS; ++s) sf[s] = load_op<M>(hand + s * 2048);
+        f32x4 back_s[2];   // half: of the rows' columns, of either half of the state
+        if constexpr (HALF_E) {
+          back_s[0] = lds_read<f32x4>(units + 16 * g);
+          back_s[1] = lds_read<f32x4>(units + 64 + 16 * g);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          back_s[0][r] = inverse_unit<M>(back_s[0][r]);
-          back_s[1][r] = inverse_unit<M>(back_s[1][r]);
-        }
-      }
-      float q_inv = 1.f, p_inv = 1.f;
-      if constexpr (HALF_E) {
-        q_inv = lds_read<float>(gates + 776);
-        p_inv = q_inv * lds_read<float>(gates + 772);
-      }
-      f32x4 o[4], oo[4];   // transposed: rows are columns of the state, a lane has the token lane % 16
-      float zi[2];         // half: the inverse units of Z
-      Pair<M> pf[6], tf[6], zp[2];
-#pragma unroll
-      for (int m = 0; m < 4; ++m) o[m] = oo[m] = zero;
-#pragma unroll
-      for (int s = 0; s < KS; ++s)
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          if (HALF_E && s >= HS) oo[m] = mma(sf[s], at.state_row(0, m, s), oo[m]);
-          else o[m] = mma(sf[s], at.state_row(0, m, s), o[m]);
-        }
-      if constexpr (ALL_AHEAD) at.move_state_places((n & 1) ? (unsigned)-L::SECOND : (unsigned)L::SECOND);
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const float since = lds_read<float>(gates + 4 * (16 * m + i16));
-        if constexpr (HALF_E) o[m] = (o[m] * back_s[0] + oo[m] * back_s[1]) * (since * q_inv);
-        else o[m] *= since;
-      }
-#pragma unroll
-      for (int i = 0; i < 6; ++i) {
-        tf[i] = load_op<M>(ops + i * REC_OP);
-        pf[i] = load_op<M>(ops + REC_TRIANGLE + i * REC_OP);
-      }
-      middle(n);
-      zp[0] = load_op<M>(hand_z);
-      zp[1] = load_op<M>(hand_z + 2048);
-      if constexpr (HALF_E)
-#pragma unroll
-        for (int s = 0; s < 2; ++s) zi[s] = inverse_unit<M>(lds_read<float>(units + Tile<M, DK>::OCTET * 4 + 4 * i16 + 64 * s));
-      f32x4 u[4], uo[4], p[4], back_u = zero;
-#pragma unroll
-      for (int m = 0; m < 4; ++m) u[m] = uo[m] = zero;
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-          if (s <= m / 2) {
-            if (HALF_E && s == 1) uo[m] = mma(tf[lower_op(m, s)], zp[s], uo[m]);
-            else u[m] = mma(tf[lower_op(m, s)], zp[s], u[m]);
-          }
-      if constexpr (HALF_E)
-#pragma unroll
-        for (int m = 0; m < 4; ++m) u[m] = u[m] * zi[0] + uo[m] * zi[1];
-      Pair<M> up[2];
-      const float unit = column_unit<M>(u), inv = inverse_unit<M>(unit);
-      pairs_of<M>(up, u, unit);
-      if constexpr (HALF_E) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) back_u[r] = __shfl(inv, 4 * g + r, 64);
-      }
-#pragma unroll
-      for (int m = 0; m < 4; ++m) p[m] = HALF_E ? zero : o[m];
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-          if (s <= m / 2) p[m] = mma(up[s], pf[lower_op(m, s)], p[m]);
-      E* oh = (E*)a.o + h * a.dv + w0 + 4 * g;
-      if (w0 + 4 * g < a.dv)
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          const int t = DELTA_C * c + 16 * m + i16;
-          if constexpr (HALF_E) p[m] = p[m] * (back_u * p_inv) + o[m];
-          if (t < count) {
-            typedef E quad_t __attribute__((ext_vector_type(4)));
-            quad_t w;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) w[r] = from_f<E>(fp32_value(p[m][r] * a.scale));
-            *reinterpret_cast<quad_t*>(oh + (first + t) * a.ldo) = w;
+          for (int r = 0; r < 4; ++r) {
+            back_s[0][r] = inverse_unit<M>(back_s[0][r]);
+            back_s[1][r] = inverse_unit<M>(back_s[1][r]);
           }
         }
-      end_chunk(n);
-    }
-  } else {
-    TileOps<M, DK> at;
-    at.state_places(smem + L::Q, lane);
-    const TileOps<E, 64> at_v(smem + L::V, lane);
-    for (int n = 0; n < chunks; ++n, c += step) {
-      const unsigned gates = smem + (AHEAD ? (unsigned)(n & 1) * L::FIRST : 0u) + L::R, gates4 = gates + 16 * g, ops = gates + REC_GATES + 16 * lane;
-      const int64_t rec = (int64_t)(chunk0 + c) * a.nv + h;
-      begin_chunk(n);
-      // the state, as its pairs are: what the gradients' products take
-      float* to = (BACK ? a.dstates : a.states) + rec * DK * a.dvp + col;
-      Pair<M> sf[KS];
+        float q_inv = 1.f, p_inv = 1.f;
+        if constexpr (HALF_E) {
+          q_inv = lds_read<float>(gates + 776);
+          p_inv = q_inv * lds_read<float>(gates + 772);
+        }
+        f32x4 o[MT], oo[MT];   // transposed: rows are columns of the state, a lane has the token lane % 16
+        float zi[2];         // half: the inverse units of Z
+        Pair<M> pf[6], tf[6], zp[2];   // those that these tiles need
 #pragma unroll
-      for (int s = 0; s < KS; ++s) sf[s] = load_op<M>(hand + s * 2048);
-      float inv[2] = {1.f, 1.f};
-      if constexpr (HALF_E) {
-        inv[0] = inverse_unit<M>(lds_read<float>(units + 4 * i16));
-        inv[1] = inverse_unit<M>(lds_read<float>(units + 64 + 4 * i16));
-      }
-      if (col < a.dvp)
+        for (int m = 0; m < MT; ++m) o[m] = oo[m] = zero;
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float x = (float)sf[s].t[0][e];
-            if constexpr (PAIR<M> == 2) x += (float)sf[s].t[1][e];
-            to[(32 * s + 8 * g + e) * a.dvp] = HALF_E ? x * inv[s >= HS] : x;
+          for (int m = 0; m < MT; ++m) {
+            if (HALF_E && s >= HS) oo[m] = mma(sf[s], at.state_row(0, M0 + m, s), oo[m]);
+            else o[m] = mma(sf[s], at.state_row(0, M0 + m, s), o[m]);
           }
-      if constexpr (BACK) {   // scale Q^T (exp(G) dO)
-        const unsigned second = ALL_AHEAD ? (unsigned)(n & 1) * L::SECOND : 0u;
-        Opnd<E, 1> vf[2];
-        vf[0] = at_v.column(second, mine, 0);
-        vf[1] = at_v.column(second, mine, 1);
-        f32x4 d[4], add[RT];
+        if constexpr (ALL_AHEAD) at.move_state_places((n & 1) ? (unsigned)-L::SECOND : (unsigned)L::SECOND);
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          const f32x4 since = lds_read<f32x4>(gates4 + 64 * m);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) d[m][r] = a.scale * since[r] * (float)vf[m >> 1].t[0][4 * (m & 1) + r];
+        for (int m = 0; m < MT; ++m) {
+          const float since = lds_read<float>(gates + 4 * (16 * (M0 + m) + i16));
+          if constexpr (HALF_E) o[m] = (o[m] * back_s[0] + oo[m] * back_s[1]) * (since * q_inv);
+          else o[m] *= since;
         }
-        Pair<M> dp[2];
-        const float unit = column_unit<M>(d), back = inverse_unit<M>(unit);
-        pairs_of<M>(dp, d, unit);
 #pragma unroll
-        for (int i = 0; i < RT; ++i) add[i] = zero;
+        for (int i = 0; i < 6; ++i) {
+          tf[i] = load_op<M>(ops + i * REC_OP);
+          pf[i] = load_op<M>(ops + REC_TRIANGLE + i * REC_OP);
+        }
+        middle(n);
+        zp[0] = load_op<M>(hand_z);
+        zp[1] = load_op<M>(hand_z + 2048);
+        if constexpr (HALF_E)
+#pragma unroll
+          for (int s = 0; s < 2; ++s) zi[s] = inverse_unit<M>(lds_read<float>(units + Tile<M, DK>::OCTET * 4 + 4 * i16 + 64 * s));
+        f32x4 u[UT], uo[UT], p[MT], back_u = zero;
+#pragma unroll
+        for (int m = 0; m < UT; ++m) u[m] = uo[m] = zero;
+#pragma unroll
+        for (int s = 0; s < UT / 2; ++s)
+#pragma unroll
+          for (int m = 0; m < UT; ++m)
+            if (s <= m / 2) {
+              if (HALF_E && s == 1) uo[m] = mma(tf[lower_op(m, s)], zp[s], uo[m]);
+              else u[m] = mma(tf[lower_op(m, s)], zp[s], u[m]);
+            }
+        if constexpr (HALF_E)
+#pragma unroll
+          for (int m = 0; m < UT; ++m) u[m] = u[m] * zi[0] + uo[m] * zi[1];
+        Pair<M> up[UT / 2];
+        const float unit = column_unit<M>(u), inv = inverse_unit<M>(unit);
+        pairs_of<M>(up, u, unit);
+        if constexpr (HALF_E) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) back_u[r] = __shfl(inv, 4 * g + r, 64);
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) p[m] = HALF_E ? zero : o[m];
+#pragma unroll
+        for (int s = 0; s < UT / 2; ++s)
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+            if (s <= (M0 + m) / 2) p[m] = mma(up[s], pf[lower_op(M0 + m, s)], p[m]);
+        E* oh = (E*)a.o + h * a.dv + w0 + 4 * g;
+        if (w0 + 4 * g < a.dv)
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            const int t = DELTA_C * c + 16 * (M0 + m) + i16;
+            if constexpr (HALF_E) p[m] = p[m] * (back_u * p_inv) + o[m];
+            if (t < count) {
+              typedef E quad_t __attribute__((ext_vector_type(4)));
+              quad_t w;
+#pragma unroll
+              for (int r = 0; r < 4; ++r) w[r] = from_f<E>(fp32_value(p[m][r] * a.scale));
+              *reinterpret_cast<quad_t*>(oh + (first + t) * a.ldo) = w;
+            }
+          }
+        end_chunk(n);
+      }
+    } else {
+      constexpr int IT = RT / HELPERS, I0 = part.value * IT;
+      TileOps<M, DK> at;
+      at.state_places(smem + L::Q, lane);
+      const TileOps<E, 64> at_v(smem + L::V, lane);
+      for (int n = 0; n < chunks; ++n, c += step) {
+        const unsigned gates = smem + (AHEAD ? (unsigned)(n & 1) * L::FIRST : 0u) + L::R, gates4 = gates + 16 * g, ops = gates + REC_GATES + 16 * lane;
+        const int64_t rec = (int64_t)(chunk0 + c) * a.nv + h;
+        begin_chunk(n);
+        // The state, as its pairs are, for the gradients' products.  Half: read transposed, so that a lane has four columns of a row, and stored in the
+        // other phase: as a lane's rows of one column, 32 stores of 4 bytes, this wave kept the chain waiting for 2000 cycles a chunk.
+        float* to = (BACK ? a.dstates : a.states) + rec * DK * a.dvp;
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        union Quad { s16x4 w; f16 v[4]; } sq[HALF_E ? IT : 1][2];
+        f32x4 inv[2];
+        if constexpr (HALF_E) {
+          const unsigned across = hand - 16 * lane + 256 * ((i16 & 3) >> 1) + 64 * g + 16 * (i16 >> 2) + 8 * (i16 & 1);
+#pragma unroll
+          for (int i = 0; i < IT; ++i)
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+              sq[i][p].w = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)(across + ((I0 + i) >> 1) * 2048 + p * 1024 + ((I0 + i) & 1) * 512));
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            inv[p] = lds_read<f32x4>(units + 64 * p + 16 * g);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) inv[p][r] = inverse_unit<M>(inv[p][r]);
+          }
+        } else if (col < a.dvp) {
+#pragma unroll
+          for (int s = I0 / 2; s < (I0 + IT) / 2; ++s) {
+            const Pair<M> sf = load_op<M>(hand + s * 2048);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) to[(32 * s + 8 * g + e) * a.dvp + col] = sf.t[0][e];
+          }
+        }
+        if constexpr (BACK) {   // scale Q^T (exp(G) dO)
+          const unsigned second = ALL_AHEAD ? (unsigned)(n & 1) * L::SECOND : 0u;
+          Opnd<E, 1> vf[2];
+          vf[0] = at_v.column(second, mine, 0);
+          vf[1] = at_v.column(second, mine, 1);
+          f32x4 d[4], add[IT];
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            const f32x4 since = lds_read<f32x4>(gates4 + 64 * m);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) d[m][r] = a.scale * since[r] * (float)vf[m >> 1].t[0][4 * (m & 1) + r];
+          }
+          Pair<M> dp[2];
+          const float unit = column_unit<M>(d), back = inverse_unit<M>(unit);
+          pairs_of<M>(dp, d, unit);
+#pragma unroll
+          for (int i = 0; i < IT; ++i) add[i] = zero;
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < IT; ++i) add[i] = mma(at.state_column(0, I0 + i, s), dp[s], add[i]);
+          if constexpr (ALL_AHEAD) at.move_state_places((n & 1) ? (unsigned)-L::SECOND : (unsigned)L::SECOND);
+#pragma unroll
+          for (int i = 0; i < IT; ++i) lds_write(hand_add + (I0 + i) * 1024, HALF_E ? add[i] * (back * lds_read<float>(gates + 776)) : add[i]);
+        }
+        Pair<M> tf[6], zp[2];
+#pragma unroll
+        for (int i = 0; i < 6; ++i) tf[i] = load_op<M>(ops + (BACK ? REC_TRIANGLE : 0) + i * REC_OP);
+        middle(n);
+        if constexpr (HALF_E) {
+          if (w0 < a.dvp)
+#pragma unroll
+            for (int i = 0; i < IT; ++i) {
+              f32x4 x;
+#pragma unroll
+              for (int r = 0; r < 4; ++r) x[r] = ((float)sq[i][0].v[r] + (float)sq[i][1].v[r]) * inv[I0 + i >= HT][r];
+              *reinterpret_cast<f32x4*>(to + (16 * (I0 + i) + i16) * a.dvp + w0 + 4 * g) = x;
+            }
+        }
+        f32x4 u[MT], uo[MT], back_z[2];   // transposed: rows are columns of the state
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          zp[s] = load_op<M>(hand_z + s * 2048);
+          if constexpr (HALF_E) {
+            back_z[s] = lds_read<f32x4>(units + Tile<M, DK>::OCTET * 4 + 64 * s + 16 * g);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) back_z[s][r] = inverse_unit<M>(back_z[s][r]);
+          }
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) u[m] = uo[m] = zero;
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int i = 0; i < RT; ++i) add[i] = mma(at.state_column(0, i, s), dp[s], add[i]);
-        if constexpr (ALL_AHEAD) at.move_state_places((n & 1) ? (unsigned)-L::SECOND : (unsigned)L::SECOND);
+          for (int m = 0; m < MT; ++m)
+            if (BACK ? s >= (M0 + m) / 2 : s <= (M0 + m) / 2) {
+              const Pair<M>& t = tf[BACK ? upper_op(M0 + m, s) : lower_op(M0 + m, s)];
+              if (HALF_E && s == 1) uo[m] = mma(zp[s], t, uo[m]);
+              else u[m] = mma(zp[s], t, u[m]);
+            }
+        float* to_u = (BACK ? a.y : a.u) + rec * DELTA_C * a.dvp + i16 * a.dvp + w0 + 4 * g;
+        if (w0 + 4 * g < a.dvp)
 #pragma unroll
-        for (int i = 0; i < RT; ++i) lds_write(hand_add + i * 1024, HALF_E ? add[i] * (back * lds_read<float>(gates + 776)) : add[i]);
+          for (int m = 0; m < MT; ++m) *reinterpret_cast<f32x4*>(to_u + 16 * (M0 + m) * a.dvp) = HALF_E ? u[m] * back_z[0] + uo[m] * back_z[1] : u[m];
+        end_chunk(n);
       }
-      Pair<M> tf[6], zp[2];
-#pragma unroll
-      for (int i = 0; i < 6; ++i) tf[i] = load_op<M>(ops + (BACK ? REC_TRIANGLE : 0) + i * REC_OP);
-      middle(n);
-      f32x4 u[4], uo[4], back_z[2];   // transposed: rows are columns of the state
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        zp[s] = load_op<M>(hand_z + s * 2048);
-        if constexpr (HALF_E) {
-          back_z[s] = lds_read<f32x4>(units + Tile<M, DK>::OCTET * 4 + 64 * s + 16 * g);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) back_z[s][r] = inverse_unit<M>(back_z[s][r]);
-        }
-      }
-#pragma unroll
-      for (int m = 0; m < 4; ++m) u[m] = uo[m] = zero;
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-          if (BACK ? s >= m / 2 : s <= m / 2) {
-            const Pair<M>& t = tf[BACK ? upper_op(m, s) : lower_op(m, s)];
-            if (HALF_E && s == 1) uo[m] = mma(zp[s], t, uo[m]);
-            else u[m] = mma(zp[s], t, u[m]);
-          }
-      float* to_u = (BACK ? a.y : a.u) + rec * DELTA_C * a.dvp + i16 * a.dvp + w0 + 4 * g;
-      if (w0 + 4 * g < a.dvp)
-#pragma unroll
-        for (int m = 0; m < 4; ++m) *reinterpret_cast<f32x4*>(to_u + 16 * m * a.dvp) = HALF_E ? u[m] * back_z[0] + uo[m] * back_z[1] : u[m];
-      end_chunk(n);
     }
-  }
+  };
+  if (wave < 3 * NW) help(Int<BACK ? 0 : 1>());
+  else help(Int<BACK ? 1 : 0>());   // the smaller one
 }
 
 // Block of the grid -> document and head, and columns: the blocks that share keys and matrices lie eight apart, on one XCD.
