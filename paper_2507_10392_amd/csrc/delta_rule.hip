@@ -197,7 +197,7 @@ DeltaScratch delta_layout(DType dt, bool backward, int T, int ndocs, int nk, int
     return p;
   };
   s.records = take(n * (backward ? DELTA_RECORD_BWD : DELTA_RECORD_FWD));
-  s.halves = take(backward && dt == BF16 ? chunks * nk * 2 * DELTA_CHUNK * rows * 2 : 0);   // bf16 keys and queries
+  s.halves = take(dt == BF16 ? chunks * nk * 2 * DELTA_CHUNK * rows * 2 : 0);   // bf16 keys and queries
   if (backward) {
     s.states = take(n * rows * dvp * 4);
     s.dstates = take(n * rows * dvp * 4);

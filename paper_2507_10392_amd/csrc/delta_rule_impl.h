@@ -17,12 +17,12 @@
 // (delta_grad_kernel).  No atomics: a repeat gives the same bits.
 //
 // Precision.  q, k, v and dO are operands as they stand.  What is computed stays fp32 in registers; where it is an operand it is the sum of two or three
-// values of 16 bits, in two to six products.  Forward: two of the type (16 bits of a bf16 pair, 22 of a half pair), since the states, the final one
-// among them, are sums over the whole document and the walk waits for its own last product more than for the matrix cores.  Backward dg is what is left of
-// larger terms: with bf16 pairs throughout it was off by up to 1.5e-5 of its norm.  So the backward's walks take half pairs for bf16 too (keys and
-// queries as halves times a power of two that prep finds, computed values times one per column, so that no size of state or gradient leaves
-// a half's range), and a chunk's gradients three bf16, which are an fp32, of S, dS, U and Y: 1.2e-6, for 15 us in 104 and 5 in 112 (16 heads, 8192 tokens,
-// head widths of 128).  What only goes into dq and dk, which are rounded to 16 bits, stays pairs.  fp32: v_mfma_f32_16x16x4, no pairs.
+// values of 16 bits, in two to six products.  Forward without last states: two of the type (16 bits of a bf16 pair, 22 of a half pair), since what comes of them is
+// rounded to the type.  The last states are fp32, and dg and dbeta are what is left of larger terms: with bf16 pairs throughout these were off by up to 5.2e-6
+// and 1.5e-5 of their norms.  So where last states are wanted, and backward, the walks take half pairs for bf16 too (keys and queries as
+// halves times a power of two that prep finds, computed values times one per column, so that no size of state or gradient leaves
+// a half's range), and a chunk's gradients three bf16, which are an fp32, of S, dS, U and Y: 3e-7 and 1.2e-6, for 15 us in 104 and 5 in 112 (gradients; 16 heads,
+// 8192 tokens, head widths of 128).  What only goes into dq and dk, which are rounded to 16 bits, stays pairs.  fp32: v_mfma_f32_16x16x4, no pairs.
 #pragma once
 #include "attention_docs_tiles.h"
 
@@ -139,9 +139,9 @@ __device__ __forceinline__ float columns_sum(float x) {
   return x + dpp<0x140>(x);
 }
 
-// What a walk and a chunk's own matrices are computed in: backward bf16 as half.
-template <typename E, bool BWD> struct WalkOf { typedef E type; };
-template <> struct WalkOf<bf16, true> { typedef f16 type; };
+// What walks whose states are results, and a chunk's own matrices for them, are computed in: bf16 as half.
+template <typename E> struct WalkOf { typedef E type; };
+template <> struct WalkOf<bf16> { typedef f16 type; };
 
 // Half: the power of two that brings the largest of a column's values, which lie in the four lanes that share lane % 16, to 2^13 .. 2^14; else 1.
 template <typename M, int N> __device__ __forceinline__ float column_unit(const f32x4 (&x)[N]) {
@@ -448,9 +448,8 @@ template <typename E> __device__ __forceinline__ void fill_rows(E* p, int64_t ld
 constexpr int prep_lds(int tile) { return 2 * tile > 2 * 64 * TRI_LD * 4 ? 2 * tile : 2 * 64 * TRI_LD * 4; }   // A and T take the place of keys and queries
 template <typename E, int DK> constexpr int PREP_LDS = prep_lds(Tile<E, DK>::bytes(DELTA_C));
 template <typename E, int DK> constexpr int PREP_GROUPS = PREP_LDS<E, DK> <= 36 * 1024 ? 4 : 2;   // on a CU
-template <typename E, int DK, bool BWD> __global__ __launch_bounds__(256, (PREP_GROUPS<E, DK>)) void delta_prep_kernel(DeltaRule a) {
+template <typename E, typename A16, int DK, bool BWD> __global__ __launch_bounds__(256, (PREP_GROUPS<E, DK>)) void delta_prep_kernel(DeltaRule a) {
   typedef Tile<E, DK> TL;
-  typedef typename WalkOf<E, BWD>::type A16;
   constexpr int TILE = TL::bytes(DELTA_C), KS = DK / 32;
   __shared__ __align__(16) char tiles[PREP_LDS<E, DK>];
   float *A = reinterpret_cast<float*>(tiles), *Tm = A + 64 * TRI_LD;
@@ -636,8 +635,8 @@ constexpr int walk_loaders(int NW) { return NW == 1 ? 4 : 0; }   // waves that o
 constexpr int walk_threads(int NW) { return 64 * ((2 + HELPERS) * NW + walk_loaders(NW)); }
 template <int V> struct Int { static constexpr int value = V; };
 
-template <typename E, int DK, int NW, int KIND> struct WalkLds {
-  typedef Tile<typename WalkOf<E, KIND != WALK_RESULTS>::type, DK> TL;
+template <typename E, typename M, int DK, int NW, int KIND> struct WalkLds {
+  typedef Tile<M, DK> TL;
   typedef Tile<E, 64> VL;
   static constexpr int REC = KIND == WALK_STATES ? REC_P : REC_FWD;   // gates and T; and P; or gates, P^T and T^T
   static constexpr int VSIZE = VL::bytes(DELTA_C), QSIZE = KIND == WALK_STATES ? 0 : TL::bytes(DELTA_C);
@@ -662,9 +661,9 @@ template <typename M> __device__ __forceinline__ void write_op(unsigned lds_of_l
   }
 }
 
-template <typename E, int DK, int NW, int KIND> __device__ __forceinline__ void delta_walk(char* smem_raw, const DeltaRule& a, int doc_rank, int h, int c0) {
-  typedef WalkLds<E, DK, NW, KIND> L;
-  typedef typename WalkOf<E, KIND != WALK_RESULTS>::type M;   // of the products
+// M: what its products are of.
+template <typename E, typename M, int DK, int NW, int KIND> __device__ __forceinline__ void delta_walk(char* smem_raw, const DeltaRule& a, int doc_rank, int h, int c0) {
+  typedef WalkLds<E, M, DK, NW, KIND> L;
   constexpr int RT = DK / 16, KS = DK / 32, HT = RT / 2, HS = KS / 2, LOADERS = walk_loaders(NW), FW = LOADERS ? LOADERS : NW;
   constexpr bool HALF_E = __is_same(M, f16), COPIES = !__is_same(M, E), BACK = KIND == WALK_GRADIENTS, RESULTS = KIND == WALK_RESULTS, AHEAD = L::NBUF == 2, ALL_AHEAD = L::VBUF == 2;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = wave % NW, g = lane >> 4, i16 = lane & 15;
@@ -1201,20 +1200,21 @@ __device__ __forceinline__ WalkBlock walk_block(const DeltaRule& a, int block, i
   const int j = block / 8, pair = j / slices * 8 + block % 8;
   return WalkBlock{pair / a.nv, pair % a.nv, j % slices * width, pair < a.ndocs * a.nv};
 }
-template <typename E, int DK, int NW> __global__ __launch_bounds__(walk_threads(NW), 1) void delta_walk_kernel(DeltaRule a, int slices) {
-  __shared__ __align__(16) char smem[WalkLds<E, DK, NW, WALK_RESULTS>::BYTES];
+template <typename E, typename M, int DK, int NW> __global__ __launch_bounds__(walk_threads(NW), 1) void delta_walk_kernel(DeltaRule a, int slices) {
+  __shared__ __align__(16) char smem[WalkLds<E, M, DK, NW, WALK_RESULTS>::BYTES];
   const WalkBlock b = walk_block(a, blockIdx.x, slices, 16 * NW);
-  if (b.in) delta_walk<E, DK, NW, WALK_RESULTS>(smem, a, b.doc, b.h, b.c0);
+  if (b.in) delta_walk<E, M, DK, NW, WALK_RESULTS>(smem, a, b.doc, b.h, b.c0);
 }
 // Both walks of the backward: they need nothing of one another.
 template <typename E, int DK, int NW> __global__ __launch_bounds__(walk_threads(NW), 1) void delta_walks_kernel(DeltaRule a, int slices, int blocks) {
-  constexpr int LS = WalkLds<E, DK, NW, WALK_STATES>::BYTES, LG = WalkLds<E, DK, NW, WALK_GRADIENTS>::BYTES;
+  typedef typename WalkOf<E>::type M;
+  constexpr int LS = WalkLds<E, M, DK, NW, WALK_STATES>::BYTES, LG = WalkLds<E, M, DK, NW, WALK_GRADIENTS>::BYTES;
   __shared__ __align__(16) char smem[LS > LG ? LS : LG];
   const bool back = (int)blockIdx.x < blocks;
   const WalkBlock b = walk_block(a, back ? (int)blockIdx.x : (int)blockIdx.x - blocks, slices, 16 * NW);
   if (!b.in) return;
-  if (back) delta_walk<E, DK, NW, WALK_GRADIENTS>(smem, a, b.doc, b.h, b.c0);
-  else delta_walk<E, DK, NW, WALK_STATES>(smem, a, b.doc, b.h, b.c0);
+  if (back) delta_walk<E, M, DK, NW, WALK_GRADIENTS>(smem, a, b.doc, b.h, b.c0);
+  else delta_walk<E, M, DK, NW, WALK_STATES>(smem, a, b.doc, b.h, b.c0);
 }
 
 // ------------------------------------------------------------------------------------------ gradients of a chunk
@@ -1584,9 +1584,9 @@ template <typename E, int DK, bool SHARED> __global__ __launch_bounds__(64 * gra
 }
 
 // ------------------------------------------------------------------------------------------ launches
-template <typename E, int DK, int NW> hipError_t delta_walk_results(hipStream_t st, const DeltaRule& a) {
+template <typename E, typename M, int DK, int NW> hipError_t delta_walk_results(hipStream_t st, const DeltaRule& a) {
   const int slices = (int)cdiv(a.dv, 16 * NW), blocks = (int)(cdiv((int64_t)a.ndocs * a.nv, 8) * 8 * slices);
-  hipLaunchKernelGGL((delta_walk_kernel<E, DK, NW>), dim3((unsigned)blocks), dim3(walk_threads(NW)), 0, st, a, slices);
+  hipLaunchKernelGGL((delta_walk_kernel<E, M, DK, NW>), dim3((unsigned)blocks), dim3(walk_threads(NW)), 0, st, a, slices);
   return hipGetLastError();
 }
 template <typename E, int DK, int NW> hipError_t delta_walks(hipStream_t st, const DeltaRule& a) {
@@ -1594,21 +1594,29 @@ template <typename E, int DK, int NW> hipError_t delta_walks(hipStream_t st, con
   hipLaunchKernelGGL((delta_walks_kernel<E, DK, NW>), dim3((unsigned)(2 * blocks)), dim3(walk_threads(NW)), 0, st, a, slices, blocks);
   return hipGetLastError();
 }
-template <typename E, int DK> hipError_t delta_run(hipStream_t st, const DeltaRule& a, bool backward) {
-  const dim3 prep((unsigned)(a.nchunks + DELTA_FILL), (unsigned)a.nk);
-  if (backward) hipLaunchKernelGGL((delta_prep_kernel<E, DK, true>), prep, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((delta_prep_kernel<E, DK, false>), prep, dim3(256), 0, st, a);
+// Workgroups of several 16 columns share what they bring into LDS; of fewer where that would leave CUs without one.
+inline bool walks_are_wide(const DeltaRule& a, int walks) { return (int64_t)a.ndocs * a.nv * cdiv(a.dv, 16) * walks >= 512; }
+template <typename E, typename M, int DK> hipError_t delta_forward(hipStream_t st, const DeltaRule& a) {
+  hipLaunchKernelGGL((delta_prep_kernel<E, M, DK, false>), dim3((unsigned)(a.nchunks + DELTA_FILL), (unsigned)a.nk), dim3(256), 0, st, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.ndocs == 0) return e;
+  return walks_are_wide(a, 1) ? delta_walk_results<E, M, DK, 2>(st, a) : delta_walk_results<E, M, DK, 1>(st, a);
+}
+template <typename E, int DK> hipError_t delta_backward(hipStream_t st, const DeltaRule& a) {
+  hipLaunchKernelGGL((delta_prep_kernel<E, typename WalkOf<E>::type, DK, true>), dim3((unsigned)(a.nchunks + DELTA_FILL), (unsigned)a.nk), dim3(256), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.ndocs == 0) return e;
-  // Workgroups of several 16 columns share what they bring into LDS; of fewer where that would leave CUs without one.
-  const int64_t sets = (int64_t)a.ndocs * a.nv * cdiv(a.dv, 16) * (backward ? 2 : 1);
-  if (backward) e = sets >= 512 ? delta_walks<E, DK, 2>(st, a) : delta_walks<E, DK, 1>(st, a);
-  else e = sets >= 512 ? delta_walk_results<E, DK, 2>(st, a) : delta_walk_results<E, DK, 1>(st, a);
-  if (e != hipSuccess || !backward || a.nchunks == 0) return e;
+  e = walks_are_wide(a, 2) ? delta_walks<E, DK, 2>(st, a) : delta_walks<E, DK, 1>(st, a);
+  if (e != hipSuccess || a.nchunks == 0) return e;
   const dim3 grid((unsigned)a.nchunks, (unsigned)a.nk);
   if (a.nv == a.nk) hipLaunchKernelGGL((delta_grad_kernel<E, DK, false>), grid, dim3(64 * grad_waves(DK)), 0, st, a);
   else hipLaunchKernelGGL((delta_grad_kernel<E, DK, true>), grid, dim3(64 * grad_waves(DK)), 0, st, a);
   return hipGetLastError();
+}
+template <typename E, int DK> hipError_t delta_run(hipStream_t st, const DeltaRule& a, bool backward) {
+  if (backward) return delta_backward<E, DK>(st, a);
+  // Rounded results need less than last states do.  8192 tokens of bf16, 16 heads, widths of 128: 66 us and with them 78 in documents, 204 and 268 in one.
+  return a.ht ? delta_forward<E, typename WalkOf<E>::type, DK>(st, a) : delta_forward<E, E, DK>(st, a);
 }
 template <typename E> hipError_t delta_rule_of(hipStream_t st, const DeltaRule& a, bool backward) {
   return a.dk <= 64 ? delta_run<E, 64>(st, a, backward) : delta_run<E, 128>(st, a, backward);

@@ -310,16 +310,42 @@ def test_a_document_in_two_calls(gpu_device, dtype):
 
 
 @gpu
-def test_results_that_are_not_wanted(gpu_device):
-    """No last states, no gradient of the first: the others keep their bits."""
-    say("not wanted")
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+def test_results_that_are_not_wanted(gpu_device, dtype):
+    """No last states, no gradient of the first: the others keep their bits, but for results of bf16 beside last states, which are of finer products; either way
+    they keep their bound."""
+    say("not wanted", dtype)
     c = Case(200, 1, 1, 64, 64, [90, 110])
-    r = Run(c, 1, c.inputs(1))
+    x, exact = reference(c, dtype)
+    r = Run(c, dtype, x)
     want = r.all()
     r.ht = r.dh0 = None
     r.fwd().bwd()
     for p, n in zip((want[0],) + tuple(want[2:7]), ("o", "dq", "dk", "dv", "dg", "dbeta")):
-        assert torch.equal(p, getattr(r, n))
+        assert torch.equal(p, getattr(r, n)) or (dtype == 1 and n == "o")
+        check(n, getattr(r, n), exact[n], dtype, 2)
+
+
+@gpu
+@pytest.mark.parametrize("case", [CASES[2], CASES[4], CASES[6], CASES[7]], ids=str)
+def test_results_of_bfloat16_without_last_states(gpu_device, case):
+    say("no states", case)
+    x, want = reference(case, 1)
+    r = Run(case, 1, x)
+    r.ht = None
+    r.table().fwd()
+    check("o", r.o, want["o"], 1, -(-max(case.lengths) // 64))
+
+
+@gpu
+def test_many_documents_without_last_states(gpu_device):
+    say("many, no states")
+    c = Case(420, 4, 8, 128, 64, [1, 64, 0, 7, 65] + [9] * 28 + [20], first=2, h0=True)
+    x, want = reference(c, 1)
+    r = Run(c, 1, x)
+    r.ht = None
+    r.table().fwd()
+    check("o", r.o, want["o"], 1, 2)
 
 
 @gpu
