@@ -373,6 +373,15 @@ template <int KB, int NW> __device__ __forceinline__ void bytes_ahead(unsigned l
   }
 }
 
+// A tile of 64 rows whose squares lie in order.
+template <typename TL, int NW> __device__ __forceinline__ void squares_ahead(unsigned lds, const void* from, int wave, int lane) {
+#pragma unroll
+  for (int i = 0; i < 8 / NW; ++i) {
+    const int oct = wave + NW * i;
+    load_ahead<TL::SQUARES>(lds + oct * TL::OCTET, from, 8 * TL::SQUARES * 1024, (unsigned)(oct * TL::SQUARES * 1024 + 16 * lane));
+  }
+}
+
 // ------------------------------------------------------------------------------------------ a chunk's own matrices
 constexpr int TRI_LD = 68;   // floats of a row of a 64 x 64 matrix in LDS: rows 16 bytes aligned, four banks apart
 // T = (1 + A)^-1 of a strictly lower A, both in LDS, by four waves.  Blocks of 16 on the diagonal by substitution, a lane per column; then block by
@@ -519,7 +528,8 @@ template <typename E, typename A16, int DK, bool BWD> __global__ __launch_bounds
         f16x8 h;
 #pragma unroll
         for (int e = 0; e < 8; ++e) h[e] = (f16)((float)x[t][i][e] * (t ? q_unit : k_unit));
-        *reinterpret_cast<f16x8*>(to + t * 64 * DK + ((int)threadIdx.x + 256 * i) * 8) = h;
+        const int piece = (int)threadIdx.x + 256 * i, row = piece / PIECES, p = piece % PIECES;   // squares as they will lie in LDS
+        *reinterpret_cast<f16x8*>(to + t * 64 * DK + (row / 8 * TL::SQUARES + (p >> 3)) * 512 + TL::place(row & 7, p & 7) / 2) = h;
       }
   }
   const float p_unit = k_unit * q_unit, k_inv = 1.f / k_unit, q_inv = 1.f / q_unit;   // powers of two
@@ -679,7 +689,7 @@ template <typename E, typename M, int DK, int NW, int KIND> __device__ __forcein
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
 
   // ---- loads
-  const TileLoad<M, DK, DELTA_C, FW> load_k(COPIES ? DK : a.ldk, lane, COPIES ? DK : a.dk), load_q(COPIES ? DK : a.ldq, lane, COPIES ? DK : a.dk);
+  const TileLoad<E, DK, DELTA_C, FW> load_k(a.ldk, lane, a.dk), load_q(a.ldq, lane, a.dk);
   const TileLoad<E, 64, DELTA_C, FW> load_v(BACK ? a.ldo : a.ldv, lane, min(a.dv - c0, 16 * NW));
   // Loads of a wave, at least: of the keys, of the chunk's matrices, of values and queries.
   constexpr int KEYS = TileLoad<M, DK, DELTA_C, FW>::N, MATS = (L::REC - REC_GATES) / 1024 / FW;
@@ -687,8 +697,8 @@ template <typename E, typename M, int DK, int NW, int KIND> __device__ __forcein
   auto copies = [&](int c) { return a.halves + ((int64_t)(chunk0 + c) * a.nk + kv) * (2 * DELTA_C * DK); };
   auto fetch_keys = [&](int c, unsigned to) {
     const int t0 = first + DELTA_C * c, end = min(first + count, t0 + DELTA_C);
-    if constexpr (COPIES) tile_ahead(load_k, to + L::K, copies(c), 0, DELTA_C, fw);
-    else tile_ahead(load_k, to + L::K, (const M*)a.k + kv * a.dk, t0, end, fw);
+    if constexpr (COPIES) squares_ahead<Tile<M, DK>, FW>(to + L::K, copies(c), fw, lane);
+    else tile_ahead(load_k, to + L::K, (const E*)a.k + kv * a.dk, t0, end, fw);
   };
   auto fetch_mats = [&](int c, unsigned to) {
     const char* rec = a.records + ((int64_t)(chunk0 + c) * a.nv + h) * (RESULTS ? REC_FWD : REC_BWD);
@@ -699,8 +709,8 @@ template <typename E, typename M, int DK, int NW, int KIND> __device__ __forcein
     const int t0 = first + DELTA_C * c, end = min(first + count, t0 + DELTA_C);
     tile_ahead(load_v, smem + L::V + by, (BACK ? (const E*)a.dout : (const E*)a.v) + h * a.dv + c0, t0, end, fw);
     if constexpr (KIND != WALK_STATES) {
-      if constexpr (COPIES) tile_ahead(load_q, smem + L::Q + by, copies(c) + DELTA_C * DK, 0, DELTA_C, fw);
-      else tile_ahead(load_q, smem + L::Q + by, (const M*)a.q + kv * a.dk, t0, end, fw);
+      if constexpr (COPIES) squares_ahead<Tile<M, DK>, FW>(smem + L::Q + by, copies(c) + DELTA_C * DK, fw, lane);
+      else tile_ahead(load_q, smem + L::Q + by, (const E*)a.q + kv * a.dk, t0, end, fw);
     }
   };
   auto fetch_all = [&](int c) {
@@ -714,34 +724,29 @@ template <typename E, typename M, int DK, int NW, int KIND> __device__ __forcein
     if (AHEAD && chunks > 1) {
       fetch_keys(c + step, smem + L::FIRST);
       if constexpr (ALL_AHEAD) fetch_second(c + step, L::SECOND);
-      else fetch_mats(c + step, smem + L::FIRST);
-      loads_but<KEYS + (ALL_AHEAD ? SECOND : MATS)>();
+      loads_but<KEYS + (ALL_AHEAD ? SECOND : 0)>();
     } else tile_wait();
   }
   // The two barriers of chunk n, and the loading waves' part of them: what they have to see arrived before, what they ask for behind.  After the second one
-  // nothing of the chunk's keys, values and queries is read from LDS any more, and the chunk after the next takes their place; its matrices, where all
-  // is there twice, follow in the next phase, so that a wave has about as much to ask for in either.
+  // nothing of the chunk's keys, values and queries is read from LDS any more, and the chunk after the next takes their place; its matrices
+  // follow in the next phase, so that a wave has about as much to ask for in either.
   auto begin_chunk = [&](int n) {
-    if (ALL_AHEAD && loads && n + 1 < chunks) fetch_mats(c + step, smem + ((n + 1) & 1) * L::FIRST);
+    if (AHEAD && loads && n + 1 < chunks) fetch_mats(c + step, smem + ((n + 1) & 1) * L::FIRST);
   };
   auto middle = [&](int n) {
-    if (AHEAD && loads && n + 1 < chunks) {   // the next keys
-      if constexpr (ALL_AHEAD) loads_but<MATS + SECOND>();
-      else tile_wait();
-    }
+    if (AHEAD && loads && n + 1 < chunks) loads_but<MATS + (ALL_AHEAD ? SECOND : 0)>();   // the next keys
     __syncthreads();
     if (AHEAD && loads && n + 1 < chunks) {
       if constexpr (!ALL_AHEAD) fetch_second(c + step, 0);
       if (n + 2 < chunks) {
         fetch_keys(c + 2 * step, smem + (n & 1) * L::FIRST);
         if constexpr (ALL_AHEAD) fetch_second(c + 2 * step, (n & 1) * L::SECOND);
-        else fetch_mats(c + 2 * step, smem + (n & 1) * L::FIRST);
       }
     }
   };
   auto end_chunk = [&](int n) {
     if (AHEAD && loads) {   // the next matrices, values and queries
-      if (n + 2 < chunks) loads_but<KEYS + (ALL_AHEAD ? SECOND : MATS)>();
+      if (n + 2 < chunks) loads_but<KEYS + (ALL_AHEAD ? SECOND : 0)>();
       else tile_wait();
     }
     __syncthreads();
