@@ -201,7 +201,7 @@ int stage_op_attention_docs_bwd(void* stream, int32_t dtype, int32_t T, int32_t 
  * A_ij = beta_i exp(g_(j+1) + .. + g_i) k_i.k_j (j < i, of 64 tokens), which a stable rule bounds; bf16, the same: digits are lost where the largest of
  * 64 tokens' keys, or queries, is above 2^65 or under 2^-50.  o of bf16 is formed in finer products, and may be rounded otherwise, where ht is wanted.
  * dk and dv: multiples of 8, dk up to 128, dv up to 256.  Rows start at multiples of 16 bytes, strides are multiples of 16 bytes and at most
- * 2^22 elements; states are 16-byte aligned; T <= 2^26, nv <= 4096, T * nv <= 2^30, ndocs <= 2^20 and ndocs * nv <= 2^20.  scale is finite.
+ * 2^22 elements; states are 16-byte aligned; T <= 2^26, nv <= 4096, T * nv <= 2^30, ndocs and ndocs * nv <= 2^18.  scale is finite.
  * No output overlaps an input or another output.  T = 0 and ndocs = 0 together do nothing.  The GPU that owns `stream` must be the
  * current device.  scratch: device, 256-byte aligned, at least the bytes of the function beside each call (host only; never less for more
  * tokens or documents; negative STAGE_ERR_ARG for invalid sizes), the caller's, free again when the call's work on the stream has finished; calls that may
@@ -283,7 +283,7 @@ int stage_op_adamw(void* stream, int32_t dtype, int64_t n, int64_t begin, void* 
 
 /* The norm of many gradient tensors taken together, and clipping by it.  tensors: HOST array of ntensors >= 0 (the pointers and sizes are read during the
  * call): in: device, n >= 0 elements of dtype, at a multiple of the element's size; out: for stage_op_grad_scale alone (else NULL is fine), the
- * same place as in, or n elements that overlap none of the list's; n = 0: both may be NULL.  In total less than 2^52 bytes.
+ * same place as in, or n elements elsewhere, and over no other tensor of the list (STAGE_ERR_ARG); n = 0: both may be NULL.  In total less than 2^52 bytes.
  * Squares and sums are formed in 64 bits and in a fixed order: no overflow, the same bits on every call with the same sizes.
  *
  * stage_op_grad_norm: *sumsq = the sum of all squares; *norm = scale sqrt(sumsq), scale > 0 finite (1 / loss scale);

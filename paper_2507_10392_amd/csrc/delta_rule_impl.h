@@ -21,8 +21,8 @@
 // rounded to the type.  The last states are fp32, and dg and dbeta are what is left of larger terms: with bf16 pairs throughout these were off by up to 5.2e-6
 // and 1.5e-5 of their norms.  So where last states are wanted, and backward, the walks take half pairs for bf16 too (keys and queries as
 // halves times a power of two that prep finds, computed values times one per column, so that no size of state or gradient leaves
-// a half's range), and a chunk's gradients three bf16, which are an fp32, of S, dS, U and Y: 3e-7 and 1.2e-6, for 15 us in 104 and 5 in 112 (gradients; 16 heads,
-// 8192 tokens, head widths of 128).  What only goes into dq and dk, which are rounded to 16 bits, stays pairs.  fp32: v_mfma_f32_16x16x4, no pairs.
+// a half's range), and a chunk's gradients three bf16, which are an fp32, of S, dS, U and Y: 3e-7 and 1.2e-6, for 15 us in 104 and 8 in 112 (gradients; 4096
+// tokens, 16 heads, head widths of 128).  What only goes into dq and dk, which are rounded to 16 bits, stays pairs.  fp32: v_mfma_f32_16x16x4, no pairs.
 #pragma once
 #include "attention_docs_tiles.h"
 
@@ -453,7 +453,9 @@ template <typename E> __device__ __forceinline__ void fill_rows(E* p, int64_t ld
   }
 }
 
-// A workgroup per chunk and key head; the value heads of the key head one after the other.
+// A workgroup per chunk and key head; the value heads of the key head one after the other: K K^T and Q K^T are formed once for them.  Bound by the latencies of the
+// inverse, 16 steps of a substitution and three of blocks one after the other, of which four workgroups on a CU hide a part: 4096 tokens of 16 heads of 128
+// 21 us, 28 with what the gradients take besides (they write 28 and 42 MB, 6 and 9 us at the rate of a large copy).
 constexpr int prep_lds(int tile) { return 2 * tile > 2 * 64 * TRI_LD * 4 ? 2 * tile : 2 * 64 * TRI_LD * 4; }   // A and T take the place of keys and queries
 template <typename E, int DK> constexpr int PREP_LDS = prep_lds(Tile<E, DK>::bytes(DELTA_C));
 template <typename E, int DK> constexpr int PREP_GROUPS = PREP_LDS<E, DK> <= 36 * 1024 ? 4 : 2;   // on a CU
@@ -636,9 +638,10 @@ template <typename E, typename A16, int DK, bool BWD> __global__ __launch_bounds
 // once more for the results, what the gradients' walk adds to its state, the stores of states and u), with 12 KB of LDS between the four; the loads
 // are waves' of their own, or, with 32 columns, where these would be a third wave on a SIMD, the second helpers'.  Two barriers a chunk: the first publishes the
 // state, and matrices, values and queries of the chunk, the second Z, and the next chunk's keys.  All of these come straight into LDS, a chunk ahead where
-// two of them fit.  What bounds a walk: that chain, 3000 cycles a chunk (1.4 us) of a document alone, 4100 where two sets of columns and their
-// helpers share the SIMDs; with 16 heads and widths of 128, 8192 tokens in one document 177 us, in documents 47 (one helper, and loads out
-// of step with what it does: 188 and 53); the two of the backward together 114, in which they write 440 MB of states and u.
+// two of them fit.  What bounds a walk: that chain, 3000 cycles a chunk (1.4 us) of 16 columns alone on a CU, 4100 where two sets of columns and their
+// helpers share the SIMDs.  bf16, widths of 128: one document of 8192 tokens, 32 heads over 16, 177 us; 4096 tokens in documents, 16 heads, 47 (with one
+// helper, and more to load in one phase than in the other: 188 and 53), and both walks of their gradients 110: 7900 cycles a chunk, in which the helpers are
+// what the others wait for (2000 to 3700 cycles for what a gradient gets from Q and dO, as long for the stores of states and y).
 enum DeltaWalk { WALK_RESULTS = 0, WALK_STATES = 1, WALK_GRADIENTS = 2 };   // o and the last state; the states and u for the gradients; the states' gradients and y
 constexpr int HELPERS = 2;                                       // of 16 columns
 constexpr int walk_loaders(int NW) { return NW == 1 ? 4 : 0; }   // waves that only load; to ask for 1 KB takes a wave 50 to 70 cycles
@@ -1259,6 +1262,9 @@ template <typename M> __device__ __forceinline__ GradOpnd<M> load_terms(unsigned
 // head's columns of dq and dk, for all tokens: results are transposed (rows are columns of the head, a lane has a token), so that a
 // state's rows are read by one wave only and a token's factors are a lane's own.  The matrices of tokens by tokens are shared out by tiles: wave
 // w has the row tile w % 4, and of its column tiles those of its parity where there are eight waves.  Columns of the value head come in blocks of 64.
+// A workgroup fills a CU (157 KB of LDS, 242 registers), so what it loads is asked for ahead, states 32 columns, u and y 64, and the first of them before its
+// row of the table is there.  4096 tokens of 16 heads of 128 in bf16: 120 us in 4.3 rounds of 256 workgroups, 213 MB of states, u and y at 1.8 TB/s; a round is
+// bound by its phases one after the other, of which the products take about a third.
 constexpr int grad_waves(int DK) { return DK / 16; }
 template <typename E, int DK, bool SHARED> __global__ __launch_bounds__(64 * grad_waves(DK), 1) void delta_grad_kernel(DeltaRule a) {
   typedef typename GradOf<E>::type M;
@@ -1620,7 +1626,8 @@ template <typename E, int DK> hipError_t delta_backward(hipStream_t st, const De
 }
 template <typename E, int DK> hipError_t delta_run(hipStream_t st, const DeltaRule& a, bool backward) {
   if (backward) return delta_backward<E, DK>(st, a);
-  // Rounded results need less than last states do.  8192 tokens of bf16, 16 heads, widths of 128: 66 us and with them 78 in documents, 204 and 268 in one.
+  // Rounded results need less than last states do.  bf16, widths of 128, the whole call: 4096 tokens in documents, 16 heads, 66 us and with last states 78; one
+  // document of 8192, 32 heads over 16, 204 and 268.
   return a.ht ? delta_forward<E, typename WalkOf<E>::type, DK>(st, a) : delta_forward<E, E, DK>(st, a);
 }
 template <typename E> hipError_t delta_rule_of(hipStream_t st, const DeltaRule& a, bool backward) {

@@ -3,8 +3,11 @@
 #include "../../include/stage_ops.h"
 #include "kernels.h"
 
+#include <algorithm>
 #include <cmath>
+#include <memory>
 #include <mutex>
+#include <new>
 
 using namespace zs;
 
@@ -334,14 +337,15 @@ int stage_op_attention_docs_bwd(void* stream, int32_t dtype, int32_t T, int32_t 
 
 }  // extern "C"
 namespace {
-constexpr int DELTA_MAX_TOKENS = 1 << 26, DELTA_MAX_HEADS = 4096, DELTA_MAX_DOCS = 1 << 20;   // documents, and documents times value heads: threads of a launch
+// Walks: documents times value heads.  A launch has less than 2^32 threads: 2^18 walks in eight slices, two directions, 512 threads each are 2^31.
+constexpr int DELTA_MAX_TOKENS = 1 << 26, DELTA_MAX_HEADS = 4096, DELTA_MAX_DOCS = 1 << 18, DELTA_MAX_WALKS = 1 << 18;
 bool aligned16(const void* p) { return !((uintptr_t)p & 15); }   // or nothing
 bool delta_heads_ok(int dtype, int nk, int nv, int dk, int dv) {
   return dt_ok(dtype) && nk >= 1 && nv >= nk && nv % nk == 0 && nv <= DELTA_MAX_HEADS && dk >= 8 && dk % 8 == 0 && dk <= 128 && dv >= 8 && dv % 8 == 0 && dv <= 256;
 }
 bool delta_docs_ok(int T, int ndocs) { return T >= 0 && T <= DELTA_MAX_TOKENS && ndocs >= 0 && ndocs <= DELTA_MAX_DOCS; }
 bool delta_shape_ok(int dtype, int T, int ndocs, int nk, int nv, int dk, int dv) {
-  return delta_heads_ok(dtype, nk, nv, dk, dv) && delta_docs_ok(T, ndocs) && (int64_t)T * nv <= 1 << 30 && (int64_t)ndocs * nv <= DELTA_MAX_DOCS;
+  return delta_heads_ok(dtype, nk, nv, dk, dv) && delta_docs_ok(T, ndocs) && (int64_t)T * nv <= 1 << 30 && (int64_t)ndocs * nv <= DELTA_MAX_WALKS;
 }
 bool delta_rows_ok(int dtype, int nk, int nv, int dk, int dv, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
                    const float* g, const float* beta, float scale, const void* o, int64_t ldo) {
@@ -465,6 +469,27 @@ bool tensors_ok(int32_t n, const stage_op_tensor* t, bool out) {
   }
   return true;
 }
+// No output over another tensor's input or output, nor beside its own input over a part of it: two workgroups would write what one of them reads.
+bool outputs_apart(int32_t n, const stage_op_tensor* t) {
+  struct Span { uintptr_t begin, end; bool out; };
+  std::unique_ptr<Span[]> spans(new (std::nothrow) Span[2 * (size_t)n + 1]);
+  if (!spans) return false;
+  size_t m = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const uintptr_t bytes = (uintptr_t)t[i].n * (t[i].dtype == 0 ? 4 : 2), in = (uintptr_t)t[i].in, out = (uintptr_t)t[i].out;
+    if (!bytes) continue;
+    spans[m++] = Span{out, out + bytes, true};
+    if (in != out) spans[m++] = Span{in, in + bytes, false};
+  }
+  std::sort(spans.get(), spans.get() + m, [](const Span& a, const Span& b) { return a.begin < b.begin; });
+  uintptr_t in_end = 0, out_end = 0;   // of those that begin before
+  for (size_t i = 0; i < m; ++i) {
+    const Span& x = spans[i];
+    if (x.begin < out_end || (x.out && x.begin < in_end)) return false;
+    (x.out ? out_end : in_end) = std::max(x.out ? out_end : in_end, x.end);
+  }
+  return true;
+}
 bool clip_ok(float scale, float max_norm, const double* sumsq, const float* norm, const float* factor, const int32_t* overflow) {
   return scale > 0.f && !std::isinf(scale) && max_norm >= 0.f && !((uintptr_t)sumsq & 7) && words_ok(norm) && words_ok(factor) && words_ok(overflow);
 }
@@ -490,7 +515,7 @@ int stage_op_grad_factor(void* stream, int32_t nsums, const double* sums, float 
 }
 
 int stage_op_grad_scale(void* stream, int32_t ntensors, const stage_op_tensor* tensors, const float* factor) {
-  if (!tensors_ok(ntensors, tensors, true) || !factor || !words_ok(factor)) return STAGE_ERR_ARG;
+  if (!tensors_ok(ntensors, tensors, true) || !factor || !words_ok(factor) || !outputs_apart(ntensors, tensors)) return STAGE_ERR_ARG;
   return rc(grad_scale((hipStream_t)stream, grad_tensors(tensors), ntensors, factor));
 }
 

@@ -349,6 +349,26 @@ def test_many_documents_without_last_states(gpu_device):
 
 
 @gpu
+def test_as_many_documents_as_there_may_be(gpu_device):
+    """2^18 walks, the first and the last one with tokens: states of the others pass through, tokens have the bits of two documents by themselves."""
+    say("most")
+    n = 1 << 18
+    few = Case(65, 1, 1, 8, 256, [64, 1], h0=True, ht=True)
+    x = few.inputs(1)
+    want = Run(few, 1, x).all()
+    many = Case(65, 1, 1, 8, 256, [64])
+    many.lengths, many.offsets = [64] + [0] * (n - 2) + [1], [0] + [64] * (n - 1) + [65]
+    r = Run(many, 1, {**x, "h0": None, "dht": None})
+    r.h0, r.dht = (torch.full((n, 1, 8, 256), v, device="cuda") for v in (0.5, -0.25))
+    for state, name in ((r.h0, "h0"), (r.dht, "dht")):
+        state[[0, n - 1]] = x[name].float().cuda()
+    got = r.all()
+    for p, q in zip(want, got):
+        assert torch.equal(p, q[[0, n - 1]] if q.shape[0] == n else q)
+    assert (got[1][1:n - 1] == 0.5).all() and (got[7][1:n - 1] == -0.25).all()
+
+
+@gpu
 def test_no_documents_and_no_tokens(gpu_device):
     say("nothing")
     c = Case(70, 1, 1, 64, 64, [])
@@ -564,6 +584,13 @@ def test_other_refusals():
         assert L.stage_op_delta_chunks(None, 10, 1, offsets, chunks) == zs.STAGE_ERR_ARG
     for f in (L.stage_op_delta_fwd_scratch_bytes, L.stage_op_delta_bwd_scratch_bytes):
         assert f(1, 10, 1, 2, 3, 64, 64) == -zs.STAGE_ERR_ARG
+
+
+def test_the_most_documents():
+    L = zs.lib()
+    for f in (L.stage_op_delta_fwd_scratch_bytes, L.stage_op_delta_bwd_scratch_bytes):
+        assert f(1, 10, 1 << 16, 4, 4, 64, 64) > 0 and f(1, 10, (1 << 16) + 1, 4, 4, 64, 64) == -zs.STAGE_ERR_ARG
+        assert f(1, 10, 1 << 18, 1, 1, 64, 64) > 0 and f(1, 10, (1 << 18) + 1, 1, 1, 64, 64) == -zs.STAGE_ERR_ARG
 
 
 def test_scratch_and_table_never_shrink():

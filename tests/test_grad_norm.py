@@ -238,6 +238,32 @@ def test_other_refusals():
     assert L.stage_set_grad_factor(None, 4096) == zs.STAGE_ERR_ARG
 
 
+@pytest.mark.parametrize("rows", [[(4096, 4096, 64, 0)] * 2, [(4096, 4096, 64, 0), (4224, 4224, 64, 1)], [(4096, 8192, 64, 0), (16384, 8320, 64, 0)],
+                                  [(4096, 8192, 64, 0), (8444, 8444, 64, 0)], [(4096, 4100, 64, 0)], [(4100, 4096, 64, 1)], [(4096, 8192, 64, 0), (8192, 16384, 8, 0)]], ids=str)
+def test_scaling_over_another_tensor_is_refused(rows):
+    """The same tensor twice, outputs over one another or over inputs; the norm of such lists is fine."""
+    L, t = zs.lib(), tensors(*rows)
+    assert L.stage_op_grad_scale(None, len(rows), t, 4096) == zs.STAGE_ERR_ARG
+    assert L.stage_op_grad_norm_scratch_bytes(len(rows), t) > 0
+
+
+@gpu
+def test_lists_that_share_what_is_only_read(gpu_device):
+    """The same input twice, to outputs of its own each, and a tensor that begins where another one ends."""
+    say("shared inputs")
+    rng = np.random.default_rng(5)
+    x = draw(rng, 5000, torch.float32)
+    a, b = x[:3000], x[3000:]
+    outs = [torch.zeros(3000, device="cuda"), torch.zeros(3000, device="cuda"), b]
+    run = Norm([a, a, b], outs)(1.0, 0.01)
+    run.check([a, a, b], 1.0, 0.01)
+    want = [t * run.factor for t in (a, a, b)]
+    zs.grad_scale(stream(), run.list, run.factor)
+    assert float(run.factor) < 1
+    for o, w in zip(outs, want):
+        assert torch.equal(o, w)
+
+
 def test_lists_of_other_tensors_are_refused():
     x = torch.zeros(4, 4)
     for bad in ([x], [x.to(torch.int32)]):
