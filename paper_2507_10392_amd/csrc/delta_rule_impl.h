@@ -1263,8 +1263,9 @@ template <typename M> __device__ __forceinline__ GradOpnd<M> load_terms(unsigned
 // state's rows are read by one wave only and a token's factors are a lane's own.  The matrices of tokens by tokens are shared out by tiles: wave
 // w has the row tile w % 4, and of its column tiles those of its parity where there are eight waves.  Columns of the value head come in blocks of 64.
 // A workgroup fills a CU (157 KB of LDS, 242 registers), so what it loads is asked for ahead, states 32 columns, u and y 64, and the first of them before its
-// row of the table is there.  4096 tokens of 16 heads of 128 in bf16: 120 us in 4.3 rounds of 256 workgroups, 213 MB of states, u and y at 1.8 TB/s; a round is
-// bound by its phases one after the other, of which the products take about a third.
+// row of the table is there.  4096 tokens of 16 heads of 128 in bf16: 120 us in 4.3 rounds of 256 workgroups, 213 MB of states, u and y at 1.8 TB/s; a
+// workgroup's phases follow one another: of 45000 cycles alone 12700 until the first loads are there, 10800 the products with states, 8600 the matrices of
+// tokens and the sums over them, 7300 the products with these, and fewer registers would spill (128, two workgroups a CU: 245 us).
 constexpr int grad_waves(int DK) { return DK / 16; }
 template <typename E, int DK, bool SHARED> __global__ __launch_bounds__(64 * grad_waves(DK), 1) void delta_grad_kernel(DeltaRule a) {
   typedef typename GradOf<E>::type M;
@@ -1605,7 +1606,9 @@ template <typename E, int DK, int NW> hipError_t delta_walks(hipStream_t st, con
   hipLaunchKernelGGL((delta_walks_kernel<E, DK, NW>), dim3((unsigned)(2 * blocks)), dim3(walk_threads(NW)), 0, st, a, slices, blocks);
   return hipGetLastError();
 }
-// Workgroups of several 16 columns share what they bring into LDS; of fewer where that would leave CUs without one.
+// Workgroups of 32 columns share what they bring into LDS; of 16 where 32 would leave CUs without one.  bf16, widths of 128, us of the walk with 16 and 32: 3
+// documents of 4 heads (96 sets of 16 columns) 6.0 and 8.5, one of 32 heads (256) 177 and 229, 6 of 16 heads (768) 51.5 and 47, backward (1536) 145 and 110;
+// half, 6 of 8 heads (576) 35.8 and 34.
 inline bool walks_are_wide(const DeltaRule& a, int walks) { return (int64_t)a.ndocs * a.nv * cdiv(a.dv, 16) * walks >= 512; }
 template <typename E, typename M, int DK> hipError_t delta_forward(hipStream_t st, const DeltaRule& a) {
   hipLaunchKernelGGL((delta_prep_kernel<E, M, DK, false>), dim3((unsigned)(a.nchunks + DELTA_FILL), (unsigned)a.nk), dim3(256), 0, st, a);
