@@ -132,11 +132,23 @@ __device__ __forceinline__ float rows_max(float x) {
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 template <int CTRL> __device__ __forceinline__ float dpp(float x) { return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xf, 0xf, true)); }
+template <int CTRL> __device__ __forceinline__ unsigned dpp(unsigned x) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true); }
 __device__ __forceinline__ float columns_sum(float x) {
   x += dpp<0xb1>(x);    // neighbours
   x += dpp<0x4e>(x);    // pairs
   x += dpp<0x141>(x);   // the two quads of eight lanes
   return x + dpp<0x140>(x);
+}
+
+__device__ __forceinline__ unsigned wave_most(unsigned x) {
+  x = max(x, dpp<0xb1>(x));
+  x = max(x, dpp<0x4e>(x));
+  x = max(x, dpp<0x141>(x));
+  x = max(x, dpp<0x140>(x));
+  auto a = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  x = max(a[0], a[1]);
+  auto b = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return max(b[0], b[1]);
 }
 
 // What walks whose states are results, and a chunk's own matrices for them, are computed in: bf16 as half.
@@ -384,42 +396,58 @@ template <typename TL, int NW> __device__ __forceinline__ void squares_ahead(uns
 
 // ------------------------------------------------------------------------------------------ a chunk's own matrices
 constexpr int TRI_LD = 68;   // floats of a row of a 64 x 64 matrix in LDS: rows 16 bytes aligned, four banks apart
-// T = (1 + A)^-1 of a strictly lower A, both in LDS, by four waves.  Blocks of 16 on the diagonal by substitution, a lane per column; then block by
-// block away from it, T_ij = -T_ii (sum over k of A_ik T_kj), in fp32 products.  Every step solves for values of T itself, which are bounded where the
+// T = (1 + A)^-1 of a strictly lower A, both in LDS, by four waves.  Blocks of 16 on the diagonal by substitution, four rows
+// at a time, by the lanes that hold them, and what these leave of the others by a product; then block by block away from it, T_ij = -T_ii (sum over k of A_ik T_kj), in fp32 products.  Every step solves for values of T itself, which are bounded where the
 // rule is stable; powers of A, which are not, do not occur.
 __device__ __forceinline__ void invert_lower(const float* A, float* T, int wave, int lane) {
   const int g = lane >> 4, c = lane & 15;
-  if (lane < 16) {
-    float x[16];
+  {
+    const float* block = A + (16 * wave) * TRI_LD + 16 * wave;
+    const f32x4 column = *reinterpret_cast<const f32x4*>(block + c * TRI_LD + 4 * g);   // of row c
+    f32x4 own[4], x;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      float s[2] = {r == c ? 1.f : 0.f, 0.f};
-#pragma unroll
-      for (int q = 0; q < (r + 3) / 4; ++q) {
-        const f32x4 a = *reinterpret_cast<const f32x4*>(A + (16 * wave + r) * TRI_LD + 16 * wave + 4 * q);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (4 * q + e < r) s[e & 1] = fmaf(-a[e], x[4 * q + e], s[e & 1]);
-      }
-      x[r] = s[0] + s[1];
+    for (int r = 0; r < 4; ++r) {
+      own[r] = *reinterpret_cast<const f32x4*>(block + (4 * g + r) * TRI_LD + 4 * g);
+      x[r] = 4 * g + r == c ? 1.f : 0.f;
     }
 #pragma unroll
-    for (int r = 0; r < 16; ++r) T[(16 * wave + r) * TRI_LD + 16 * wave + c] = x[r];
+    for (int q = 0; q < 4; ++q) {
+      const bool now = g == q;
+      f32x4 y = x;
+#pragma unroll
+      for (int r = 1; r < 4; ++r)
+#pragma unroll
+        for (int e = 0; e < r; ++e) y[r] = fmaf(-own[r][e], y[e], y[r]);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) y[r] = now ? y[r] : x[r];
+      x = y;
+      if (q < 3) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_16x16x4f32(now ? -column[e] : 0.f, now ? y[e] : 0.f, x, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = now ? y[r] : x[r];
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) T[(16 * wave + 4 * g + r) * TRI_LD + 16 * wave + c] = x[r];
   }
+#pragma unroll
   for (int d = 1; d < 4; ++d) {
     __syncthreads();
     const int i = wave, j = wave - d;
     if (j >= 0) {
-      f32x4 x = {0.f, 0.f, 0.f, 0.f};
-      for (int k = j; k < i; ++k) {
-        const f32x4 a = *reinterpret_cast<const f32x4*>(A + (16 * i + c) * TRI_LD + 16 * k + 4 * g);
+      f32x4 x[3] = {};   // a sum of its own for each block, so that none waits for another
+      const f32x4 t = *reinterpret_cast<const f32x4*>(T + (16 * i + c) * TRI_LD + 16 * i + 4 * g);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], T[(16 * k + 4 * g + e) * TRI_LD + 16 * j + c], x, 0, 0, 0);
+      for (int k = 0; k < d; ++k) {
+        const f32x4 a = *reinterpret_cast<const f32x4*>(A + (16 * i + c) * TRI_LD + 16 * (j + k) + 4 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[k] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], T[(16 * (j + k) + 4 * g + e) * TRI_LD + 16 * j + c], x[k], 0, 0, 0);
       }
-      const f32x4 a = *reinterpret_cast<const f32x4*>(T + (16 * i + c) * TRI_LD + 16 * i + 4 * g);
+      const f32x4 sum = d == 1 ? x[0] : d == 2 ? x[0] + x[1] : x[0] + x[1] + x[2];
       f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], x[e], y, 0, 0, 0);
+      for (int e = 0; e < 4; ++e) y = __builtin_amdgcn_mfma_f32_16x16x4f32(t[e], sum[e], y, 0, 0, 0);
 #pragma unroll
       for (int r = 0; r < 4; ++r) T[(16 * i + 4 * g + r) * TRI_LD + 16 * j + c] = -y[r];
     }
@@ -485,43 +513,64 @@ template <typename E, typename A16, int DK, bool BWD> __global__ __launch_bounds
   const ChunkRow c = chunk_row(a, blockIdx.x);
   if (c.count <= 0) return;
   const unsigned smem = lds_address(tiles);
+  const bool in = lane < c.count;   // the first wave's token, and its gates; before keys and queries, since loads come back in order
+  const int64_t first_gate = (int64_t)(c.first + (in ? lane : 0)) * a.nv + kv * group;
+  float g_in = a.g[first_gate], beta_in = a.beta[first_gate];
+  __builtin_amdgcn_sched_barrier(0);
   {
     const TileLoad<E, DK, DELTA_C, 4> load_k(a.ldk, lane, a.dk), load_q(a.ldq, lane, a.dk);
     load_k.fetch(smem, (const E*)a.k + kv * a.dk, c.first, c.first + c.count, wave);
     load_q.fetch(smem + TILE, (const E*)a.q + kv * a.dk, c.first, c.first + c.count, wave);
   }
+  // A head's gates, by the first wave: the first head's while keys and queries are under way (after them: 3700 of 17700 cycles).
+  auto gates_of = [&](int h) {
+    char* rec = a.records + ((int64_t)blockIdx.x * a.nv + h) * (BWD ? REC_BWD : REC_FWD);
+    const float gl = in ? g_in * 1.4426950408889634f : 0.f, beta = in ? beta_in : 0.f;
+    const double sum = running_sum((double)(gl < DELTA_FORGETS ? DELTA_FORGETS : gl), lane), last = __shfl(sum, 63, 64);
+    G[lane] = sum;
+    B[lane] = beta;
+    float* gates = reinterpret_cast<float*>(rec);
+    gates[lane] = in ? decay(sum, 0.0) : 0.f;
+    gates[64 + lane] = in ? decay(last, sum) : 0.f;
+    gates[128 + lane] = beta;
+    if (lane == 0) gates[192] = decay(last, 0.0);
+    if constexpr (BWD) reinterpret_cast<double*>(rec + REC_G)[lane] = sum;
+  };
+  if (wave == 0) gates_of(kv * group);
   tile_wait();
   __syncthreads();
   const TileOps<E, DK> at(smem, lane);
   float k_unit = 1.f, q_unit = 1.f;
   if constexpr (!__is_same(A16, E)) {   // keys and queries as halves, times powers of two that bring the largest of either to 2^3 .. 2^4
     constexpr int PIECES = DK / 8, MINE = 64 * PIECES / 256;
+    typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+    __shared__ unsigned most_of[2][4];
     bf16x8 x[2][MINE];
-    float most[2] = {0.f, 0.f};
+    unsigned most[2];   // of the bits below the sign, which compare as the values do
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < 2; ++t) {
+      u16x8 m = {};
 #pragma unroll
       for (int i = 0; i < MINE; ++i) {
         const int piece = (int)threadIdx.x + 256 * i, row = piece / PIECES, p = piece % PIECES;
-        x[t][i] = lds_read<bf16x8>(smem + t * TILE + row / 8 * TL::OCTET + (p >> 3) * 1024 + TL::place(row & 7, p & 7));
-#pragma unroll
-        for (int e = 0; e < 8; ++e) most[t] = fmaxf(most[t], fabsf((float)x[t][i][e]));
+        const u16x8 bits = lds_read<u16x8>(smem + t * TILE + row / 8 * TL::OCTET + (p >> 3) * 1024 + TL::place(row & 7, p & 7));
+        x[t][i] = __builtin_bit_cast(bf16x8, bits);
+        m = __builtin_elementwise_max(m, bits & (unsigned short)0x7fff);
       }
+      most[t] = 0;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) most[t] = wave_max(most[t]);
-    __syncthreads();
-    if (lane == 0) {
-      B[wave] = most[0];
-      B[4 + wave] = most[1];
+      for (int e = 0; e < 8; ++e) most[t] = max(most[t], (unsigned)m[e]);
+      most[t] = wave_most(most[t]);
+      if (lane == 0) most_of[t][wave] = most[t];
     }
     __syncthreads();
-    auto unit = [&](int at) {
-      const float m = fmaxf(fmaxf(B[at], B[at + 1]), fmaxf(B[at + 2], B[at + 3]));
-      const int e = (int)(__float_as_uint(m) >> 23);
-      return m > 0.f && e < 255 ? __uint_as_float((unsigned)min(max(257 - e, 77), 177) << 23) : 1.f;
+    auto unit = [&](int t) {
+      const unsigned m = max(max(most_of[t][0], most_of[t][1]), max(most_of[t][2], most_of[t][3]));
+      const int e = (int)(m >> 7);
+      return m > 0 && e < 255 ? __uint_as_float((unsigned)min(max(257 - e, 77), 177) << 23) : 1.f;
     };
     k_unit = unit(0);
-    q_unit = unit(4);
+    q_unit = unit(1);
     f16* to = a.halves + ((int64_t)blockIdx.x * a.nk + kv) * (2 * 64 * DK);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -535,42 +584,35 @@ template <typename E, typename A16, int DK, bool BWD> __global__ __launch_bounds
       }
   }
   const float p_unit = k_unit * q_unit, k_inv = 1.f / k_unit, q_inv = 1.f / q_unit;   // powers of two
-  // This wave's rows (kk, and qk of P^T backward: rows j) or columns (qk of P: rows of P^T are keys) against all tiles of the other side.
+  // This wave's rows (kk, and qk of P^T backward: rows j) or columns (qk of P: rows of P^T are keys) against all tiles of the other side.  Of triangles, so that
+  // its columns of P are from the other end.
+  const int pw = BWD ? wave : 3 - wave;
   f32x4 kk[4], qk[4];
 #pragma unroll
   for (int n = 0; n < 4; ++n) kk[n] = qk[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
-    const Opnd<E, 1> mine = at.row(0, wave, s), q_mine = at.row(TILE, wave, s);
+    const Opnd<E, 1> mine = at.row(0, wave, s), q_mine = at.row(TILE, pw, s);
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       const Opnd<E, 1> k_n = at.row(0, n, s);
       if (n <= wave) kk[n] = mma(mine, k_n, kk[n]);                                     // rows i of this wave, columns j of tile n
       if constexpr (BWD) {
         if (n >= wave) qk[n] = mma(at.row(TILE, n, s), mine, qk[n]);                    // rows i of tile n, columns j of this wave
-      } else if (n <= wave) qk[n] = mma(k_n, q_mine, qk[n]);                            // rows j of tile n, columns i of this wave
+      } else if (n <= pw) qk[n] = mma(k_n, q_mine, qk[n]);                              // rows j of tile n, columns i of this wave
     }
   }
   for (int hg = 0; hg < group; ++hg) {
     const int h = kv * group + hg;
     char* rec = a.records + ((int64_t)blockIdx.x * a.nv + h) * (BWD ? REC_BWD : REC_FWD);
-    __syncthreads();   // the head before is done with the LDS
-    if (wave == 0) {
-      const bool in = lane < c.count;
-      const int64_t t = (int64_t)(c.first + (in ? lane : 0)) * a.nv + h;
-      const float gl = in ? a.g[t] * 1.4426950408889634f : 0.f;
-      const double sum = running_sum((double)(gl < DELTA_FORGETS ? DELTA_FORGETS : gl), lane), last = __shfl(sum, 63, 64);
-      const float beta = in ? a.beta[t] : 0.f;
-      G[lane] = sum;
-      B[lane] = beta;
-      float* gates = reinterpret_cast<float*>(rec);
-      gates[lane] = in ? decay(sum, 0.0) : 0.f;
-      gates[64 + lane] = in ? decay(last, sum) : 0.f;
-      gates[128 + lane] = beta;
-      gates[192 + lane] = lane == 0 ? decay(last, 0.0) : lane == 1 ? k_inv : lane == 2 ? q_inv : 0.f;
-      if constexpr (BWD) reinterpret_cast<double*>(rec + REC_G)[lane] = sum;
+    __syncthreads();   // the head before, or keys and queries, are done with the LDS
+    if (wave == 0 && hg > 0) {
+      g_in = a.g[first_gate + hg];
+      beta_in = a.beta[first_gate + hg];
+      gates_of(h);
     }
-    __syncthreads();
+    if (wave == 0 && lane < 2) reinterpret_cast<float*>(rec)[193 + lane] = lane ? q_inv : k_inv;
+    if (hg > 0) __syncthreads();
     {   // A
       double gi[4];
       float bi[4];
@@ -592,12 +634,12 @@ template <typename E, typename A16, int DK, bool BWD> __global__ __launch_bounds
     }
     // P: tiles as they lie, two of them an operand
     f32x4 p[4];
-    const double gc = G[16 * wave + i16];
+    const double gc = G[16 * pw + i16];
 #pragma unroll
     for (int n = 0; n < 4; ++n)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int row = 16 * n + 4 * g + r, col = 16 * wave + i16;
+        const int row = 16 * n + 4 * g + r, col = 16 * pw + i16;
         const double gr = G[row];
         if constexpr (BWD) p[n][r] = row >= col ? p_unit * qk[n][r] * decay(gr, gc) : 0.f;   // P_row,col
         else p[n][r] = row <= col ? p_unit * qk[n][r] * decay(gc, gr) : 0.f;                 // P_col,row
@@ -606,7 +648,7 @@ template <typename E, typename A16, int DK, bool BWD> __global__ __launch_bounds
     for (int s = 0; s < 2; ++s) {
       if constexpr (BWD) {
         if (2 * s + 1 >= wave) store_op<A16>(rec + REC_P + upper_op(wave, s) * REC_OP, pair_of<A16>(p[2 * s], p[2 * s + 1]), lane);
-      } else if (2 * s <= wave) store_op<A16>(rec + REC_P + lower_op(wave, s) * REC_OP, pair_of<A16>(p[2 * s], p[2 * s + 1]), lane);
+      } else if (2 * s <= pw) store_op<A16>(rec + REC_P + lower_op(pw, s) * REC_OP, pair_of<A16>(p[2 * s], p[2 * s + 1]), lane);
     }
     __syncthreads();
     invert_lower(A, Tm, wave, lane);
