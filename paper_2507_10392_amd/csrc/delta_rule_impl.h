@@ -481,9 +481,10 @@ template <typename E> __device__ __forceinline__ void fill_rows(E* p, int64_t ld
   }
 }
 
-// A workgroup per chunk and key head; the value heads of the key head one after the other: K K^T and Q K^T are formed once for them.  Bound by the latencies of the
-// inverse, 16 steps of a substitution and three of blocks one after the other, of which four workgroups on a CU hide a part: 4096 tokens of 16 heads of 128
-// 21 us, 28 with what the gradients take besides (they write 28 and 42 MB, 6 and 9 us at the rate of a large copy).
+// A workgroup per chunk and key head; the value heads of the key head one after the other: K K^T and Q K^T are formed once for them.  Bound by phases that follow
+// one another, of which four workgroups on a CU hide a part; of 17600 cycles 3500 until keys and queries are there, 4300 their products, 3900 A and P, 4000 the
+// inverse (5500 with a lane per column and row after row in its diagonal blocks).  4096 tokens of 16 heads of 128 19.5 us, 25 with what the gradients take
+// besides (they write 28 and 42 MB, 6 and 9 us at the rate of a large copy).
 constexpr int prep_lds(int tile) { return 2 * tile > 2 * 64 * TRI_LD * 4 ? 2 * tile : 2 * 64 * TRI_LD * 4; }   // A and T take the place of keys and queries
 template <typename E, int DK> constexpr int PREP_LDS = prep_lds(Tile<E, DK>::bytes(DELTA_C));
 template <typename E, int DK> constexpr int PREP_GROUPS = PREP_LDS<E, DK> <= 36 * 1024 ? 4 : 2;   // on a CU
