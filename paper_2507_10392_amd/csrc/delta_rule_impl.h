@@ -347,12 +347,12 @@ template <int RUN = 1> __device__ __forceinline__ void load_ahead(unsigned lds, 
                  : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(rs) : "memory");
   else if constexpr (RUN == 2)
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\t"
-                 "buffer_load_dwordx4 %2, %3, 0 offen offset:1024 lds\n\ts_mov_b32 m0, %0"
+                 "buffer_load_dwordx4 %2, %3, 0 offen offset:0x400 lds\n\ts_mov_b32 m0, %0"
                  : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(rs) : "memory");
   else
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\t"
-                 "buffer_load_dwordx4 %2, %3, 0 offen offset:1024 lds\n\tbuffer_load_dwordx4 %2, %3, 0 offen offset:2048 lds\n\t"
-                 "buffer_load_dwordx4 %2, %3, 0 offen offset:3072 lds\n\ts_mov_b32 m0, %0"
+                 "buffer_load_dwordx4 %2, %3, 0 offen offset:0x400 lds\n\tbuffer_load_dwordx4 %2, %3, 0 offen offset:0x800 lds\n\t"
+                 "buffer_load_dwordx4 %2, %3, 0 offen offset:0xc00 lds\n\ts_mov_b32 m0, %0"
                  : "=&s"(m0) : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(offset), "s"(rs) : "memory");
 }
 template <typename E, int D, int ROWS, int NW> __device__ __forceinline__ void tile_ahead(const TileLoad<E, D, ROWS, NW>& t, unsigned lds, const E* head, int row0, int end, int wave) {
