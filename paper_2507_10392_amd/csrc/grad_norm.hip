@@ -1,13 +1,13 @@
 // The norm of many gradient tensors taken together, the factor that clips them, and the tensors times that factor.
 //
 // Memory bound: every element is read once for the norm, and once more and written for the clipping, which cannot begin before.  A launch takes up to
-// 128 tensors, whatever their types and sizes, in its arguments (no table on the device that could be out of date); its workgroups take pieces of them
+// 160 tensors, whatever their types and sizes, in its arguments (no table on the device that could be out of date); its workgroups take pieces of them
 // of one size, which grows with the total so that there are some thousand pieces at most.  A tensor's pieces begin at multiples of 16 bytes behind its
 // first aligned element, whose predecessors belong to the first piece.
 //
 // Squares are formed and added in 64 bits: gradients may be larger than 2^64 or smaller than 2^-75, whose squares fp32 does not hold, and a sum over
 // 10^9 elements keeps its digits.  That costs two instructions per element, of which the memory leaves time for ten.  The pieces' sums are added in
-// their order by a workgroup of a second kernel, so a repeat gives the same bits.  405 M fp32 in 18 tensors: norm 300 us, clipping 600, both at 5.4 TB/s; 26 tensors of
+// their order by a workgroup of a second kernel, so a repeat gives the same bits.  405 M fp32 in 18 tensors: norm 290 to 300 us, clipping 570 to 600, both at 5.4 to 5.6 TB/s; 26 tensors of
 // 1.6 M together 4 + 2 us.  Clipping in the opposite order, for what the norm left in the last-level cache, was no faster.
 #include "kernels.h"
 
@@ -17,28 +17,31 @@
 namespace zs {
 namespace {
 
-constexpr int PACK = 128;          // tensors of a launch: its arguments stay below 4096 bytes
+constexpr int PACK = 160;          // tensors of a launch: its arguments stay below 4096 bytes (with sizes and first pieces apart 128 would; 300 tensors: 116 us, 125)
 constexpr int THREADS = 256;
 constexpr int AHEAD = 8;           // vectors that a thread has in flight
 struct TensorPack {
   const void* in[PACK];
   void* out[PACK];
-  int64_t n[PACK];
-  int32_t first[PACK];             // of the launch's pieces
+  uint64_t place[PACK];            // elements, below 2^51, and behind them the tensor's first of the launch's pieces, below 2^13
   uint8_t type[PACK];
   int32_t count, pieces;
   int64_t piece;                   // bytes
 };
-static_assert(sizeof(TensorPack) < 4000, "");
+static_assert(sizeof(TensorPack) + sizeof(void*) <= 4096, "");
+constexpr int MOST_PIECES = 4096;  // and one more of every tensor
+static_assert(MOST_PIECES + PACK < 1 << 13, "");
+__device__ __forceinline__ int first_of(const TensorPack& p, int t) { return (int)(p.place[t] & 8191); }
+__device__ __forceinline__ int64_t size_of(const TensorPack& p, int t) { return (int64_t)(p.place[t] >> 13); }
 
 // The tensor that a piece belongs to: the last one whose first piece is not behind it.
 __device__ __forceinline__ int tensor_of(const TensorPack& p, int piece) {
   const int lane = threadIdx.x & 63;
   int at = -1;
 #pragma unroll
-  for (int i = 0; i < PACK / 64; ++i) {
+  for (int i = 0; i < (PACK + 63) / 64; ++i) {
     const int t = lane + 64 * i;
-    at += __popcll(__ballot(t < p.count && p.first[t] <= piece));
+    at += __popcll(__ballot(t < p.count && first_of(p, min(t, PACK - 1)) <= piece));
   }
   return __builtin_amdgcn_readfirstlane(at);
 }
@@ -92,9 +95,9 @@ template <int NW> __device__ __forceinline__ double block_sum(double v, double* 
 
 __global__ __launch_bounds__(THREADS) void grad_norm_kernel(TensorPack p, double* __restrict__ sums) {
   __shared__ double red[THREADS / 64];
-  const int t = tensor_of(p, blockIdx.x), k = (int)blockIdx.x - p.first[t], type = p.type[t];
+  const int t = tensor_of(p, blockIdx.x), k = (int)blockIdx.x - first_of(p, t), type = p.type[t];
   const void* x = p.in[t];
-  const int64_t n = p.n[t];
+  const int64_t n = size_of(p, t);
   double s;
   if (type == F32) s = sum_squares((const float*)x, piece_of((const float*)x, n, p.piece, k));
   else if (type == BF16) s = sum_squares((const bf16*)x, piece_of((const bf16*)x, n, p.piece, k));
@@ -151,22 +154,22 @@ template <typename E> __device__ __forceinline__ void scale_piece(const E* x, E*
 
 __global__ __launch_bounds__(THREADS) void grad_scale_kernel(TensorPack p, const float* __restrict__ factor) {
   const float f = *factor;
-  const int t = tensor_of(p, blockIdx.x), k = (int)blockIdx.x - p.first[t], type = p.type[t];
+  const int t = tensor_of(p, blockIdx.x), k = (int)blockIdx.x - first_of(p, t), type = p.type[t];
   const void* x = p.in[t];
   void* y = p.out[t];
   if (f == 1.f && x == y) return;
-  const int64_t n = p.n[t];
+  const int64_t n = size_of(p, t);
   if (type == F32) scale_piece((const float*)x, (float*)y, piece_of((const float*)x, n, p.piece, k), f);
   else if (type == BF16) scale_piece((const bf16*)x, (bf16*)y, piece_of((const bf16*)x, n, p.piece, k), f);
   else scale_piece((const f16*)x, (f16*)y, piece_of((const f16*)x, n, p.piece, k), f);
 }
 
 int64_t bytes_of(const GradTensor& t) { return t.n * (t.dtype == F32 ? 4 : 2); }
-// Pieces of 16 KB, larger ones where that would be more than 4096 of them.
+// Pieces of 16 KB, larger ones where that would be more than MOST_PIECES of them.
 int64_t piece_bytes(const GradTensor* t, int count) {
   int64_t total = 0, piece = 16 << 10;
   for (int i = 0; i < count; ++i) total += bytes_of(t[i]);
-  while (total / piece > 4096) piece *= 2;
+  while (total / piece > MOST_PIECES) piece *= 2;
   return piece;
 }
 int64_t pieces_of(const GradTensor& t, int64_t piece) {   // up to 15 bytes may lie before the first
@@ -183,9 +186,9 @@ template <typename F> hipError_t for_packs(const GradTensor* t, int count, F&& f
     const int64_t k = pieces_of(t[i], p.piece);
     if (k) {
       const int c = p.count++;
-      p.in[c] = t[i].in; p.out[c] = t[i].out; p.n[c] = t[i].n; p.type[c] = (uint8_t)t[i].dtype;
-      p.first[c] = p.pieces;
-      p.pieces += (int32_t)k;   // a tensor has 4096 + 1 at most
+      p.in[c] = t[i].in; p.out[c] = t[i].out; p.type[c] = (uint8_t)t[i].dtype;
+      p.place[c] = (uint64_t)t[i].n << 13 | (uint64_t)p.pieces;
+      p.pieces += (int32_t)k;
     }
     if (p.count == PACK || (i + 1 == count && p.count)) {
       const hipError_t e = f(p, before);
