@@ -187,7 +187,7 @@ int stage_op_attention_docs_bwd(void* stream, int32_t dtype, int32_t T, int32_t 
  * stage_op_delta_chunks writes the table of the documents' chunks of 64 tokens that the two calls below read: one call per microbatch serves all
  * layers, forward and backward.  chunks: device int32[stage_op_delta_chunks_ints(T, ndocs)] (host only; negative STAGE_ERR_ARG), 16-byte aligned.  The
  * offsets live on the device and are not checked: ones that fall, or leave [0, T], make documents of unspecified tokens, but nothing outside of [0, T] is
- * read or written for them.
+ * read or written for them, nor for a table that holds anything else.
  * stage_op_delta_fwd: o (stride ldo); h0: the documents' first states, or NULL for zeros; ht: receives their last ones (of an empty document its
  * first one), or NULL.
  * stage_op_delta_bwd: from dout (stride ldo) and dht, the gradient of ht (NULL: zeros), the gradients of all inputs: dq, dk_out, dv_out (strides lddq,

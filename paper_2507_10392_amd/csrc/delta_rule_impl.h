@@ -466,10 +466,18 @@ __device__ __forceinline__ double running_sum(double x, int lane) {
 }
 __device__ __forceinline__ float decay(double to, double from) { return __builtin_amdgcn_exp2f((float)(to - from)); }
 
-struct ChunkRow { int first, count, doc, index; };
+// Rows of the table.  Whatever it holds, they lie inside the tokens, chunks and documents.
+struct ChunkRow { int first, count; };
 __device__ __forceinline__ ChunkRow chunk_row(const DeltaRule& a, int c) {
   const int4 r = reinterpret_cast<const int4*>(a.chunks)[1 + a.ndocs + c];
-  return ChunkRow{r.x, r.y, r.z, r.w};
+  const int first = min(max(r.x, 0), a.T);
+  return ChunkRow{first, min(max(r.y, 0), min(DELTA_C, a.T - first))};
+}
+struct DocRow { int first, count, chunk0, doc; };
+__device__ __forceinline__ DocRow doc_row(const DeltaRule& a, int rank) {
+  const int4 r = reinterpret_cast<const int4*>(a.chunks)[1 + rank];
+  const int first = min(max(r.x, 0), a.T), chunk0 = min(max(r.z, 0), a.nchunks);
+  return DocRow{first, min(min(max(r.y, 0), a.T - first), (a.nchunks - chunk0) * DELTA_C), chunk0, min(max(r.w, 0), a.ndocs - 1)};
 }
 
 // Rows of no document become zeros: the last DELTA_FILL blocks of a grid of chunks share them.
@@ -725,8 +733,8 @@ template <typename E, typename M, int DK, int NW, int KIND> __device__ __forcein
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), mine = wave % NW, g = lane >> 4, i16 = lane & 15;
   const bool chain = wave < 2 * NW, loads = wave >= (LOADERS ? 4 : 3) * NW;
   const int fw = wave - (LOADERS ? 4 : 3) * NW;
-  const int4 row = reinterpret_cast<const int4*>(a.chunks)[1 + doc_rank];   // first token, tokens, first chunk, document
-  const int first = row.x, count = row.y, chunk0 = row.z, doc = row.w, chunks = (count + DELTA_C - 1) / DELTA_C;
+  const DocRow row = doc_row(a, doc_rank);
+  const int first = row.first, count = row.count, chunk0 = row.chunk0, doc = row.doc, chunks = (count + DELTA_C - 1) / DELTA_C;
   const int kv = h / (a.nv / a.nk), w0 = c0 + 16 * mine, col = w0 + i16;    // the wave's first column and the lane's
   const unsigned smem = lds_address(smem_raw), hand = smem + L::H + mine * L::HAND + 16 * lane, hand_z = hand + DK * 64, hand_add = hand_z + 4096;
   const unsigned units = smem + L::UNITS + mine * Tile<M, DK>::OCTET;       // of the state's columns, and 64 bytes on of Z's

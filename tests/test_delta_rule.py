@@ -430,6 +430,27 @@ def test_table_of_offsets_that_fall_or_leave_the_tokens(gpu_device):
             assert (chunks[:, 0] >= 0).all() and (chunks[:, 1] >= 0).all() and (chunks[:, 1] <= 64).all() and (chunks[:, 0] + chunks[:, 1] <= T).all()
 
 
+@gpu
+@pytest.mark.parametrize("dtype", [0, 1, 2])
+def test_a_table_of_anything(gpu_device, dtype):
+    """Results are unspecified then; what lies beside and behind them keeps its values, and calls with a right table theirs."""
+    say("any table", dtype)
+    c = Case(200, 1, 2, 64, 32, [90, 0, 110], h0=True, ht=True)
+    x = c.inputs(dtype)
+    want = Run(c, dtype, x).all()
+    rng = np.random.default_rng(9)
+    for most in (300, 2 ** 31 - 1):
+        r = Run(c, dtype, x, pad=8)
+        r.chunks.copy_(torch.from_numpy(rng.integers(-most, most, r.chunks.numel(), dtype=np.int64).astype(np.int32)))
+        outs = [t._base for t in (r.o, r.dq, r.dk, r.dv)]
+        r.fwd().bwd()
+        torch.cuda.synchronize()
+        for t in outs:
+            assert torch.isnan(t[:, -8:]).all()
+        for p, q in zip(want, Run(c, dtype, x).all()):
+            assert torch.equal(p, q)
+
+
 # ---------------------------------------------------------------------------------------------- single tokens
 def step(r, rows_, slots, state, o=None):
     c = r.c
