@@ -12,11 +12,11 @@ hipError_t delta_rule_f32(hipStream_t st, const DeltaRule& a, bool backward);
 namespace {
 
 // ------------------------------------------------------------------------------------------ chunks
-// One workgroup.  Whatever the offsets hold, documents are clipped to [0, T] and to the chunks that the table has room for, so that no row of the table
-// leads outside.  Rows of documents come longest first where there are at most SORTED (the walks from chunk to chunk take as long as the longest), those of more
-// as they are.  Layout, rows of four: (0, first and end of the documents' tokens, 0); per document (first token, tokens, first
-// chunk, document); per chunk (first token, tokens or 0: no chunk, document, place in it).
-constexpr int TABLE_THREADS = 1024, SORTED = 1024;
+// One workgroup.  Whatever the offsets hold, documents are clipped to [0, T] and to the chunks that the table has room for (delta_table.h), so that no row
+// of the table leads outside, and none is written outside of the table.  Rows of documents come longest first where there are at most SORTED (the walks from
+// chunk to chunk take as long as the longest), those of more as they are.  Layout, rows of four: (0, first and end of the documents' tokens, 0); per document
+// (first token, tokens, first chunk, document); per chunk (first token, tokens or 0: no chunk, document, place in it).
+constexpr int TABLE_THREADS = DELTA_TURN, SORTED = DELTA_TURN;
 __global__ __launch_bounds__(TABLE_THREADS) void delta_chunks_kernel(int T, int ndocs, int nchunks, const int32_t* __restrict__ offsets, int4* __restrict__ table) {
   __shared__ int waves[TABLE_THREADS / 64], lengths[SORTED];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -25,7 +25,7 @@ __global__ __launch_bounds__(TABLE_THREADS) void delta_chunks_kernel(int T, int 
     const int begin = min(max(offsets[0], 0), T);
     table[0] = make_int4(0, begin, min(max(offsets[ndocs], begin), T), 0);
   }
-  int before = 0;   // chunks of the documents of earlier turns
+  int before = 0;   // chunks of the documents of earlier turns, nchunks at most
   for (int d0 = 0; d0 < ndocs; d0 += TABLE_THREADS) {
     const int d = d0 + tid;
     int first = 0, count = 0;
@@ -33,7 +33,7 @@ __global__ __launch_bounds__(TABLE_THREADS) void delta_chunks_kernel(int T, int 
       first = min(max(offsets[d], 0), T);
       count = max(min(max(offsets[d + 1], 0), T) - first, 0);
     }
-    const int mine = (count + DELTA_CHUNK - 1) / DELTA_CHUNK;
+    const int mine = delta_chunks_of(count);
     int sum = mine;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -43,13 +43,15 @@ __global__ __launch_bounds__(TABLE_THREADS) void delta_chunks_kernel(int T, int 
     if (lane == 63) waves[wave] = sum;
     if (ndocs <= SORTED && d < ndocs) lengths[d] = count;
     __syncthreads();
-    int base = before;
+    int base = 0, turn = 0;
     for (int w = 0; w < TABLE_THREADS / 64; ++w) {
       if (w < wave) base += waves[w];
-      before += waves[w];
+      turn += waves[w];
     }
-    const int chunk0 = base + sum - mine;
-    count = min(count, max(nchunks - chunk0, 0) * DELTA_CHUNK);
+    const DeltaPlace at = delta_place(before, base + sum - mine, count, nchunks);
+    const int chunk0 = at.chunk0;
+    count = at.tokens;
+    before = delta_turn_end(before, turn, nchunks);
     if (d < ndocs) {
       int place = d;
       if (ndocs <= SORTED) {
@@ -62,7 +64,7 @@ __global__ __launch_bounds__(TABLE_THREADS) void delta_chunks_kernel(int T, int 
     // the wave's documents' chunks, a document after the other
     for (int l = 0; l < 64; ++l) {
       const int f = __shfl(first, l, 64), n = __shfl(count, l, 64), c0 = __shfl(chunk0, l, 64);
-      for (int i = lane; i < (n + DELTA_CHUNK - 1) / DELTA_CHUNK; i += 64)
+      for (int i = lane; i < delta_chunks_of(n); i += 64)
         chunks[c0 + i] = make_int4(f + DELTA_CHUNK * i, min(n - DELTA_CHUNK * i, DELTA_CHUNK), d0 + 64 * wave + l, i);
     }
     __syncthreads();

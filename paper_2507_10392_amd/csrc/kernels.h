@@ -2,6 +2,7 @@
 // launcher only enqueues on the given stream and returns the launch status.
 #pragma once
 #include "common.h"
+#include "delta_table.h"
 
 #include <initializer_list>
 
@@ -250,7 +251,6 @@ hipError_t rope_axes(hipStream_t st, DType dt, int T, int d, const RopeHeads& q,
 // The gated delta rule inside packed documents (delta_rule_impl.h has the formulas): rows of nk heads of q and k, dk wide, and of nv heads of v and o,
 // dv wide; value head h reads key head h / (nv / nk).  g, beta: float[T, nv].  chunks: the table that delta_chunks writes.  States are
 // float[ndocs, nv, dk, dv].
-constexpr int DELTA_CHUNK = 64;   // tokens of a document that are worked on together
 constexpr int DELTA_FILL = 16;    // blocks that clear the rows of no document
 constexpr int DELTA_RECORD_FWD = 25600, DELTA_RECORD_BWD = 38400;   // bytes of a chunk's own matrices
 struct DeltaRule {

@@ -338,7 +338,7 @@ int stage_op_attention_docs_bwd(void* stream, int32_t dtype, int32_t T, int32_t 
 }  // extern "C"
 namespace {
 // Walks: documents times value heads.  A launch has less than 2^32 threads: 2^18 walks in eight slices, two directions, 512 threads each are 2^31.
-constexpr int DELTA_MAX_TOKENS = 1 << 26, DELTA_MAX_HEADS = 4096, DELTA_MAX_DOCS = 1 << 18, DELTA_MAX_WALKS = 1 << 18;
+constexpr int DELTA_MAX_HEADS = 4096, DELTA_MAX_WALKS = 1 << 18;
 bool aligned16(const void* p) { return !((uintptr_t)p & 15); }   // or nothing
 bool delta_heads_ok(int dtype, int nk, int nv, int dk, int dv) {
   return dt_ok(dtype) && nk >= 1 && nv >= nk && nv % nk == 0 && nv <= DELTA_MAX_HEADS && dk >= 8 && dk % 8 == 0 && dk <= 128 && dv >= 8 && dv % 8 == 0 && dv <= 256;
