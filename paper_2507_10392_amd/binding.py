@@ -214,6 +214,15 @@ def _ptr(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
+def _check_result(what, t, dtype, gpu):
+    """A result (or factor) of one element on GPU number `gpu` (None: on any), which the kernels reach by its address alone; or None."""
+    if t is None:
+        return
+    at = t.get_device()   # -1: the host
+    if t.dtype != dtype or at < 0 or (gpu is not None and at != gpu) or t.numel() < 1:
+        raise ValueError(f"{what}: a {dtype} tensor of one element on the GPU of the others")
+
+
 class Stage:
     """One stage bound to torch device tensors.  The tensors are kept alive by this object."""
 
@@ -250,8 +259,10 @@ class Stage:
 
     def set_grad_factor(self, factor):
         """factor: a float32 tensor of one element on the stage's GPU, or None."""
-        self._factor = factor
+        import torch
+        _check_result("set_grad_factor", factor, torch.float32, self.stream.device.index)
         _check(lib().stage_set_grad_factor(self.h, _ptr(factor)), self.h)
+        self._factor = factor   # kept alive while the library has its address
 
     def profile(self, enable):
         _check(lib().stage_profile(self.h, 1 if enable else 0), self.h)
@@ -450,7 +461,7 @@ class TensorList:
             if not (x.is_cuda and y.device == x.device == tensors[0].device):
                 raise ValueError("tensor_list: all tensors lie on one GPU")
         self._keep = (list(tensors), list(outs))
-        self.n = len(tensors)
+        self.n, self.gpu = len(tensors), tensors[0].get_device() if len(tensors) else None
         self.c = (TensorC * max(1, self.n))(*[TensorC(x.data_ptr(), y.data_ptr(), x.numel(), types[x.dtype], 0) for x, y in zip(tensors, outs)])
 
 
@@ -468,10 +479,21 @@ def grad_norm_scratch_bytes(tensors):
 
 
 def grad_norm(stream, tensors, scale, max_norm, sumsq, norm, factor, overflow, scratch):
-    """stage_op_grad_norm of a tensor_list; sumsq, norm, factor, overflow: device tensors or None."""
+    """stage_op_grad_norm of a tensor_list; sumsq (float64), norm, factor (float32), overflow (int32): device tensors or None."""
+    import torch
+    gpu = tensors.gpu
+    _check_result("sumsq", sumsq, torch.float64, gpu)
+    _check_result("norm", norm, torch.float32, gpu)
+    _check_result("factor", factor, torch.float32, gpu)
+    _check_result("overflow", overflow, torch.int32, gpu)
+    at = scratch.get_device()
+    if at < 0 or (gpu is not None and at != gpu) or not scratch.is_contiguous():
+        raise ValueError("scratch: a contiguous tensor on the GPU of the others")
     ops.grad_norm(stream, tensors.n, tensors.c, scale, max_norm, sumsq, norm, factor, overflow, scratch, scratch.numel() * scratch.element_size())
 
 
 def grad_scale(stream, tensors, factor):
-    """stage_op_grad_scale of a tensor_list."""
+    """stage_op_grad_scale of a tensor_list; factor: a float32 device tensor of one element."""
+    import torch
+    _check_result("factor", factor, torch.float32, tensors.gpu)
     ops.grad_scale(stream, tensors.n, tensors.c, factor)
