@@ -287,9 +287,10 @@ int stage_op_adamw(void* stream, int32_t dtype, int64_t n, int64_t begin, void* 
  * Squares and sums are formed in 64 bits and in a fixed order: no overflow, the same bits on every call with the same sizes.
  *
  * stage_op_grad_norm: *sumsq = the sum of all squares; *norm = scale sqrt(sumsq), scale > 0 finite (1 / loss scale);
- * *factor = max_norm / norm where norm > max_norm >= 0, else 1.  Where the norm is inf or NaN (some gradient is), the factor is 1 and 1 is ORed into
- * *overflow (int32, cleared by the caller; what stage_set_overflow_flag takes).  sumsq (double), norm, factor (float), overflow:
- * device, any of them may be NULL.  scratch: device, 256-byte aligned, stage_op_grad_norm_scratch_bytes (host only, of the same list; negative
+ * *factor = max_norm / norm where norm > max_norm >= 0, else 1.  Both are formed in 64 bits and rounded to fp32 once.  Where some gradient is inf or NaN, the
+ * factor is 1 and 1 is ORed into *overflow (int32, cleared by the caller; what stage_set_overflow_flag takes): *overflow alone tells that.  Finite
+ * gradients whose norm is beyond fp32 (3.4e38) leave inf in *norm, no flag, and the factor of the norm in 64 bits, of which fp32 holds fewer digits below
+ * 2^-126 and which is 0 below 2^-150.  sumsq (double), norm, factor (float), overflow: device, any of them may be NULL.  scratch: device, 256-byte aligned, stage_op_grad_norm_scratch_bytes (host only, of the same list; negative
  * STAGE_ERR_ARG for an invalid one), free again when the call's work on the stream has finished; calls that may overlap need scratch of their
  * own.  STAGE_ERR_WORKSPACE when it is missing, misaligned or too small.
  * stage_op_grad_factor: the same from nsums >= 1 sums of squares (device double[nsums], added in their order: of stages, or of shards after a gather).

@@ -310,8 +310,8 @@ hipError_t fill_zero(hipStream_t st, float* p, int64_t n);
 hipError_t nonfinite_check(hipStream_t st, const float* g, int64_t n, int* flag);
 // Gradient tensors of any types (DType) and sizes; in and out may be the same.
 struct GradTensor { const void* in; void* out; int64_t n; int32_t dtype, reserved; };
-// norm = scale sqrt(sum of squares); factor = max_norm / norm where the norm is above that, else 1; *overflow |= 1 where it is inf or NaN (the factor is 1
-// then).  Any of the results may be NULL.
+// norm = scale sqrt(sum of squares); factor = max_norm / norm where the norm is above that, else 1; *overflow |= 1 where the norm in 64 bits is inf or
+// NaN, that is, where a gradient is (the factor is 1 then).  Any of the results may be NULL.
 struct GradClip { float scale, max_norm; double* sumsq; float *norm, *factor; int* overflow; };
 int64_t grad_norm_pieces(const GradTensor* t, int count);   // of the pieces, a double each, that grad_norm leaves in sums
 hipError_t grad_norm(hipStream_t st, const GradTensor* t, int count, const GradClip& c, double* sums);
