@@ -294,7 +294,8 @@ int stage_op_adamw(void* stream, int32_t dtype, int64_t n, int64_t begin, void* 
  * STAGE_ERR_ARG for an invalid one), free again when the call's work on the stream has finished; calls that may overlap need scratch of their
  * own.  STAGE_ERR_WORKSPACE when it is missing, misaligned or too small.
  * stage_op_grad_factor: the same from nsums >= 1 sums of squares (device double[nsums], added in their order: of stages, or of shards after a gather).
- * stage_op_grad_scale: out = in * *factor, rounded once; where the factor is 1 and out is in, nothing is touched. */
+ * stage_op_grad_scale: out = in * *factor, rounded once; where the factor is 1 and out is in, nothing is touched.  The factor lies in no output
+ * (STAGE_ERR_ARG). */
 typedef struct {
   const void* in;
   void* out;

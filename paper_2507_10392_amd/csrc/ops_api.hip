@@ -469,12 +469,14 @@ bool tensors_ok(int32_t n, const stage_op_tensor* t, bool out) {
   }
   return true;
 }
-// No output over another tensor's input or output, nor beside its own input over a part of it: two workgroups would write what one of them reads.
-bool outputs_apart(int32_t n, const stage_op_tensor* t) {
+// No output over another tensor's input or output, nor beside its own input over a part of it, nor over the factor: two workgroups would write what one of
+// them reads.
+bool outputs_apart(int32_t n, const stage_op_tensor* t, const float* factor) {
   struct Span { uintptr_t begin, end; bool out; };
   std::unique_ptr<Span[]> spans(new (std::nothrow) Span[2 * (size_t)n + 1]);
   if (!spans) return false;
   size_t m = 0;
+  spans[m++] = Span{(uintptr_t)factor, (uintptr_t)factor + 4, false};
   for (int32_t i = 0; i < n; ++i) {
     const uintptr_t bytes = (uintptr_t)t[i].n * (t[i].dtype == 0 ? 4 : 2), in = (uintptr_t)t[i].in, out = (uintptr_t)t[i].out;
     if (!bytes) continue;
@@ -515,7 +517,7 @@ int stage_op_grad_factor(void* stream, int32_t nsums, const double* sums, float 
 }
 
 int stage_op_grad_scale(void* stream, int32_t ntensors, const stage_op_tensor* tensors, const float* factor) {
-  if (!tensors_ok(ntensors, tensors, true) || !factor || !words_ok(factor) || !outputs_apart(ntensors, tensors)) return STAGE_ERR_ARG;
+  if (!tensors_ok(ntensors, tensors, true) || !factor || !words_ok(factor) || !outputs_apart(ntensors, tensors, factor)) return STAGE_ERR_ARG;
   return rc(grad_scale((hipStream_t)stream, grad_tensors(tensors), ntensors, factor));
 }
 
