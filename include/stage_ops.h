@@ -197,9 +197,11 @@ int stage_op_attention_docs_bwd(void* stream, int32_t dtype, int32_t T, int32_t 
  * The rule is stable where beta |k|^2 lies between 0 and 2 and g <= 0, so keys have length one (stage_op_norm_fwd, RMSNorm over heads with gains 1/sqrt(dk)).
  * g below -138, -inf too, forgets everything and counts as that; its own dg is a difference of sums that cancel.  inf or NaN in a token's q, k, v, g, beta or
  * dout may reach every result of its document for the value heads that read it, and no other document's.
- * Sizes.  Half: |q_i.k_j| stays below 65504.  Half, and bf16 where ht or gradients are wanted: so do the elements of the inverse of 1 + A,
- * A_ij = beta_i exp(g_(j+1) + .. + g_i) k_i.k_j (j < i, of 64 tokens), which a stable rule bounds; bf16, the same: digits are lost where the largest of
- * 64 tokens' keys, or queries, is above 2^65 or under 2^-50.  o of bf16 is formed in finer products, and may be rounded otherwise, where ht is wanted.
+ * Sizes.  Half: |q_i.k_j| stays below 65504.  Half, and bf16 where ht or gradients are wanted, hold the inverse of 1 + A, A_ij = beta_i exp(g_(j+1) + .. + g_i)
+ * k_i.k_j (j < i, of 64 tokens), in half: a stable rule bounds its elements by 2 |k_j| / |k_i|.  So of a chunk's 64 tokens no key may be more than 2^14 times as
+ * long as a later one, and where the longest is r times as long as the shortest, up to log2 r of the results' 22 bits are lost: none for keys of one length.  bf16,
+ * the same: keys, and queries, are held to 2^-28 of the largest element of their 64 tokens, and digits are lost where that is above 2^65 or under 2^-50.
+ * o of bf16 is formed in finer products, and may be rounded otherwise, where ht is wanted.
  * dk and dv: multiples of 8, dk up to 128, dv up to 256.  Rows start at multiples of 16 bytes, strides are multiples of 16 bytes and at most
  * 2^22 elements; states are 16-byte aligned; T <= 2^26, nv <= 4096, T * nv <= 2^30, ndocs and ndocs * nv <= 2^18.  scale is finite.
  * No output overlaps an input or another output.  T = 0 and ndocs = 0 together do nothing.  The GPU that owns `stream` must be the

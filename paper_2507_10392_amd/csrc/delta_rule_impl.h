@@ -23,6 +23,8 @@
 // halves times a power of two that prep finds, computed values times one per column, so that no size of state or gradient leaves
 // a half's range), and a chunk's gradients three bf16, which are an fp32, of S, dS, U and Y: 3e-7 and 1.2e-6, for 15 us in 104 and 8 in 112 (gradients; 4096
 // tokens, 16 heads, head widths of 128).  What only goes into dq and dk, which are rounded to 16 bits, stays pairs.  fp32: v_mfma_f32_16x16x4, no pairs.
+// The halves of T, keys and queries have no unit of their own per token: where the keys of a chunk differ in length by a factor of r, |T_ij| is up to
+// 2 |k_j| / |k_i|, which half holds for r up to 2^14, and results lose up to log2 r bits (r = 8, 64, 1024, 8192: ht off by 4.6e-7, 2.2e-6, 3.3e-5, 3e-4 of its norm).
 #pragma once
 #include "attention_docs_tiles.h"
 
