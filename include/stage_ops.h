@@ -198,9 +198,9 @@ int stage_op_attention_docs_bwd(void* stream, int32_t dtype, int32_t T, int32_t 
  * g below -138, -inf too, forgets everything and counts as that; its own dg is a difference of sums that cancel.  inf or NaN in a token's q, k, v, g, beta or
  * dout may reach every result of its document for the value heads that read it, and no other document's.
  * Sizes.  Half: |q_i.k_j| stays below 65504.  Half, and bf16 where ht or gradients are wanted, hold the inverse of 1 + A, A_ij = beta_i exp(g_(j+1) + .. + g_i)
- * k_i.k_j (j < i, of 64 tokens), in half: a stable rule bounds its elements by 2 |k_j| / |k_i|.  So of a chunk's 64 tokens no key may be more than 2^14 times as
- * long as a later one, and where the longest is r times as long as the shortest, up to log2 r of the results' 22 bits are lost: none for keys of one length.  bf16,
- * the same: keys, and queries, are held to 2^-28 of the largest element of their 64 tokens, and digits are lost where that is above 2^65 or under 2^-50.
+ * k_i.k_j (j < i, of 64 tokens), in half.  A stable rule bounds its elements by beta_i |k_i| |k_j|, so by 2 for keys of one length and by 2 |k_j| / |k_i| else:
+ * that stays below 65504, and where it reaches r, up to log2 r of the results' 22 bits are lost.  bf16, the same: keys, and queries, are held to
+ * 2^-28 of the largest element of their 64 tokens, and digits are lost where that is above 2^65 or under 2^-50.
  * o of bf16 is formed in finer products, and may be rounded otherwise, where ht is wanted.
  * dk and dv: multiples of 8, dk up to 128, dv up to 256.  Rows start at multiples of 16 bytes, strides are multiples of 16 bytes and at most
  * 2^22 elements; states are 16-byte aligned; T <= 2^26, nv <= 4096, T * nv <= 2^30, ndocs and ndocs * nv <= 2^18.  scale is finite.
