@@ -17,12 +17,12 @@
 // (delta_grad_kernel).  No atomics: a repeat gives the same bits.
 //
 // Precision.  q, k, v and dO are operands as they stand.  What is computed stays fp32 in registers; where it is an operand it is the sum of two or three
-// values of 16 bits, in two to six products.  Forward without last states: two of the type (16 bits of a bf16 pair, 22 of a half pair), since what comes of them is
-// rounded to the type.  The last states are fp32, and dg and dbeta are what is left of larger terms: with bf16 pairs throughout these were off by up to 5.2e-6
-// and 1.5e-5 of their norms.  So where last states are wanted, and backward, the walks take half pairs for bf16 too (keys and queries as
-// halves times a power of two that prep finds, computed values times one per column, so that no size of state or gradient leaves
-// a half's range), and a chunk's gradients three bf16, which are an fp32, of S, dS, U and Y: 3e-7 and 1.2e-6, for 15 us in 104 and 8 in 112 (gradients; 4096
-// tokens, 16 heads, head widths of 128).  What only goes into dq and dk, which are rounded to 16 bits, stays pairs.  fp32: v_mfma_f32_16x16x4, no pairs.
+// values of 16 bits, in two to six products.  Forward without last states: two of the type (16 bits of a bf16 pair, 22 of a half pair), since what comes of
+// them is rounded to the type.  The last states are fp32, and dg and dbeta are what is left of larger terms: with bf16 pairs throughout these were off by up to
+// 5.2e-6 and 1.5e-5 of their norms.  So where last states are wanted, and backward, the walks take half pairs for bf16 too (keys and queries as halves times
+// a power of two that prep finds, computed values times one per column, so that no size of state or gradient leaves a half's range), and a chunk's
+// gradients three bf16, which are an fp32, of S, dS, U and Y: 3e-7 and 1.2e-6, for 15 us in 104 and 8 in 112 (gradients; 4096 tokens, 16 heads, head
+// widths of 128).  What only goes into dq and dk, which are rounded to 16 bits, stays pairs.  fp32: v_mfma_f32_16x16x4, no pairs.
 // The halves of T, keys and queries have no unit of their own per token: where the keys of a chunk differ in length by a factor of r, |T_ij| is up to
 // 2 |k_j| / |k_i|, which half holds for r up to 2^14, and results lose up to log2 r bits (r = 8, 64, 1024, 8192: ht off by 4.6e-7, 2.2e-6, 3.3e-5, 3e-4 of its norm).
 #pragma once
@@ -46,7 +46,8 @@ __device__ __forceinline__ f32x4 mma1(op8<float> a, op8<float> b, f32x4 c) {
   for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
   return c;
 }
-// A value as one operand, or as the sum of two or three, each of what the ones before leave.  Products smaller than the last terms' are left out; small ones come first.
+// A value as one operand, or as the sum of two or three, each of what the ones before leave.  Products smaller than the last terms' are left out; small ones
+// come first.
 template <typename E, int TERMS> struct Opnd { op8<E> t[TERMS]; };
 template <typename E, int A, int B> __device__ __forceinline__ f32x4 mma(const Opnd<E, A>& a, const Opnd<E, B>& b, f32x4 c) {
   constexpr int MOST = A > B ? A : B;
@@ -398,9 +399,9 @@ template <typename TL, int NW> __device__ __forceinline__ void squares_ahead(uns
 
 // ------------------------------------------------------------------------------------------ a chunk's own matrices
 constexpr int TRI_LD = 68;   // floats of a row of a 64 x 64 matrix in LDS: rows 16 bytes aligned, four banks apart
-// T = (1 + A)^-1 of a strictly lower A, both in LDS, by four waves.  Blocks of 16 on the diagonal by substitution, four rows
-// at a time, by the lanes that hold them, and what these leave of the others by a product; then block by block away from it, T_ij = -T_ii (sum over k of A_ik T_kj), in fp32 products.  Every step solves for values of T itself, which are bounded where the
-// rule is stable; powers of A, which are not, do not occur.
+// T = (1 + A)^-1 of a strictly lower A, both in LDS, by four waves.  Blocks of 16 on the diagonal by substitution, four rows at a time, by the lanes that hold
+// them, and what these leave of the others by a product; then block by block away from it, T_ij = -T_ii (sum over k of A_ik T_kj), in fp32 products.  Every
+// step solves for values of T itself, which are bounded where the rule is stable; powers of A, which are not, do not occur.
 __device__ __forceinline__ void invert_lower(const float* A, float* T, int wave, int lane) {
   const int g = lane >> 4, c = lane & 15;
   {
@@ -711,7 +712,10 @@ template <typename E, typename M, int DK, int NW, int KIND> struct WalkLds {
   // Two buffers of all a chunk brings, or of its keys and matrices, or one.
   static constexpr int NBUF = 2 * FIRST + SECOND <= ROOM ? 2 : 1, VBUF = 2 * (FIRST + SECOND) <= ROOM ? 2 : 1;
   static constexpr int K = 0, R = TL::bytes(DELTA_C), V = NBUF * FIRST, Q = V + VSIZE, H = V + VBUF * SECOND, BYTES = H + NW * HAND;
-  static constexpr int UNITS = TL::OCTET - 128;   // half's units of 16 columns: the gap behind an octet of the first keys
+  // Half's units, in the gaps of 128 bytes behind octets of the first keys.  Of set n of 16 columns: behind octet n those of the state, of its two halves of
+  // rows 64 bytes each; behind octet 4 + n those of Z, of its two halves of tokens.
+  static constexpr int UNITS = TL::OCTET - 128, UNITS_Z = 4 * TL::OCTET;
+  static_assert(NW <= 4 && TL::OCTET - 128 >= TL::SQUARES * 1024 && TL::bytes(DELTA_C) >= 8 * TL::OCTET, "");
   static_assert(BYTES <= 160 * 1024, "");
 };
 
@@ -739,7 +743,7 @@ template <typename E, typename M, int DK, int NW, int KIND> __device__ __forcein
   const int first = row.first, count = row.count, chunk0 = row.chunk0, doc = row.doc, chunks = (count + DELTA_C - 1) / DELTA_C;
   const int kv = h / (a.nv / a.nk), w0 = c0 + 16 * mine, col = w0 + i16;    // the wave's first column and the lane's
   const unsigned smem = lds_address(smem_raw), hand = smem + L::H + mine * L::HAND + 16 * lane, hand_z = hand + DK * 64, hand_add = hand_z + 4096;
-  const unsigned units = smem + L::UNITS + mine * Tile<M, DK>::OCTET;       // of the state's columns, and 64 bytes on of Z's
+  const unsigned units = smem + L::UNITS + mine * Tile<M, DK>::OCTET;
   const int step = BACK ? -1 : 1;
   const int64_t states = (int64_t)a.dk * a.dv;
   const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
@@ -948,7 +952,7 @@ template <typename E, typename M, int DK, int NW, int KIND> __device__ __forcein
         Pair<M> zp[1];
         pairs_of<M>(zp, z, unit);
         write_op<M>(hand_z + half * 2048, zp[0]);
-        if (HALF_E && lane < 16) lds_write(units + Tile<M, DK>::OCTET * 4 + 64 * half + 4 * lane, unit);
+        if (HALF_E && lane < 16) lds_write(units + L::UNITS_Z + 64 * half + 4 * lane, unit);
       }
       __builtin_amdgcn_sched_barrier(0);
       Opnd<M, 1> kc[HT][2];   // columns of the keys, this half's rows of the state
@@ -969,7 +973,7 @@ template <typename E, typename M, int DK, int NW, int KIND> __device__ __forcein
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         zp[s] = load_op<M>(hand_z + s * 2048);
-        if constexpr (HALF_E) zi[s] = inverse_unit<M>(lds_read<float>(units + Tile<M, DK>::OCTET * 4 + 64 * s + 4 * i16));
+        if constexpr (HALF_E) zi[s] = inverse_unit<M>(lds_read<float>(units + L::UNITS_Z + 64 * s + 4 * i16));
       }
       f32x4 add[HT];
       if constexpr (BACK)
@@ -1101,7 +1105,7 @@ template <typename E, typename M, int DK, int NW, int KIND> __device__ __forcein
         zp[1] = load_op<M>(hand_z + 2048);
         if constexpr (HALF_E)
 #pragma unroll
-          for (int s = 0; s < 2; ++s) zi[s] = inverse_unit<M>(lds_read<float>(units + Tile<M, DK>::OCTET * 4 + 4 * i16 + 64 * s));
+          for (int s = 0; s < 2; ++s) zi[s] = inverse_unit<M>(lds_read<float>(units + L::UNITS_Z + 4 * i16 + 64 * s));
         f32x4 u[UT], uo[UT], p[MT], back_u = zero;
 #pragma unroll
         for (int m = 0; m < UT; ++m) u[m] = uo[m] = zero;
@@ -1227,7 +1231,7 @@ template <typename E, typename M, int DK, int NW, int KIND> __device__ __forcein
         for (int s = 0; s < 2; ++s) {
           zp[s] = load_op<M>(hand_z + s * 2048);
           if constexpr (HALF_E) {
-            back_z[s] = lds_read<f32x4>(units + Tile<M, DK>::OCTET * 4 + 64 * s + 16 * g);
+            back_z[s] = lds_read<f32x4>(units + L::UNITS_Z + 64 * s + 16 * g);
 #pragma unroll
             for (int r = 0; r < 4; ++r) back_z[s][r] = inverse_unit<M>(back_z[s][r]);
           }
