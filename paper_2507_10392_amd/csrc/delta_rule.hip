@@ -16,6 +16,8 @@ namespace {
 // of the table leads outside, and none is written outside of the table.  Rows of documents come longest first where there are at most SORTED (the walks from
 // chunk to chunk take as long as the longest), those of more as they are.  Layout, rows of four: (0, first and end of the documents' tokens, 0); per document
 // (first token, tokens, first chunk, document); per chunk (first token, tokens or 0: no chunk, document, place in it).
+// Bound by steps that follow one another, of which every wave has one per document for the rows of its chunks: 11.4 us for up to 64 documents, 53 for 1024 of 64
+// tokens (more than half of it their order), 3 ms for 2^18.  Once a microbatch, for all layers and both directions, so one workgroup was left to do it.
 constexpr int TABLE_THREADS = DELTA_TURN, SORTED = DELTA_TURN;
 __global__ __launch_bounds__(TABLE_THREADS) void delta_chunks_kernel(int T, int ndocs, int nchunks, const int32_t* __restrict__ offsets, int4* __restrict__ table) {
   __shared__ int waves[TABLE_THREADS / 64], lengths[SORTED];

@@ -1320,9 +1320,10 @@ template <typename M> __device__ __forceinline__ GradOpnd<M> load_terms(unsigned
 // state's rows are read by one wave only and a token's factors are a lane's own.  The matrices of tokens by tokens are shared out by tiles: wave
 // w has the row tile w % 4, and of its column tiles those of its parity where there are eight waves.  Columns of the value head come in blocks of 64.
 // A workgroup fills a CU (157 KB of LDS, 242 registers), so what it loads is asked for ahead, states 32 columns, u and y 64, and the first of them before its
-// row of the table is there.  4096 tokens of 16 heads of 128 in bf16: 120 us in 4.3 rounds of 256 workgroups, 213 MB of states, u and y at 1.8 TB/s; a
-// workgroup's phases follow one another: of 45000 cycles alone 12700 until the first loads are there, 10800 the products with states, 8600 the matrices of
-// tokens and the sums over them, 7300 the products with these, and fewer registers would spill (128, two workgroups a CU: 245 us).
+// row of the table is there.  4096 tokens of 16 heads of 128 in bf16: 120 us in 4.3 rounds of 256 workgroups, 278 MB read at 2.3 TB/s (214 of them states, u and
+// y), the matrix cores busy in 0.15 of the cycles; a workgroup's phases follow one another: of 45000 cycles alone 12700 until the first loads are there, 10800 the
+// products with states, 8600 the matrices of tokens and the sums over them, 7300 the products with these, and fewer registers would spill (128, two
+// workgroups a CU: 245 us).
 constexpr int grad_waves(int DK) { return DK / 16; }
 template <typename E, int DK, bool SHARED> __global__ __launch_bounds__(64 * grad_waves(DK), 1) void delta_grad_kernel(DeltaRule a) {
   typedef typename GradOf<E>::type M;

@@ -7,8 +7,8 @@
 //
 // Squares are formed and added in 64 bits: gradients may be larger than 2^64 or smaller than 2^-75, whose squares fp32 does not hold, and a sum over
 // 10^9 elements keeps its digits.  That costs two instructions per element, of which the memory leaves time for ten.  The pieces' sums are added in
-// their order by a workgroup of a second kernel, so a repeat gives the same bits.  405 M fp32 in 18 tensors: norm 290 to 300 us, clipping 570 to 600, both at
-// 5.4 to 5.6 TB/s; 26 tensors of 1.6 M together 4 + 2 us.  Clipping in the opposite order, for what the norm left in the last-level cache, was no faster.
+// their order by a workgroup of a second kernel, so a repeat gives the same bits.  405 M fp32 in 18 tensors: norm 290 to 300 us, clipping 560 to 606, both at
+// 5.3 to 5.8 TB/s; 26 tensors of 1.6 M together 4 + 2 us.  Clipping in the opposite order, for what the norm left in the last-level cache, was no faster.
 #include "kernels.h"
 
 #include <algorithm>
