@@ -286,7 +286,7 @@ int stage_op_adamw(void* stream, int32_t dtype, int64_t n, int64_t begin, void* 
 /* The norm of many gradient tensors taken together, and clipping by it.  tensors: HOST array of ntensors >= 0 (the pointers and sizes are read during the
  * call): in: device, n >= 0 elements of dtype, at a multiple of the element's size; out: for stage_op_grad_scale alone (else NULL is fine), the
  * same place as in, or n elements elsewhere, and over no other tensor of the list (STAGE_ERR_ARG); n = 0: both may be NULL.  In total less than 2^52 bytes.
- * Squares and sums are formed in 64 bits and in a fixed order: no overflow, the same bits on every call with the same sizes.
+ * Squares and sums are formed in 64 bits and in an order that the sizes and the places modulo 16 bytes fix: no overflow, and a repeat gives the same bits.
  *
  * stage_op_grad_norm: *sumsq = the sum of all squares; *norm = scale sqrt(sumsq), scale > 0 finite (1 / loss scale);
  * *factor = max_norm / norm where norm > max_norm >= 0, else 1.  Both are formed in 64 bits and rounded to fp32 once.  Where some gradient is inf or NaN, the
